@@ -92,7 +92,12 @@ typedef enum {
     VELORA_OP_LINEAR_BACKWARD_EXPLICIT = 5,
     VELORA_OP_UPDATE_V = 6,
     VELORA_OP_Z8_CALIBRATE = 7,
-    /* added to one of the layer's or the explicit gradient's: with room for copies of operands on odd rows */
+    VELORA_OP_CHECKPOINT_WEIGHT_GRAD = 8,
+    VELORA_OP_HEAD_LOSS = 9,              /* O: the vocabulary; Dsub is not used (1) */
+    VELORA_OP_HEAD_LOSS_BACKWARD = 10,    /* the same */
+    /* added to one of these three: operands in fp32 */
+    VELORA_OP_F32 = 512,
+    /* added to one of the layer's, the explicit gradient's or the last three: with room for copies of operands on odd rows */
     VELORA_OP_ANY_ROWS = 256
 } velora_op;
 
@@ -124,8 +129,9 @@ size_t velora_workspace_bytes(int op, int64_t N, int64_t D, int64_t O, int Dsub)
  * fed by a tile copy or by the tensor cores) gives up after one second instead of spinning for ever.
  * velora_workspace_init zeroes the header (asynchronously, on `stream`): call it once after
  * allocating a workspace.  velora_workspace_status synchronises `stream`, reads the flag and returns
- * VELORA_OK or VELORA_ERR_TIMEOUT; outputs of a call that raised the flag are undefined.  (The one other
- * value is VELORA_ERR_DEGENERATE_V, which velora_update_v leaves there instead of synchronising.)
+ * VELORA_OK or VELORA_ERR_TIMEOUT; outputs of a call that raised the flag are undefined.  (The two other
+ * values are VELORA_ERR_DEGENERATE_V, which velora_update_v leaves there instead of synchronising, and
+ * VELORA_ERR_INVALID_ARG, left by velora_head_loss and its backward pass for a target that is no column of W.)
  * The paper has no counterpart: this is run-time hygiene of the implementation.
  */
 int velora_workspace_init(void* ws, size_t ws_bytes, void* stream);
@@ -365,6 +371,54 @@ int velora_linear_step_host(const void* hX, const void* hdY, void* hY, void* hdX
                             const void* W, const float* v, void* staging, size_t staging_bytes,
                             int64_t N, int64_t D, int64_t O, int Dsub,
                             void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * 8-bit checkpoints of a layer's input, for layers that the projection is not used on (Section 4 applies it to some of a block's
+ * layers; the inputs of the others are kept whole there): one byte per element and one per block of 32 columns.
+ * A row of X is cut into blocks of 32 columns (the last may be shorter).  With a = max |x| over a block, its step is the smallest
+ * power of two s = 2^e with a <= 127 s, -126 <= e <= 121 (e = 121 where there is none), and
+ *     Q[n, d] = round(X[n, d] / s), ties to even, at most 127 in size;   E[n, d / 32] = e + 127;   Xhat[n, d] = Q[n, d] * 2^(E - 127)
+ * Xhat is exact in bf16 and fp32, at most s / 2 <= a / 127 from X (s where a > 127 * 2^121).  A block that holds an infinity or a NaN has
+ * E = 255 and codes of zero and reads back as NaN.  Q: int8 [N, D], ldq bytes; E: bytes [N, ceil(D / 32)], lde bytes.
+ *   velora_checkpoint_store        X (bf16 or f32) -> Q, E
+ *   velora_checkpoint_load         Q, E -> Xhat (bf16 or f32)
+ *   velora_checkpoint_weight_grad  dW[o, d] = beta * dW[o, d] + sum_n dY[n, o] * Xhat[n, d]   (fp32 accumulation; types of dY and dW as in
+ *                                  velora_weight_grad);  ws: velora_workspace_bytes(VELORA_OP_CHECKPOINT_WEIGHT_GRAD, N, D, O, 1) bytes,
+ *                                  | VELORA_OP_F32 for an fp32 dY, initialised
+ * N == 0 as in velora_compress and velora_weight_grad.  Any rows are taken; fastest are X and Xhat on 16-byte boundaries with ldq a
+ * multiple of 16 and lde of 4.
+ */
+#define VELORA_CHECKPOINT_BLOCK 32
+int velora_checkpoint_store(const void* X, int x_dtype, int64_t N, int64_t D, int64_t ldx,
+                            int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, void* stream);
+int velora_checkpoint_load(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int64_t D,
+                           void* Xhat, int x_dtype, int64_t ldxhat, void* stream);
+int velora_checkpoint_weight_grad(const void* dY, int dy_dtype, int64_t N, int64_t O, int64_t lddy,
+                                  const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t D,
+                                  void* dW, int dw_dtype, int64_t lddw, int beta, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Softmax cross entropy of a linear head W[V, D] (the model's last layer and its loss), without keeping the logits, which for a
+ * vocabulary of tens of thousands are the largest activation of a step:
+ *     l[n, v] = sum_d X[n, d] W[v, d],   lse[n] = log sum_v exp l[n, v],   loss[n] = lse[n] - l[n, target[n]]
+ * and its backward pass, given dloss[n], the gradient of loss[n] (1 / count for a mean), and the lse that the forward pass returned:
+ *     G[n, v] = dloss[n] (exp(l[n, v] - lse[n]) - [v = target[n]]),   dX = G W,   dW = beta * dW + G^T X
+ * (dX == NULL or dW == NULL: skipped).  `dtype`: X, W and dX; loss, lse, dloss: fp32 [N], dense; target: int64 [N], dense.  Logits,
+ * their maxima and sums and the sums of dX and dW are fp32; G is rounded to bf16 once where X and W are bf16.
+ *   - A token with target < 0 (padding, a prompt) has no part in it: loss, lse and its row of dX are 0, and nothing of its row of X,
+ *     NaN or infinity included, nor its lse and dloss, reaches dW.  Such tokens cost no products.
+ *   - A target >= V is no column: the token's loss is NaN, it has no part in the gradients, and the workspace's status
+ *     word says VELORA_ERR_INVALID_ARG (velora_workspace_status) until velora_workspace_init.
+ *   - N == 0: the loss writes nothing, the backward pass dW = beta * dW.
+ * ws: velora_workspace_bytes(VELORA_OP_HEAD_LOSS or VELORA_OP_HEAD_LOSS_BACKWARD, N, D, V, 1) bytes (| VELORA_OP_F32 for fp32,
+ * | VELORA_OP_ANY_ROWS for bf16 rows of W that are not 16-byte aligned), initialised.  It holds a piece of the vocabulary of the logits or
+ * their gradients; a call also runs in less, in smaller pieces (of 256 columns at least), and the order of dX's sums goes by them.
+ */
+int velora_head_loss(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* target, float* loss, float* lse,
+                     int dtype, int64_t N, int64_t D, int64_t V, void* ws, size_t ws_bytes, void* stream);
+int velora_head_loss_backward(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* target,
+                              const float* lse, const float* dloss, void* dX, int64_t lddx, void* dW, int dw_dtype, int64_t lddw, int beta,
+                              int dtype, int64_t N, int64_t D, int64_t V, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -16,5 +16,7 @@ from .binding import (  # noqa: F401
     velora_dense_product, PRODUCT_A_BT, PRODUCT_A_B, PRODUCT_AT_B,
     velora_weight_grad_p, velora_expand_p,
     velora_host_step_staging_bytes, velora_linear_step_host,
+    velora_checkpoint_store, velora_checkpoint_load, velora_checkpoint_weight_grad, OP_CHECKPOINT_WEIGHT_GRAD, OP_F32, CHECKPOINT_BLOCK,
+    velora_head_loss, velora_head_loss_backward, OP_HEAD_LOSS, OP_HEAD_LOSS_BACKWARD,
 )
 from .memory_model import saved_activation_bytes  # noqa: F401

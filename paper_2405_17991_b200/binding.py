@@ -22,8 +22,11 @@ F32, BF16, FP8_E4M3 = 0, 1, 2
 WG_FACTORED, WG_EXPLICIT = 0, 1
 PRODUCT_A_BT, PRODUCT_A_B, PRODUCT_AT_B = 0, 1, 2
 (OP_INIT_V, OP_WEIGHT_GRAD_FACTORED, OP_WEIGHT_GRAD_EXPLICIT, OP_LINEAR_FORWARD,
- OP_LINEAR_BACKWARD_FACTORED, OP_LINEAR_BACKWARD_EXPLICIT, OP_UPDATE_V, OP_Z8_CALIBRATE) = range(8)
+ OP_LINEAR_BACKWARD_FACTORED, OP_LINEAR_BACKWARD_EXPLICIT, OP_UPDATE_V, OP_Z8_CALIBRATE,
+ OP_CHECKPOINT_WEIGHT_GRAD, OP_HEAD_LOSS, OP_HEAD_LOSS_BACKWARD) = range(11)
 OP_ANY_ROWS = 256                                    # see velora_workspace_bytes
+OP_F32 = 512
+CHECKPOINT_BLOCK = 32
 
 _p, _i64, _int, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t
 
@@ -55,6 +58,12 @@ SIGNATURES = {
                                      _int, _i64, _i64, _i64, _int, _p, _sz, _p]),
     "velora_linear_backward": (_int, [_p, _i64, _p, _i64, _p, _int, _i64, _p, _p, _i64, _p, _int, _i64, _int, _int,
                                       _int, _i64, _i64, _i64, _int, _p, _sz, _p]),
+    "velora_checkpoint_store": (_int, [_p, _int, _i64, _i64, _i64, _p, _i64, _p, _i64, _p]),
+    "velora_checkpoint_load": (_int, [_p, _i64, _p, _i64, _i64, _i64, _p, _int, _i64, _p]),
+    "velora_checkpoint_weight_grad": (_int, [_p, _int, _i64, _i64, _i64, _p, _i64, _p, _i64, _i64, _p, _int, _i64, _int, _p, _sz, _p]),
+    "velora_head_loss": (_int, [_p, _i64, _p, _i64, _p, _p, _p, _int, _i64, _i64, _i64, _p, _sz, _p]),
+    "velora_head_loss_backward": (_int, [_p, _i64, _p, _i64, _p, _p, _p, _p, _i64, _p, _int, _i64, _int,
+                                         _int, _i64, _i64, _i64, _p, _sz, _p]),
 }
 
 
@@ -457,3 +466,131 @@ def velora_expand_p(P: torch.Tensor, v: torch.Tensor, D: int, dW: Optional[torch
     rc = lib().velora_expand_p(pp, ldp, _vec(v), O, D, Dsub, wp, _dt(dW), lddw, beta, _stream(stream))
     _check(rc, "velora_expand_p")
     return dW
+
+
+def _codes(Q: torch.Tensor, E: torch.Tensor):
+    if Q.dtype != torch.int8 or E.dtype != torch.uint8:
+        raise ValueError("Q must be int8 and E uint8")
+    qp, ldq = _mat(Q, "Q")
+    ep, lde = _mat(E, "E")
+    if E.shape != (Q.shape[0], -(-Q.shape[1] // CHECKPOINT_BLOCK)):
+        raise ValueError("E must be [N, ceil(D / %d)] for Q's [N, D]" % CHECKPOINT_BLOCK)
+    return qp, ldq, ep, lde
+
+
+def velora_checkpoint_store(X: torch.Tensor, Q: Optional[torch.Tensor] = None, E: Optional[torch.Tensor] = None, stream=None):
+    """X in 8 bits: codes Q (int8 [N, D]) and block exponents E (uint8 [N, ceil(D / 32)]).  Rows of those allocated here start on
+    16-byte boundaries, where velora_checkpoint_weight_grad is fastest."""
+    xp, ldx = _mat(X, "X")
+    N, D = X.shape
+    blocks = -(-D // CHECKPOINT_BLOCK)
+    if Q is None:
+        Q = torch.empty((N, -(-D // 16) * 16), dtype=torch.int8, device=X.device)[:, :D]
+    if E is None:
+        E = torch.empty((N, -(-blocks // 16) * 16), dtype=torch.uint8, device=X.device)[:, :blocks]
+    if Q.shape != X.shape:
+        raise ValueError("Q must have X's shape")
+    qp, ldq, ep, lde = _codes(Q, E)
+    _check(lib().velora_checkpoint_store(xp, _dt(X), N, D, ldx, qp, ldq, ep, lde, _stream(stream)), "velora_checkpoint_store")
+    return Q, E
+
+
+def velora_checkpoint_load(Q: torch.Tensor, E: torch.Tensor, Xhat: Optional[torch.Tensor] = None,
+                           x_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    qp, ldq, ep, lde = _codes(Q, E)
+    N, D = Q.shape
+    if Xhat is None:
+        Xhat = torch.empty((N, D), dtype=x_dtype, device=Q.device)
+    if Xhat.shape != Q.shape:
+        raise ValueError("Xhat must have Q's shape")
+    xp, ldx = _mat(Xhat, "Xhat")
+    _check(lib().velora_checkpoint_load(qp, ldq, ep, lde, N, D, xp, _dt(Xhat), ldx, _stream(stream)), "velora_checkpoint_load")
+    return Xhat
+
+
+def velora_checkpoint_weight_grad(dY: torch.Tensor, Q: torch.Tensor, E: torch.Tensor, dW: Optional[torch.Tensor] = None,
+                                  dw_dtype=None, beta: int = 0, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """dW = beta * dW + dY^T Xhat with the input kept in 8 bits (velora_checkpoint_store)."""
+    yp, lddy = _mat(dY, "dY")
+    qp, ldq, ep, lde = _codes(Q, E)
+    N, O = dY.shape
+    D = Q.shape[1]
+    if Q.shape[0] != N:
+        raise ValueError("Q must have dY's rows")
+    if dW is None:
+        if beta:
+            raise ValueError("beta = 1 adds to a dW that is passed in")
+        dW = torch.empty((O, D), dtype=dw_dtype or dY.dtype, device=dY.device)
+    if dW.shape != (O, D):
+        raise ValueError("dW must be [O, D]")
+    wp, lddw = _mat(dW, "dW")
+    if ws is None:
+        op = OP_CHECKPOINT_WEIGHT_GRAD | (OP_F32 if dY.dtype == torch.float32 else 0)
+        ws = velora_workspace_alloc(velora_workspace_bytes(op, N, D, O, 1, _odd_rows(dY, yp, lddy)), dY.device)
+    rc = lib().velora_checkpoint_weight_grad(yp, _dt(dY), N, O, lddy, qp, ldq, ep, lde, D, wp, _dt(dW), lddw, beta,
+                                             ws.data_ptr(), ws.numel(), _stream(stream))
+    _check(rc, "velora_checkpoint_weight_grad")
+    return dW
+
+
+def _tokens(t: torch.Tensor, n: int, dtype, name: str) -> int:
+    if t.ndim != 1 or t.shape[0] != n or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s CUDA tensor with one element per token" % (name, dtype))
+    return t.data_ptr()
+
+
+def _head(X: torch.Tensor, W: torch.Tensor):
+    if W.ndim != 2 or X.ndim != 2 or W.shape[1] != X.shape[1] or W.dtype != X.dtype:
+        raise ValueError("W must be [V, D] with X's dtype")
+    return (*_mat(X, "X"), *_mat(W, "W"))
+
+
+def _head_workspace(op: int, X: torch.Tensor, W: torch.Tensor, wp: int, ldw: int) -> torch.Tensor:
+    op |= OP_F32 if X.dtype == torch.float32 else 0
+    return velora_workspace_alloc(velora_workspace_bytes(op, X.shape[0], X.shape[1], W.shape[0], 1, _odd_rows(W, wp, ldw)), X.device)
+
+
+def velora_head_loss(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, loss: Optional[torch.Tensor] = None,
+                     lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """Cross entropy of every token under the linear head W, without the logits: (loss, lse), both fp32 [N].  Tokens with
+    target < 0 have none."""
+    xp, ldx, wp, ldw = _head(X, W)
+    N, D = X.shape
+    V = W.shape[0]
+    tp = _tokens(target, N, torch.int64, "target")
+    if loss is None:
+        loss = torch.empty(N, dtype=torch.float32, device=X.device)
+    if lse is None:
+        lse = torch.empty(N, dtype=torch.float32, device=X.device)
+    lp, sp = _tokens(loss, N, torch.float32, "loss"), _tokens(lse, N, torch.float32, "lse")
+    if ws is None:
+        ws = _head_workspace(OP_HEAD_LOSS, X, W, wp, ldw)
+    rc = lib().velora_head_loss(xp, ldx, wp, ldw, tp, lp, sp, _dt(X), N, D, V, ws.data_ptr(), ws.numel(), _stream(stream))
+    _check(rc, "velora_head_loss")
+    return loss, lse
+
+
+def velora_head_loss_backward(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
+                              dX: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None, need_dX: bool = True,
+                              need_dW: bool = True, dw_dtype=None, beta: int = 0, ws: Optional[torch.Tensor] = None, stream=None):
+    """(dX, dW) of velora_head_loss, given the gradient of every token's loss and the lse it returned."""
+    xp, ldx, wp, ldw = _head(X, W)
+    N, D = X.shape
+    V = W.shape[0]
+    tp, sp, gp = _tokens(target, N, torch.int64, "target"), _tokens(lse, N, torch.float32, "lse"), _tokens(dloss, N, torch.float32, "dloss")
+    if need_dX and dX is None:
+        dX = torch.empty((N, D), dtype=X.dtype, device=X.device)
+    if need_dW and dW is None:
+        if beta:
+            raise ValueError("beta = 1 adds to a dW that is passed in")
+        dW = torch.empty((V, D), dtype=dw_dtype or X.dtype, device=X.device)
+    if (need_dX and (dX.shape != X.shape or dX.dtype != X.dtype)) or (need_dW and dW.shape != W.shape):
+        raise ValueError("dX must be like X, dW of W's shape")
+    dxp, lddx = _mat(dX, "dX") if need_dX else (None, D)
+    dwp, lddw = _mat(dW, "dW") if need_dW else (None, D)
+    if ws is None:
+        ws = _head_workspace(OP_HEAD_LOSS_BACKWARD, X, W, wp, ldw)
+    rc = lib().velora_head_loss_backward(xp, ldx, wp, ldw, tp, sp, gp, dxp, lddx, dwp, _dt(dW) if need_dW else F32, lddw, beta,
+                                         _dt(X), N, D, V, ws.data_ptr(), ws.numel(), _stream(stream))
+    _check(rc, "velora_head_loss_backward")
+    return dX, dW

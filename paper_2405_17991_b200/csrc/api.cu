@@ -1,7 +1,9 @@
 // C-ABI entry points of the VeLoRA library: host-side validation and routing.
 // Every argument check happens here, before any launch.
+#include "checkpoint.cuh"
 #include "common.cuh"
 #include "gemm_tc.cuh"
+#include "head_loss.cuh"
 
 namespace velora {
 
@@ -191,6 +193,31 @@ int check_weight_grad_args(const void* dY, int dy_dtype, int64_t N, int64_t O, i
     return VELORA_OK;
 }
 
+// ---- 8-bit checkpoints ----
+int check_checkpoint(const void* Q, int64_t ldq, const void* E, int64_t lde, int64_t N, int64_t D)
+{
+    if (N < 0 || D < 1) return VELORA_ERR_INVALID_ARG;
+    if (D > (1 << 30) || N > (static_cast<int64_t>(1) << 40)) return VELORA_ERR_UNSUPPORTED;
+    if (N == 0) return VELORA_OK;                        /* an empty batch may carry NULL pointers */
+    if (!Q || !E || ldq < D || lde < ceil_div64(D, VELORA_CHECKPOINT_BLOCK)) return VELORA_ERR_INVALID_ARG;
+    return VELORA_OK;
+}
+
+// Xhat in dY's type, and a packed copy of a bf16 dY whose rows TMA cannot address.
+size_t checkpoint_grad_bytes(int64_t N, int64_t D, int dtype) { return kStatusBytes + align256(static_cast<size_t>(N) * round_up8(D) * dtype_size(dtype)); }
+
+// ---- loss of a linear head ----
+int check_head(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* target, int dtype, int64_t N, int64_t D, int64_t V)
+{
+    if (N < 0 || D < 1 || V < 1) return VELORA_ERR_INVALID_ARG;
+    if (N > (1 << 30) || D > (1 << 30) || V > (1 << 30)) return VELORA_ERR_UNSUPPORTED;
+    if (!valid_dtype(dtype)) return VELORA_ERR_UNSUPPORTED;
+    if (N == 0) return VELORA_OK;
+    if (!X || !W || !target || ldx < D || ldw < D) return VELORA_ERR_INVALID_ARG;
+    if (!elem_aligned(X, dtype) || !elem_aligned(W, dtype) || reinterpret_cast<uintptr_t>(target) % 8) return VELORA_ERR_ALIGNMENT;
+    return VELORA_OK;
+}
+
 }  // namespace
 }  // namespace velora
 
@@ -233,7 +260,7 @@ int velora_workspace_status(const void* ws, void* stream)
     if (cudaMemcpyAsync(&word, ws, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess) return VELORA_ERR_CUDA;
     if (cudaStreamSynchronize(s) != cudaSuccess) return VELORA_ERR_CUDA;
     if (word == 0) return VELORA_OK;
-    return word == VELORA_ERR_DEGENERATE_V ? VELORA_ERR_DEGENERATE_V : VELORA_ERR_TIMEOUT;
+    return word == VELORA_ERR_DEGENERATE_V || word == VELORA_ERR_INVALID_ARG ? word : VELORA_ERR_TIMEOUT;
 }
 
 const char* velora_status_string(int status)
@@ -255,7 +282,8 @@ size_t velora_workspace_bytes(int op, int64_t N, int64_t D, int64_t O, int Dsub)
 {
     if (N < 0 || D < 1 || Dsub < 1 || Dsub > D || Dsub > VELORA_MAX_DSUB) return 0;
     const bool any_rows = (op & VELORA_OP_ANY_ROWS) != 0;
-    switch (op & ~VELORA_OP_ANY_ROWS) {
+    const int dtype = (op & VELORA_OP_F32) != 0 ? VELORA_F32 : VELORA_BF16;
+    switch (op & ~(VELORA_OP_ANY_ROWS | VELORA_OP_F32)) {
         case VELORA_OP_INIT_V: return init_v_workspace_bytes(Dsub);
         case VELORA_OP_WEIGHT_GRAD_FACTORED: return O < 1 ? 0 : factored_bytes(N, D, O, Dsub, true);
         case VELORA_OP_LINEAR_BACKWARD_FACTORED:
@@ -265,6 +293,10 @@ size_t velora_workspace_bytes(int op, int64_t N, int64_t D, int64_t O, int Dsub)
         case VELORA_OP_LINEAR_FORWARD: return kStatusBytes + pack_bytes_if_ragged(N, D, any_rows) + pack_bytes_if_ragged(O, D, any_rows);
         case VELORA_OP_UPDATE_V: return update_v_workspace_bytes(Dsub);
         case VELORA_OP_Z8_CALIBRATE: return z8_calibrate_workspace_bytes(N, D, Dsub);
+        case VELORA_OP_CHECKPOINT_WEIGHT_GRAD:
+            return O < 1 ? 0 : checkpoint_grad_bytes(N, D, dtype) + pack_bytes_if_ragged(N, O, any_rows && dtype == VELORA_BF16);
+        case VELORA_OP_HEAD_LOSS: return O < 1 ? 0 : head_loss_bytes(false, dtype, N, D, O, any_rows);
+        case VELORA_OP_HEAD_LOSS_BACKWARD: return O < 1 ? 0 : head_loss_bytes(true, dtype, N, D, O, any_rows);
         default: return 0;
     }
 }
@@ -603,6 +635,106 @@ int velora_expand_p(const float* P, int64_t ldp, const float* v, int64_t O, int6
     if (!elem_aligned(P, VELORA_F32) || !elem_aligned(v, VELORA_F32) || !elem_aligned(dW, dw_dtype))
         return VELORA_ERR_ALIGNMENT;
     return launch_expand_p(P, 1, 0, ldp, v, O, D, Dsub, dW, dw_dtype, lddw, beta, static_cast<cudaStream_t>(stream));
+}
+
+int velora_checkpoint_store(const void* X, int x_dtype, int64_t N, int64_t D, int64_t ldx,
+                            int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, void* stream)
+{
+    const int rc = check_checkpoint(Q, ldq, E, lde, N, D);
+    if (rc != VELORA_OK) return rc;
+    if (!valid_dtype(x_dtype)) return VELORA_ERR_UNSUPPORTED;
+    if (N == 0) return VELORA_OK;
+    if (!X || ldx < D) return VELORA_ERR_INVALID_ARG;
+    if (!elem_aligned(X, x_dtype)) return VELORA_ERR_ALIGNMENT;
+    return launch_checkpoint_store(X, x_dtype, N, D, ldx, Q, ldq, E, lde, static_cast<cudaStream_t>(stream));
+}
+
+int velora_checkpoint_load(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int64_t D,
+                           void* Xhat, int x_dtype, int64_t ldxhat, void* stream)
+{
+    const int rc = check_checkpoint(Q, ldq, E, lde, N, D);
+    if (rc != VELORA_OK) return rc;
+    if (!valid_dtype(x_dtype)) return VELORA_ERR_UNSUPPORTED;
+    if (N == 0) return VELORA_OK;
+    if (!Xhat || ldxhat < D) return VELORA_ERR_INVALID_ARG;
+    if (!elem_aligned(Xhat, x_dtype)) return VELORA_ERR_ALIGNMENT;
+    return launch_checkpoint_load(Q, ldq, E, lde, N, D, Xhat, x_dtype, ldxhat, static_cast<cudaStream_t>(stream));
+}
+
+int velora_checkpoint_weight_grad(const void* dY, int dy_dtype, int64_t N, int64_t O, int64_t lddy,
+                                  const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t D,
+                                  void* dW, int dw_dtype, int64_t lddw, int beta, void* ws, size_t ws_bytes, void* stream)
+{
+    if (O < 1 || O > (1 << 30) || !dW || lddw < D || (beta != 0 && beta != 1)) return VELORA_ERR_INVALID_ARG;
+    int rc = check_checkpoint(Q, ldq, E, lde, N, D);
+    if (rc != VELORA_OK) return rc;
+    if (!valid_dtype(dy_dtype) || !valid_dtype(dw_dtype)) return VELORA_ERR_UNSUPPORTED;
+    if (!elem_aligned(dW, dw_dtype)) return VELORA_ERR_ALIGNMENT;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (N == 0) {                                            /* empty sum: dW = beta * dW */
+        if (beta) return VELORA_OK;
+        const size_t es = dtype_size(dw_dtype);
+        return cudaMemset2DAsync(dW, static_cast<size_t>(lddw) * es, 0, static_cast<size_t>(D) * es,
+                                 static_cast<size_t>(O), s) == cudaSuccess ? VELORA_OK : VELORA_ERR_CUDA;
+    }
+    if (!dY || lddy < O) return VELORA_ERR_INVALID_ARG;
+    if (!elem_aligned(dY, dy_dtype)) return VELORA_ERR_ALIGNMENT;
+    const size_t used = checkpoint_grad_bytes(N, D, dy_dtype);
+    if (!ws || ws_bytes < used) return VELORA_ERR_WORKSPACE;
+    if (!aligned16(ws)) return VELORA_ERR_ALIGNMENT;
+    Operand y{dY, lddy, N, O};
+    if (dy_dtype == VELORA_BF16) {
+        Operand* ops[1] = {&y};
+        rc = pack_operands(ops, 1, ws, ws_bytes, used, s);
+        if (rc != VELORA_OK) return rc;
+    }
+    char* xhat = static_cast<char*>(ws) + kStatusBytes;
+    const int64_t ldxh = round_up8(D);
+    rc = launch_checkpoint_load(Q, ldq, E, lde, N, D, xhat, dy_dtype, ldxh, s);
+    if (rc != VELORA_OK) return rc;
+    rc = launch_gemm_tc(GEMM_TN_MN_MN, y.p, y.ld, xhat, ldxh, dW, dw_dtype, lddw, beta, O, D, N, dy_dtype, static_cast<int*>(ws), s);
+    if (rc != VELORA_ERR_UNSUPPORTED) return rc;
+    return launch_gemm_simt(dY, dy_dtype, 1, lddy, xhat, dy_dtype, 1, ldxh, dW, dw_dtype, lddw, beta, O, D, N, s);
+}
+
+int velora_head_loss(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* target, float* loss, float* lse,
+                     int dtype, int64_t N, int64_t D, int64_t V, void* ws, size_t ws_bytes, void* stream)
+{
+    int rc = check_head(X, ldx, W, ldw, target, dtype, N, D, V);
+    if (rc != VELORA_OK) return rc;
+    if (N == 0) return VELORA_OK;
+    if (!loss || !lse) return VELORA_ERR_INVALID_ARG;
+    if (!elem_aligned(loss, VELORA_F32) || !elem_aligned(lse, VELORA_F32)) return VELORA_ERR_ALIGNMENT;
+    if (!ws) return VELORA_ERR_WORKSPACE;
+    if (!aligned16(ws)) return VELORA_ERR_ALIGNMENT;
+    return launch_head_loss(HeadArgs{X, ldx, W, ldw, target, dtype, N, D, V, static_cast<char*>(ws), ws_bytes, static_cast<cudaStream_t>(stream)}, loss, lse);
+}
+
+int velora_head_loss_backward(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* target,
+                              const float* lse, const float* dloss, void* dX, int64_t lddx, void* dW, int dw_dtype, int64_t lddw, int beta,
+                              int dtype, int64_t N, int64_t D, int64_t V, void* ws, size_t ws_bytes, void* stream)
+{
+    int rc = check_head(X, ldx, W, ldw, target, dtype, N, D, V);
+    if (rc != VELORA_OK) return rc;
+    if (dW) {
+        if (!valid_dtype(dw_dtype)) return VELORA_ERR_UNSUPPORTED;
+        if (lddw < D || (beta != 0 && beta != 1)) return VELORA_ERR_INVALID_ARG;
+        if (!elem_aligned(dW, dw_dtype)) return VELORA_ERR_ALIGNMENT;
+    }
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (N == 0) {
+        if (!dW || beta) return VELORA_OK;
+        const size_t es = dtype_size(dw_dtype);
+        return cudaMemset2DAsync(dW, static_cast<size_t>(lddw) * es, 0, static_cast<size_t>(D) * es,
+                                 static_cast<size_t>(V), s) == cudaSuccess ? VELORA_OK : VELORA_ERR_CUDA;
+    }
+    if (!lse || !dloss || (dX && lddx < D)) return VELORA_ERR_INVALID_ARG;
+    if (!elem_aligned(lse, VELORA_F32) || !elem_aligned(dloss, VELORA_F32) || (dX && !elem_aligned(dX, dtype))) return VELORA_ERR_ALIGNMENT;
+    if (!ws) return VELORA_ERR_WORKSPACE;
+    if (!aligned16(ws)) return VELORA_ERR_ALIGNMENT;
+    if (!dX && !dW) return VELORA_OK;
+    return launch_head_loss_backward(HeadArgs{X, ldx, W, ldw, target, dtype, N, D, V, static_cast<char*>(ws), ws_bytes, s}, lse, dloss, dX, lddx,
+                                     dW, dw_dtype, lddw, beta);
 }
 
 }  // extern "C"

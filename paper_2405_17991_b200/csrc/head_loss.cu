@@ -1,0 +1,394 @@
+// Softmax cross entropy of a linear head without its logits, and its gradients.
+//   l[n, v] = sum_d X[n, d] W[v, d],  lse[n] = log sum_v exp l[n, v],  loss[n] = lse[n] - l[n, t[n]]
+//   G[n, v] = g[n] (exp(l[n, v] - lse[n]) - [v = t[n]]),   dX = G W,   dW = beta dW + G^T X
+// The logits exist a piece of the vocabulary at a time.  Tokens without a target have no part in any of it; they are moved behind the
+// others and their rows of X taken as zeros, so nothing that stands there (a NaN of an unused buffer) can reach dW through 0 * NaN.
+#include "head_loss.cuh"
+
+#include "gemm_tc.cuh"
+
+namespace velora {
+
+namespace {
+
+constexpr int kRowThreads = 256;
+constexpr int64_t kPieceElements = 1 << 24;         // of logits that exist at a time, where the workspace has the room
+constexpr int kPieceStep = 256;                     // pieces are multiples of this
+
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+int64_t round_up(int64_t x, int64_t to) { return ceil_div64(x, to) * to; }
+
+// The arrays in front of the piece.
+HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D)
+{
+    HeadLayout l{};
+    const size_t n = static_cast<size_t>(N);
+    size_t at = kStatusBytes;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += up256(bytes);
+        return here;
+    };
+    l.ldx = round_up(D, 8);
+    l.live = take(4);
+    l.order = take(4 * n);
+    l.target = take(4 * n);
+    if (backward) {
+        l.scale = take(4 * n);
+        l.lse = take(4 * n);
+        l.sum = take(n * static_cast<size_t>(l.ldx) * 4);
+    } else {
+        l.at_target = take(4 * n);
+        l.running = take(8 * n);
+    }
+    l.x = take(n * static_cast<size_t>(l.ldx) * dtype_size(dtype));
+    l.piece = at;
+    return l;
+}
+
+size_t piece_column_bytes(int64_t N) { return static_cast<size_t>(N) * 4; }
+
+int64_t wanted_piece(int64_t N, int64_t V)
+{
+    int64_t cols = kPieceElements / (N < 1 ? 1 : N) / kPieceStep * kPieceStep;
+    if (cols < 4 * kPieceStep) cols = 4 * kPieceStep;
+    const int64_t all = round_up(V, kPieceStep);
+    return cols < all ? cols : all;
+}
+
+// As many columns a piece as there is room for.
+int head_layout(HeadLayout* l, bool backward, const HeadArgs& a)
+{
+    *l = head_front(backward, a.dtype, a.N, a.D);
+    if (a.ws_bytes < l->piece) return VELORA_ERR_WORKSPACE;
+    const int64_t fit = static_cast<int64_t>((a.ws_bytes - l->piece) / piece_column_bytes(a.N)) / kPieceStep * kPieceStep;
+    const int64_t want = wanted_piece(a.N, a.V);
+    l->piece_cols = fit < want ? fit : want;
+    return l->piece_cols < kPieceStep ? VELORA_ERR_WORKSPACE : VELORA_OK;
+}
+
+// ---- rows in order of having a target ----
+// Every CTA counts all targets (8 bytes a token, from L2) rather than wait for another CTA's count, then moves its own rows.
+struct RowsArgs {
+    const void* X;
+    int64_t ldx;
+    const int64_t* target;
+    const float* dloss;             // backward only
+    const float* lse;
+    int N, V, D, rows_per_cta;
+    int* live;
+    int* order;
+    int* target_out;
+    float* scale_out;
+    float* lse_out;
+    void* x_out;
+    int64_t ldx_out;
+    int* status;
+};
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kRowThreads)
+head_rows_kernel(const RowsArgs a)
+{
+    __shared__ int counts[2];
+    __shared__ int warp_live[kRowThreads / 32];
+    __shared__ int row_to[kRowThreads];               // where a row goes; negative: -1 - that, and zeros are written
+    pdl_wait();
+    pdl_trigger();
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+    const int r0 = blockIdx.x * a.rows_per_cta, r1 = min(a.N, r0 + a.rows_per_cta);
+    if (t < 2) counts[t] = 0;
+    __syncthreads();
+    int before = 0, total = 0;
+    for (int i0 = 0; i0 < a.N; i0 += kRowThreads * 8) {
+        int64_t v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = i0 + j * kRowThreads + t;
+            v[j] = i < a.N ? a.target[i] : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int is = v[j] >= 0 && v[j] < a.V;
+            total += is;
+            before += is && i0 + j * kRowThreads + t < r0;
+        }
+    }
+    before = __reduce_add_sync(0xffffffffu, before);
+    total = __reduce_add_sync(0xffffffffu, total);
+    if (lane == 0) {
+        atomicAdd(&counts[0], before);
+        atomicAdd(&counts[1], total);
+    }
+    __syncthreads();
+    before = counts[0];
+    total = counts[1];
+    if (blockIdx.x == 0 && t == 0) *a.live = total;
+    for (int b0 = r0; b0 < r1; b0 += kRowThreads) {
+        const int n = b0 + t;
+        const int64_t v = n < r1 ? a.target[n] : -1;
+        const bool is = v >= 0 && v < a.V;
+        const unsigned votes = __ballot_sync(0xffffffffu, is);
+        if (lane == 0) warp_live[warp] = __popc(votes);
+        __syncthreads();
+        int first = before, all = 0;
+        for (int w = 0; w < kRowThreads / 32; ++w) {
+            if (w < warp) first += warp_live[w];
+            all += warp_live[w];
+        }
+        first += __popc(votes & ((1u << lane) - 1u));              // live rows before this one
+        if (n < r1) {
+            const int to = is ? first : total + (n - first);
+            row_to[t] = is ? to : -1 - to;
+            a.order[to] = n;
+            a.target_out[to] = is ? static_cast<int>(v) : (v < 0 ? -1 : -2);
+            if (a.scale_out) {
+                a.scale_out[to] = is ? a.dloss[n] : 0.f;
+                a.lse_out[to] = is ? a.lse[n] : 0.f;
+            }
+            if (v >= a.V && a.status) atomicCAS(a.status, 0, VELORA_ERR_INVALID_ARG);
+        }
+        __syncthreads();
+        for (int i = warp; i < min(kRowThreads, r1 - b0); i += kRowThreads / 32) {
+            const int code = row_to[i];
+            const bool zero = code < 0;
+            const T* src = static_cast<const T*>(a.X) + static_cast<int64_t>(b0 + i) * a.ldx;
+            T* dst = static_cast<T*>(a.x_out) + static_cast<int64_t>(zero ? -1 - code : code) * a.ldx_out;
+            if (VEC) {
+                constexpr int per = 16 / sizeof(T);
+                const int chunks = a.D / per;                      // D is a multiple of 8
+#pragma unroll 4
+                for (int c = lane; c < chunks; c += 32)
+                    reinterpret_cast<uint4*>(dst)[c] = ld_stream_if(src + c * per, !zero);
+            } else {
+                for (int c = lane; c < a.ldx_out; c += 32) Elem<T>::store(dst + c, zero || c >= a.D ? 0.f : Elem<T>::load(src + c));
+            }
+        }
+        before += all;
+        __syncthreads();
+    }
+}
+
+int launch_rows(const HeadArgs& a, const HeadLayout& l, const float* lse, const float* dloss)
+{
+    DeviceInfo di;
+    const int rc = device_info(&di);
+    if (rc != VELORA_OK) return rc;
+    RowsArgs r{};
+    r.X = a.X;
+    r.ldx = a.ldx;
+    r.target = a.target;
+    r.N = static_cast<int>(a.N);
+    r.V = static_cast<int>(a.V);
+    r.D = static_cast<int>(a.D);
+    r.live = reinterpret_cast<int*>(a.ws + l.live);
+    r.order = reinterpret_cast<int*>(a.ws + l.order);
+    r.target_out = reinterpret_cast<int*>(a.ws + l.target);
+    if (dloss) {
+        r.dloss = dloss;
+        r.lse = lse;
+        r.scale_out = reinterpret_cast<float*>(a.ws + l.scale);
+        r.lse_out = reinterpret_cast<float*>(a.ws + l.lse);
+    }
+    r.x_out = a.ws + l.x;
+    r.ldx_out = l.ldx;
+    r.status = reinterpret_cast<int*>(a.ws);
+    // Eight rows a CTA (one a warp) as long as that leaves no more than four CTAs per SM.
+    const int64_t most = static_cast<int64_t>(di.sm_count) * 4;
+    r.rows_per_cta = static_cast<int>(round_up(ceil_div64(a.N, most), 8));
+    const dim3 grid(static_cast<unsigned>(ceil_div64(a.N, r.rows_per_cta)));
+    const bool vec = a.D % 8 == 0 && aligned16(a.X) && (a.ldx * dtype_size(a.dtype)) % 16 == 0;
+    if (a.dtype == VELORA_BF16)
+        return vec ? launch_chained(head_rows_kernel<__nv_bfloat16, true>, grid, kRowThreads, 0, a.stream, r)
+                   : launch_chained(head_rows_kernel<__nv_bfloat16, false>, grid, kRowThreads, 0, a.stream, r);
+    return vec ? launch_chained(head_rows_kernel<float, true>, grid, kRowThreads, 0, a.stream, r)
+               : launch_chained(head_rows_kernel<float, false>, grid, kRowThreads, 0, a.stream, r);
+}
+
+__device__ __forceinline__ float warp_max(float x)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+    return x;
+}
+__device__ __forceinline__ float warp_sum(float x)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+
+// A row's loss and log sum exp to where its token is.
+__device__ __forceinline__ void write_loss(float* loss, float* lse, int n, int target, float m, float s, float at_target)
+{
+    const float l = m + logf(s);
+    loss[n] = target >= 0 ? l - at_target : (target == -1 ? 0.f : __int_as_float(0x7fc00000));
+    lse[n] = target >= 0 ? l : 0.f;
+}
+
+// A warp per row takes the piece's maximum, then its exponentials, into what the pieces before have left; behind the last one the loss.
+__global__ void __launch_bounds__(kRowThreads)
+head_stats_kernel(const float* logits, int64_t ld, int cols, int v0, int N, const int* live, const int* order, const int* target, float* at_target,
+                  float2* running, int first, int last, float* loss, float* lse)
+{
+    pdl_wait();
+    pdl_trigger();
+    const int row = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (row >= N) return;
+    const int t = target[row];
+    float2 ms = make_float2(0.f, 1.f);
+    float hit = 0.f;
+    if (row < *live) {
+        const float* l = logits + row * ld;
+        float m = -INFINITY;
+        for (int c = lane; c < cols; c += 32) m = fmaxf(m, l[c]);
+        m = warp_max(m);
+        float before = 0.f;
+        if (!first) {
+            const float2 old = running[row];
+            const float both = fmaxf(m, old.x);
+            before = old.y * expf(old.x - both);
+            m = both;
+            hit = at_target[row];
+        }
+        float s = 0.f;
+        for (int c = lane; c < cols; c += 32) s += expf(l[c] - m);
+        ms = make_float2(m, warp_sum(s) + before);
+        if (t >= v0 && t < v0 + cols) hit = l[t - v0];
+        __syncwarp();
+        if (lane == 0) {
+            running[row] = ms;
+            at_target[row] = hit;
+        }
+    }
+    if (last && lane == 0) write_loss(loss, lse, order[row], t, ms.x, ms.y, hit);
+}
+
+// Logits to their gradients, in place.  GT = bf16: packed to the front of the row's bytes, which the warp has read by then.
+template <typename GT>
+__global__ void __launch_bounds__(kRowThreads)
+head_gradient_kernel(float* logits, int64_t ld, int cols, int v0, int N, const int* target, const float* scale, const float* lse)
+{
+    pdl_wait();
+    pdl_trigger();
+    const int row = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (row >= N) return;
+    const float* l = logits + row * ld;
+    GT* out = reinterpret_cast<GT*>(logits + row * ld);
+    const int t = target[row] - v0;
+    const bool is = target[row] >= 0;
+    const float g = scale[row], z = lse[row];
+    for (int c0 = 0; c0 < cols; c0 += 32) {
+        const int c = c0 + lane;
+        float x = 0.f;
+        if (c < cols && is) x = g * (expf(l[c] - z) - (c == t ? 1.f : 0.f));
+        __syncwarp();
+        if (c < cols) Elem<GT>::store(out + c, x);
+        __syncwarp();
+    }
+}
+
+// dX from its fp32 sums, rows back to their tokens.
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads)
+head_rows_back_kernel(const float* sum, int64_t ld, int N, int D, const int* live, const int* order, T* dX, int64_t lddx)
+{
+    pdl_wait();
+    pdl_trigger();
+    const int row = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (row >= N) return;
+    T* dst = dX + order[row] * lddx;
+    const bool is = row < *live;
+    for (int c = lane; c < D; c += 32) Elem<T>::store(dst + c, is ? sum[row * ld + c] : 0.f);
+}
+
+// C = beta C + op(A) op(B): the tensor cores where they take the operands.
+int product(int kind, const void* A, int a_dtype, int64_t lda, const void* B, int b_dtype, int64_t ldb, void* C, int c_dtype, int64_t ldc, int beta,
+            int64_t M, int64_t N, int64_t K, int* status, cudaStream_t stream)
+{
+    if (a_dtype == b_dtype) {
+        const int rc = launch_gemm_tc(kind, A, lda, B, ldb, C, c_dtype, ldc, beta, M, N, K, a_dtype, status, stream);
+        if (rc != VELORA_ERR_UNSUPPORTED) return rc;
+    }
+    const bool a_t = kind == GEMM_TN_MN_MN, b_t = kind == GEMM_NT_K_K;
+    return launch_gemm_simt(A, a_dtype, a_t ? 1 : lda, a_t ? lda : 1, B, b_dtype, b_t ? ldb : 1, b_t ? 1 : ldb, C, c_dtype, ldc, beta, M, N, K, stream);
+}
+
+}  // namespace
+
+size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool any_rows)
+{
+    if (N < 1) return kStatusBytes;
+    (void)any_rows;
+    return head_front(backward, dtype, N, D).piece + up256(piece_column_bytes(N) * static_cast<size_t>(wanted_piece(N, V)));
+}
+
+int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
+{
+    HeadLayout l;
+    int rc = head_layout(&l, false, a);
+    if (rc != VELORA_OK) return rc;
+    rc = launch_rows(a, l, nullptr, nullptr);
+    if (rc != VELORA_OK) return rc;
+    int* status = reinterpret_cast<int*>(a.ws);
+    const dim3 grid(static_cast<unsigned>(ceil_div64(a.N, kRowThreads / 32)));
+    float* piece = reinterpret_cast<float*>(a.ws + l.piece);
+    for (int64_t v0 = 0; v0 < a.V; v0 += l.piece_cols) {
+        const int64_t cols = a.V - v0 < l.piece_cols ? a.V - v0 : l.piece_cols;
+        const char* W = static_cast<const char*>(a.W) + static_cast<size_t>(v0) * a.ldw * dtype_size(a.dtype);
+        rc = product(GEMM_NT_K_K, a.ws + l.x, a.dtype, l.ldx, W, a.dtype, a.ldw, piece, VELORA_F32, l.piece_cols, 0, a.N, cols, a.D, status, a.stream);
+        if (rc != VELORA_OK) return rc;
+        rc = launch_chained(head_stats_kernel, grid, kRowThreads, 0, a.stream, piece, l.piece_cols, static_cast<int>(cols), static_cast<int>(v0),
+                            static_cast<int>(a.N), reinterpret_cast<int*>(a.ws + l.live), reinterpret_cast<int*>(a.ws + l.order),
+                            reinterpret_cast<int*>(a.ws + l.target), reinterpret_cast<float*>(a.ws + l.at_target),
+                            reinterpret_cast<float2*>(a.ws + l.running), v0 == 0 ? 1 : 0, v0 + cols == a.V ? 1 : 0, loss, lse);
+        if (rc != VELORA_OK) return rc;
+    }
+    return VELORA_OK;
+}
+
+int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* dloss, void* dX, int64_t lddx,
+                              void* dW, int dw_dtype, int64_t lddw, int beta)
+{
+    HeadLayout l;
+    int rc = head_layout(&l, true, a);
+    if (rc != VELORA_OK) return rc;
+    rc = launch_rows(a, l, lse, dloss);
+    if (rc != VELORA_OK) return rc;
+    int* status = reinterpret_cast<int*>(a.ws);
+    const dim3 grid(static_cast<unsigned>(ceil_div64(a.N, kRowThreads / 32)));
+    float* piece = reinterpret_cast<float*>(a.ws + l.piece);
+    // Gradients of the logits are rounded to bf16 once where the tensor cores take W as bf16: 2^-9 of each, independent of one another.
+    const bool g_bf16 = a.dtype == VELORA_BF16 && tc_operand_ok(a.W, a.ldw);
+    const int g_dtype = g_bf16 ? VELORA_BF16 : VELORA_F32;
+    const int64_t ldg = g_bf16 ? 2 * l.piece_cols : l.piece_cols;
+    for (int64_t v0 = 0; v0 < a.V; v0 += l.piece_cols) {
+        const int64_t cols = a.V - v0 < l.piece_cols ? a.V - v0 : l.piece_cols;
+        const char* W = static_cast<const char*>(a.W) + static_cast<size_t>(v0) * a.ldw * dtype_size(a.dtype);
+        rc = product(GEMM_NT_K_K, a.ws + l.x, a.dtype, l.ldx, W, a.dtype, a.ldw, piece, VELORA_F32, l.piece_cols, 0, a.N, cols, a.D, status, a.stream);
+        if (rc != VELORA_OK) return rc;
+        rc = launch_chained(g_bf16 ? head_gradient_kernel<__nv_bfloat16> : head_gradient_kernel<float>, grid, kRowThreads, 0, a.stream, piece, l.piece_cols,
+                            static_cast<int>(cols), static_cast<int>(v0), static_cast<int>(a.N), reinterpret_cast<int*>(a.ws + l.target),
+                            reinterpret_cast<float*>(a.ws + l.scale), reinterpret_cast<float*>(a.ws + l.lse));
+        if (rc != VELORA_OK) return rc;
+        if (dW) {
+            char* dw = static_cast<char*>(dW) + static_cast<size_t>(v0) * lddw * dtype_size(dw_dtype);
+            rc = product(GEMM_TN_MN_MN, piece, g_dtype, ldg, a.ws + l.x, a.dtype, l.ldx, dw, dw_dtype, lddw, beta, cols, a.D, a.N, status, a.stream);
+            if (rc != VELORA_OK) return rc;
+        }
+        if (dX) {
+            rc = product(GEMM_NN_K_MN, piece, g_dtype, ldg, W, a.dtype, a.ldw, a.ws + l.sum, VELORA_F32, l.ldx, v0 > 0 ? 1 : 0, a.N, a.D, cols, status, a.stream);
+            if (rc != VELORA_OK) return rc;
+        }
+    }
+    if (!dX) return VELORA_OK;
+    const float* sum = reinterpret_cast<float*>(a.ws + l.sum);
+    const int n = static_cast<int>(a.N), d = static_cast<int>(a.D);
+    int* live = reinterpret_cast<int*>(a.ws + l.live);
+    int* order = reinterpret_cast<int*>(a.ws + l.order);
+    if (a.dtype == VELORA_BF16)
+        return launch_chained(head_rows_back_kernel<__nv_bfloat16>, grid, kRowThreads, 0, a.stream, sum, l.ldx, n, d, live, order, static_cast<__nv_bfloat16*>(dX), lddx);
+    return launch_chained(head_rows_back_kernel<float>, grid, kRowThreads, 0, a.stream, sum, l.ldx, n, d, live, order, static_cast<float*>(dX), lddx);
+}
+
+}  // namespace velora

@@ -1,0 +1,44 @@
+// Softmax cross entropy of a linear head without its logits, and its gradients: layout of the workspace and the pieces.
+#pragma once
+
+#include "common.cuh"
+
+namespace velora {
+
+// Where things lie in a call's workspace, in bytes from its start.  Rows of the arrays below are the tokens in another order: those with
+// a target first, in their own order, then the others; `order` says which token a row is.
+struct HeadLayout {
+    size_t live;            // int32: how many rows have a target
+    size_t order;           // int32[N]
+    size_t target;          // int32[N]: column, -1 without one, -2 where it is no column
+    size_t scale, lse;      // fp32[N]: gradient of the row's loss, log sum exp (backward)
+    size_t at_target;       // fp32[N]: logit of the target (forward)
+    size_t running;         // float2[N] or float2[tiles][N]: maximum, and the sum of exponentials relative to it (forward)
+    size_t x;               // the rows of X, pitch ldx elements; zeros for rows without a target
+    size_t w;               // W with a pitch that tensor maps take, where W's own is not
+    size_t sum;             // fp32, pitch ldx: dX so far (backward)
+    size_t piece;           // a piece of the vocabulary: logits or their gradient, pitch `piece_cols` elements
+    int64_t ldx, piece_cols;
+    size_t bytes;
+};
+
+struct HeadArgs {
+    const void* X;
+    int64_t ldx;
+    const void* W;
+    int64_t ldw;
+    const int64_t* target;
+    int dtype;
+    int64_t N, D, V;
+    char* ws;
+    size_t ws_bytes;
+    cudaStream_t stream;
+};
+
+// What velora_workspace_bytes reports.
+size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool any_rows);
+int launch_head_loss(const HeadArgs& a, float* loss, float* lse);
+int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* dloss, void* dX, int64_t lddx,
+                              void* dW, int dw_dtype, int64_t lddw, int beta);
+
+}  // namespace velora
