@@ -43,7 +43,7 @@ bool tc_operand_ok(const void* p, int64_t ld_elems)
 
 int launch_gemm_tc(int kind, const void* A, int64_t lda, const void* B, int64_t ldb,
                    void* C, int c_dtype, int64_t ldc, int beta,
-                   int64_t Mdim, int64_t Ndim, int64_t Kdim, int in_dtype, int* status, cudaStream_t stream)
+                   int64_t Mdim, int64_t Ndim, int64_t Kdim, int in_dtype, int* status, cudaStream_t stream, const int* live)
 {
     if (in_dtype == VELORA_F32 && c_dtype == VELORA_F32)
         return launch_gemm_f32_tc(kind, A, lda, B, ldb, C, ldc, beta, Mdim, Ndim, Kdim, status, stream);
@@ -61,7 +61,7 @@ int launch_gemm_tc(int kind, const void* A, int64_t lda, const void* B, int64_t 
     if (rc != VELORA_OK) return rc;
     GemmShape shape = gemm_shape(Mdim, Ndim, Kdim, di.sm_count, false);
     if (shape.pair) {
-        const int prc = launch_gemm_tc_pair(kind, A, lda, B, ldb, C, c_dtype, ldc, beta, Mdim, Ndim, Kdim, in_dtype, status, stream);
+        const int prc = launch_gemm_tc_pair(kind, A, lda, B, ldb, C, c_dtype, ldc, beta, Mdim, Ndim, Kdim, in_dtype, status, stream, live);
         if (prc != VELORA_ERR_UNSUPPORTED) return prc;
         shape = GemmShape{false, 256, 1};
     }

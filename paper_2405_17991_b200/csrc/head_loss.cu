@@ -18,8 +18,10 @@ constexpr int kPieceStep = 256;                     // pieces are multiples of t
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 int64_t round_up(int64_t x, int64_t to) { return ceil_div64(x, to) * to; }
 
-// The arrays in front of the piece.
-HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D)
+size_t piece_element(int dtype, bool backward) { return dtype == VELORA_BF16 && backward ? 2 : 4; }
+
+// The arrays in front of the piece; bf16 needs none for the forward pass.
+HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool pack_w)
 {
     HeadLayout l{};
     const size_t n = static_cast<size_t>(N);
@@ -39,14 +41,13 @@ HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D)
         l.sum = take(n * static_cast<size_t>(l.ldx) * 4);
     } else {
         l.at_target = take(4 * n);
-        l.running = take(8 * n);
+        l.running = take(8 * n * (dtype == VELORA_BF16 ? 2 * static_cast<size_t>(ceil_div64(V, 256)) : 1));
     }
     l.x = take(n * static_cast<size_t>(l.ldx) * dtype_size(dtype));
+    if (pack_w) l.w = take(pack_rows_bytes(V, D));
     l.piece = at;
     return l;
 }
-
-size_t piece_column_bytes(int64_t N) { return static_cast<size_t>(N) * 4; }
 
 int64_t wanted_piece(int64_t N, int64_t V)
 {
@@ -59,9 +60,10 @@ int64_t wanted_piece(int64_t N, int64_t V)
 // As many columns a piece as there is room for.
 int head_layout(HeadLayout* l, bool backward, const HeadArgs& a)
 {
-    *l = head_front(backward, a.dtype, a.N, a.D);
+    *l = head_front(backward, a.dtype, a.N, a.D, a.V, a.dtype == VELORA_BF16 && !tc_operand_ok(a.W, a.ldw));
     if (a.ws_bytes < l->piece) return VELORA_ERR_WORKSPACE;
-    const int64_t fit = static_cast<int64_t>((a.ws_bytes - l->piece) / piece_column_bytes(a.N)) / kPieceStep * kPieceStep;
+    if (a.dtype == VELORA_BF16 && !backward) return VELORA_OK;
+    const int64_t fit = static_cast<int64_t>((a.ws_bytes - l->piece) / (piece_element(a.dtype, backward) * static_cast<size_t>(a.N))) / kPieceStep * kPieceStep;
     const int64_t want = wanted_piece(a.N, a.V);
     l->piece_cols = fit < want ? fit : want;
     return l->piece_cols < kPieceStep ? VELORA_ERR_WORKSPACE : VELORA_OK;
@@ -264,8 +266,41 @@ head_stats_kernel(const float* logits, int64_t ld, int cols, int v0, int N, cons
     if (last && lane == 0) write_loss(loss, lse, order[row], t, ms.x, ms.y, hit);
 }
 
-// Logits to their gradients, in place.  GT = bf16: packed to the front of the row's bytes, which the warp has read by then.
-template <typename GT>
+// A block takes 32 rows: eight slices of their parts (128 columns each), then the eight together.
+__global__ void __launch_bounds__(kRowThreads)
+head_merge_kernel(const float2* running, int parts, int N, const int* live, const int* order, const int* target, const float* at_target, float* loss, float* lse)
+{
+    __shared__ float2 slice[kRowThreads / 32][32];
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
+    float m = -INFINITY, s = 0.f;
+    if (row < *live) {
+        for (int p = warp; p < parts; p += kRowThreads / 32) {
+            const float2 x = running[static_cast<int64_t>(p) * N + row];
+            const float both = x.x > m ? x.x : (x.x == x.x ? m : x.x);      // a NaN stays one
+            const float ref = both == -INFINITY ? 0.f : both;
+            s = s * expf(m - ref) + x.y * expf(x.x - ref);
+            m = both;
+        }
+    }
+    slice[warp][lane] = make_float2(m, s);
+    __syncthreads();
+    if (warp != 0 || row >= N) return;
+    m = -INFINITY;
+    bool nan = false;
+    for (int w = 0; w < kRowThreads / 32; ++w) {
+        m = fmaxf(m, slice[w][lane].x);
+        nan |= slice[w][lane].x != slice[w][lane].x;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    s = nan ? __int_as_float(0x7fc00000) : 0.f;
+    for (int w = 0; w < kRowThreads / 32; ++w) s += slice[w][lane].y * expf(slice[w][lane].x - ref);
+    const int t = target[row];
+    write_loss(loss, lse, order[row], t, m, s, t >= 0 ? at_target[row] : 0.f);
+}
+
+// Logits to their gradients, in place.
 __global__ void __launch_bounds__(kRowThreads)
 head_gradient_kernel(float* logits, int64_t ld, int cols, int v0, int N, const int* target, const float* scale, const float* lse)
 {
@@ -273,19 +308,11 @@ head_gradient_kernel(float* logits, int64_t ld, int cols, int v0, int N, const i
     pdl_trigger();
     const int row = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (row >= N) return;
-    const float* l = logits + row * ld;
-    GT* out = reinterpret_cast<GT*>(logits + row * ld);
+    float* l = logits + row * ld;
     const int t = target[row] - v0;
     const bool is = target[row] >= 0;
     const float g = scale[row], z = lse[row];
-    for (int c0 = 0; c0 < cols; c0 += 32) {
-        const int c = c0 + lane;
-        float x = 0.f;
-        if (c < cols && is) x = g * (expf(l[c] - z) - (c == t ? 1.f : 0.f));
-        __syncwarp();
-        if (c < cols) Elem<GT>::store(out + c, x);
-        __syncwarp();
-    }
+    for (int c = lane; c < cols; c += 32) l[c] = is ? g * (expf(l[c] - z) - (c == t ? 1.f : 0.f)) : 0.f;
 }
 
 // dX from its fp32 sums, rows back to their tokens.
@@ -304,10 +331,10 @@ head_rows_back_kernel(const float* sum, int64_t ld, int N, int D, const int* liv
 
 // C = beta C + op(A) op(B): the tensor cores where they take the operands.
 int product(int kind, const void* A, int a_dtype, int64_t lda, const void* B, int b_dtype, int64_t ldb, void* C, int c_dtype, int64_t ldc, int beta,
-            int64_t M, int64_t N, int64_t K, int* status, cudaStream_t stream)
+            int64_t M, int64_t N, int64_t K, int* status, const int* live, cudaStream_t stream)
 {
     if (a_dtype == b_dtype) {
-        const int rc = launch_gemm_tc(kind, A, lda, B, ldb, C, c_dtype, ldc, beta, M, N, K, a_dtype, status, stream);
+        const int rc = launch_gemm_tc(kind, A, lda, B, ldb, C, c_dtype, ldc, beta, M, N, K, a_dtype, status, stream, live);
         if (rc != VELORA_ERR_UNSUPPORTED) return rc;
     }
     const bool a_t = kind == GEMM_TN_MN_MN, b_t = kind == GEMM_NT_K_K;
@@ -319,29 +346,74 @@ int product(int kind, const void* A, int a_dtype, int64_t lda, const void* B, in
 size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool any_rows)
 {
     if (N < 1) return kStatusBytes;
-    (void)any_rows;
-    return head_front(backward, dtype, N, D).piece + up256(piece_column_bytes(N) * static_cast<size_t>(wanted_piece(N, V)));
+    const size_t front = head_front(backward, dtype, N, D, V, any_rows && dtype == VELORA_BF16).piece;
+    if (dtype == VELORA_BF16 && !backward) return front;
+    return front + up256(piece_element(dtype, backward) * static_cast<size_t>(N) * static_cast<size_t>(wanted_piece(N, V)));
 }
+
+namespace {
+
+// W as the tensor cores take it: a copy in the workspace where its rows do not start on 16-byte boundaries.
+int head_weights(const HeadArgs& a, const HeadLayout& l, const char** W, int64_t* ldw)
+{
+    *W = static_cast<const char*>(a.W);
+    *ldw = a.ldw;
+    if (l.w == 0) return VELORA_OK;
+    const PackJob job{a.W, a.ldw, a.V, a.D, a.ws + l.w};
+    *W = a.ws + l.w;
+    *ldw = pack_rows_pitch(a.D);
+    return launch_pack_rows(&job, 1, a.stream);
+}
+
+HeadTile head_tile(const HeadArgs& a, const HeadLayout& l, int64_t v0, int64_t cols)
+{
+    HeadTile h{};
+    h.live = reinterpret_cast<const int*>(a.ws + l.live);
+    h.target = reinterpret_cast<const int*>(a.ws + l.target);
+    h.scale = reinterpret_cast<const float*>(a.ws + l.scale);
+    h.lse = reinterpret_cast<const float*>(a.ws + l.lse);
+    h.at_target = reinterpret_cast<float*>(a.ws + l.at_target);
+    h.running = reinterpret_cast<float2*>(a.ws + l.running);
+    h.N = static_cast<int>(a.N);
+    h.D = static_cast<int>(a.D);
+    h.cols = static_cast<int>(cols);
+    h.v0 = static_cast<int>(v0);
+    return h;
+}
+
+}  // namespace
 
 int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
 {
     HeadLayout l;
     int rc = head_layout(&l, false, a);
     if (rc != VELORA_OK) return rc;
+    const char* W;
+    int64_t ldw;
+    rc = head_weights(a, l, &W, &ldw);
+    if (rc != VELORA_OK) return rc;
     rc = launch_rows(a, l, nullptr, nullptr);
     if (rc != VELORA_OK) return rc;
     int* status = reinterpret_cast<int*>(a.ws);
+    const int n = static_cast<int>(a.N);
+    if (a.dtype == VELORA_BF16) {
+        const HeadTile h = head_tile(a, l, 0, a.V);
+        rc = launch_head_tiles(a.ws + l.x, l.ldx, W, ldw, nullptr, 0, h, status, a.stream);
+        if (rc != VELORA_OK) return rc;
+        return launch_chained(head_merge_kernel, dim3(static_cast<unsigned>(ceil_div64(a.N, 32))), kRowThreads, 0, a.stream, h.running,
+                              static_cast<int>(ceil_div64(a.V, 128)), n, h.live, reinterpret_cast<int*>(a.ws + l.order), h.target, h.at_target, loss, lse);
+    }
     const dim3 grid(static_cast<unsigned>(ceil_div64(a.N, kRowThreads / 32)));
     float* piece = reinterpret_cast<float*>(a.ws + l.piece);
     for (int64_t v0 = 0; v0 < a.V; v0 += l.piece_cols) {
         const int64_t cols = a.V - v0 < l.piece_cols ? a.V - v0 : l.piece_cols;
-        const char* W = static_cast<const char*>(a.W) + static_cast<size_t>(v0) * a.ldw * dtype_size(a.dtype);
-        rc = product(GEMM_NT_K_K, a.ws + l.x, a.dtype, l.ldx, W, a.dtype, a.ldw, piece, VELORA_F32, l.piece_cols, 0, a.N, cols, a.D, status, a.stream);
+        rc = product(GEMM_NT_K_K, a.ws + l.x, a.dtype, l.ldx, W + static_cast<size_t>(v0) * ldw * dtype_size(a.dtype), a.dtype, ldw, piece, VELORA_F32,
+                     l.piece_cols, 0, a.N, cols, a.D, status, nullptr, a.stream);
         if (rc != VELORA_OK) return rc;
-        rc = launch_chained(head_stats_kernel, grid, kRowThreads, 0, a.stream, piece, l.piece_cols, static_cast<int>(cols), static_cast<int>(v0),
-                            static_cast<int>(a.N), reinterpret_cast<int*>(a.ws + l.live), reinterpret_cast<int*>(a.ws + l.order),
-                            reinterpret_cast<int*>(a.ws + l.target), reinterpret_cast<float*>(a.ws + l.at_target),
-                            reinterpret_cast<float2*>(a.ws + l.running), v0 == 0 ? 1 : 0, v0 + cols == a.V ? 1 : 0, loss, lse);
+        rc = launch_chained(head_stats_kernel, grid, kRowThreads, 0, a.stream, piece, l.piece_cols, static_cast<int>(cols), static_cast<int>(v0), n,
+                            reinterpret_cast<int*>(a.ws + l.live), reinterpret_cast<int*>(a.ws + l.order), reinterpret_cast<int*>(a.ws + l.target),
+                            reinterpret_cast<float*>(a.ws + l.at_target), reinterpret_cast<float2*>(a.ws + l.running), v0 == 0 ? 1 : 0,
+                            v0 + cols == a.V ? 1 : 0, loss, lse);
         if (rc != VELORA_OK) return rc;
     }
     return VELORA_OK;
@@ -353,39 +425,45 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
     HeadLayout l;
     int rc = head_layout(&l, true, a);
     if (rc != VELORA_OK) return rc;
+    const char* W;
+    int64_t ldw;
+    rc = head_weights(a, l, &W, &ldw);
+    if (rc != VELORA_OK) return rc;
     rc = launch_rows(a, l, lse, dloss);
     if (rc != VELORA_OK) return rc;
     int* status = reinterpret_cast<int*>(a.ws);
+    const int n = static_cast<int>(a.N);
     const dim3 grid(static_cast<unsigned>(ceil_div64(a.N, kRowThreads / 32)));
-    float* piece = reinterpret_cast<float*>(a.ws + l.piece);
-    // Gradients of the logits are rounded to bf16 once where the tensor cores take W as bf16: 2^-9 of each, independent of one another.
-    const bool g_bf16 = a.dtype == VELORA_BF16 && tc_operand_ok(a.W, a.ldw);
-    const int g_dtype = g_bf16 ? VELORA_BF16 : VELORA_F32;
-    const int64_t ldg = g_bf16 ? 2 * l.piece_cols : l.piece_cols;
+    const int* live = reinterpret_cast<const int*>(a.ws + l.live);
+    // In bf16 the logits' gradients are rounded once, for the tensor cores: by half a step each, independent of one another.
+    char* G = a.ws + l.piece;
     for (int64_t v0 = 0; v0 < a.V; v0 += l.piece_cols) {
         const int64_t cols = a.V - v0 < l.piece_cols ? a.V - v0 : l.piece_cols;
-        const char* W = static_cast<const char*>(a.W) + static_cast<size_t>(v0) * a.ldw * dtype_size(a.dtype);
-        rc = product(GEMM_NT_K_K, a.ws + l.x, a.dtype, l.ldx, W, a.dtype, a.ldw, piece, VELORA_F32, l.piece_cols, 0, a.N, cols, a.D, status, a.stream);
-        if (rc != VELORA_OK) return rc;
-        rc = launch_chained(g_bf16 ? head_gradient_kernel<__nv_bfloat16> : head_gradient_kernel<float>, grid, kRowThreads, 0, a.stream, piece, l.piece_cols,
-                            static_cast<int>(cols), static_cast<int>(v0), static_cast<int>(a.N), reinterpret_cast<int*>(a.ws + l.target),
-                            reinterpret_cast<float*>(a.ws + l.scale), reinterpret_cast<float*>(a.ws + l.lse));
+        const char* w = W + static_cast<size_t>(v0) * ldw * dtype_size(a.dtype);
+        if (a.dtype == VELORA_BF16) {
+            rc = launch_head_tiles(a.ws + l.x, l.ldx, w, ldw, G, l.piece_cols, head_tile(a, l, v0, cols), status, a.stream);
+        } else {
+            rc = product(GEMM_NT_K_K, a.ws + l.x, a.dtype, l.ldx, w, a.dtype, ldw, G, VELORA_F32, l.piece_cols, 0, a.N, cols, a.D, status, nullptr, a.stream);
+            if (rc != VELORA_OK) return rc;
+            rc = launch_chained(head_gradient_kernel, grid, kRowThreads, 0, a.stream, reinterpret_cast<float*>(G), l.piece_cols, static_cast<int>(cols),
+                                static_cast<int>(v0), n, reinterpret_cast<int*>(a.ws + l.target), reinterpret_cast<float*>(a.ws + l.scale),
+                                reinterpret_cast<float*>(a.ws + l.lse));
+        }
         if (rc != VELORA_OK) return rc;
         if (dW) {
             char* dw = static_cast<char*>(dW) + static_cast<size_t>(v0) * lddw * dtype_size(dw_dtype);
-            rc = product(GEMM_TN_MN_MN, piece, g_dtype, ldg, a.ws + l.x, a.dtype, l.ldx, dw, dw_dtype, lddw, beta, cols, a.D, a.N, status, a.stream);
+            rc = product(GEMM_TN_MN_MN, G, a.dtype, l.piece_cols, a.ws + l.x, a.dtype, l.ldx, dw, dw_dtype, lddw, beta, cols, a.D, a.N, status, live, a.stream);
             if (rc != VELORA_OK) return rc;
         }
         if (dX) {
-            rc = product(GEMM_NN_K_MN, piece, g_dtype, ldg, W, a.dtype, a.ldw, a.ws + l.sum, VELORA_F32, l.ldx, v0 > 0 ? 1 : 0, a.N, a.D, cols, status, a.stream);
+            rc = product(GEMM_NN_K_MN, G, a.dtype, l.piece_cols, w, a.dtype, ldw, a.ws + l.sum, VELORA_F32, l.ldx, v0 > 0 ? 1 : 0, a.N, a.D, cols, status, live, a.stream);
             if (rc != VELORA_OK) return rc;
         }
     }
     if (!dX) return VELORA_OK;
     const float* sum = reinterpret_cast<float*>(a.ws + l.sum);
-    const int n = static_cast<int>(a.N), d = static_cast<int>(a.D);
-    int* live = reinterpret_cast<int*>(a.ws + l.live);
-    int* order = reinterpret_cast<int*>(a.ws + l.order);
+    const int d = static_cast<int>(a.D);
+    const int* order = reinterpret_cast<const int*>(a.ws + l.order);
     if (a.dtype == VELORA_BF16)
         return launch_chained(head_rows_back_kernel<__nv_bfloat16>, grid, kRowThreads, 0, a.stream, sum, l.ldx, n, d, live, order, static_cast<__nv_bfloat16*>(dX), lddx);
     return launch_chained(head_rows_back_kernel<float>, grid, kRowThreads, 0, a.stream, sum, l.ldx, n, d, live, order, static_cast<float*>(dX), lddx);

@@ -13,7 +13,7 @@ struct HeadLayout {
     size_t target;          // int32[N]: column, -1 without one, -2 where it is no column
     size_t scale, lse;      // fp32[N]: gradient of the row's loss, log sum exp (backward)
     size_t at_target;       // fp32[N]: logit of the target (forward)
-    size_t running;         // float2[N] or float2[tiles][N]: maximum, and the sum of exponentials relative to it (forward)
+    size_t running;         // float2[N], or float2[128-column blocks][N]: maximum, and the sum of exponentials relative to it (forward)
     size_t x;               // the rows of X, pitch ldx elements; zeros for rows without a target
     size_t w;               // W with a pitch that tensor maps take, where W's own is not
     size_t sum;             // fp32, pitch ldx: dX so far (backward)
@@ -34,6 +34,19 @@ struct HeadArgs {
     size_t ws_bytes;
     cudaStream_t stream;
 };
+
+// A product's worth of logits, columns v0 .. v0 + cols of the vocabulary; arrays as in HeadLayout.
+struct HeadTile {
+    const int* live;
+    const int* target;
+    const float* scale;
+    const float* lse;
+    float* at_target;
+    float2* running;
+    int N, D, cols, v0;
+};
+// G == nullptr: statistics of bf16 x W^T; otherwise its gradient to G [N, ldg].  W: its row v0.  (head_loss_tc.cu)
+int launch_head_tiles(const void* x, int64_t ldx, const void* W, int64_t ldw, void* G, int64_t ldg, const HeadTile& h, int* status, cudaStream_t stream);
 
 // What velora_workspace_bytes reports.
 size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool any_rows);
