@@ -468,12 +468,21 @@ def velora_expand_p(P: torch.Tensor, v: torch.Tensor, D: int, dW: Optional[torch
     return dW
 
 
+def _here(*tensors) -> None:
+    """All on the current device, whose stream the kernels are launched on."""
+    current = _raw_device() if _raw_device is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
+    for t in tensors:
+        if t.get_device() != current:
+            raise ValueError("tensors must be on the current device (%s), got one on %s" % (current, t.device))
+
+
 def _codes(Q: torch.Tensor, E: torch.Tensor):
     if Q.dtype != torch.int8 or E.dtype != torch.uint8:
         raise ValueError("Q must be int8 and E uint8")
     qp, ldq = _mat(Q, "Q")
     ep, lde = _mat(E, "E")
-    if E.shape != (Q.shape[0], -(-Q.shape[1] // CHECKPOINT_BLOCK)):
+    N, D = Q.shape
+    if E.shape != (N, -(-D // CHECKPOINT_BLOCK)):
         raise ValueError("E must be [N, ceil(D / %d)] for Q's [N, D]" % CHECKPOINT_BLOCK)
     return qp, ldq, ep, lde
 
@@ -485,12 +494,13 @@ def velora_checkpoint_store(X: torch.Tensor, Q: Optional[torch.Tensor] = None, E
     N, D = X.shape
     blocks = -(-D // CHECKPOINT_BLOCK)
     if Q is None:
-        Q = torch.empty((N, -(-D // 16) * 16), dtype=torch.int8, device=X.device)[:, :D]
+        Q = torch.empty_strided((N, D), (-(-D // 16) * 16, 1), dtype=torch.int8, device=X.device)
     if E is None:
-        E = torch.empty((N, -(-blocks // 16) * 16), dtype=torch.uint8, device=X.device)[:, :blocks]
+        E = torch.empty_strided((N, blocks), (-(-blocks // 16) * 16, 1), dtype=torch.uint8, device=X.device)
     if Q.shape != X.shape:
         raise ValueError("Q must have X's shape")
     qp, ldq, ep, lde = _codes(Q, E)
+    _here(X, Q, E)
     _check(lib().velora_checkpoint_store(xp, _dt(X), N, D, ldx, qp, ldq, ep, lde, _stream(stream)), "velora_checkpoint_store")
     return Q, E
 
@@ -504,6 +514,7 @@ def velora_checkpoint_load(Q: torch.Tensor, E: torch.Tensor, Xhat: Optional[torc
     if Xhat.shape != Q.shape:
         raise ValueError("Xhat must have Q's shape")
     xp, ldx = _mat(Xhat, "Xhat")
+    _here(Q, E, Xhat)
     _check(lib().velora_checkpoint_load(qp, ldq, ep, lde, N, D, xp, _dt(Xhat), ldx, _stream(stream)), "velora_checkpoint_load")
     return Xhat
 
@@ -524,6 +535,7 @@ def velora_checkpoint_weight_grad(dY: torch.Tensor, Q: torch.Tensor, E: torch.Te
     if dW.shape != (O, D):
         raise ValueError("dW must be [O, D]")
     wp, lddw = _mat(dW, "dW")
+    _here(dY, Q, E, dW)
     if ws is None:
         op = OP_CHECKPOINT_WEIGHT_GRAD | (OP_F32 if dY.dtype == torch.float32 else 0)
         ws = velora_workspace_alloc(velora_workspace_bytes(op, N, D, O, 1, _odd_rows(dY, yp, lddy)), dY.device)
@@ -563,6 +575,7 @@ def velora_head_loss(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, los
     if lse is None:
         lse = torch.empty(N, dtype=torch.float32, device=X.device)
     lp, sp = _tokens(loss, N, torch.float32, "loss"), _tokens(lse, N, torch.float32, "lse")
+    _here(X, W, target, loss, lse)
     if ws is None:
         ws = _head_workspace(OP_HEAD_LOSS, X, W, wp, ldw)
     rc = lib().velora_head_loss(xp, ldx, wp, ldw, tp, lp, sp, _dt(X), N, D, V, ws.data_ptr(), ws.numel(), _stream(stream))
@@ -588,6 +601,7 @@ def velora_head_loss_backward(X: torch.Tensor, W: torch.Tensor, target: torch.Te
         raise ValueError("dX must be like X, dW of W's shape")
     dxp, lddx = _mat(dX, "dX") if need_dX else (None, D)
     dwp, lddw = _mat(dW, "dW") if need_dW else (None, D)
+    _here(X, W, target, lse, dloss, *([dX] if need_dX else []), *([dW] if need_dW else []))
     if ws is None:
         ws = _head_workspace(OP_HEAD_LOSS_BACKWARD, X, W, wp, ldw)
     rc = lib().velora_head_loss_backward(xp, ldx, wp, ldw, tp, sp, gp, dxp, lddx, dwp, _dt(dW) if need_dW else F32, lddw, beta,

@@ -150,6 +150,15 @@ __device__ __forceinline__ void store_rows_staged(CT* block, int64_t ldc, int ro
     __syncwarp();
 }
 
+// A product's factor, before it is rounded or added to anything.
+__device__ __forceinline__ void scale_block(uint32_t (&r)[2][32], float alpha)
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 32; ++i) r[h][i] = __float_as_uint(__uint_as_float(r[h][i]) * alpha);
+}
+
 // How outputs are written: rows on odd boundaries by store_rows_staged, others by Store32 or as tiles by store_block.
 enum CRows { C_ELEMENTS = 0, C_VECTORS = 1, C_TILES = 2 };
 

@@ -43,9 +43,9 @@ bool tc_operand_ok(const void* p, int64_t ld_elems)
 
 int launch_gemm_tc(int kind, const void* A, int64_t lda, const void* B, int64_t ldb,
                    void* C, int c_dtype, int64_t ldc, int beta,
-                   int64_t Mdim, int64_t Ndim, int64_t Kdim, int in_dtype, int* status, cudaStream_t stream, const int* live)
+                   int64_t Mdim, int64_t Ndim, int64_t Kdim, int in_dtype, int* status, cudaStream_t stream, const GemmMore& more)
 {
-    if (in_dtype == VELORA_F32 && c_dtype == VELORA_F32)
+    if (in_dtype == VELORA_F32 && c_dtype == VELORA_F32 && !more.alpha)
         return launch_gemm_f32_tc(kind, A, lda, B, ldb, C, ldc, beta, Mdim, Ndim, Kdim, status, stream);
     if (in_dtype != VELORA_BF16) return VELORA_ERR_UNSUPPORTED;
     if (Mdim < 1 || Ndim < 1 || Kdim < 1) return VELORA_ERR_UNSUPPORTED;
@@ -61,7 +61,7 @@ int launch_gemm_tc(int kind, const void* A, int64_t lda, const void* B, int64_t 
     if (rc != VELORA_OK) return rc;
     GemmShape shape = gemm_shape(Mdim, Ndim, Kdim, di.sm_count, false);
     if (shape.pair) {
-        const int prc = launch_gemm_tc_pair(kind, A, lda, B, ldb, C, c_dtype, ldc, beta, Mdim, Ndim, Kdim, in_dtype, status, stream, live);
+        const int prc = launch_gemm_tc_pair(kind, A, lda, B, ldb, C, c_dtype, ldc, beta, Mdim, Ndim, Kdim, in_dtype, status, stream, more);
         if (prc != VELORA_ERR_UNSUPPORTED) return prc;
         shape = GemmShape{false, 256, 1};
     }
@@ -77,10 +77,10 @@ int launch_gemm_tc(int kind, const void* A, int64_t lda, const void* B, int64_t 
     const int m = static_cast<int>(Mdim), n = static_cast<int>(Ndim), k = static_cast<int>(Kdim);
 #define VELORA_GEMM_WIDTH(AMN, BMN, CT)                                                                                          \
     switch (shape.bn) {                                                                                                          \
-        case 64: return launch_kernel<AMN, BMN, CT, 0, 64>(ta, tb, C, ldc, beta, m, n, k, shape.splits, status, stream);         \
-        case 128: return launch_kernel<AMN, BMN, CT, 0, 128>(ta, tb, C, ldc, beta, m, n, k, shape.splits, status, stream);       \
-        case 192: return launch_kernel<AMN, BMN, CT, 0, 192>(ta, tb, C, ldc, beta, m, n, k, shape.splits, status, stream);       \
-        default: return launch_kernel<AMN, BMN, CT, 0, 256>(ta, tb, C, ldc, beta, m, n, k, shape.splits, status, stream);        \
+        case 64: return launch_kernel<AMN, BMN, CT, 0, 64>(ta, tb, C, ldc, beta, m, n, k, shape.splits, status, stream, FuseArgs{}, more.alpha);         \
+        case 128: return launch_kernel<AMN, BMN, CT, 0, 128>(ta, tb, C, ldc, beta, m, n, k, shape.splits, status, stream, FuseArgs{}, more.alpha);       \
+        case 192: return launch_kernel<AMN, BMN, CT, 0, 192>(ta, tb, C, ldc, beta, m, n, k, shape.splits, status, stream, FuseArgs{}, more.alpha);       \
+        default: return launch_kernel<AMN, BMN, CT, 0, 256>(ta, tb, C, ldc, beta, m, n, k, shape.splits, status, stream, FuseArgs{}, more.alpha);        \
     }
 #define VELORA_GEMM_CASE(AMN, BMN)                                                    \
     if (c_dtype == VELORA_BF16) { VELORA_GEMM_WIDTH(AMN, BMN, __nv_bfloat16) }       \

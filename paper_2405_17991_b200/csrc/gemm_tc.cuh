@@ -14,15 +14,22 @@ enum GemmKind {
     GEMM_TN_MN_MN = 2   // dW = dY^T Xh: A[K, Mdim] contiguous in Mdim,   B[K, Ndim] contiguous in Ndim
 };
 
+// What the products of the head's gradients add to a product; device words, either may be NULL.
+//   live   how many of A's first rows count, where the others hold zeros (GEMM_TN_MN_MN: rows of the contraction, which the kernel
+//          may leave out; otherwise rows of C, which it may leave unwritten)
+//   alpha  a factor of op(A) op(B)
+struct GemmMore {
+    const int* live = nullptr;
+    const float* alpha = nullptr;
+};
+
 // `status` (may be NULL) is a device word that a kernel sets to VELORA_ERR_TIMEOUT if one of its bounded
 // waits expires; nothing ever clears it but velora_workspace_init.
 // Returns VELORA_ERR_UNSUPPORTED (nothing launched) when the operands do not meet the tensor-core
 // path's requirements (bf16 data, 16-byte aligned rows); the caller then uses the CUDA-core GEMM.
-// `live` (may be NULL): a device word that says how many of A's first rows count, where the others hold zeros (GEMM_TN_MN_MN: rows
-// of the contraction, which the kernel may leave out; otherwise rows of C, which it may leave unwritten).
 int launch_gemm_tc(int kind, const void* A, int64_t lda, const void* B, int64_t ldb,
                    void* C, int c_dtype, int64_t ldc, int beta,
-                   int64_t Mdim, int64_t Ndim, int64_t Kdim, int in_dtype, int* status, cudaStream_t stream, const int* live = nullptr);
+                   int64_t Mdim, int64_t Ndim, int64_t Kdim, int in_dtype, int* status, cudaStream_t stream, const GemmMore& more = GemmMore{});
 
 // The same products for fp32 operands and an fp32 result, to fp32 accuracy, any row pitch and alignment.  VELORA_ERR_UNSUPPORTED
 // (nothing launched) where the CUDA cores are faster.  (gemm_f32_tc.cu)
@@ -32,7 +39,7 @@ int launch_gemm_f32_tc(int kind, const void* A, int64_t lda, const void* B, int6
 // The same product with CTA pairs (tcgen05 cta_group::2, 256 x 256 tile per pair).  (gemm_tc2.cu)
 int launch_gemm_tc_pair(int kind, const void* A, int64_t lda, const void* B, int64_t ldb,
                         void* C, int c_dtype, int64_t ldc, int beta,
-                        int64_t Mdim, int64_t Ndim, int64_t Kdim, int in_dtype, int* status, cudaStream_t stream, const int* live = nullptr);
+                        int64_t Mdim, int64_t Ndim, int64_t Kdim, int in_dtype, int* status, cudaStream_t stream, const GemmMore& more = GemmMore{});
 
 int launch_linear_forward_tc_pair(const void* X, int64_t ldx, const void* W, int64_t ldw, const float* v,
                                   void* Y, int64_t ldy, void* Z, int z_dtype, int64_t ldz,

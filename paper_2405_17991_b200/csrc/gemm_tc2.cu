@@ -57,7 +57,7 @@ template <bool A_MN, bool B_MN, typename CT, int FUSE>
 __global__ void __launch_bounds__(FUSE ? P_FUSE_THREADS : P_THREADS, 1)
 gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                  const __grid_constant__ CUtensorMap tmC, CT* __restrict__ C, int64_t ldc, int beta, int Mdim, int Ndim, int Kdim,
-                 int all_tiles_m, int tiles_n, int c_vec, int* __restrict__ status, const int* live, const FuseArgs fz)
+                 int all_tiles_m, int tiles_n, int c_vec, int* __restrict__ status, const GemmMore more, const FuseArgs fz)
 {
     static_assert(FUSE == 0 || (!A_MN && !B_MN), "compress rides on the K-major forward GEMM only");
     namespace cg = cooperative_groups;
@@ -80,10 +80,10 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
     volatile int* tiles_started = reinterpret_cast<volatile int*>(tail + 16 * P_STAGES + 60);   // producer's progress, read by the compress warps
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    // `live`: see launch_gemm_tc.  At least one tile, one k-block: an empty product is made of rows of zeros.
+    // At least one tile, one k-block: a product without a row that counts is made of rows of zeros.
     int tiles_m = all_tiles_m, kblocks = (Kdim + P_BK - 1) / P_BK;
-    if (live) {
-        const int rows = max(*live, 1);
+    if (more.live) {
+        const int rows = max(*more.live, 1);
         if (A_MN) kblocks = min(kblocks, (rows + P_BK - 1) / P_BK);
         else tiles_m = min(tiles_m, (rows + 2 * P_BM - 1) / (2 * P_BM));
     }
@@ -227,6 +227,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         const int quarter = warp & 3;
         const uint32_t lead_tempty0 = map_to_cta(tempty, 0);
         const uint32_t block = smem_u32(staging) + quarter * kStoreBytes;
+        const float alpha = more.alpha ? *more.alpha : 1.f;
         uint32_t t = 0;
         for (int tile = pair; tile < num_tiles && !failed; tile += num_pairs, ++t) {
             const PairTile t0 = pair_tile(tile, tiles_m, tiles_n, 2 * P_BM, P_BN);
@@ -247,6 +248,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(lead_tempty0 + 8 * acc);
                 }
+                if (more.alpha) scale_block(r, alpha);
                 const int valid = Ndim - (t0.n0 + c * 32);
                 if (sizeof(CT) == 2 && c_vec == C_TILES && (valid >= 64 || Ndim % 8 == 0)) {
                     if (row - lane < Mdim && valid > 0) store_block(&tmC, block, r, t0.n0 + c * 32, row - lane, lane);
@@ -281,7 +283,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
 template <bool A_MN, bool B_MN, typename CT, int FUSE = 0>
 int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, void* C, int64_t ldc, int beta,
                 int Mdim, int Ndim, int Kdim, int* status, int sm_count, cudaStream_t stream,
-                const FuseArgs fz = FuseArgs{}, const int* live = nullptr)
+                const FuseArgs fz = FuseArgs{}, const GemmMore& more = GemmMore{})
 {
     constexpr size_t smem_bytes = FUSE ? P_FUSE_SMEM : P_SMEM;
     static DeviceOnce configured;
@@ -312,7 +314,7 @@ int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, void* C, int64_t l
     int c_vec = c_rows_vec(C, ldc, sizeof(CT)) ? C_VECTORS : C_ELEMENTS;
     CUtensorMap tc = ta;
     if (sizeof(CT) == 2 && c_vec && !beta && tc_operand_ok(C, ldc) && make_tmap_bf16_2d(&tc, C, Ndim, Mdim, ldc, 64, 32) == VELORA_OK) c_vec = C_TILES;
-    if (cudaLaunchKernelEx(&cfg, kern, ta, tb, tc, static_cast<CT*>(C), ldc, beta, Mdim, Ndim, Kdim, tiles_m, tiles_n, c_vec, status, live, fz) !=
+    if (cudaLaunchKernelEx(&cfg, kern, ta, tb, tc, static_cast<CT*>(C), ldc, beta, Mdim, Ndim, Kdim, tiles_m, tiles_n, c_vec, status, more, fz) !=
         cudaSuccess) {
         cudaGetLastError();
         return VELORA_ERR_CUDA;
@@ -324,7 +326,7 @@ int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, void* C, int64_t l
 
 int launch_gemm_tc_pair(int kind, const void* A, int64_t lda, const void* B, int64_t ldb,
                         void* C, int c_dtype, int64_t ldc, int beta,
-                        int64_t Mdim, int64_t Ndim, int64_t Kdim, int in_dtype, int* status, cudaStream_t stream, const int* live)
+                        int64_t Mdim, int64_t Ndim, int64_t Kdim, int in_dtype, int* status, cudaStream_t stream, const GemmMore& more)
 {
     if (in_dtype != VELORA_BF16) return VELORA_ERR_UNSUPPORTED;
     if (Mdim < 1 || Ndim < 1 || Kdim < 1) return VELORA_ERR_UNSUPPORTED;
@@ -347,8 +349,8 @@ int launch_gemm_tc_pair(int kind, const void* A, int64_t lda, const void* B, int
     const int m = static_cast<int>(Mdim), n = static_cast<int>(Ndim), k = static_cast<int>(Kdim);
 #define VELORA_PAIR_CASE(AMN, BMN)                                                                              \
     return c_dtype == VELORA_BF16                                                                               \
-               ? launch_pair<AMN, BMN, __nv_bfloat16>(ta, tb, C, ldc, beta, m, n, k, status, di.sm_count, stream, FuseArgs{}, live) \
-               : launch_pair<AMN, BMN, float>(ta, tb, C, ldc, beta, m, n, k, status, di.sm_count, stream, FuseArgs{}, live)
+               ? launch_pair<AMN, BMN, __nv_bfloat16>(ta, tb, C, ldc, beta, m, n, k, status, di.sm_count, stream, FuseArgs{}, more) \
+               : launch_pair<AMN, BMN, float>(ta, tb, C, ldc, beta, m, n, k, status, di.sm_count, stream, FuseArgs{}, more)
     if (!a_mn && !b_mn) { VELORA_PAIR_CASE(false, false); }
     if (!a_mn && b_mn) { VELORA_PAIR_CASE(false, true); }
     VELORA_PAIR_CASE(true, true);

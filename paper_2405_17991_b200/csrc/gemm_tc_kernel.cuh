@@ -82,7 +82,7 @@ template <bool A_MN, bool B_MN, typename CT, int FUSE, int BN>
 __global__ void __launch_bounds__(FUSE ? FUSE_THREADS : GEMM_THREADS_SHORT, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                const __grid_constant__ CUtensorMap tmC, CT* __restrict__ C, int64_t ldc, int beta, int Mdim, int Ndim, int Kdim,
-               int tiles_m, int tiles_n, int kb_per_split, int c_vec, int* __restrict__ status, const FuseArgs fz)
+               int tiles_m, int tiles_n, int kb_per_split, int c_vec, int* __restrict__ status, const FuseArgs fz, const float* alpha_at)
 {
     typedef TileShape<BN> S;
     constexpr int B_BYTES = S::kBBytes, STAGES = S::kStages, TMEM_COLS = S::kTmemCols;
@@ -136,6 +136,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     const uint32_t tmem_base = *tmem_slot;
     pdl_wait();                                              // nothing in global memory has been touched so far
     if (splits == 1) pdl_trigger();
+    const float alpha = alpha_at ? *alpha_at : 1.f;          // a factor of the product
 
     bool failed = false;
     if (warp == 0) {
@@ -278,6 +279,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                     __syncwarp();
                     if (lane == 0) mbar_arrive(tempty + 8 * acc);
                 }
+                if (alpha_at) scale_block(r, alpha);
                 const int valid = Ndim - (tc0.n0 + c * 32);
                 if (sizeof(CT) == 2 && c_vec == C_TILES && (valid >= 64 || Ndim % 8 == 0)) {
                     if (row - lane < Mdim && valid > 0) store_block(&tmC, block, r, tc0.n0 + c * 32, row - lane, lane);
@@ -329,6 +331,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 #pragma unroll
             for (int s = 1; s < MAX_SPLITS; ++s)               // fixed order
                 if (s < splits) { y[0] += x[s].x; y[1] += x[s].y; y[2] += x[s].z; y[3] += x[s].w; }
+            if (alpha_at) { y[0] *= alpha; y[1] *= alpha; y[2] *= alpha; y[3] *= alpha; }
             CT* p = C + static_cast<int64_t>(tc0.m0 + r) * ldc + tc0.n0 + col;
             if (c_vec && left >= 4) {
                 Store4<CT>::run(p, y, beta);
@@ -348,7 +351,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 
 template <bool A_MN, bool B_MN, typename CT, int FUSE, int BN>
 int launch_kernel(const CUtensorMap& ta, const CUtensorMap& tb, void* C, int64_t ldc, int beta,
-                  int Mdim, int Ndim, int Kdim, int splits, int* status, cudaStream_t stream, const FuseArgs fz = FuseArgs{})
+                  int Mdim, int Ndim, int Kdim, int splits, int* status, cudaStream_t stream, const FuseArgs fz = FuseArgs{}, const float* alpha = nullptr)
 {
     typedef TileShape<BN> S;
     static DeviceOnce configured;
@@ -376,7 +379,7 @@ int launch_kernel(const CUtensorMap& ta, const CUtensorMap& tb, void* C, int64_t
     if (splits <= 1) {
         const int grid = static_cast<int>(tiles < di.sm_count ? tiles : di.sm_count);
         return launch_chained(kern, dim3(static_cast<unsigned>(grid)), threads, S::kSmem, stream,
-                              ta, tb, tc, static_cast<CT*>(C), ldc, beta, Mdim, Ndim, Kdim, tiles_m, tiles_n, kblocks, c_vec, status, fz);
+                              ta, tb, tc, static_cast<CT*>(C), ldc, beta, Mdim, Ndim, Kdim, tiles_m, tiles_n, kblocks, c_vec, status, fz, alpha);
     }
     const int kb_per_split = (kblocks + splits - 1) / splits;
     splits = (kblocks + kb_per_split - 1) / kb_per_split;             // no split without k-blocks
@@ -393,9 +396,9 @@ int launch_kernel(const CUtensorMap& ta, const CUtensorMap& tb, void* C, int64_t
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, kern, ta, tb, tc, static_cast<CT*>(C), ldc, beta, Mdim, Ndim, Kdim, tiles_m, tiles_n, kb_per_split, c_vec,
-                           status, fz) != cudaSuccess) {
+                           status, fz, alpha) != cudaSuccess) {
         cudaGetLastError();                                           // a refused cluster: the same tiles, one CTA each
-        return launch_kernel<A_MN, B_MN, CT, FUSE, BN>(ta, tb, C, ldc, beta, Mdim, Ndim, Kdim, 1, status, stream, fz);
+        return launch_kernel<A_MN, B_MN, CT, FUSE, BN>(ta, tb, C, ldc, beta, Mdim, Ndim, Kdim, 1, status, stream, fz, alpha);
     }
     return after_launch();
 }

@@ -5,6 +5,7 @@
 // others and their rows of X taken as zeros, so nothing that stands there (a NaN of an unused buffer) can reach dW through 0 * NaN.
 #include "head_loss.cuh"
 
+#include "gemm_store.cuh"
 #include "gemm_tc.cuh"
 
 namespace velora {
@@ -12,7 +13,7 @@ namespace velora {
 namespace {
 
 constexpr int kRowThreads = 256;
-constexpr int64_t kPieceElements = 1 << 24;         // of logits that exist at a time, where the workspace has the room
+constexpr int64_t kPieceElements = 1 << 26;         // logits that exist at a time where the workspace has the room: 128 MB in bf16 (fp32: half as many)
 constexpr int kPieceStep = 256;                     // pieces are multiples of this
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -36,6 +37,7 @@ HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D, int64_t V,
     l.order = take(4 * n);
     l.target = take(4 * n);
     if (backward) {
+        l.common = take(4);
         l.scale = take(4 * n);
         l.lse = take(4 * n);
         l.sum = take(n * static_cast<size_t>(l.ldx) * 4);
@@ -49,12 +51,29 @@ HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D, int64_t V,
     return l;
 }
 
-int64_t wanted_piece(int64_t N, int64_t V)
+// Pieces of equal width, as few as fit the room but for up to two more where those fill the last wave of tiles better.  What a piece
+// costs, in k-blocks of 256 x 256 tiles on 74 pairs: its products, and the sums of dX that each but the first reads and writes (about 9 k-blocks
+// of a tile).
+int64_t piece_width(int64_t N, int64_t D, int64_t V, int64_t room_cols)
 {
-    int64_t cols = kPieceElements / (N < 1 ? 1 : N) / kPieceStep * kPieceStep;
-    if (cols < 4 * kPieceStep) cols = 4 * kPieceStep;
-    const int64_t all = round_up(V, kPieceStep);
-    return cols < all ? cols : all;
+    const int64_t tm = ceil_div64(N, 256), td = ceil_div64(D, 256), least = ceil_div64(V, room_cols);
+    int64_t best = 0, best_cost = 0;
+    for (int64_t p = least; p <= least + 2; ++p) {
+        const int64_t cols = round_up(ceil_div64(V, p), kPieceStep), tv = cols / 256;
+        const int64_t cost = p * (ceil_div64(tm * tv, 74) * ceil_div64(D, 64) + ceil_div64(tv * td, 74) * ceil_div64(N, 64) + ceil_div64(tm * td, 74) * (4 * tv + 9));
+        if (best == 0 || cost < best_cost) {
+            best = cols;
+            best_cost = cost;
+        }
+    }
+    return best;
+}
+
+int64_t room_wanted(int dtype, int64_t N, int64_t V)          // in columns
+{
+    const int64_t cols = (dtype == VELORA_BF16 ? kPieceElements : kPieceElements / 2) / N / kPieceStep * kPieceStep, all = round_up(V, kPieceStep);
+    const int64_t least = cols < 4 * kPieceStep ? 4 * kPieceStep : cols;
+    return least < all ? least : all;
 }
 
 // As many columns a piece as there is room for.
@@ -64,9 +83,10 @@ int head_layout(HeadLayout* l, bool backward, const HeadArgs& a)
     if (a.ws_bytes < l->piece) return VELORA_ERR_WORKSPACE;
     if (a.dtype == VELORA_BF16 && !backward) return VELORA_OK;
     const int64_t fit = static_cast<int64_t>((a.ws_bytes - l->piece) / (piece_element(a.dtype, backward) * static_cast<size_t>(a.N))) / kPieceStep * kPieceStep;
-    const int64_t want = wanted_piece(a.N, a.V);
-    l->piece_cols = fit < want ? fit : want;
-    return l->piece_cols < kPieceStep ? VELORA_ERR_WORKSPACE : VELORA_OK;
+    if (fit < kPieceStep) return VELORA_ERR_WORKSPACE;
+    const int64_t want = room_wanted(a.dtype, a.N, a.V);
+    l->piece_cols = piece_width(a.N, a.D, a.V, fit < want ? fit : want);
+    return VELORA_OK;
 }
 
 // ---- rows in order of having a target ----
@@ -77,10 +97,12 @@ struct RowsArgs {
     const int64_t* target;
     const float* dloss;             // backward only
     const float* lse;
+    int take_common;                // whether a factor is taken out of the dloss
     int N, V, D, rows_per_cta;
     int* live;
     int* order;
     int* target_out;
+    float* common;
     float* scale_out;
     float* lse_out;
     void* x_out;
@@ -92,16 +114,17 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(kRowThreads)
 head_rows_kernel(const RowsArgs a)
 {
-    __shared__ int counts[2];
+    __shared__ int counts[3];                         // live rows before this CTA's, all of them, bits of the largest |dloss|
     __shared__ int warp_live[kRowThreads / 32];
     __shared__ int row_to[kRowThreads];               // where a row goes; negative: -1 - that, and zeros are written
     pdl_wait();
     pdl_trigger();
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
     const int r0 = blockIdx.x * a.rows_per_cta, r1 = min(a.N, r0 + a.rows_per_cta);
-    if (t < 2) counts[t] = 0;
+    if (t < 3) counts[t] = 0;
     __syncthreads();
     int before = 0, total = 0;
+    float top = 0.f;
     for (int i0 = 0; i0 < a.N; i0 += kRowThreads * 8) {
         int64_t v[8];
 #pragma unroll
@@ -114,18 +137,27 @@ head_rows_kernel(const RowsArgs a)
             const int is = v[j] >= 0 && v[j] < a.V;
             total += is;
             before += is && i0 + j * kRowThreads + t < r0;
+            if (is && a.take_common) top = fmaxf(top, fabsf(a.dloss[i0 + j * kRowThreads + t]));
         }
     }
     before = __reduce_add_sync(0xffffffffu, before);
     total = __reduce_add_sync(0xffffffffu, total);
+    const int top_bits = static_cast<int>(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
     if (lane == 0) {
+        atomicMax(&counts[2], top_bits);
         atomicAdd(&counts[0], before);
         atomicAdd(&counts[1], total);
     }
     __syncthreads();
     before = counts[0];
     total = counts[1];
-    if (blockIdx.x == 0 && t == 0) *a.live = total;
+    // The common factor: none where it could not be divided by.
+    float common = __int_as_float(counts[2]);
+    if (!(common >= 1.17549435e-38f && common <= 3.4e38f)) common = 1.f;
+    if (blockIdx.x == 0 && t == 0) {
+        *a.live = total;
+        if (a.scale_out) *a.common = common;
+    }
     for (int b0 = r0; b0 < r1; b0 += kRowThreads) {
         const int n = b0 + t;
         const int64_t v = n < r1 ? a.target[n] : -1;
@@ -145,7 +177,7 @@ head_rows_kernel(const RowsArgs a)
             a.order[to] = n;
             a.target_out[to] = is ? static_cast<int>(v) : (v < 0 ? -1 : -2);
             if (a.scale_out) {
-                a.scale_out[to] = is ? a.dloss[n] : 0.f;
+                a.scale_out[to] = is ? a.dloss[n] / common : 0.f;
                 a.lse_out[to] = is ? a.lse[n] : 0.f;
             }
             if (v >= a.V && a.status) atomicCAS(a.status, 0, VELORA_ERR_INVALID_ARG);
@@ -171,7 +203,7 @@ head_rows_kernel(const RowsArgs a)
     }
 }
 
-int launch_rows(const HeadArgs& a, const HeadLayout& l, const float* lse, const float* dloss)
+int launch_rows(const HeadArgs& a, const HeadLayout& l, const float* lse, const float* dloss, bool take_common)
 {
     DeviceInfo di;
     const int rc = device_info(&di);
@@ -189,6 +221,8 @@ int launch_rows(const HeadArgs& a, const HeadLayout& l, const float* lse, const 
     if (dloss) {
         r.dloss = dloss;
         r.lse = lse;
+        r.take_common = take_common ? 1 : 0;
+        r.common = reinterpret_cast<float*>(a.ws + l.common);
         r.scale_out = reinterpret_cast<float*>(a.ws + l.scale);
         r.lse_out = reinterpret_cast<float*>(a.ws + l.lse);
     }
@@ -276,11 +310,20 @@ head_merge_kernel(const float2* running, int parts, int N, const int* live, cons
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
     float m = -INFINITY, s = 0.f;
     if (row < *live) {
-        for (int p = warp; p < parts; p += kRowThreads / 32) {
-            const float2 x = running[static_cast<int64_t>(p) * N + row];
-            const float both = x.x > m ? x.x : (x.x == x.x ? m : x.x);      // a NaN stays one
+        for (int p0 = warp; p0 < parts; p0 += kRowThreads / 32 * 8) {        // eight loads in flight
+            float2 x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int p = p0 + kRowThreads / 32 * i;
+                x[i] = p < parts ? running[static_cast<int64_t>(p) * N + row] : make_float2(-INFINITY, 0.f);
+            }
+            float both = m;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) both = x[i].x > both ? x[i].x : (x[i].x == x[i].x ? both : x[i].x);      // a NaN stays one
             const float ref = both == -INFINITY ? 0.f : both;
-            s = s * expf(m - ref) + x.y * expf(x.x - ref);
+            s *= expf(m - ref);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += x[i].y * expf(x[i].x - ref);
             m = both;
         }
     }
@@ -315,10 +358,10 @@ head_gradient_kernel(float* logits, int64_t ld, int cols, int v0, int N, const i
     for (int c = lane; c < cols; c += 32) l[c] = is ? g * (expf(l[c] - z) - (c == t ? 1.f : 0.f)) : 0.f;
 }
 
-// dX from its fp32 sums, rows back to their tokens.
-template <typename T>
+// dX from its fp32 sums, rows back to their tokens; eight columns a lane where dX's rows start on 16-byte boundaries.
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(kRowThreads)
-head_rows_back_kernel(const float* sum, int64_t ld, int N, int D, const int* live, const int* order, T* dX, int64_t lddx)
+head_rows_back_kernel(const float* sum, int64_t ld, int N, int D, const int* live, const int* order, const float* common, T* dX, int64_t lddx)
 {
     pdl_wait();
     pdl_trigger();
@@ -326,17 +369,32 @@ head_rows_back_kernel(const float* sum, int64_t ld, int N, int D, const int* liv
     if (row >= N) return;
     T* dst = dX + order[row] * lddx;
     const bool is = row < *live;
-    for (int c = lane; c < D; c += 32) Elem<T>::store(dst + c, is ? sum[row * ld + c] : 0.f);
+    const float f = *common;
+    if (VEC) {                                           // D is a multiple of 8
+#pragma unroll 2
+        for (int c = 8 * lane; c < D; c += 256) {
+            const uint4 x = ld_stream_if(sum + row * ld + c, is), z = ld_stream_if(sum + row * ld + c + 4, is);
+            const float y[8] = {__uint_as_float(x.x) * f, __uint_as_float(x.y) * f, __uint_as_float(x.z) * f, __uint_as_float(x.w) * f,
+                                __uint_as_float(z.x) * f, __uint_as_float(z.y) * f, __uint_as_float(z.z) * f, __uint_as_float(z.w) * f};
+            if (sizeof(T) == 2)
+                __stcs(reinterpret_cast<uint4*>(dst + c), make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])));
+            else
+                store_f32x8(reinterpret_cast<float*>(dst + c), y);
+        }
+    } else {
+        for (int c = lane; c < D; c += 32) Elem<T>::store(dst + c, is ? sum[row * ld + c] * f : 0.f);
+    }
 }
 
 // C = beta C + op(A) op(B): the tensor cores where they take the operands.
 int product(int kind, const void* A, int a_dtype, int64_t lda, const void* B, int b_dtype, int64_t ldb, void* C, int c_dtype, int64_t ldc, int beta,
-            int64_t M, int64_t N, int64_t K, int* status, const int* live, cudaStream_t stream)
+            int64_t M, int64_t N, int64_t K, int* status, const GemmMore& more, cudaStream_t stream)
 {
     if (a_dtype == b_dtype) {
-        const int rc = launch_gemm_tc(kind, A, lda, B, ldb, C, c_dtype, ldc, beta, M, N, K, a_dtype, status, stream, live);
+        const int rc = launch_gemm_tc(kind, A, lda, B, ldb, C, c_dtype, ldc, beta, M, N, K, a_dtype, status, stream, more);
         if (rc != VELORA_ERR_UNSUPPORTED) return rc;
     }
+    if (more.alpha) return VELORA_ERR_UNSUPPORTED;
     const bool a_t = kind == GEMM_TN_MN_MN, b_t = kind == GEMM_NT_K_K;
     return launch_gemm_simt(A, a_dtype, a_t ? 1 : lda, a_t ? lda : 1, B, b_dtype, b_t ? ldb : 1, b_t ? 1 : ldb, C, c_dtype, ldc, beta, M, N, K, stream);
 }
@@ -348,7 +406,7 @@ size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V
     if (N < 1) return kStatusBytes;
     const size_t front = head_front(backward, dtype, N, D, V, any_rows && dtype == VELORA_BF16).piece;
     if (dtype == VELORA_BF16 && !backward) return front;
-    return front + up256(piece_element(dtype, backward) * static_cast<size_t>(N) * static_cast<size_t>(wanted_piece(N, V)));
+    return front + up256(piece_element(dtype, backward) * static_cast<size_t>(N) * static_cast<size_t>(room_wanted(dtype, N, V)));
 }
 
 namespace {
@@ -392,7 +450,7 @@ int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
     int64_t ldw;
     rc = head_weights(a, l, &W, &ldw);
     if (rc != VELORA_OK) return rc;
-    rc = launch_rows(a, l, nullptr, nullptr);
+    rc = launch_rows(a, l, nullptr, nullptr, false);
     if (rc != VELORA_OK) return rc;
     int* status = reinterpret_cast<int*>(a.ws);
     const int n = static_cast<int>(a.N);
@@ -408,7 +466,7 @@ int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
     for (int64_t v0 = 0; v0 < a.V; v0 += l.piece_cols) {
         const int64_t cols = a.V - v0 < l.piece_cols ? a.V - v0 : l.piece_cols;
         rc = product(GEMM_NT_K_K, a.ws + l.x, a.dtype, l.ldx, W + static_cast<size_t>(v0) * ldw * dtype_size(a.dtype), a.dtype, ldw, piece, VELORA_F32,
-                     l.piece_cols, 0, a.N, cols, a.D, status, nullptr, a.stream);
+                     l.piece_cols, 0, a.N, cols, a.D, status, GemmMore{}, a.stream);
         if (rc != VELORA_OK) return rc;
         rc = launch_chained(head_stats_kernel, grid, kRowThreads, 0, a.stream, piece, l.piece_cols, static_cast<int>(cols), static_cast<int>(v0), n,
                             reinterpret_cast<int*>(a.ws + l.live), reinterpret_cast<int*>(a.ws + l.order), reinterpret_cast<int*>(a.ws + l.target),
@@ -429,13 +487,17 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
     int64_t ldw;
     rc = head_weights(a, l, &W, &ldw);
     if (rc != VELORA_OK) return rc;
-    rc = launch_rows(a, l, lse, dloss);
+    // In bf16 the logits' gradients are rounded once, for the tensor cores: by half a step each.  A mean's 1 / count in all of them would be the same
+    // rounding again and again, which does not average out (relative error of dX and dW up to 4e-3 by the count alone); so the largest dloss
+    // is taken out and multiplied back in fp32, wherever the product that writes dW takes a factor.
+    const bool take_common = a.dtype == VELORA_BF16 && (!dW || dw_dtype == VELORA_BF16 || c_rows_vec(dW, lddw, sizeof(float)));
+    rc = launch_rows(a, l, lse, dloss, take_common);
     if (rc != VELORA_OK) return rc;
     int* status = reinterpret_cast<int*>(a.ws);
     const int n = static_cast<int>(a.N);
     const dim3 grid(static_cast<unsigned>(ceil_div64(a.N, kRowThreads / 32)));
     const int* live = reinterpret_cast<const int*>(a.ws + l.live);
-    // In bf16 the logits' gradients are rounded once, for the tensor cores: by half a step each, independent of one another.
+    const float* common = reinterpret_cast<const float*>(a.ws + l.common);
     char* G = a.ws + l.piece;
     for (int64_t v0 = 0; v0 < a.V; v0 += l.piece_cols) {
         const int64_t cols = a.V - v0 < l.piece_cols ? a.V - v0 : l.piece_cols;
@@ -443,7 +505,7 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
         if (a.dtype == VELORA_BF16) {
             rc = launch_head_tiles(a.ws + l.x, l.ldx, w, ldw, G, l.piece_cols, head_tile(a, l, v0, cols), status, a.stream);
         } else {
-            rc = product(GEMM_NT_K_K, a.ws + l.x, a.dtype, l.ldx, w, a.dtype, ldw, G, VELORA_F32, l.piece_cols, 0, a.N, cols, a.D, status, nullptr, a.stream);
+            rc = product(GEMM_NT_K_K, a.ws + l.x, a.dtype, l.ldx, w, a.dtype, ldw, G, VELORA_F32, l.piece_cols, 0, a.N, cols, a.D, status, GemmMore{}, a.stream);
             if (rc != VELORA_OK) return rc;
             rc = launch_chained(head_gradient_kernel, grid, kRowThreads, 0, a.stream, reinterpret_cast<float*>(G), l.piece_cols, static_cast<int>(cols),
                                 static_cast<int>(v0), n, reinterpret_cast<int*>(a.ws + l.target), reinterpret_cast<float*>(a.ws + l.scale),
@@ -452,11 +514,11 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
         if (rc != VELORA_OK) return rc;
         if (dW) {
             char* dw = static_cast<char*>(dW) + static_cast<size_t>(v0) * lddw * dtype_size(dw_dtype);
-            rc = product(GEMM_TN_MN_MN, G, a.dtype, l.piece_cols, a.ws + l.x, a.dtype, l.ldx, dw, dw_dtype, lddw, beta, cols, a.D, a.N, status, live, a.stream);
+            rc = product(GEMM_TN_MN_MN, G, a.dtype, l.piece_cols, a.ws + l.x, a.dtype, l.ldx, dw, dw_dtype, lddw, beta, cols, a.D, a.N, status, GemmMore{live, take_common ? common : nullptr}, a.stream);
             if (rc != VELORA_OK) return rc;
         }
         if (dX) {
-            rc = product(GEMM_NN_K_MN, G, a.dtype, l.piece_cols, w, a.dtype, ldw, a.ws + l.sum, VELORA_F32, l.ldx, v0 > 0 ? 1 : 0, a.N, a.D, cols, status, live, a.stream);
+            rc = product(GEMM_NN_K_MN, G, a.dtype, l.piece_cols, w, a.dtype, ldw, a.ws + l.sum, VELORA_F32, l.ldx, v0 > 0 ? 1 : 0, a.N, a.D, cols, status, GemmMore{live, nullptr}, a.stream);
             if (rc != VELORA_OK) return rc;
         }
     }
@@ -464,9 +526,15 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
     const float* sum = reinterpret_cast<float*>(a.ws + l.sum);
     const int d = static_cast<int>(a.D);
     const int* order = reinterpret_cast<const int*>(a.ws + l.order);
-    if (a.dtype == VELORA_BF16)
-        return launch_chained(head_rows_back_kernel<__nv_bfloat16>, grid, kRowThreads, 0, a.stream, sum, l.ldx, n, d, live, order, static_cast<__nv_bfloat16*>(dX), lddx);
-    return launch_chained(head_rows_back_kernel<float>, grid, kRowThreads, 0, a.stream, sum, l.ldx, n, d, live, order, static_cast<float*>(dX), lddx);
+    const bool vec = a.D % 8 == 0 && c_rows_vec(dX, lddx, dtype_size(a.dtype));
+    if (a.dtype == VELORA_BF16) {
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(dX);
+        return vec ? launch_chained(head_rows_back_kernel<__nv_bfloat16, true>, grid, kRowThreads, 0, a.stream, sum, l.ldx, n, d, live, order, common, out, lddx)
+                   : launch_chained(head_rows_back_kernel<__nv_bfloat16, false>, grid, kRowThreads, 0, a.stream, sum, l.ldx, n, d, live, order, common, out, lddx);
+    }
+    float* out = static_cast<float*>(dX);
+    return vec ? launch_chained(head_rows_back_kernel<float, true>, grid, kRowThreads, 0, a.stream, sum, l.ldx, n, d, live, order, common, out, lddx)
+               : launch_chained(head_rows_back_kernel<float, false>, grid, kRowThreads, 0, a.stream, sum, l.ldx, n, d, live, order, common, out, lddx);
 }
 
 }  // namespace velora

@@ -4,9 +4,13 @@
 // l = X W^T, bf16 operands K-major, 256 x 256 logits a pair (tcgen05 cta_group::2; the pipeline is that of gemm_tc2.cu).
 //
 // The tensor cores add with truncation, 16 products at a time: over D = 4096 that shrinks a logit by some 5e-6 of itself, and a loss with
-// it (2e-6 against 64 bits).  So a tile's contraction is cut into segments of 1024, each into an accumulator of its own (two,
-// alternating), and the epilogue adds the segments up in registers, rounded to nearest: eight warps with 128 sums a thread.  The next segment's
-// products run meanwhile, so what a tile's exponentials have to hide behind is a segment (6 us; they take under 2).
+// it (1.5e-6 against 64 bits for 4096 tokens of 32000 columns; fp32 multiply-adds: 3.1e-7).  So for the statistics a tile's contraction
+// is cut into segments of 1024, each into an accumulator of its own (two, alternating), and the epilogue adds the segments up in registers,
+// rounded to nearest: eight warps with 128 sums a thread (3.5e-7; segments of 2048: 7.3e-7).  The next segment's products run meanwhile;
+// 8192 x 4096 of 32000: 1615 us, 1577 in one segment.  The gradient's logits take one: what they lose is below G's rounding.
+//
+// Bound by the power limit and by what the operands' way from L2 costs of it: the same launch in bands of 4 row blocks 1728 us, 8: 1643, 16: 1615 (W
+// crosses HBM twice, X stays in L2), 32: 1689.
 //
 // Roles per CTA (320 threads): warp 0 lane 0 TMA producer, warp 1 lane 0 MMA issuer (leader only), warps 2..9 epilogue: TMEM lanes
 // 32 * (w % 4) .., columns 128 * (w >= 6) ...  Barriers as in gemm_tc2.cu.  Every wait is bounded; both CTAs reach the closing
@@ -27,7 +31,8 @@ namespace {
 constexpr int H_BM = 128;                  // rows per CTA (256 per pair)
 constexpr int H_BN = 256;                  // columns per pair; half of them staged by each CTA
 constexpr int H_BK = 64;
-constexpr int H_SEGMENT = 16;              // k-blocks that an accumulator adds up
+constexpr int H_SEGMENT = 16;              // k-blocks that an accumulator adds up for the statistics
+constexpr int H_BAND = 16;                 // row blocks that are walked together
 constexpr int H_STAGES = 6;
 constexpr int H_A_BYTES = H_BM * H_BK * 2;
 constexpr int H_STAGE_BYTES = H_A_BYTES + (H_BN / 2) * H_BK * 2;
@@ -70,6 +75,7 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int kblocks = (h.D + H_BK - 1) / H_BK;
+    const int segment = ROLE == HEAD_STATS ? H_SEGMENT : kblocks;
     const int live = *h.live;
     const int tiles_m = (live + 2 * H_BM - 1) / (2 * H_BM);          // rows without a target are not computed
     const int tiles_n = (h.cols + H_BN - 1) / H_BN;
@@ -106,7 +112,7 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
         if (lane == 0) {
             uint32_t it = 0;
             for (int tile = pair; tile < num_tiles && !failed; tile += num_pairs) {
-                const PairTile t0 = pair_tile(tile, tiles_m, tiles_n, 2 * H_BM, H_BN);
+                const PairTile t0 = pair_tile<H_BAND>(tile, tiles_m, tiles_n, 2 * H_BM, H_BN);
                 const int m0 = t0.m0 + static_cast<int>(rank) * H_BM;
                 const int n0 = t0.n0 + static_cast<int>(rank) * (H_BN / 2);
                 for (int kb = 0; kb < kblocks; ++kb, ++it) {
@@ -142,12 +148,12 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
             constexpr uint32_t idesc = umma_idesc_bf16(2 * H_BM, H_BN, false, false);
             uint32_t it = 0, seg = 0;
             for (int tile = pair; tile < num_tiles && !failed; tile += num_pairs) {
-                for (int k0 = 0; k0 < kblocks && !failed; k0 += H_SEGMENT, ++seg) {
+                for (int k0 = 0; k0 < kblocks && !failed; k0 += segment, ++seg) {
                     const uint32_t acc = seg & 1u, aph = (seg >> 1) & 1u;
                     if (!mbar_wait(tempty + 8 * acc, aph ^ 1u, abort_flag)) { failed = true; break; }
                     tc_fence_after_sync();
                     const uint32_t d_tmem = tmem_base + acc * H_BN;
-                    const int k1 = min(kblocks, k0 + H_SEGMENT);
+                    const int k1 = min(kblocks, k0 + segment);
                     for (int kb = k0; kb < k1; ++kb, ++it) {
                         const uint32_t s = it % H_STAGES, ph = (it / H_STAGES) & 1u;
                         if (!mbar_wait(full + 8 * s, ph, abort_flag)) { failed = true; break; }
@@ -171,7 +177,7 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
         const uint32_t block = staging + (warp - 2) * kStoreBytes;
         uint32_t seg = 0;
         for (int tile = pair; tile < num_tiles && !failed; tile += num_pairs) {
-            const PairTile t0 = pair_tile(tile, tiles_m, tiles_n, 2 * H_BM, H_BN);
+            const PairTile t0 = pair_tile<H_BAND>(tile, tiles_m, tiles_n, 2 * H_BM, H_BN);
             const int row0 = t0.m0 + static_cast<int>(rank) * H_BM + quarter * 32, row = row0 + lane;
             const int col0 = t0.n0 + half * 128, valid = h.cols - col0;
             float l[4][32];
@@ -179,7 +185,7 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
             for (int c = 0; c < 4; ++c)
 #pragma unroll
                 for (int i = 0; i < 32; ++i) l[c][i] = 0.f;
-            for (int k0 = 0; k0 < kblocks; k0 += H_SEGMENT, ++seg) {
+            for (int k0 = 0; k0 < kblocks; k0 += segment, ++seg) {
                 const uint32_t acc = seg & 1u, aph = (seg >> 1) & 1u;
                 if (!mbar_wait_warp(tfull + 8 * acc, aph, abort_flag, 256)) { failed = true; break; }
                 tc_fence_after_sync();

@@ -87,10 +87,10 @@ __device__ __forceinline__ bool mbar_try_wait_acquire_cluster(uint32_t bar, uint
 struct PairTile {
     int m0, n0;
 };
-// Tiles of tile_m x tile_n walked in bands of 4 m-tiles so that pairs running together share B in L2.
+// Tiles of tile_m x tile_n walked in bands of BAND m-tiles so that pairs running together share B in L2.
+template <int BAND = 4>
 __device__ __forceinline__ PairTile pair_tile(int tile, int tiles_m, int tiles_n, int tile_m, int tile_n)
 {
-    constexpr int BAND = 4;
     const int per_band = BAND * tiles_n;
     const int band = tile / per_band;
     const int in_band = tile - band * per_band;
