@@ -8,6 +8,7 @@
 // NaN.  Both are bound by HBM: N D (b + 1 + 1/32) bytes each way.
 #include "checkpoint.cuh"
 #include "gemm_store.cuh"
+#include "row_chunks.cuh"
 
 namespace velora {
 
@@ -35,57 +36,109 @@ struct UnitWalk {
     }
 };
 
-// Eight elements at a 16-byte boundary as loaded.
+// Eight consecutive elements of a row as loaded, rows on 16-byte boundaries.  `begin` and `end` bound the matrix.
 template <typename T> struct Raw8;
 template <> struct Raw8<__nv_bfloat16> {
     uint4 w;
-    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool take) { w = ld_stream_if(p, take); }
-    __device__ __forceinline__ void get(float (&x)[8]) const
+    __device__ __forceinline__ void load(const __nv_bfloat16* row, int col, int D, bool in, int, const char*, const char*) { w = ld_stream_if(row + col, in && col + 8 <= D); }
+    // The elements, zeros behind the row's end; the largest of their bits without signs.
+    __device__ __forceinline__ uint32_t get(float (&x)[8], const __nv_bfloat16* row, int col, int D, bool in, int)
+    {
+        if (in && col < D && col + 8 > D) {
+            uint32_t v[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e < D) v[e >> 1] |= static_cast<uint32_t>(__bfloat16_as_ushort(row[col + e])) << (16 * (e & 1));
+            w = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+        return unpack(x, w);
+    }
+    static __device__ __forceinline__ uint32_t unpack(float (&x)[8], const uint4& w)
     {
         x[0] = bf16_lo(w.x); x[1] = bf16_hi(w.x); x[2] = bf16_lo(w.y); x[3] = bf16_hi(w.y);
         x[4] = bf16_lo(w.z); x[5] = bf16_hi(w.z); x[6] = bf16_lo(w.w); x[7] = bf16_hi(w.w);
+        const uint32_t m = __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
+        return max(m << 16, m & 0xffff0000u);
     }
 };
 template <> struct Raw8<float> {
     uint4 w[2];
-    __device__ __forceinline__ void load(const float* p, bool take)
+    __device__ __forceinline__ void load(const float* row, int col, int D, bool in, int, const char*, const char*)
     {
-        w[0] = ld_stream_if(p, take);
-        w[1] = ld_stream_if(p + 4, take);
+        w[0] = ld_stream_if(row + col, in && col + 8 <= D);
+        w[1] = ld_stream_if(row + col + 4, in && col + 8 <= D);
     }
-    __device__ __forceinline__ void get(float (&x)[8]) const
+    __device__ __forceinline__ uint32_t get(float (&x)[8], const float* row, int col, int D, bool in, int) const
     {
         x[0] = __uint_as_float(w[0].x); x[1] = __uint_as_float(w[0].y); x[2] = __uint_as_float(w[0].z); x[3] = __uint_as_float(w[0].w);
         x[4] = __uint_as_float(w[1].x); x[5] = __uint_as_float(w[1].y); x[6] = __uint_as_float(w[1].z); x[7] = __uint_as_float(w[1].w);
+        if (in && col < D && col + 8 > D) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e < D) x[e] = row[col + e];
+        }
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+        return top;
+    }
+};
+// bf16 rows on any boundary: a lane loads the aligned 16 bytes that its first element lies in, its neighbour has the rest.
+struct Raw8Odd {
+    uint4 w, over;
+    __device__ __forceinline__ void load(const __nv_bfloat16* row, int col, int D, bool in, int lane, const char* begin, const char* end)
+    {
+        const char* a = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(row + col) & ~static_cast<uintptr_t>(15));
+        const char* row_end = reinterpret_cast<const char*>(row + D);
+        w = over = make_uint4(0u, 0u, 0u, 0u);
+        if (in && a < row_end) w = load_aligned_chunk(a, begin, end);
+        if (in && lane == 31 && a + 16 < row_end) over = load_aligned_chunk(a + 16, begin, end);
+    }
+    __device__ __forceinline__ uint32_t get(float (&x)[8], const __nv_bfloat16* row, int col, int D, bool, int lane)
+    {
+        uint4 next = make_uint4(__shfl_down_sync(0xffffffffu, w.x, 1), __shfl_down_sync(0xffffffffu, w.y, 1),
+                                __shfl_down_sync(0xffffffffu, w.z, 1), __shfl_down_sync(0xffffffffu, w.w, 1));
+        if (lane == 31) next = over;
+        w = shift_chunks(w, next, static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row + col) & 15));
+        if (col + 8 > D) {                                             // what follows is the next row's
+            uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e >= D) v[e >> 1] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+            w = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+        return Raw8<__nv_bfloat16>::unpack(x, w);
     }
 };
 
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&y)[8])
+__device__ __forceinline__ uint4 pack8(const float (&y)[8])
 {
-    __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])));
+    return make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
 }
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&y)[8]) { __stcs(reinterpret_cast<uint4*>(p), pack8(y)); }
 __device__ __forceinline__ void store8(float* p, const float (&y)[8]) { store_f32x8(p, y); }
 
-// Rows of X on 16-byte boundaries, rows of Q on 8-byte ones.
-template <typename T, int U>
+// Rows of Q on 8-byte boundaries; RAW says which rows of X.
+template <typename T, typename RAW, int U>
 __global__ void __launch_bounds__(kStreamThreads)
 checkpoint_store_vec_kernel(const T* X, int64_t ldx, int64_t N, int D, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, int segs)
 {
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31;
+    const char* begin = reinterpret_cast<const char*>(X);
+    const char* end = reinterpret_cast<const char*>(X + (N - 1) * ldx + D);
     const int64_t warp = static_cast<int64_t>(blockIdx.x) * (kStreamThreads / 32) + (threadIdx.x >> 5);
     const int64_t stride = static_cast<int64_t>(gridDim.x) * (kStreamThreads / 32) * U;
     const int64_t step_rows = stride / segs;
     const int step_segs = static_cast<int>(stride - step_rows * segs);
     UnitWalk at;
     for (at.start(warp * U, segs); at.row < N; at.step(step_rows, step_segs, segs)) {
-        Raw8<T> raw[U];
+        RAW raw[U];
         UnitWalk u = at;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const int col = u.seg * kSegment + lane * 8;
-            raw[i].load(X + u.row * ldx + col, u.row < N && col + 8 <= D);
+            raw[i].load(X + u.row * ldx, u.seg * kSegment + lane * 8, D, u.row < N, lane, begin, end);
             u.step(0, 1, segs);
         }
         u = at;
@@ -93,29 +146,19 @@ checkpoint_store_vec_kernel(const T* X, int64_t ldx, int64_t N, int D, int8_t* Q
         for (int i = 0; i < U; ++i) {
             const int col = u.seg * kSegment + lane * 8;
             float x[8];
-            raw[i].get(x);
-            const bool tail = u.row < N && col < D && col + 8 > D;
-            if (tail) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (col + e < D) x[e] = Elem<T>::load(X + u.row * ldx + col + e);
-            }
-            uint32_t top = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+            uint32_t top = raw[i].get(x, X + u.row * ldx, col, D, u.row < N, lane);
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const uint32_t exponent = checkpoint_exponent(top);
-            uint32_t q[2];
-            checkpoint_codes(x, exponent, q);
+            const uint2 q = checkpoint_codes(x, exponent);
             if (u.row < N && col < D) {
                 int8_t* dst = Q + u.row * ldq + col;
-                if (!tail) {
-                    __stcs(reinterpret_cast<uint2*>(dst), make_uint2(q[0], q[1]));
+                if (col + 8 <= D) {
+                    __stcs(reinterpret_cast<uint2*>(dst), q);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (col + e < D) dst[e] = static_cast<int8_t>(q[e / 4] >> (8 * (e % 4)));
+                        if (col + e < D) dst[e] = static_cast<int8_t>((e < 4 ? q.x : q.y) >> (8 * (e % 4)));
                 }
                 if ((lane & 3) == 0) E[u.row * lde + col / kCheckpointBlock] = static_cast<uint8_t>(exponent);
             }
@@ -124,7 +167,7 @@ checkpoint_store_vec_kernel(const T* X, int64_t ldx, int64_t N, int D, int8_t* Q
     }
 }
 
-// Any rows: one element per lane, so a warp reads and writes consecutive ones; the block's maximum over the warp's lanes.
+// Everything else: one element per lane, so a warp reads and writes consecutive ones; the block's maximum over the warp's lanes.
 template <typename T>
 __global__ void __launch_bounds__(kStreamThreads)
 checkpoint_store_elem_kernel(const T* X, int64_t ldx, int64_t N, int D, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, int segs)
@@ -154,7 +197,25 @@ checkpoint_store_elem_kernel(const T* X, int64_t ldx, int64_t N, int D, int8_t* 
     }
 }
 
-template <typename T, int U>
+// Eight values of a bf16 row on any boundary.  A lane puts the aligned 16 bytes that its first element lies in together with its
+// neighbour's last elements; what has no such neighbour is written one element at a time.
+__device__ __forceinline__ void store8_odd(__nv_bfloat16* p, const float (&y)[8], int count, int lane)
+{
+    const uint4 v = pack8(y);
+    const uint32_t s = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p) & 15);        // bytes of the chunk that are the neighbour's
+    const uint4 before = make_uint4(__shfl_up_sync(0xffffffffu, v.x, 1), __shfl_up_sync(0xffffffffu, v.y, 1),
+                                    __shfl_up_sync(0xffffffffu, v.z, 1), __shfl_up_sync(0xffffffffu, v.w, 1));
+    const int mine = static_cast<int>(16 - s) / 2;                                        // elements in the chunk
+    const bool whole = (lane > 0 || s == 0) && count >= mine;
+    const bool next_whole = __shfl_down_sync(0xffffffffu, static_cast<int>(whole), 1) != 0 && lane < 31;
+    if (whole) __stcs(reinterpret_cast<uint4*>(reinterpret_cast<char*>(p) - s), s == 0 ? v : shift_chunks(before, v, 16 - s));
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < count && (e < mine ? !whole : !next_whole)) p[e] = __float2bfloat16_rn(y[e]);
+}
+
+// Rows of Q on 8-byte boundaries, rows of Xhat on 16-byte ones unless ODD.
+template <typename T, int U, bool ODD = false>
 __global__ void __launch_bounds__(kStreamThreads)
 checkpoint_load_vec_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int D, T* Xhat, int64_t ldx, int segs)
 {
@@ -195,12 +256,12 @@ checkpoint_load_vec_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int64
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const int col = u.seg * kSegment + lane * 8;
-            if (u.row < N && col < D) {
-                const float s = checkpoint_step(exponent[i]);
-                float y[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = static_cast<float>(static_cast<int8_t>((e < 4 ? q[i].x : q[i].y) >> (8 * (e % 4)))) * s;
-                T* dst = Xhat + u.row * ldx + col;
+            float y[8];
+            checkpoint_values(q[i], exponent[i], y);
+            T* dst = Xhat + u.row * ldx + col;
+            if constexpr (ODD) {
+                store8_odd(dst, y, u.row < N ? min(max(D - col, 0), 8) : 0, lane);
+            } else if (u.row < N && col < D) {
                 if (col + 8 <= D) {
                     store8(dst, y);
                 } else {
@@ -254,10 +315,16 @@ int store_typed(const void* X, int64_t N, int64_t D, int64_t ldx, int8_t* Q, int
     const int d = static_cast<int>(D), segs = static_cast<int>(ceil_div64(D, kSegment));
     const int64_t units = N * segs;
     const T* x = static_cast<const T*>(X);
-    if (c_rows_vec(X, ldx, sizeof(T)) && reinterpret_cast<uintptr_t>(Q) % 8 == 0 && ldq % 8 == 0) {
-        if (units > static_cast<int64_t>(sm_count) * kStreamCtasPerSm * (kStreamThreads / 32))
-            return launch_chained(checkpoint_store_vec_kernel<T, 4>, dim3(grid_for(units, 4, sm_count)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, segs);
-        return launch_chained(checkpoint_store_vec_kernel<T, 1>, dim3(grid_for(units, 1, sm_count)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, segs);
+    const bool many = units > static_cast<int64_t>(sm_count) * kStreamCtasPerSm * (kStreamThreads / 32);
+    if (reinterpret_cast<uintptr_t>(Q) % 8 == 0 && ldq % 8 == 0) {
+        if (c_rows_vec(X, ldx, sizeof(T))) {
+            if (many) return launch_chained(checkpoint_store_vec_kernel<T, Raw8<T>, 4>, dim3(grid_for(units, 4, sm_count)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, segs);
+            return launch_chained(checkpoint_store_vec_kernel<T, Raw8<T>, 1>, dim3(grid_for(units, 1, sm_count)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, segs);
+        }
+        if constexpr (sizeof(T) == 2) {
+            if (many) return launch_chained(checkpoint_store_vec_kernel<T, Raw8Odd, 4>, dim3(grid_for(units, 4, sm_count)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, segs);
+            return launch_chained(checkpoint_store_vec_kernel<T, Raw8Odd, 1>, dim3(grid_for(units, 1, sm_count)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, segs);
+        }
     }
     return launch_chained(checkpoint_store_elem_kernel<T>, dim3(grid_for(units, 1, sm_count)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, segs);
 }
@@ -268,10 +335,16 @@ int load_typed(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int6
     const int d = static_cast<int>(D), segs = static_cast<int>(ceil_div64(D, kSegment));
     const int64_t units = N * segs;
     T* x = static_cast<T*>(Xhat);
-    if (c_rows_vec(Xhat, ldx, sizeof(T)) && reinterpret_cast<uintptr_t>(Q) % 8 == 0 && ldq % 8 == 0) {
-        if (units > static_cast<int64_t>(sm_count) * kStreamCtasPerSm * (kStreamThreads / 32))
-            return launch_chained(checkpoint_load_vec_kernel<T, 4>, dim3(grid_for(units, 4, sm_count)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, segs);
-        return launch_chained(checkpoint_load_vec_kernel<T, 1>, dim3(grid_for(units, 1, sm_count)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, segs);
+    const bool many = units > static_cast<int64_t>(sm_count) * kStreamCtasPerSm * (kStreamThreads / 32);
+    if (reinterpret_cast<uintptr_t>(Q) % 8 == 0 && ldq % 8 == 0) {
+        if (c_rows_vec(Xhat, ldx, sizeof(T))) {
+            if (many) return launch_chained(checkpoint_load_vec_kernel<T, 4>, dim3(grid_for(units, 4, sm_count)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, segs);
+            return launch_chained(checkpoint_load_vec_kernel<T, 1>, dim3(grid_for(units, 1, sm_count)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, segs);
+        }
+        if constexpr (sizeof(T) == 2) {
+            if (many) return launch_chained(checkpoint_load_vec_kernel<T, 4, true>, dim3(grid_for(units, 4, sm_count)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, segs);
+            return launch_chained(checkpoint_load_vec_kernel<T, 1, true>, dim3(grid_for(units, 1, sm_count)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, segs);
+        }
     }
     return launch_chained(checkpoint_load_elem_kernel<T>, dim3(grid_for(units, 1, sm_count)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, segs);
 }

@@ -23,25 +23,41 @@ __device__ __forceinline__ uint32_t checkpoint_exponent(uint32_t a_bits)
 // 2^(E - 127); infinite for E = 255, so that its codes of zero give NaN.
 __device__ __forceinline__ float checkpoint_step(uint32_t exponent) { return __uint_as_float(exponent << 23); }
 
-// Low byte: q.  x 2^-e is exact but where it is far below one half; adding 3 * 2^22 rounds it to an integer, ties to even.  Only the clamped
-// exponent 248 leaves more than 127.
+// Low byte: q.  x 2^-e is exact, so adding 3 * 2^22 in the same operation rounds it to an integer, ties to even.  Only under the clamped
+// exponent 248 can it be more than 127.
 __device__ __forceinline__ uint32_t checkpoint_code(float x, uint32_t exponent)
 {
-    const float inverse = __uint_as_float((254u - exponent) << 23);
-    const float t = fminf(fmaxf(x * inverse, -127.f), 127.f);
-    const uint32_t q = __float_as_uint(__fadd_rn(t, 12582912.f)) & 0xffu;
-    return exponent == kCheckpointNaN ? 0u : q;
+    const float inverse = __uint_as_float((254u - min(exponent, 248u)) << 23);
+    if (exponent >= 248u) x = exponent == kCheckpointNaN ? 0.f : fminf(fmaxf(x, -127.f / inverse), 127.f / inverse);
+    return __float_as_uint(fmaf(x, inverse, 12582912.f)) & 0xffu;
 }
-__device__ __forceinline__ void checkpoint_codes(const float (&x)[8], uint32_t exponent, uint32_t (&q)[2])
+// Eight of them, packed.
+__device__ __forceinline__ uint2 checkpoint_codes(float (&x)[8], uint32_t exponent)
 {
-    const float inverse = __uint_as_float((254u - exponent) << 23);
+    const float inverse = __uint_as_float((254u - min(exponent, 248u)) << 23);
+    if (exponent >= 248u) {
+        const float most = 127.f / inverse;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = exponent == kCheckpointNaN ? 0.f : fminf(fmaxf(x[e], -most), most);
+    }
     uint32_t r[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(__fadd_rn(fminf(fmaxf(x[e] * inverse, -127.f), 127.f), 12582912.f));
+    for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(fmaf(x[e], inverse, 12582912.f));
+    return make_uint2(__byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410),
+                      __byte_perm(__byte_perm(r[4], r[5], 0x0040), __byte_perm(r[6], r[7], 0x0040), 0x5410));
+}
+
+// Eight codes to their values.  A code with its top bit turned over is q + 128; as the low byte of 2^23 + .. it is exact in fp32.
+__device__ __forceinline__ void checkpoint_values(const uint2& q, uint32_t exponent, float (&y)[8])
+{
+    const float s = checkpoint_step(exponent);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const uint32_t lo = __byte_perm(r[4 * h], r[4 * h + 1], 0x0040), hi = __byte_perm(r[4 * h + 2], r[4 * h + 3], 0x0040);
-        q[h] = exponent == kCheckpointNaN ? 0u : __byte_perm(lo, hi, 0x5410);
+        const uint32_t w = (h ? q.y : q.x) ^ 0x80808080u;
+        y[4 * h] = (__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7650)) - 8388736.f) * s;
+        y[4 * h + 1] = (__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7651)) - 8388736.f) * s;
+        y[4 * h + 2] = (__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7652)) - 8388736.f) * s;
+        y[4 * h + 3] = (__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7653)) - 8388736.f) * s;
     }
 }
 #endif

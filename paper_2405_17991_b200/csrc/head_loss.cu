@@ -277,6 +277,7 @@ head_stats_kernel(const float* logits, int64_t ld, int cols, int v0, int N, cons
     if (row < *live) {
         const float* l = logits + row * ld;
         float m = -INFINITY;
+#pragma unroll 8
         for (int c = lane; c < cols; c += 32) m = fmaxf(m, l[c]);
         m = warp_max(m);
         float before = 0.f;
@@ -288,6 +289,7 @@ head_stats_kernel(const float* logits, int64_t ld, int cols, int v0, int N, cons
             hit = at_target[row];
         }
         float s = 0.f;
+#pragma unroll 8
         for (int c = lane; c < cols; c += 32) s += expf(l[c] - m);
         ms = make_float2(m, warp_sum(s) + before);
         if (t >= v0 && t < v0 + cols) hit = l[t - v0];
@@ -343,19 +345,27 @@ head_merge_kernel(const float2* running, int parts, int N, const int* live, cons
     write_loss(loss, lse, order[row], t, m, s, t >= 0 ? at_target[row] : 0.f);
 }
 
-// Logits to their gradients, in place.
+// Logits to their gradients, in place; a warp takes 128 columns of a row at a time, dealt over the blocks of its row.
 __global__ void __launch_bounds__(kRowThreads)
-head_gradient_kernel(float* logits, int64_t ld, int cols, int v0, int N, const int* target, const float* scale, const float* lse)
+head_gradient_kernel(float* logits, int64_t ld, int cols, int v0, const int* target, const float* scale, const float* lse)
 {
     pdl_wait();
     pdl_trigger();
-    const int row = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (row >= N) return;
+    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     float* l = logits + row * ld;
     const int t = target[row] - v0;
     const bool is = target[row] >= 0;
     const float g = scale[row], z = lse[row];
-    for (int c = lane; c < cols; c += 32) l[c] = is ? g * (expf(l[c] - z) - (c == t ? 1.f : 0.f)) : 0.f;
+    for (int c0 = (static_cast<int>(blockIdx.y) * (kRowThreads / 32) + warp) * 128; c0 < cols; c0 += static_cast<int>(gridDim.y) * (kRowThreads / 32) * 128) {
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = is && c0 + lane + 32 * i < cols ? l[c0 + lane + 32 * i] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = c0 + lane + 32 * i;
+            if (c < cols) l[c] = is ? g * (expf(x[i] - z) - (c == t ? 1.f : 0.f)) : 0.f;
+        }
+    }
 }
 
 // dX from its fp32 sums, rows back to their tokens; eight columns a lane where dX's rows start on 16-byte boundaries.
@@ -507,8 +517,9 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
         } else {
             rc = product(GEMM_NT_K_K, a.ws + l.x, a.dtype, l.ldx, w, a.dtype, ldw, G, VELORA_F32, l.piece_cols, 0, a.N, cols, a.D, status, GemmMore{}, a.stream);
             if (rc != VELORA_OK) return rc;
-            rc = launch_chained(head_gradient_kernel, grid, kRowThreads, 0, a.stream, reinterpret_cast<float*>(G), l.piece_cols, static_cast<int>(cols),
-                                static_cast<int>(v0), n, reinterpret_cast<int*>(a.ws + l.target), reinterpret_cast<float*>(a.ws + l.scale),
+            const int64_t blocks = ceil_div64(cols, 128 * (kRowThreads / 32));
+            rc = launch_chained(head_gradient_kernel, dim3(static_cast<unsigned>(a.N), static_cast<unsigned>(blocks < 16 ? blocks : 16)), kRowThreads,
+                                0, a.stream, reinterpret_cast<float*>(G), l.piece_cols, static_cast<int>(cols), static_cast<int>(v0), reinterpret_cast<int*>(a.ws + l.target), reinterpret_cast<float*>(a.ws + l.scale),
                                 reinterpret_cast<float*>(a.ws + l.lse));
         }
         if (rc != VELORA_OK) return rc;

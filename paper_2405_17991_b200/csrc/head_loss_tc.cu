@@ -180,23 +180,31 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
             const PairTile t0 = pair_tile<H_BAND>(tile, tiles_m, tiles_n, 2 * H_BM, H_BN);
             const int row0 = t0.m0 + static_cast<int>(rank) * H_BM + quarter * 32, row = row0 + lane;
             const int col0 = t0.n0 + half * 128, valid = h.cols - col0;
-            float l[4][32];
+            uint32_t l[4][32];                               // fp32 bits
+            if (ROLE == HEAD_STATS) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+                for (int c = 0; c < 4; ++c)
 #pragma unroll
-                for (int i = 0; i < 32; ++i) l[c][i] = 0.f;
+                    for (int i = 0; i < 32; ++i) l[c][i] = 0u;
+            }
             for (int k0 = 0; k0 < kblocks; k0 += segment, ++seg) {
                 const uint32_t acc = seg & 1u, aph = (seg >> 1) & 1u;
                 if (!mbar_wait_warp(tfull + 8 * acc, aph, abort_flag, 256)) { failed = true; break; }
                 tc_fence_after_sync();
                 const uint32_t taddr = tmem_base + acc * H_BN + half * 128 + (static_cast<uint32_t>(quarter * 32) << 16);
+                if (ROLE == HEAD_STATS) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t r[32];
-                    tmem_ld_32x32(taddr + c * 32, r);
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t r[32];
+                        tmem_ld_32x32(taddr + c * 32, r);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(__uint_as_float(l[c][i]) + __uint_as_float(r[i]));
+                    }
+                } else {                                     // one segment
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_ld_32x32(taddr + c * 32, l[c]);
                     tmem_ld_wait();
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) l[c][i] += __uint_as_float(r[i]);
                 }
                 tc_fence_before_sync();
                 __syncwarp();
@@ -211,20 +219,22 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                     for (int c = 0; c < 4; ++c)
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (32 * c + i >= valid) l[c][i] = -INFINITY;
+                            if (32 * c + i >= valid) l[c][i] = 0xff800000u;
                 }
-                float m = l[0][0];
+                float m = __uint_as_float(l[0][0]);
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) m = fmaxf(m, l[c][i]);
-                const float ref = m == -INFINITY ? 0.f : m;
+                    for (int i = 0; i < 32; ++i) m = fmaxf(m, __uint_as_float(l[c][i]));
+                // 2^(l log2 e - c) with c = m log2 e as rounded, in one multiply-add each; what c lost is put right in the sum.
+                const float ref = m == -INFINITY ? 0.f : m, c2 = ref * kLog2e, lost = fmaf(ref, kLog2e, -c2);
                 float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) s[i & 3] += exp2_fast((l[c][i] - ref) * kLog2e);
-                if (in) h.running[static_cast<int64_t>((t0.n0 >> 7) + half) * h.N + row] = make_float2(m, (s[0] + s[1]) + (s[2] + s[3]));
+                    for (int i = 0; i < 32; ++i) s[i & 3] += exp2_fast(fmaf(__uint_as_float(l[c][i]), kLog2e, -c2));
+                const float sum = ((s[0] + s[1]) + (s[2] + s[3])) * (1.f - lost * 0.69314718f);
+                if (in) h.running[static_cast<int64_t>((t0.n0 >> 7) + half) * h.N + row] = make_float2(m, sum);
                 const bool hit = t >= 0 && t < 128;
                 if (__any_sync(0xffffffffu, hit)) {
                     float x = 0.f;
@@ -232,25 +242,30 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                     for (int c = 0; c < 4; ++c)
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (t == 32 * c + i) x = l[c][i];
+                            if (t == 32 * c + i) x = __uint_as_float(l[c][i]);
                     if (hit) h.at_target[row] = x;
                 }
             } else {
                 const bool is = in && h.target[row] >= 0;
-                const float g = is ? h.scale[row] : 0.f, z = is ? h.lse[row] : 0.f;
+                const float g = is ? h.scale[row] : 0.f, z = is ? -h.lse[row] * kLog2e : 0.f;
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    uint32_t r[2][32];
+                for (int c = 0; c < 4; ++c) {
 #pragma unroll
-                    for (int c = 0; c < 2; ++c)
+                    for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(l[c][i]), kLog2e, z)) * g);
+                    if (__any_sync(0xffffffffu, t >= 32 * c && t < 32 * c + 32)) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            float p = exp2_fast((l[2 * b + c][i] - z) * kLog2e);
-                            if (t == 64 * b + 32 * c + i) p -= 1.f;
-                            r[c][i] = is ? __float_as_uint(p * g) : 0u;
-                        }
-                    if (row0 < h.N && valid > 64 * b) store_block(&tmG, block, r, col0 + 64 * b, row0, lane);
+                        for (int i = 0; i < 32; ++i)
+                            if (t == 32 * c + i) l[c][i] = __float_as_uint(__uint_as_float(l[c][i]) - g);
+                    }
+                    if (!__all_sync(0xffffffffu, is)) {      // rows without a target, whatever W holds
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) l[c][i] = is ? l[c][i] : 0u;
+                    }
                 }
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+                    if (row0 < h.N && valid > 64 * b)
+                        store_block(&tmG, block, *reinterpret_cast<uint32_t(*)[2][32]>(&l[2 * b]), col0 + 64 * b, row0, lane);
             }
         }
         if (ROLE == HEAD_GRADIENT && !failed) {
