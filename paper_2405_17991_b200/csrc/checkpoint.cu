@@ -16,39 +16,46 @@ namespace {
 
 constexpr int kSegment = 256;                       // columns of a row that a warp takes at a time: 8 per lane, 4 lanes a block
 
-// Units (row, segment) dealt to warps U at a time; one division at the start, then steps.
-struct UnitWalk {
-    int64_t row;
-    int seg;
-    __device__ __forceinline__ void start(int64_t unit, int segs)
+// Runs of `U` segments of a row dealt to warps; one division at the start, then steps.  Both streams were held up by instructions before
+// HBM (16 an element and 70 % of the issue slots with the addresses of every segment worked out anew): a run works out its
+// addresses once, its segments are constant offsets.
+struct RunWalk {
+    int64_t row, step_rows;
+    int run, step_runs, runs;
+    __device__ __forceinline__ RunWalk(int runs_a_row) : runs(runs_a_row)
     {
-        row = unit / segs;
-        seg = static_cast<int>(unit - row * segs);
+        const int64_t warp = static_cast<int64_t>(blockIdx.x) * (kStreamThreads / 32) + (threadIdx.x >> 5);
+        const int64_t warps = static_cast<int64_t>(gridDim.x) * (kStreamThreads / 32);
+        row = warp / runs;
+        run = static_cast<int>(warp - row * runs);
+        step_rows = warps / runs;
+        step_runs = static_cast<int>(warps - step_rows * runs);
     }
-    __device__ __forceinline__ void step(int64_t rows, int by, int segs)
+    __device__ __forceinline__ void next()
     {
-        row += rows;
-        seg += by;
-        if (seg >= segs) {
-            seg -= segs;
+        row += step_rows;
+        run += step_runs;
+        if (run >= runs) {
+            run -= runs;
             ++row;
         }
     }
 };
 
-// Eight consecutive elements of a row as loaded, rows on 16-byte boundaries.  `begin` and `end` bound the matrix.
+// Eight elements of a row as loaded, from p on, of which `left` (may be negative, or more than 8) belong to the row.
+// Rows on 16-byte boundaries:
 template <typename T> struct Raw8;
 template <> struct Raw8<__nv_bfloat16> {
     uint4 w;
-    __device__ __forceinline__ void load(const __nv_bfloat16* row, int col, int D, bool in, int, const char*, const char*) { w = ld_stream_if(row + col, in && col + 8 <= D); }
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, int left, bool, int) { w = ld_stream_if(p, left >= 8); }
     // The elements, zeros behind the row's end; the largest of their bits without signs.
-    __device__ __forceinline__ uint32_t get(float (&x)[8], const __nv_bfloat16* row, int col, int D, bool in, int)
+    __device__ __forceinline__ uint32_t get(float (&x)[8], const __nv_bfloat16* p, int left, int)
     {
-        if (in && col < D && col + 8 > D) {
+        if (left > 0 && left < 8) {
             uint32_t v[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (col + e < D) v[e >> 1] |= static_cast<uint32_t>(__bfloat16_as_ushort(row[col + e])) << (16 * (e & 1));
+            for (int e = 0; e < 7; ++e)
+                if (e < left) v[e >> 1] |= static_cast<uint32_t>(__bfloat16_as_ushort(p[e])) << (16 * (e & 1));
             w = make_uint4(v[0], v[1], v[2], v[3]);
         }
         return unpack(x, w);
@@ -63,19 +70,19 @@ template <> struct Raw8<__nv_bfloat16> {
 };
 template <> struct Raw8<float> {
     uint4 w[2];
-    __device__ __forceinline__ void load(const float* row, int col, int D, bool in, int, const char*, const char*)
+    __device__ __forceinline__ void load(const float* p, int left, bool, int)
     {
-        w[0] = ld_stream_if(row + col, in && col + 8 <= D);
-        w[1] = ld_stream_if(row + col + 4, in && col + 8 <= D);
+        w[0] = ld_stream_if(p, left >= 8);
+        w[1] = ld_stream_if(p + 4, left >= 8);
     }
-    __device__ __forceinline__ uint32_t get(float (&x)[8], const float* row, int col, int D, bool in, int) const
+    __device__ __forceinline__ uint32_t get(float (&x)[8], const float* p, int left, int) const
     {
         x[0] = __uint_as_float(w[0].x); x[1] = __uint_as_float(w[0].y); x[2] = __uint_as_float(w[0].z); x[3] = __uint_as_float(w[0].w);
         x[4] = __uint_as_float(w[1].x); x[5] = __uint_as_float(w[1].y); x[6] = __uint_as_float(w[1].z); x[7] = __uint_as_float(w[1].w);
-        if (in && col < D && col + 8 > D) {
+        if (left > 0 && left < 8) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (col + e < D) x[e] = row[col + e];
+            for (int e = 0; e < 7; ++e)
+                if (e < left) x[e] = p[e];
         }
         uint32_t top = 0;
 #pragma unroll
@@ -83,31 +90,43 @@ template <> struct Raw8<float> {
         return top;
     }
 };
-// bf16 rows on any boundary: a lane loads the aligned 16 bytes that its first element lies in, its neighbour has the rest.
+// bf16 rows on any boundary: a lane loads the aligned 16 bytes that its first element lies in, its neighbour has the rest.  On the
+// matrix's first and last row (`edge`), whose aligned bytes may lie outside it, element by element.
 struct Raw8Odd {
     uint4 w, over;
-    __device__ __forceinline__ void load(const __nv_bfloat16* row, int col, int D, bool in, int lane, const char* begin, const char* end)
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, int left, bool edge, int lane)
     {
-        const char* a = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(row + col) & ~static_cast<uintptr_t>(15));
-        const char* row_end = reinterpret_cast<const char*>(row + D);
         w = over = make_uint4(0u, 0u, 0u, 0u);
-        if (in && a < row_end) w = load_aligned_chunk(a, begin, end);
-        if (in && lane == 31 && a + 16 < row_end) over = load_aligned_chunk(a + 16, begin, end);
+        if (edge) return;
+        const int s = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15);
+        const char* a = reinterpret_cast<const char*>(p) - s;
+        w = ld_stream_if(a, left + s / 2 > 0);
+        over = ld_stream_if(a + 16, lane == 31 && left + s / 2 > 8);
     }
-    __device__ __forceinline__ uint32_t get(float (&x)[8], const __nv_bfloat16* row, int col, int D, bool, int lane)
+    __device__ __forceinline__ uint32_t get(float (&x)[8], const __nv_bfloat16* p, int left, int lane)
     {
         uint4 next = make_uint4(__shfl_down_sync(0xffffffffu, w.x, 1), __shfl_down_sync(0xffffffffu, w.y, 1),
                                 __shfl_down_sync(0xffffffffu, w.z, 1), __shfl_down_sync(0xffffffffu, w.w, 1));
         if (lane == 31) next = over;
-        w = shift_chunks(w, next, static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row + col) & 15));
-        if (col + 8 > D) {                                             // what follows is the next row's
+        w = shift_chunks(w, next, static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p) & 15));
+        if (left < 8) {                                               // what follows is the next row's
             uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (col + e >= D) v[e >> 1] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+                if (e >= left) v[e >> 1] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
             w = make_uint4(v[0], v[1], v[2], v[3]);
         }
         return Raw8<__nv_bfloat16>::unpack(x, w);
+    }
+    static __device__ __forceinline__ uint32_t get_edge(float (&x)[8], const __nv_bfloat16* p, int left)
+    {
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[e] = e < left ? __bfloat162float(p[e]) : 0.f;
+            top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+        }
+        return top;
     }
 };
 
@@ -118,51 +137,47 @@ __device__ __forceinline__ uint4 pack8(const float (&y)[8])
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&y)[8]) { __stcs(reinterpret_cast<uint4*>(p), pack8(y)); }
 __device__ __forceinline__ void store8(float* p, const float (&y)[8]) { store_f32x8(p, y); }
 
+// CTAs on an SM, by the registers that four segments in flight take.
+template <typename RAW> constexpr int kResident = sizeof(RAW) == 16 ? 5 : 4;
+constexpr int kResidentLoad = 5;
+
 // Rows of Q on 8-byte boundaries; RAW says which rows of X.
 template <typename T, typename RAW, int U>
-__global__ void __launch_bounds__(kStreamThreads)
-checkpoint_store_vec_kernel(const T* X, int64_t ldx, int64_t N, int D, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, int segs)
+__global__ void __launch_bounds__(kStreamThreads, kResident<RAW>)
+checkpoint_store_vec_kernel(const T* X, int64_t ldx, int64_t N, int D, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, int runs)
 {
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31;
-    const char* begin = reinterpret_cast<const char*>(X);
-    const char* end = reinterpret_cast<const char*>(X + (N - 1) * ldx + D);
-    const int64_t warp = static_cast<int64_t>(blockIdx.x) * (kStreamThreads / 32) + (threadIdx.x >> 5);
-    const int64_t stride = static_cast<int64_t>(gridDim.x) * (kStreamThreads / 32) * U;
-    const int64_t step_rows = stride / segs;
-    const int step_segs = static_cast<int>(stride - step_rows * segs);
-    UnitWalk at;
-    for (at.start(warp * U, segs); at.row < N; at.step(step_rows, step_segs, segs)) {
+    for (RunWalk at(runs); at.row < N; at.next()) {
+        const int col0 = at.run * (U * kSegment) + lane * 8, left0 = D - col0;
+        const T* src = X + at.row * ldx + col0;
+        const bool edge = at.row == 0 || at.row == N - 1;
         RAW raw[U];
-        UnitWalk u = at;
+#pragma unroll
+        for (int i = 0; i < U; ++i) raw[i].load(src + i * kSegment, left0 - i * kSegment, edge, lane);
+        int8_t* dst = Q + at.row * ldq + col0;
+        uint8_t* exps = E + at.row * lde + col0 / kCheckpointBlock;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            raw[i].load(X + u.row * ldx, u.seg * kSegment + lane * 8, D, u.row < N, lane, begin, end);
-            u.step(0, 1, segs);
-        }
-        u = at;
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int col = u.seg * kSegment + lane * 8;
+            const int left = left0 - i * kSegment;
+            if (D - at.run * (U * kSegment) <= i * kSegment) break;            // for the whole warp
             float x[8];
-            uint32_t top = raw[i].get(x, X + u.row * ldx, col, D, u.row < N, lane);
+            uint32_t top = raw[i].get(x, src + i * kSegment, left, lane);
+            if constexpr (sizeof(RAW) == sizeof(Raw8Odd) && sizeof(T) == 2)
+                if (edge) top = Raw8Odd::get_edge(x, src + i * kSegment, left);
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const uint32_t exponent = checkpoint_exponent(top);
             const uint2 q = checkpoint_codes(x, exponent);
-            if (u.row < N && col < D) {
-                int8_t* dst = Q + u.row * ldq + col;
-                if (col + 8 <= D) {
-                    __stcs(reinterpret_cast<uint2*>(dst), q);
-                } else {
+            if (left >= 8) {
+                __stcs(reinterpret_cast<uint2*>(dst + i * kSegment), q);
+            } else if (left > 0) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (col + e < D) dst[e] = static_cast<int8_t>((e < 4 ? q.x : q.y) >> (8 * (e % 4)));
-                }
-                if ((lane & 3) == 0) E[u.row * lde + col / kCheckpointBlock] = static_cast<uint8_t>(exponent);
+                for (int e = 0; e < 7; ++e)
+                    if (e < left) dst[i * kSegment + e] = static_cast<int8_t>((e < 4 ? q.x : q.y) >> (8 * (e % 4)));
             }
-            u.step(0, 1, segs);
+            if ((lane & 3) == 0 && left > 0) exps[i * (kSegment / kCheckpointBlock)] = static_cast<uint8_t>(exponent);
         }
     }
 }
@@ -170,18 +185,13 @@ checkpoint_store_vec_kernel(const T* X, int64_t ldx, int64_t N, int D, int8_t* Q
 // Everything else: one element per lane, so a warp reads and writes consecutive ones; the block's maximum over the warp's lanes.
 template <typename T>
 __global__ void __launch_bounds__(kStreamThreads)
-checkpoint_store_elem_kernel(const T* X, int64_t ldx, int64_t N, int D, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, int segs)
+checkpoint_store_elem_kernel(const T* X, int64_t ldx, int64_t N, int D, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, int runs)
 {
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31;
-    const int64_t stride = static_cast<int64_t>(gridDim.x) * (kStreamThreads / 32);
-    const int64_t step_rows = stride / segs;
-    const int step_segs = static_cast<int>(stride - step_rows * segs);
-    UnitWalk at;
-    for (at.start(static_cast<int64_t>(blockIdx.x) * (kStreamThreads / 32) + (threadIdx.x >> 5), segs); at.row < N;
-         at.step(step_rows, step_segs, segs)) {
-        const int col0 = at.seg * kSegment + lane;
+    for (RunWalk at(runs); at.row < N; at.next()) {
+        const int col0 = at.run * kSegment + lane;
         const T* src = X + at.row * ldx + col0;
         float x[8];
 #pragma unroll
@@ -193,7 +203,7 @@ checkpoint_store_elem_kernel(const T* X, int64_t ldx, int64_t N, int D, int8_t* 
             if (lane == i) mine = exponent;
             if (col0 + 32 * i < D) Q[at.row * ldq + col0 + 32 * i] = static_cast<int8_t>(checkpoint_code(x[i], exponent));
         }
-        if (lane < 8 && at.seg * kSegment + 32 * lane < D) E[at.row * lde + at.seg * (kSegment / 32) + lane] = static_cast<uint8_t>(mine);
+        if (lane < 8 && at.run * kSegment + 32 * lane < D) E[at.row * lde + at.run * (kSegment / 32) + lane] = static_cast<uint8_t>(mine);
     }
 }
 
@@ -209,92 +219,78 @@ __device__ __forceinline__ void store8_odd(__nv_bfloat16* p, const float (&y)[8]
     const bool whole = (lane > 0 || s == 0) && count >= mine;
     const bool next_whole = __shfl_down_sync(0xffffffffu, static_cast<int>(whole), 1) != 0 && lane < 31;
     if (whole) __stcs(reinterpret_cast<uint4*>(reinterpret_cast<char*>(p) - s), s == 0 ? v : shift_chunks(before, v, 16 - s));
+    if (!whole || !next_whole) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < count && (e < mine ? !whole : !next_whole)) p[e] = __float2bfloat16_rn(y[e]);
+        for (int e = 0; e < 8; ++e)
+            if (e < count && (e < mine ? !whole : !next_whole)) p[e] = __float2bfloat16_rn(y[e]);
+    }
 }
 
 // Rows of Q on 8-byte boundaries, rows of Xhat on 16-byte ones unless ODD.
-template <typename T, int U, bool ODD = false>
-__global__ void __launch_bounds__(kStreamThreads)
-checkpoint_load_vec_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int D, T* Xhat, int64_t ldx, int segs)
+template <typename T, int U, bool ODD>
+__global__ void __launch_bounds__(kStreamThreads, kResidentLoad)
+checkpoint_load_vec_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int D, T* Xhat, int64_t ldx, int runs)
 {
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31;
-    const int64_t warp = static_cast<int64_t>(blockIdx.x) * (kStreamThreads / 32) + (threadIdx.x >> 5);
-    const int64_t stride = static_cast<int64_t>(gridDim.x) * (kStreamThreads / 32) * U;
-    const int64_t step_rows = stride / segs;
-    const int step_segs = static_cast<int>(stride - step_rows * segs);
-    UnitWalk at;
-    for (at.start(warp * U, segs); at.row < N; at.step(step_rows, step_segs, segs)) {
+    for (RunWalk at(runs); at.row < N; at.next()) {
+        const int col0 = at.run * (U * kSegment) + lane * 8, left0 = D - col0;
+        const int8_t* src = Q + at.row * ldq + col0;
+        const uint8_t* exps = E + at.row * lde + col0 / kCheckpointBlock;
         uint2 q[U];
         uint32_t exponent[U];
-        UnitWalk u = at;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const int col = u.seg * kSegment + lane * 8;
-            const bool in = u.row < N && col < D;
+            const int left = left0 - i * kSegment;
             q[i] = make_uint2(0, 0);
             exponent[i] = 0;
-            if (in) {
-                exponent[i] = E[u.row * lde + col / kCheckpointBlock];
-                const int8_t* src = Q + u.row * ldq + col;
-                if (col + 8 <= D) {
-                    q[i] = __ldcs(reinterpret_cast<const uint2*>(src));
+            if (left > 0) {
+                exponent[i] = exps[i * (kSegment / kCheckpointBlock)];
+                if (left >= 8) {
+                    q[i] = __ldcs(reinterpret_cast<const uint2*>(src + i * kSegment));
                 } else {
-                    for (int e = 0; e < D - col; ++e) {
-                        const uint32_t byte = static_cast<uint8_t>(src[e]);
-                        if (e < 4) q[i].x |= byte << (8 * e);
-                        else q[i].y |= byte << (8 * e - 32);
-                    }
+#pragma unroll
+                    for (int e = 0; e < 7; ++e)
+                        if (e < left) (e < 4 ? q[i].x : q[i].y) |= static_cast<uint32_t>(static_cast<uint8_t>(src[i * kSegment + e])) << (8 * (e % 4));
                 }
             }
-            u.step(0, 1, segs);
         }
-        u = at;
+        T* dst = Xhat + at.row * ldx + col0;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const int col = u.seg * kSegment + lane * 8;
+            const int left = left0 - i * kSegment;
+            if (D - at.run * (U * kSegment) <= i * kSegment) break;            // for the whole warp
             float y[8];
             checkpoint_values(q[i], exponent[i], y);
-            T* dst = Xhat + u.row * ldx + col;
             if constexpr (ODD) {
-                store8_odd(dst, y, u.row < N ? min(max(D - col, 0), 8) : 0, lane);
-            } else if (u.row < N && col < D) {
-                if (col + 8 <= D) {
-                    store8(dst, y);
-                } else {
+                store8_odd(dst + i * kSegment, y, min(max(left, 0), 8), lane);
+            } else if (left >= 8) {
+                store8(dst + i * kSegment, y);
+            } else if (left > 0) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (col + e < D) Elem<T>::store(dst + e, y[e]);
-                }
+                for (int e = 0; e < 7; ++e)
+                    if (e < left) Elem<T>::store(dst + i * kSegment + e, y[e]);
             }
-            u.step(0, 1, segs);
         }
     }
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kStreamThreads)
-checkpoint_load_elem_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int D, T* Xhat, int64_t ldx, int segs)
+checkpoint_load_elem_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int D, T* Xhat, int64_t ldx, int runs)
 {
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31;
-    const int64_t stride = static_cast<int64_t>(gridDim.x) * (kStreamThreads / 32);
-    const int64_t step_rows = stride / segs;
-    const int step_segs = static_cast<int>(stride - step_rows * segs);
-    UnitWalk at;
-    for (at.start(static_cast<int64_t>(blockIdx.x) * (kStreamThreads / 32) + (threadIdx.x >> 5), segs); at.row < N;
-         at.step(step_rows, step_segs, segs)) {
-        const int col0 = at.seg * kSegment + lane;
+    for (RunWalk at(runs); at.row < N; at.next()) {
+        const int col0 = at.run * kSegment + lane;
         float q[8], s[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const bool in = col0 + 32 * i < D;
             q[i] = in ? static_cast<float>(Q[at.row * ldq + col0 + 32 * i]) : 0.f;
-            s[i] = in ? checkpoint_step(E[at.row * lde + at.seg * (kSegment / 32) + i]) : 0.f;
+            s[i] = in ? checkpoint_step(E[at.row * lde + at.run * (kSegment / 32) + i]) : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -302,52 +298,64 @@ checkpoint_load_elem_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int6
     }
 }
 
-// CTAs for `units` warps' worth of work, U units a warp and step.
-unsigned grid_for(int64_t units, int u, int sm_count)
+// As many CTAs as are resident at a time and no more than there is work for.
+unsigned grid_for(int64_t runs, int sm_count, int resident)
 {
-    const int64_t ctas = ceil_div64(units, static_cast<int64_t>(kStreamThreads / 32) * u), most = static_cast<int64_t>(sm_count) * kStreamCtasPerSm;
+    const int64_t ctas = ceil_div64(runs, kStreamThreads / 32), most = static_cast<int64_t>(sm_count) * resident;
     return static_cast<unsigned>(ctas < most ? ctas : most);
 }
+
+// Segments in a run: four, or fewer where the rows have fewer or the warps of the chip would not all get a run.
+int run_segments(int64_t N, int64_t D, int sm_count)
+{
+    const int64_t segs = ceil_div64(D, kSegment), warps = static_cast<int64_t>(sm_count) * kResidentLoad * (kStreamThreads / 32);
+    if (segs <= 1 || N * ceil_div64(segs, 2) < warps) return 1;
+    return segs <= 2 || N * ceil_div64(segs, 4) < warps ? 2 : 4;
+}
+
+#define VELORA_BY_SEGMENTS(LAUNCH) (u == 1 ? LAUNCH(1) : (u == 2 ? LAUNCH(2) : LAUNCH(4)))
 
 template <typename T>
 int store_typed(const void* X, int64_t N, int64_t D, int64_t ldx, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, int sm_count, cudaStream_t stream)
 {
-    const int d = static_cast<int>(D), segs = static_cast<int>(ceil_div64(D, kSegment));
-    const int64_t units = N * segs;
+    const int d = static_cast<int>(D);
     const T* x = static_cast<const T*>(X);
-    const bool many = units > static_cast<int64_t>(sm_count) * kStreamCtasPerSm * (kStreamThreads / 32);
     if (reinterpret_cast<uintptr_t>(Q) % 8 == 0 && ldq % 8 == 0) {
-        if (c_rows_vec(X, ldx, sizeof(T))) {
-            if (many) return launch_chained(checkpoint_store_vec_kernel<T, Raw8<T>, 4>, dim3(grid_for(units, 4, sm_count)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, segs);
-            return launch_chained(checkpoint_store_vec_kernel<T, Raw8<T>, 1>, dim3(grid_for(units, 1, sm_count)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, segs);
-        }
+        const int u = run_segments(N, D, sm_count), runs = static_cast<int>(ceil_div64(D, u * kSegment));
+#define VELORA_STORE(U) launch_chained(checkpoint_store_vec_kernel<T, Raw8<T>, U>, dim3(grid_for(N * runs, sm_count, kResident<Raw8<T>>)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, runs)
+        if (c_rows_vec(X, ldx, sizeof(T))) return VELORA_BY_SEGMENTS(VELORA_STORE);
+#undef VELORA_STORE
         if constexpr (sizeof(T) == 2) {
-            if (many) return launch_chained(checkpoint_store_vec_kernel<T, Raw8Odd, 4>, dim3(grid_for(units, 4, sm_count)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, segs);
-            return launch_chained(checkpoint_store_vec_kernel<T, Raw8Odd, 1>, dim3(grid_for(units, 1, sm_count)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, segs);
+#define VELORA_STORE(U) launch_chained(checkpoint_store_vec_kernel<T, Raw8Odd, U>, dim3(grid_for(N * runs, sm_count, kResident<Raw8Odd>)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, runs)
+            return VELORA_BY_SEGMENTS(VELORA_STORE);
+#undef VELORA_STORE
         }
     }
-    return launch_chained(checkpoint_store_elem_kernel<T>, dim3(grid_for(units, 1, sm_count)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, segs);
+    const int runs = static_cast<int>(ceil_div64(D, kSegment));
+    return launch_chained(checkpoint_store_elem_kernel<T>, dim3(grid_for(N * runs, sm_count, kStreamCtasPerSm)), kStreamThreads, 0, stream, x, ldx, N, d, Q, ldq, E, lde, runs);
 }
 
 template <typename T>
 int load_typed(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int64_t D, void* Xhat, int64_t ldx, int sm_count, cudaStream_t stream)
 {
-    const int d = static_cast<int>(D), segs = static_cast<int>(ceil_div64(D, kSegment));
-    const int64_t units = N * segs;
+    const int d = static_cast<int>(D);
     T* x = static_cast<T*>(Xhat);
-    const bool many = units > static_cast<int64_t>(sm_count) * kStreamCtasPerSm * (kStreamThreads / 32);
     if (reinterpret_cast<uintptr_t>(Q) % 8 == 0 && ldq % 8 == 0) {
-        if (c_rows_vec(Xhat, ldx, sizeof(T))) {
-            if (many) return launch_chained(checkpoint_load_vec_kernel<T, 4>, dim3(grid_for(units, 4, sm_count)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, segs);
-            return launch_chained(checkpoint_load_vec_kernel<T, 1>, dim3(grid_for(units, 1, sm_count)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, segs);
-        }
+        const int u = run_segments(N, D, sm_count), runs = static_cast<int>(ceil_div64(D, u * kSegment));
+        const dim3 grid(grid_for(N * runs, sm_count, kResidentLoad));
+#define VELORA_LOAD(U) launch_chained(checkpoint_load_vec_kernel<T, U, false>, grid, kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, runs)
+        if (c_rows_vec(Xhat, ldx, sizeof(T))) return VELORA_BY_SEGMENTS(VELORA_LOAD);
+#undef VELORA_LOAD
         if constexpr (sizeof(T) == 2) {
-            if (many) return launch_chained(checkpoint_load_vec_kernel<T, 4, true>, dim3(grid_for(units, 4, sm_count)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, segs);
-            return launch_chained(checkpoint_load_vec_kernel<T, 1, true>, dim3(grid_for(units, 1, sm_count)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, segs);
+#define VELORA_LOAD(U) launch_chained(checkpoint_load_vec_kernel<T, U, true>, grid, kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, runs)
+            return VELORA_BY_SEGMENTS(VELORA_LOAD);
+#undef VELORA_LOAD
         }
     }
-    return launch_chained(checkpoint_load_elem_kernel<T>, dim3(grid_for(units, 1, sm_count)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, segs);
+    const int runs = static_cast<int>(ceil_div64(D, kSegment));
+    return launch_chained(checkpoint_load_elem_kernel<T>, dim3(grid_for(N * runs, sm_count, kStreamCtasPerSm)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, runs);
 }
+#undef VELORA_BY_SEGMENTS
 
 }  // namespace
 
