@@ -493,14 +493,17 @@ def velora_checkpoint_store(X: torch.Tensor, Q: Optional[torch.Tensor] = None, E
     xp, ldx = _mat(X, "X")
     N, D = X.shape
     blocks = -(-D // CHECKPOINT_BLOCK)
-    if Q is None:
-        Q = torch.empty_strided((N, D), (-(-D // 16) * 16, 1), dtype=torch.int8, device=X.device)
-    if E is None:
-        E = torch.empty_strided((N, blocks), (-(-blocks // 16) * 16, 1), dtype=torch.uint8, device=X.device)
-    if Q.shape != X.shape:
-        raise ValueError("Q must have X's shape")
-    qp, ldq, ep, lde = _codes(Q, E)
-    _here(X, Q, E)
+    if Q is None and E is None:
+        ldq, lde, device = -(-D // 16) * 16, -(-blocks // 16) * 16, X.device
+        Q = torch.empty_strided((N, D), (ldq, 1), dtype=torch.int8, device=device)
+        E = torch.empty_strided((N, blocks), (lde, 1), dtype=torch.uint8, device=device)
+        qp, ep = Q.data_ptr(), E.data_ptr()
+        _here(X)
+    else:
+        if Q is None or E is None or Q.shape != X.shape:
+            raise ValueError("Q and E go together, Q with X's shape")
+        qp, ldq, ep, lde = _codes(Q, E)
+        _here(X, Q, E)
     _check(lib().velora_checkpoint_store(xp, _dt(X), N, D, ldx, qp, ldq, ep, lde, _stream(stream)), "velora_checkpoint_store")
     return Q, E
 
@@ -510,11 +513,14 @@ def velora_checkpoint_load(Q: torch.Tensor, E: torch.Tensor, Xhat: Optional[torc
     qp, ldq, ep, lde = _codes(Q, E)
     N, D = Q.shape
     if Xhat is None:
-        Xhat = torch.empty((N, D), dtype=x_dtype, device=Q.device)
-    if Xhat.shape != Q.shape:
-        raise ValueError("Xhat must have Q's shape")
-    xp, ldx = _mat(Xhat, "Xhat")
-    _here(Q, E, Xhat)
+        Xhat = torch.empty_strided((N, D), (D, 1), dtype=x_dtype, device=Q.device)
+        xp, ldx = Xhat.data_ptr(), D
+        _here(Q, E)
+    else:
+        if Xhat.shape != Q.shape:
+            raise ValueError("Xhat must have Q's shape")
+        xp, ldx = _mat(Xhat, "Xhat")
+        _here(Q, E, Xhat)
     _check(lib().velora_checkpoint_load(qp, ldq, ep, lde, N, D, xp, _dt(Xhat), ldx, _stream(stream)), "velora_checkpoint_load")
     return Xhat
 

@@ -154,7 +154,7 @@ head_rows_kernel(const RowsArgs a)
     // The common factor: none where it could not be divided by.
     float common = __int_as_float(counts[2]);
     if (!(common >= 1.17549435e-38f && common <= 3.4e38f)) common = 1.f;
-    if (blockIdx.x == 0 && t == 0) {
+    if (blockIdx.x == 0 && blockIdx.y == 0 && t == 0) {
         *a.live = total;
         if (a.scale_out) *a.common = common;
     }
@@ -174,15 +174,18 @@ head_rows_kernel(const RowsArgs a)
         if (n < r1) {
             const int to = is ? first : total + (n - first);
             row_to[t] = is ? to : -1 - to;
-            a.order[to] = n;
-            a.target_out[to] = is ? static_cast<int>(v) : (v < 0 ? -1 : -2);
-            if (a.scale_out) {
-                a.scale_out[to] = is ? a.dloss[n] / common : 0.f;
-                a.lse_out[to] = is ? a.lse[n] : 0.f;
+            if (blockIdx.y == 0) {
+                a.order[to] = n;
+                a.target_out[to] = is ? static_cast<int>(v) : (v < 0 ? -1 : -2);
+                if (a.scale_out) {
+                    a.scale_out[to] = is ? a.dloss[n] / common : 0.f;
+                    a.lse_out[to] = is ? a.lse[n] : 0.f;
+                }
+                if (v >= a.V && a.status) atomicCAS(a.status, 0, VELORA_ERR_INVALID_ARG);
             }
-            if (v >= a.V && a.status) atomicCAS(a.status, 0, VELORA_ERR_INVALID_ARG);
         }
         __syncthreads();
+        // Few rows: the columns of each are shared out over the blocks of the grid's other direction.
         for (int i = warp; i < min(kRowThreads, r1 - b0); i += kRowThreads / 32) {
             const int code = row_to[i];
             const bool zero = code < 0;
@@ -192,10 +195,10 @@ head_rows_kernel(const RowsArgs a)
                 constexpr int per = 16 / sizeof(T);
                 const int chunks = a.D / per;                      // D is a multiple of 8
 #pragma unroll 4
-                for (int c = lane; c < chunks; c += 32)
+                for (int c = lane + 32 * blockIdx.y; c < chunks; c += 32 * gridDim.y)
                     reinterpret_cast<uint4*>(dst)[c] = ld_stream_if(src + c * per, !zero);
             } else {
-                for (int c = lane; c < a.ldx_out; c += 32) Elem<T>::store(dst + c, zero || c >= a.D ? 0.f : Elem<T>::load(src + c));
+                for (int c = lane + 32 * blockIdx.y; c < a.ldx_out; c += 32 * gridDim.y) Elem<T>::store(dst + c, zero || c >= a.D ? 0.f : Elem<T>::load(src + c));
             }
         }
         before += all;
@@ -232,7 +235,8 @@ int launch_rows(const HeadArgs& a, const HeadLayout& l, const float* lse, const 
     // Eight rows a CTA (one a warp) as long as that leaves no more than four CTAs per SM.
     const int64_t most = static_cast<int64_t>(di.sm_count) * 4;
     r.rows_per_cta = static_cast<int>(round_up(ceil_div64(a.N, most), 8));
-    const dim3 grid(static_cast<unsigned>(ceil_div64(a.N, r.rows_per_cta)));
+    const int64_t ctas = ceil_div64(a.N, r.rows_per_cta), slices = ceil_div64(a.D, 512);          // of two chunks a lane and more
+    const dim3 grid(static_cast<unsigned>(ctas), static_cast<unsigned>(ctas * slices <= di.sm_count ? slices : 1));
     const bool vec = a.D % 8 == 0 && aligned16(a.X) && (a.ldx * dtype_size(a.dtype)) % 16 == 0;
     if (a.dtype == VELORA_BF16)
         return vec ? launch_chained(head_rows_kernel<__nv_bfloat16, true>, grid, kRowThreads, 0, a.stream, r)
@@ -466,7 +470,7 @@ int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
     const int n = static_cast<int>(a.N);
     if (a.dtype == VELORA_BF16) {
         const HeadTile h = head_tile(a, l, 0, a.V);
-        rc = launch_head_tiles(a.ws + l.x, l.ldx, W, ldw, nullptr, 0, h, status, a.stream);
+        rc = (a.N <= kHeadFew ? launch_head_few : launch_head_tiles)(a.ws + l.x, l.ldx, W, ldw, nullptr, 0, h, status, a.stream);
         if (rc != VELORA_OK) return rc;
         return launch_chained(head_merge_kernel, dim3(static_cast<unsigned>(ceil_div64(a.N, 32))), kRowThreads, 0, a.stream, h.running,
                               static_cast<int>(ceil_div64(a.V, 128)), n, h.live, reinterpret_cast<int*>(a.ws + l.order), h.target, h.at_target, loss, lse);
@@ -513,7 +517,7 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
         const int64_t cols = a.V - v0 < l.piece_cols ? a.V - v0 : l.piece_cols;
         const char* w = W + static_cast<size_t>(v0) * ldw * dtype_size(a.dtype);
         if (a.dtype == VELORA_BF16) {
-            rc = launch_head_tiles(a.ws + l.x, l.ldx, w, ldw, G, l.piece_cols, head_tile(a, l, v0, cols), status, a.stream);
+            rc = (a.N <= kHeadFew ? launch_head_few : launch_head_tiles)(a.ws + l.x, l.ldx, w, ldw, G, l.piece_cols, head_tile(a, l, v0, cols), status, a.stream);
         } else {
             rc = product(GEMM_NT_K_K, a.ws + l.x, a.dtype, l.ldx, w, a.dtype, ldw, G, VELORA_F32, l.piece_cols, 0, a.N, cols, a.D, status, GemmMore{}, a.stream);
             if (rc != VELORA_OK) return rc;

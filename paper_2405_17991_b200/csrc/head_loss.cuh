@@ -49,6 +49,20 @@ struct HeadTile {
 // G == nullptr: statistics of bf16 x W^T; otherwise its gradient to G [N, ldg].  W: its row v0.  (head_loss_tc.cu)
 int launch_head_tiles(const void* x, int64_t ldx, const void* W, int64_t ldw, void* G, int64_t ldg, const HeadTile& h, int* status, cudaStream_t stream);
 
+// The same for up to kHeadFew tokens.  (head_loss_few.cu)
+constexpr int kHeadFew = 128;
+int launch_head_few(const void* x, int64_t ldx, const void* W, int64_t ldw, void* G, int64_t ldg, const HeadTile& h, int* status, cudaStream_t stream);
+
+#ifdef __CUDACC__
+constexpr float kHeadLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float head_exp2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+#endif
+
 // What velora_workspace_bytes reports.
 size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool any_rows);
 int launch_head_loss(const HeadArgs& a, float* loss, float* lse);

@@ -1,0 +1,279 @@
+// The logits of a linear head for few tokens (up to 128), used up where they come out of the tensor cores; roles and results as in
+// head_loss_tc.cu.  What bounds it is reading W once, so W's rows are the rows of the products: tiles of 128 columns of the vocabulary,
+// the tokens (rounded up to 32, 64 or 128) are the other side, and no tensor-core time goes into rows that are not there.  Single CTAs with up to
+// 200 KB of W in flight each; a CTA that has one tile more than another finds the memory less busy, so uneven shares cost little.
+//
+// Per CTA: warp 0 lane 0 TMA producer, warp 1 lane 0 MMA issuer, warps 2..5 epilogue (32 columns of the vocabulary each).  A lane of the
+// epilogue has one column for all tokens; 32 x 32 blocks are turned over through shared memory, and then it has one token for 32
+// columns.  Contractions are cut into segments of 1024 as in head_loss_tc.cu.  1 x 4096 of 32000: 51 us, 262 MB at 5.1 TB/s (71 us with the
+// tokens as rows of 256).
+#include "gemm_tc.cuh"
+#include "head_loss.cuh"
+#include "tc_common.cuh"
+
+namespace velora {
+
+using namespace tc;
+
+namespace {
+
+constexpr int W_BM = 128;                  // columns of the vocabulary in a tile
+constexpr int W_BK = 64;
+constexpr int W_SEGMENT = 16;              // k-blocks that an accumulator adds up
+constexpr int W_THREADS = 192;
+constexpr int W_PITCH = 33;
+constexpr int W_STAGING_BYTES = 4 * 32 * W_PITCH * 4;
+constexpr int W_PARTS_BYTES = 4 * 128 * 8;                     // (maximum, sum) of each warp and token
+constexpr int W_BARRIER_BYTES = 256;
+
+template <int NT> struct FewShape {
+    static constexpr int kStageBytes = (W_BM + NT) * W_BK * 2;
+    static constexpr int kStages = 200 * 1024 / kStageBytes < 10 ? 200 * 1024 / kStageBytes : 10;
+    static constexpr int kTmemCols = 2 * NT;                   // a power of two, 64 or more
+    static constexpr size_t kSmem = 1024 + static_cast<size_t>(kStages) * kStageBytes + W_STAGING_BYTES + W_PARTS_BYTES + W_BARRIER_BYTES;
+};
+
+// All epilogue warps; true in all of them if `p` is in one.  A warp that has given up comes here as well, so nobody waits for it.
+__device__ __forceinline__ bool epilogue_any(bool p)
+{
+    uint32_t any;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(any) : "r"(static_cast<uint32_t>(p)) : "memory");
+    return any != 0;
+}
+
+template <bool GRADIENT, int NT>
+__global__ void __launch_bounds__(W_THREADS, 1)
+head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const HeadTile h, __nv_bfloat16* G, int64_t ldg,
+                int* status)
+{
+    typedef FewShape<NT> S;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    uint8_t* smem = smem_raw + (base - raw);
+    float* staging = reinterpret_cast<float*>(smem + S::kStages * S::kStageBytes);
+    float2* parts = reinterpret_cast<float2*>(smem + S::kStages * S::kStageBytes + W_STAGING_BYTES);
+    uint8_t* tail = smem + S::kStages * S::kStageBytes + W_STAGING_BYTES + W_PARTS_BYTES;
+    const uint32_t full = smem_u32(tail), empty = full + 8 * S::kStages;
+    const uint32_t tfull = full + 16 * S::kStages, tempty = tfull + 16;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 16 * S::kStages + 32);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 16 * S::kStages + 40);
+    static_assert(16 * S::kStages + 48 <= W_BARRIER_BYTES, "barriers");
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int num_tiles = (h.cols + W_BM - 1) / W_BM, kblocks = (h.D + W_BK - 1) / W_BK;
+    const int segment = GRADIENT ? kblocks : W_SEGMENT;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) {
+            mbar_init(full + 8 * s, 1);
+            mbar_init(empty + 8 * s, 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(tfull + 8 * a, 1);
+            mbar_init(tempty + 8 * a, 4);
+        }
+        *abort_flag = 0;
+        fence_mbar_init();
+        prefetch_tensormap(&tmW);
+        prefetch_tensormap(&tmX);
+    }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(tmem_slot), S::kTmemCols);
+        tmem_relinquish();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem_base = *tmem_slot;
+    pdl_wait();                                              // nothing in global memory has been touched so far
+    pdl_trigger();
+
+    bool failed = false;
+    if (warp == 0) {
+        // ------------------------------------------------ TMA producer
+        if (lane == 0) {
+            uint32_t it = 0;
+            for (int tile = blockIdx.x; tile < num_tiles && !failed; tile += gridDim.x) {
+                for (int kb = 0; kb < kblocks; ++kb, ++it) {
+                    const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1u;
+                    if (!mbar_wait(empty + 8 * s, ph ^ 1u, abort_flag)) { failed = true; break; }
+                    mbar_arrive_expect_tx(full + 8 * s, S::kStageBytes);
+                    const uint32_t dst = base + s * S::kStageBytes;
+                    tma_load_2d(dst, &tmW, full + 8 * s, kb * W_BK, tile * W_BM);
+                    tma_load_2d(dst + W_BM * W_BK * 2, &tmX, full + 8 * s, kb * W_BK, 0);
+                }
+            }
+            if (failed) {
+                *abort_flag = 1;
+                // Let the copies in flight land before shared memory is given up.
+                const unsigned long long t0 = globaltimer_ns();
+                const uint32_t back = it < S::kStages ? it : S::kStages;
+                for (uint32_t j = 1; j <= back; ++j) {
+                    const uint32_t jt = it - j;
+                    while (!mbar_try_wait(full + 8 * (jt % S::kStages), (jt / S::kStages) & 1u))
+                        if (globaltimer_ns() - t0 > kWaitLimitNs) break;
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------ MMA issuer
+        if (lane == 0) {
+            constexpr uint32_t idesc = umma_idesc_bf16(W_BM, NT, false, false);
+            uint32_t it = 0, seg = 0;
+            for (int tile = blockIdx.x; tile < num_tiles && !failed; tile += gridDim.x) {
+                for (int k0 = 0; k0 < kblocks && !failed; k0 += segment, ++seg) {
+                    const uint32_t acc = seg & 1u, aph = (seg >> 1) & 1u;
+                    if (!mbar_wait(tempty + 8 * acc, aph ^ 1u, abort_flag)) { failed = true; break; }
+                    tc_fence_after_sync();
+                    const uint32_t d_tmem = tmem_base + acc * NT;
+                    const int k1 = min(kblocks, k0 + segment);
+                    for (int kb = k0; kb < k1; ++kb, ++it) {
+                        const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1u;
+                        if (!mbar_wait(full + 8 * s, ph, abort_flag)) { failed = true; break; }
+                        tc_fence_after_sync();
+                        const uint32_t a_addr = base + s * S::kStageBytes, b_addr = a_addr + W_BM * W_BK * 2;
+#pragma unroll
+                        for (int j = 0; j < W_BK / 16; ++j)
+                            umma_bf16(d_tmem, umma_smem_desc(a_addr + j * 32, 16, 1024), umma_smem_desc(b_addr + j * 32, 16, 1024), idesc, ((kb - k0) | j) != 0);
+                        umma_commit(empty + 8 * s);
+                    }
+                    if (!failed) umma_commit(tfull + 8 * acc);
+                }
+            }
+            if (failed) *abort_flag = 1;
+        }
+    } else {
+        // ------------------------------------------------ epilogue
+        const int quarter = warp & 3;
+        float* block = staging + quarter * (32 * W_PITCH);
+        uint32_t seg = 0;
+        for (int tile = blockIdx.x; tile < num_tiles && !failed; tile += gridDim.x) {
+            uint32_t l[NT / 32][32];                         // fp32 bits
+#pragma unroll
+            for (int c = 0; c < NT / 32; ++c)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) l[c][i] = 0u;
+            for (int k0 = 0; k0 < kblocks; k0 += segment, ++seg) {
+                const uint32_t acc = seg & 1u, aph = (seg >> 1) & 1u;
+                if (!mbar_wait_warp(tfull + 8 * acc, aph, abort_flag, 64)) { failed = true; *abort_flag = 1; break; }
+                tc_fence_after_sync();
+#pragma unroll
+                for (int c = 0; c < NT / 32; ++c) {
+                    uint32_t r[32];
+                    tmem_ld_32x32(tmem_base + acc * NT + c * 32 + (static_cast<uint32_t>(quarter * 32) << 16), r);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(__uint_as_float(l[c][i]) + __uint_as_float(r[i]));
+                }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(tempty + 8 * acc);
+            }
+            if (GRADIENT ? failed : (failed = epilogue_any(failed))) break;      // behind it nobody reads the last tile's parts any more
+            const int v0 = tile * W_BM + quarter * 32, valid = min(32, h.cols - v0);      // this warp's columns; may be none
+#pragma unroll
+            for (int c = 0; c < NT / 32; ++c) {
+                const int row = 32 * c + lane;               // this lane's token behind the turn
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) block[i * W_PITCH + lane] = __uint_as_float(l[c][i]);
+                __syncwarp();
+                if (32 * c >= h.N) break;                    // for all epilogue warps
+                const int target = row < h.N ? h.target[row] : -1, t = target - h.v0 - v0;
+                const float* mine = block + lane * W_PITCH;
+                if (!GRADIENT) {
+                    float m = -INFINITY, s = 0.f;
+                    for (int i = 0; i < valid; ++i) m = fmaxf(m, mine[i]);
+                    const float ref = m == -INFINITY ? 0.f : m, c2 = ref * kHeadLog2e, lost = fmaf(ref, kHeadLog2e, -c2);
+#pragma unroll 8
+                    for (int i = 0; i < valid; ++i) s += head_exp2(fmaf(mine[i], kHeadLog2e, -c2));
+                    parts[quarter * NT + row] = make_float2(m, s * (1.f - lost * 0.69314718f));
+                    if (t >= 0 && t < valid) h.at_target[row] = mine[t];
+                } else if (row < h.N && valid > 0) {
+                    const bool is = target >= 0;
+                    const float g = is ? h.scale[row] : 0.f, z = is ? -h.lse[row] * kHeadLog2e : 0.f;
+                    uint32_t w[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float x = head_exp2(fmaf(mine[2 * i], kHeadLog2e, z)) * g, y = head_exp2(fmaf(mine[2 * i + 1], kHeadLog2e, z)) * g;
+                        if (t == 2 * i) x -= g;
+                        if (t == 2 * i + 1) y -= g;
+                        w[i] = is ? pack_bf16x2(x, y) : 0u;
+                    }
+                    // The pitch is a multiple of 256: columns past the piece's are there to be written.
+                    uint4* dst = reinterpret_cast<uint4*>(G + row * ldg + v0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) dst[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                }
+            }
+            if (!GRADIENT) {
+                epilogue_any(false);
+                const int row = static_cast<int>(threadIdx.x) - 64;
+                if (row < NT && row < h.N) {
+                    float m = -INFINITY, s = 0.f;
+                    bool nan = false;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        m = fmaxf(m, parts[w * NT + row].x);
+                        nan |= parts[w * NT + row].y != parts[w * NT + row].y;
+                    }
+                    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) s += parts[w * NT + row].y * expf(parts[w * NT + row].x - ref);
+                    h.running[static_cast<int64_t>(tile) * h.N + row] = make_float2(m, nan ? __int_as_float(0x7fc00000) : s);
+                }
+            }
+        }
+        if (failed) *abort_flag = 1;
+    }
+    if (failed && status) atomicExch(status, VELORA_ERR_TIMEOUT);
+
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (warp == 1) {
+        __syncwarp();
+        tmem_dealloc(tmem_base, S::kTmemCols);
+    }
+}
+
+template <bool GRADIENT, int NT>
+int launch_few(const CUtensorMap& tw, const CUtensorMap& tx, const HeadTile& h, void* G, int64_t ldg, int* status, int sm_count, cudaStream_t stream)
+{
+    static DeviceOnce configured;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return VELORA_ERR_CUDA;
+    auto kern = head_few_kernel<GRADIENT, NT>;
+    if (!configured.get(dev)) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(FewShape<NT>::kSmem)) != cudaSuccess) return VELORA_ERR_CUDA;
+        configured.set(dev);
+    }
+    const int tiles = (h.cols + W_BM - 1) / W_BM;
+    return launch_chained(kern, dim3(static_cast<unsigned>(tiles < sm_count ? tiles : sm_count)), W_THREADS, FewShape<NT>::kSmem, stream,
+                          tw, tx, h, static_cast<__nv_bfloat16*>(G), ldg, status);
+}
+
+}  // namespace
+
+int launch_head_few(const void* x, int64_t ldx, const void* W, int64_t ldw, void* G, int64_t ldg, const HeadTile& h, int* status, cudaStream_t stream)
+{
+    DeviceInfo di;
+    int rc = device_info(&di);
+    if (rc != VELORA_OK) return rc;
+    const int nt = h.N <= 32 ? 32 : (h.N <= 64 ? 64 : 128);
+    CUtensorMap tw, tx;
+    rc = make_tmap_bf16_2d(&tw, W, h.D, h.cols, ldw, W_BK, W_BM);
+    if (rc != VELORA_OK) return rc;
+    rc = make_tmap_bf16_2d(&tx, x, h.D, h.N, ldx, W_BK, nt);
+    if (rc != VELORA_OK) return rc;
+#define VELORA_FEW(GRAD)                                                                                      \
+    (nt == 32 ? launch_few<GRAD, 32>(tw, tx, h, G, ldg, status, di.sm_count, stream)                          \
+              : (nt == 64 ? launch_few<GRAD, 64>(tw, tx, h, G, ldg, status, di.sm_count, stream)              \
+                          : launch_few<GRAD, 128>(tw, tx, h, G, ldg, status, di.sm_count, stream)))
+    return G ? VELORA_FEW(true) : VELORA_FEW(false);
+#undef VELORA_FEW
+}
+
+}  // namespace velora

@@ -41,14 +41,6 @@ constexpr int H_THREADS = 64 + 32 * H_EPILOGUE_WARPS;
 constexpr int H_STAGING_BYTES = H_EPILOGUE_WARPS * kStoreBytes;
 constexpr int H_BARRIER_BYTES = 256;
 constexpr size_t H_SMEM = 1024 + static_cast<size_t>(H_STAGES) * H_STAGE_BYTES + H_STAGING_BYTES + H_BARRIER_BYTES;
-constexpr float kLog2e = 1.4426950408889634f;
-
-__device__ __forceinline__ float exp2_fast(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 
 enum HeadRole { HEAD_STATS = 0, HEAD_GRADIENT = 1 };
 
@@ -227,12 +219,12 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
 #pragma unroll
                     for (int i = 0; i < 32; ++i) m = fmaxf(m, __uint_as_float(l[c][i]));
                 // 2^(l log2 e - c) with c = m log2 e as rounded, in one multiply-add each; what c lost is put right in the sum.
-                const float ref = m == -INFINITY ? 0.f : m, c2 = ref * kLog2e, lost = fmaf(ref, kLog2e, -c2);
+                const float ref = m == -INFINITY ? 0.f : m, c2 = ref * kHeadLog2e, lost = fmaf(ref, kHeadLog2e, -c2);
                 float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) s[i & 3] += exp2_fast(fmaf(__uint_as_float(l[c][i]), kLog2e, -c2));
+                    for (int i = 0; i < 32; ++i) s[i & 3] += head_exp2(fmaf(__uint_as_float(l[c][i]), kHeadLog2e, -c2));
                 const float sum = ((s[0] + s[1]) + (s[2] + s[3])) * (1.f - lost * 0.69314718f);
                 if (in) h.running[static_cast<int64_t>((t0.n0 >> 7) + half) * h.N + row] = make_float2(m, sum);
                 const bool hit = t >= 0 && t < 128;
@@ -247,11 +239,11 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                 }
             } else {
                 const bool is = in && h.target[row] >= 0;
-                const float g = is ? h.scale[row] : 0.f, z = is ? -h.lse[row] * kLog2e : 0.f;
+                const float g = is ? h.scale[row] : 0.f, z = is ? -h.lse[row] * kHeadLog2e : 0.f;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(l[c][i]), kLog2e, z)) * g);
+                    for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(head_exp2(fmaf(__uint_as_float(l[c][i]), kHeadLog2e, z)) * g);
                     if (__any_sync(0xffffffffu, t >= 32 * c && t < 32 * c + 32)) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
