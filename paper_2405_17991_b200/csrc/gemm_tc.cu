@@ -60,6 +60,7 @@ int launch_gemm_tc(int kind, const void* A, int64_t lda, const void* B, int64_t 
     int rc = device_info(&di);
     if (rc != VELORA_OK) return rc;
     GemmShape shape = gemm_shape(Mdim, Ndim, Kdim, di.sm_count, false);
+    if (more.splits > 1) return launch_gemm_tc_pair(kind, A, lda, B, ldb, C, c_dtype, ldc, beta, Mdim, Ndim, Kdim, in_dtype, status, stream, more);
     if (shape.pair) {
         const int prc = launch_gemm_tc_pair(kind, A, lda, B, ldb, C, c_dtype, ldc, beta, Mdim, Ndim, Kdim, in_dtype, status, stream, more);
         if (prc != VELORA_ERR_UNSUPPORTED) return prc;

@@ -18,9 +18,13 @@ enum GemmKind {
 //   live   how many of A's first rows count, where the others hold zeros (GEMM_TN_MN_MN: rows of the contraction, which the kernel
 //          may leave out; otherwise rows of C, which it may leave unwritten)
 //   alpha  a factor of op(A) op(B)
+//   splits more than one: parts of the contraction, each to (or, with beta, onto) a C of its own, split_stride elements apart.  On CTA pairs; not
+//          for GEMM_TN_MN_MN, nor more parts than the contraction has 64s
 struct GemmMore {
     const int* live = nullptr;
     const float* alpha = nullptr;
+    int splits = 1;
+    int64_t split_stride = 0;
 };
 
 // `status` (may be NULL) is a device word that a kernel sets to VELORA_ERR_TIMEOUT if one of its bounded

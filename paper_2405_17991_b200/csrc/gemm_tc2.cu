@@ -88,6 +88,8 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         else tiles_m = min(tiles_m, (rows + 2 * P_BM - 1) / (2 * P_BM));
     }
     const int num_tiles = tiles_m * tiles_n;
+    const int kb_per_split = (kblocks + more.splits - 1) / more.splits;          // no part without k-blocks (host)
+    const int num_units = num_tiles * more.splits;           // all tiles of the first part, then of the second, ..
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < P_STAGES; ++s) {
@@ -121,12 +123,13 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         if (lane == 0) {
             uint32_t it = 0;
             int started = 0;
-            for (int tile = pair; tile < num_tiles && !failed; tile += num_pairs) {
+            for (int unit = pair; unit < num_units && !failed; unit += num_pairs) {
                 if (FUSE) *tiles_started = ++started;          // the compress warps may take this tile's row block now
-                const PairTile t0 = pair_tile(tile, tiles_m, tiles_n, 2 * P_BM, P_BN);
+                const int part = unit / num_tiles, kb0 = part * kb_per_split, kb1 = min(kblocks, kb0 + kb_per_split);
+                const PairTile t0 = pair_tile(unit - part * num_tiles, tiles_m, tiles_n, 2 * P_BM, P_BN);
                 const int m0 = t0.m0 + static_cast<int>(rank) * P_BM;
                 const int n0 = t0.n0 + static_cast<int>(rank) * (P_BN / 2);
-                for (int kb = 0; kb < kblocks; ++kb, ++it) {
+                for (int kb = kb0; kb < kb1; ++kb, ++it) {
                     const uint32_t s = it % P_STAGES, ph = (it / P_STAGES) & 1u;
                     if (!mbar_wait(empty + 8 * s, ph ^ 1u, abort_flag)) { failed = true; break; }
                     const uint32_t lead_full = map_to_cta(full + 8 * s, 0);
@@ -172,12 +175,13 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         if (lane == 0 && rank == 0) {
             constexpr uint32_t idesc = umma_idesc_bf16(2 * P_BM, P_BN, A_MN, B_MN);
             uint32_t it = 0, t = 0;
-            for (int tile = pair; tile < num_tiles && !failed; tile += num_pairs, ++t) {
+            for (int unit = pair; unit < num_units && !failed; unit += num_pairs, ++t) {
                 const uint32_t acc = t & 1u, aph = (t >> 1) & 1u;
+                const int kb0 = unit / num_tiles * kb_per_split, kb1 = min(kblocks, kb0 + kb_per_split);
                 if (!mbar_wait(tempty + 8 * acc, aph ^ 1u, abort_flag)) { failed = true; break; }
                 tc_fence_after_sync();
                 const uint32_t d_tmem = tmem_base + acc * P_BN;
-                for (int kb = 0; kb < kblocks; ++kb, ++it) {
+                for (int kb = kb0; kb < kb1; ++kb, ++it) {
                     const uint32_t s = it % P_STAGES, ph = (it / P_STAGES) & 1u;
                     if (!mbar_wait(full + 8 * s, ph, abort_flag)) { failed = true; break; }
                     tc_fence_after_sync();
@@ -188,7 +192,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                                                  : umma_smem_desc(a_addr + j * 32, 16, 1024);
                         const uint64_t db = B_MN ? umma_smem_desc(b_addr + j * 2048, P_SLAB, 1024)
                                                  : umma_smem_desc(b_addr + j * 32, 16, 1024);
-                        umma_bf16_pair(d_tmem, da, db, idesc, (kb | j) != 0);
+                        umma_bf16_pair(d_tmem, da, db, idesc, kb != kb0 || j != 0);
                     }
                     umma_commit_pair(empty + 8 * s);          // both CTAs may refill the stage
                 }
@@ -229,14 +233,15 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         const uint32_t block = smem_u32(staging) + quarter * kStoreBytes;
         const float alpha = more.alpha ? *more.alpha : 1.f;
         uint32_t t = 0;
-        for (int tile = pair; tile < num_tiles && !failed; tile += num_pairs, ++t) {
-            const PairTile t0 = pair_tile(tile, tiles_m, tiles_n, 2 * P_BM, P_BN);
+        for (int unit = pair; unit < num_units && !failed; unit += num_pairs, ++t) {
+            const int part = unit / num_tiles;
+            const PairTile t0 = pair_tile(unit - part * num_tiles, tiles_m, tiles_n, 2 * P_BM, P_BN);
             const uint32_t acc = t & 1u, aph = (t >> 1) & 1u;
             if (!mbar_wait_warp(tfull + 8 * acc, aph, abort_flag, 256)) { failed = true; break; }
             tc_fence_after_sync();
             const int row = t0.m0 + static_cast<int>(rank) * P_BM + quarter * 32 + lane;
             const uint32_t taddr = tmem_base + acc * P_BN + (static_cast<uint32_t>(quarter * 32) << 16);
-            CT* crow = C + static_cast<int64_t>(row) * ldc + t0.n0;
+            CT* crow = C + part * more.split_stride + static_cast<int64_t>(row) * ldc + t0.n0;
 #pragma unroll 1
             for (int c = 0; c < P_BN / 32; c += 2) {            // 64 columns a step: two TMEM loads in flight
                 uint32_t r[2][32];
@@ -296,9 +301,9 @@ int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, void* C, int64_t l
         configured.set(dev);
     }
     const int tiles_m = (Mdim + 2 * P_BM - 1) / (2 * P_BM), tiles_n = (Ndim + P_BN - 1) / P_BN;
-    const int64_t tiles = static_cast<int64_t>(tiles_m) * tiles_n;
+    const int64_t units = static_cast<int64_t>(tiles_m) * tiles_n * more.splits;
     int pairs = sm_count / 2;
-    if (tiles < pairs) pairs = static_cast<int>(tiles);
+    if (units < pairs) pairs = static_cast<int>(units);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs), 1, 1);
     cfg.blockDim = dim3(FUSE ? P_FUSE_THREADS : P_THREADS, 1, 1);
@@ -313,7 +318,7 @@ int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, void* C, int64_t l
     cfg.numAttrs = 1;
     int c_vec = c_rows_vec(C, ldc, sizeof(CT)) ? C_VECTORS : C_ELEMENTS;
     CUtensorMap tc = ta;
-    if (sizeof(CT) == 2 && c_vec && !beta && tc_operand_ok(C, ldc) && make_tmap_bf16_2d(&tc, C, Ndim, Mdim, ldc, 64, 32) == VELORA_OK) c_vec = C_TILES;
+    if (sizeof(CT) == 2 && c_vec && !beta && more.splits == 1 && tc_operand_ok(C, ldc) && make_tmap_bf16_2d(&tc, C, Ndim, Mdim, ldc, 64, 32) == VELORA_OK) c_vec = C_TILES;
     if (cudaLaunchKernelEx(&cfg, kern, ta, tb, tc, static_cast<CT*>(C), ldc, beta, Mdim, Ndim, Kdim, tiles_m, tiles_n, c_vec, status, more, fz) !=
         cudaSuccess) {
         cudaGetLastError();

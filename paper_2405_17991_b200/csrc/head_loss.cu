@@ -21,36 +21,6 @@ int64_t round_up(int64_t x, int64_t to) { return ceil_div64(x, to) * to; }
 
 size_t piece_element(int dtype, bool backward) { return dtype == VELORA_BF16 && backward ? 2 : 4; }
 
-// The arrays in front of the piece; bf16 needs none for the forward pass.
-HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool pack_w)
-{
-    HeadLayout l{};
-    const size_t n = static_cast<size_t>(N);
-    size_t at = kStatusBytes;
-    auto take = [&](size_t bytes) {
-        const size_t here = at;
-        at += up256(bytes);
-        return here;
-    };
-    l.ldx = round_up(D, 8);
-    l.live = take(4);
-    l.order = take(4 * n);
-    l.target = take(4 * n);
-    if (backward) {
-        l.common = take(4);
-        l.scale = take(4 * n);
-        l.lse = take(4 * n);
-        l.sum = take(n * static_cast<size_t>(l.ldx) * 4);
-    } else {
-        l.at_target = take(4 * n);
-        l.running = take(8 * n * (dtype == VELORA_BF16 ? 2 * static_cast<size_t>(ceil_div64(V, 256)) : 1));
-    }
-    l.x = take(n * static_cast<size_t>(l.ldx) * dtype_size(dtype));
-    if (pack_w) l.w = take(pack_rows_bytes(V, D));
-    l.piece = at;
-    return l;
-}
-
 // Pieces of equal width, as few as fit the room but for up to two more where those fill the last wave of tiles better.  What a piece
 // costs, in k-blocks of 256 x 256 tiles on 74 pairs: its products, and the sums of dX that each but the first reads and writes (about 9 k-blocks
 // of a tile).
@@ -76,16 +46,72 @@ int64_t room_wanted(int dtype, int64_t N, int64_t V)          // in columns
     return least < all ? least : all;
 }
 
+// Parts of the contraction that dX's products are cut into, where its tiles are few: waves of units on 74 pairs, each its k-blocks and about
+// 4 more for its sums' way.
+int gradient_splits(int dtype, int64_t N, int64_t D, int64_t V)
+{
+    if (dtype != VELORA_BF16 || N <= kHeadFew) return 1;
+    const int64_t tiles = ceil_div64(N, 256) * ceil_div64(D, 256), kblocks = ceil_div64(piece_width(N, D, V, room_wanted(dtype, N, V)), 64);
+    int best = 1;
+    int64_t best_cost = 0;
+    for (int s = 1; s <= 8 && s * 8 <= kblocks; ++s) {
+        const int64_t cost = ceil_div64(tiles * s, 74) * (ceil_div64(kblocks, s) + 4);
+        if (best_cost == 0 || cost < best_cost) {
+            best = s;
+            best_cost = cost;
+        }
+    }
+    return best;
+}
+
+// The arrays in front of the piece; bf16 needs none for the forward pass.
+HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool pack_w, int splits)
+{
+    HeadLayout l{};
+    const size_t n = static_cast<size_t>(N);
+    size_t at = kStatusBytes;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += up256(bytes);
+        return here;
+    };
+    l.ldx = round_up(D, 8);
+    l.live = take(4);
+    l.order = take(4 * n);
+    l.target = take(4 * n);
+    if (backward) {
+        l.common = take(4);
+        l.scale = take(4 * n);
+        l.lse = take(4 * n);
+        l.splits = splits;
+        l.sum = take(n * static_cast<size_t>(l.ldx) * 4 * static_cast<size_t>(l.splits));
+    } else {
+        l.at_target = take(4 * n);
+        l.running = take(8 * n * (dtype == VELORA_BF16 ? 2 * static_cast<size_t>(ceil_div64(V, 256)) : 1));
+    }
+    l.x = take(n * static_cast<size_t>(l.ldx) * dtype_size(dtype));
+    if (pack_w) l.w = take(pack_rows_bytes(V, D));
+    l.piece = at;
+    return l;
+}
+
 // As many columns a piece as there is room for.
 int head_layout(HeadLayout* l, bool backward, const HeadArgs& a)
 {
-    *l = head_front(backward, a.dtype, a.N, a.D, a.V, a.dtype == VELORA_BF16 && !tc_operand_ok(a.W, a.ldw));
+    const bool pack_w = a.dtype == VELORA_BF16 && !tc_operand_ok(a.W, a.ldw);
+    const size_t column = piece_element(a.dtype, backward) * static_cast<size_t>(a.N);
+    *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, backward ? gradient_splits(a.dtype, a.N, a.D, a.V) : 1);
+    if (l->splits > 1 && a.ws_bytes < l->piece + column * kPieceStep) *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, 1);
     if (a.ws_bytes < l->piece) return VELORA_ERR_WORKSPACE;
     if (a.dtype == VELORA_BF16 && !backward) return VELORA_OK;
-    const int64_t fit = static_cast<int64_t>((a.ws_bytes - l->piece) / (piece_element(a.dtype, backward) * static_cast<size_t>(a.N))) / kPieceStep * kPieceStep;
+    const int64_t fit = static_cast<int64_t>((a.ws_bytes - l->piece) / column) / kPieceStep * kPieceStep;
     if (fit < kPieceStep) return VELORA_ERR_WORKSPACE;
     const int64_t want = room_wanted(a.dtype, a.N, a.V);
     l->piece_cols = piece_width(a.N, a.D, a.V, fit < want ? fit : want);
+    // In every piece, the last and narrower one too, each part has k-blocks.
+    const int64_t last = a.V - (ceil_div64(a.V, l->piece_cols) - 1) * l->piece_cols;
+    auto fills = [](int64_t cols, int parts) { const int64_t kb = ceil_div64(cols, 64); return ceil_div64(kb, ceil_div64(kb, parts)) == parts; };
+    while (l->splits > 1 && !(fills(last, l->splits) && (last == a.V || fills(l->piece_cols, l->splits)))) --l->splits;
     return VELORA_OK;
 }
 
@@ -375,7 +401,7 @@ head_gradient_kernel(float* logits, int64_t ld, int cols, int v0, const int* tar
 // dX from its fp32 sums, rows back to their tokens; eight columns a lane where dX's rows start on 16-byte boundaries.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kRowThreads)
-head_rows_back_kernel(const float* sum, int64_t ld, int N, int D, const int* live, const int* order, const float* common, T* dX, int64_t lddx)
+head_rows_back_kernel(const float* sum, int64_t ld, int splits, int N, int D, const int* live, const int* order, const float* common, T* dX, int64_t lddx)
 {
     pdl_wait();
     pdl_trigger();
@@ -384,19 +410,30 @@ head_rows_back_kernel(const float* sum, int64_t ld, int N, int D, const int* liv
     T* dst = dX + order[row] * lddx;
     const bool is = row < *live;
     const float f = *common;
+    const int64_t stride = static_cast<int64_t>(N) * ld;
     if (VEC) {                                           // D is a multiple of 8
 #pragma unroll 2
         for (int c = 8 * lane; c < D; c += 256) {
-            const uint4 x = ld_stream_if(sum + row * ld + c, is), z = ld_stream_if(sum + row * ld + c + 4, is);
-            const float y[8] = {__uint_as_float(x.x) * f, __uint_as_float(x.y) * f, __uint_as_float(x.z) * f, __uint_as_float(x.w) * f,
-                                __uint_as_float(z.x) * f, __uint_as_float(z.y) * f, __uint_as_float(z.z) * f, __uint_as_float(z.w) * f};
+            float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            for (int s = 0; s < splits; ++s) {
+                const float* p = sum + s * stride + row * ld + c;
+                const uint4 x = ld_stream_if(p, is), z = ld_stream_if(p + 4, is);
+                y[0] += __uint_as_float(x.x); y[1] += __uint_as_float(x.y); y[2] += __uint_as_float(x.z); y[3] += __uint_as_float(x.w);
+                y[4] += __uint_as_float(z.x); y[5] += __uint_as_float(z.y); y[6] += __uint_as_float(z.z); y[7] += __uint_as_float(z.w);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] *= f;
             if (sizeof(T) == 2)
                 __stcs(reinterpret_cast<uint4*>(dst + c), make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])));
             else
                 store_f32x8(reinterpret_cast<float*>(dst + c), y);
         }
     } else {
-        for (int c = lane; c < D; c += 32) Elem<T>::store(dst + c, is ? sum[row * ld + c] * f : 0.f);
+        for (int c = lane; c < D; c += 32) {
+            float y = 0.f;
+            for (int s = 0; is && s < splits; ++s) y += sum[s * stride + row * ld + c];
+            Elem<T>::store(dst + c, y * f);
+        }
     }
 }
 
@@ -418,7 +455,7 @@ int product(int kind, const void* A, int a_dtype, int64_t lda, const void* B, in
 size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool any_rows)
 {
     if (N < 1) return kStatusBytes;
-    const size_t front = head_front(backward, dtype, N, D, V, any_rows && dtype == VELORA_BF16).piece;
+    const size_t front = head_front(backward, dtype, N, D, V, any_rows && dtype == VELORA_BF16, backward ? gradient_splits(dtype, N, D, V) : 1).piece;
     if (dtype == VELORA_BF16 && !backward) return front;
     return front + up256(piece_element(dtype, backward) * static_cast<size_t>(N) * static_cast<size_t>(room_wanted(dtype, N, V)));
 }
@@ -533,7 +570,8 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
             if (rc != VELORA_OK) return rc;
         }
         if (dX) {
-            rc = product(GEMM_NN_K_MN, G, a.dtype, l.piece_cols, w, a.dtype, ldw, a.ws + l.sum, VELORA_F32, l.ldx, v0 > 0 ? 1 : 0, a.N, a.D, cols, status, GemmMore{live, nullptr}, a.stream);
+            rc = product(GEMM_NN_K_MN, G, a.dtype, l.piece_cols, w, a.dtype, ldw, a.ws + l.sum, VELORA_F32, l.ldx, v0 > 0 ? 1 : 0, a.N, a.D, cols, status,
+                         GemmMore{live, nullptr, l.splits, a.N * l.ldx}, a.stream);
             if (rc != VELORA_OK) return rc;
         }
     }
@@ -544,12 +582,12 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
     const bool vec = a.D % 8 == 0 && c_rows_vec(dX, lddx, dtype_size(a.dtype));
     if (a.dtype == VELORA_BF16) {
         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(dX);
-        return vec ? launch_chained(head_rows_back_kernel<__nv_bfloat16, true>, grid, kRowThreads, 0, a.stream, sum, l.ldx, n, d, live, order, common, out, lddx)
-                   : launch_chained(head_rows_back_kernel<__nv_bfloat16, false>, grid, kRowThreads, 0, a.stream, sum, l.ldx, n, d, live, order, common, out, lddx);
+        return vec ? launch_chained(head_rows_back_kernel<__nv_bfloat16, true>, grid, kRowThreads, 0, a.stream, sum, l.ldx, l.splits, n, d, live, order, common, out, lddx)
+                   : launch_chained(head_rows_back_kernel<__nv_bfloat16, false>, grid, kRowThreads, 0, a.stream, sum, l.ldx, l.splits, n, d, live, order, common, out, lddx);
     }
     float* out = static_cast<float*>(dX);
-    return vec ? launch_chained(head_rows_back_kernel<float, true>, grid, kRowThreads, 0, a.stream, sum, l.ldx, n, d, live, order, common, out, lddx)
-               : launch_chained(head_rows_back_kernel<float, false>, grid, kRowThreads, 0, a.stream, sum, l.ldx, n, d, live, order, common, out, lddx);
+    return vec ? launch_chained(head_rows_back_kernel<float, true>, grid, kRowThreads, 0, a.stream, sum, l.ldx, l.splits, n, d, live, order, common, out, lddx)
+               : launch_chained(head_rows_back_kernel<float, false>, grid, kRowThreads, 0, a.stream, sum, l.ldx, l.splits, n, d, live, order, common, out, lddx);
 }
 
 }  // namespace velora

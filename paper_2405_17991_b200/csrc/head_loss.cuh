@@ -17,9 +17,10 @@ struct HeadLayout {
     size_t running;         // float2[N], or float2[128-column blocks][N]: maximum, and the sum of exponentials relative to it (forward)
     size_t x;               // the rows of X, pitch ldx elements; zeros for rows without a target
     size_t w;               // W with a pitch that tensor maps take, where W's own is not
-    size_t sum;             // fp32, pitch ldx: dX so far (backward)
+    size_t sum;             // fp32, pitch ldx: dX so far, `splits` partial sums (backward)
     size_t piece;           // a piece of the vocabulary: logits or their gradient, pitch `piece_cols` elements
     int64_t ldx, piece_cols;
+    int splits;
     size_t bytes;
 };
 
