@@ -384,9 +384,11 @@ int velora_linear_step_host(const void* hX, const void* hdY, void* hY, void* hdX
  *   velora_checkpoint_load         Q, E -> Xhat (bf16 or f32)
  *   velora_checkpoint_weight_grad  dW[o, d] = beta * dW[o, d] + sum_n dY[n, o] * Xhat[n, d]   (fp32 accumulation; types of dY and dW as in
  *                                  velora_weight_grad);  ws: velora_workspace_bytes(VELORA_OP_CHECKPOINT_WEIGHT_GRAD, N, D, O, 1) bytes,
- *                                  | VELORA_OP_F32 for an fp32 dY, initialised
- * N == 0 as in velora_compress and velora_weight_grad.  Any rows are taken; fastest are X and Xhat on 16-byte boundaries with ldq a
- * multiple of 16 and lde of 4.
+ *                                  | VELORA_OP_F32 for an fp32 dY, | VELORA_OP_ANY_ROWS where the rows of a bf16 dY do not start on
+ *                                  16-byte boundaries (without that room they run on the CUDA cores); initialised.  It holds Xhat in
+ *                                  dY's type while the call runs.
+ * N == 0 as in velora_compress and velora_weight_grad.  Any rows are taken; fastest are X and Xhat on 16-byte boundaries (bf16: any) with Q
+ * on 8-byte ones.
  */
 #define VELORA_CHECKPOINT_BLOCK 32
 int velora_checkpoint_store(const void* X, int x_dtype, int64_t N, int64_t D, int64_t ldx,

@@ -203,7 +203,7 @@ int check_checkpoint(const void* Q, int64_t ldq, const void* E, int64_t lde, int
     return VELORA_OK;
 }
 
-// Xhat in dY's type, and a packed copy of a bf16 dY whose rows TMA cannot address.
+// Xhat in dY's type; behind it a packed copy of a bf16 dY whose rows TMA cannot address.
 size_t checkpoint_grad_bytes(int64_t N, int64_t D, int dtype) { return kStatusBytes + align256(static_cast<size_t>(N) * round_up8(D) * dtype_size(dtype)); }
 
 // ---- loss of a linear head ----

@@ -239,3 +239,11 @@ def test_captured_replayed_and_on_another_stream(vl, N, D, O):
     got = vl.velora_checkpoint_weight_grad(dY2, q, e, ws=torch.zeros_like(ws), stream=other)
     other.synchronize()
     assert torch.equal(got, want[1])
+
+
+def test_weight_grad_refuses_a_workspace_without_room(vl):
+    N, D, O = 64, 128, 128
+    X, dY = finite_inputs(N, D, O, torch.bfloat16, 7)
+    Q, E = vl.velora_checkpoint_store(X)
+    with pytest.raises(vl.VeloraError):
+        vl.velora_checkpoint_weight_grad(dY, Q, E, ws=vl.velora_workspace_alloc(256, DEV))
