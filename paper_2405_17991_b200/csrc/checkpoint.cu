@@ -207,24 +207,37 @@ checkpoint_store_elem_kernel(const T* X, int64_t ldx, int64_t N, int D, int8_t* 
     }
 }
 
-// Eight values of a bf16 row on any boundary.  A lane puts the aligned 16 bytes that its first element lies in together with its
-// neighbour's last elements; what has no such neighbour is written one element at a time.
-__device__ __forceinline__ void store8_odd(__nv_bfloat16* p, const float (&y)[8], int count, int lane)
-{
-    const uint4 v = pack8(y);
-    const uint32_t s = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p) & 15);        // bytes of the chunk that are the neighbour's
-    const uint4 before = make_uint4(__shfl_up_sync(0xffffffffu, v.x, 1), __shfl_up_sync(0xffffffffu, v.y, 1),
-                                    __shfl_up_sync(0xffffffffu, v.z, 1), __shfl_up_sync(0xffffffffu, v.w, 1));
-    const int mine = static_cast<int>(16 - s) / 2;                                        // elements in the chunk
-    const bool whole = (lane > 0 || s == 0) && count >= mine;
-    const bool next_whole = __shfl_down_sync(0xffffffffu, static_cast<int>(whole), 1) != 0 && lane < 31;
-    if (whole) __stcs(reinterpret_cast<uint4*>(reinterpret_cast<char*>(p) - s), s == 0 ? v : shift_chunks(before, v, 16 - s));
-    if (!whole || !next_whole) {
+// A run of bf16 segments of a row that starts on any boundary.  A lane puts the aligned 16 bytes that its first element lies in together
+// with its neighbour's last elements, the first lane of a segment with those of the segment before; what has no such neighbour, at the ends of
+// the run, is written one element at a time.
+struct OddRun {
+    uint32_t s;                                                 // bytes of a chunk that are the neighbour's
+    uint4 carried;                                              // the last lane's values of the segment before
+    bool begun = false;
+    __device__ __forceinline__ OddRun(const __nv_bfloat16* p) : s(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p) & 15)) {}
+    // count: how many of this lane's eight there are; next: the same of the next segment's first lane, 0 behind the run's last.
+    __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&y)[8], int count, int next, int lane)
+    {
+        const uint4 v = pack8(y);
+        uint4 before = make_uint4(__shfl_up_sync(0xffffffffu, v.x, 1), __shfl_up_sync(0xffffffffu, v.y, 1),
+                                  __shfl_up_sync(0xffffffffu, v.z, 1), __shfl_up_sync(0xffffffffu, v.w, 1));
+        if (lane == 0) before = carried;
+        const int mine = static_cast<int>(16 - s) / 2;           // elements in the chunk
+        const bool whole = (lane > 0 || begun || s == 0) && count >= mine;
+        bool next_whole = __shfl_down_sync(0xffffffffu, static_cast<int>(whole), 1) != 0;
+        if (lane == 31) next_whole = next >= mine;
+        if (whole) __stcs(reinterpret_cast<uint4*>(reinterpret_cast<char*>(p) - s), s == 0 ? v : shift_chunks(before, v, 16 - s));
+        const int from = whole ? mine : 0, to = next_whole ? mine : count;
+        if (from < to && count > 0) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < count && (e < mine ? !whole : !next_whole)) p[e] = __float2bfloat16_rn(y[e]);
+            for (int e = 0; e < 8; ++e)
+                if (e >= from && e < to && e < count) p[e] = __float2bfloat16_rn(y[e]);
+        }
+        carried = make_uint4(__shfl_sync(0xffffffffu, v.x, 31), __shfl_sync(0xffffffffu, v.y, 31), __shfl_sync(0xffffffffu, v.z, 31),
+                             __shfl_sync(0xffffffffu, v.w, 31));
+        begun = true;
     }
-}
+};
 
 // Rows of Q on 8-byte boundaries, rows of Xhat on 16-byte ones unless ODD.
 template <typename T, int U, bool ODD>
@@ -257,6 +270,7 @@ checkpoint_load_vec_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int64
             }
         }
         T* dst = Xhat + at.row * ldx + col0;
+        OddRun odd(reinterpret_cast<const __nv_bfloat16*>(dst));
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const int left = left0 - i * kSegment;
@@ -264,7 +278,9 @@ checkpoint_load_vec_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int64
             float y[8];
             checkpoint_values(q[i], exponent[i], y);
             if constexpr (ODD) {
-                store8_odd(dst + i * kSegment, y, min(max(left, 0), 8), lane);
+                // The next segment's first lane has D - its first column left.
+                const int next = i + 1 < U ? D - at.run * (U * kSegment) - (i + 1) * kSegment : 0;
+                odd.store(dst + i * kSegment, y, min(max(left, 0), 8), min(max(next, 0), 8), lane);
             } else if (left >= 8) {
                 store8(dst + i * kSegment, y);
             } else if (left > 0) {

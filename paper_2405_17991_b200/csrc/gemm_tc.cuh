@@ -25,6 +25,7 @@ struct GemmMore {
     const float* alpha = nullptr;
     int splits = 1;
     int64_t split_stride = 0;
+    int band = 4;           // row blocks whose tiles are walked together, on CTA pairs
 };
 
 // `status` (may be NULL) is a device word that a kernel sets to VELORA_ERR_TIMEOUT if one of its bounded

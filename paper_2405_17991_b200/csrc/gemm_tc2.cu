@@ -126,7 +126,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
             for (int unit = pair; unit < num_units && !failed; unit += num_pairs) {
                 if (FUSE) *tiles_started = ++started;          // the compress warps may take this tile's row block now
                 const int part = unit / num_tiles, kb0 = part * kb_per_split, kb1 = min(kblocks, kb0 + kb_per_split);
-                const PairTile t0 = pair_tile(unit - part * num_tiles, tiles_m, tiles_n, 2 * P_BM, P_BN);
+                const PairTile t0 = pair_tile(unit - part * num_tiles, tiles_m, tiles_n, 2 * P_BM, P_BN, more.band);
                 const int m0 = t0.m0 + static_cast<int>(rank) * P_BM;
                 const int n0 = t0.n0 + static_cast<int>(rank) * (P_BN / 2);
                 for (int kb = kb0; kb < kb1; ++kb, ++it) {
@@ -218,7 +218,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
             int ti = 0;
             for (int tile = pair; tile < num_tiles; tile += num_pairs, ++ti) {
                 if (!wait_for_tile(tiles_started, ti, abort_flag)) { failed = true; break; }
-                const PairTile t0 = pair_tile(tile, tiles_m, tiles_n, 2 * P_BM, P_BN);
+                const PairTile t0 = pair_tile(tile, tiles_m, tiles_n, 2 * P_BM, P_BN, more.band);
                 const int r0 = t0.m0 + static_cast<int>(rank) * P_BM + cwi * 32;
                 CompressWalk<FUSE, vs.kParts>(fz, vs, r0, Mdim, Kdim, lane).run(t0.n0 / P_BN, tiles_n, n_groups);
             }
@@ -235,7 +235,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         uint32_t t = 0;
         for (int unit = pair; unit < num_units && !failed; unit += num_pairs, ++t) {
             const int part = unit / num_tiles;
-            const PairTile t0 = pair_tile(unit - part * num_tiles, tiles_m, tiles_n, 2 * P_BM, P_BN);
+            const PairTile t0 = pair_tile(unit - part * num_tiles, tiles_m, tiles_n, 2 * P_BM, P_BN, more.band);
             const uint32_t acc = t & 1u, aph = (t >> 1) & 1u;
             if (!mbar_wait_warp(tfull + 8 * acc, aph, abort_flag, 256)) { failed = true; break; }
             tc_fence_after_sync();

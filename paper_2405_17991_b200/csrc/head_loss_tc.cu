@@ -104,7 +104,7 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
         if (lane == 0) {
             uint32_t it = 0;
             for (int tile = pair; tile < num_tiles && !failed; tile += num_pairs) {
-                const PairTile t0 = pair_tile<H_BAND>(tile, tiles_m, tiles_n, 2 * H_BM, H_BN);
+                const PairTile t0 = pair_tile(tile, tiles_m, tiles_n, 2 * H_BM, H_BN, H_BAND);
                 const int m0 = t0.m0 + static_cast<int>(rank) * H_BM;
                 const int n0 = t0.n0 + static_cast<int>(rank) * (H_BN / 2);
                 for (int kb = 0; kb < kblocks; ++kb, ++it) {
@@ -169,7 +169,7 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
         const uint32_t block = staging + (warp - 2) * kStoreBytes;
         uint32_t seg = 0;
         for (int tile = pair; tile < num_tiles && !failed; tile += num_pairs) {
-            const PairTile t0 = pair_tile<H_BAND>(tile, tiles_m, tiles_n, 2 * H_BM, H_BN);
+            const PairTile t0 = pair_tile(tile, tiles_m, tiles_n, 2 * H_BM, H_BN, H_BAND);
             const int row0 = t0.m0 + static_cast<int>(rank) * H_BM + quarter * 32, row = row0 + lane;
             const int col0 = t0.n0 + half * 128, valid = h.cols - col0;
             uint32_t l[4][32];                               // fp32 bits

@@ -87,16 +87,15 @@ __device__ __forceinline__ bool mbar_try_wait_acquire_cluster(uint32_t bar, uint
 struct PairTile {
     int m0, n0;
 };
-// Tiles of tile_m x tile_n walked in bands of BAND m-tiles so that pairs running together share B in L2.
-template <int BAND = 4>
-__device__ __forceinline__ PairTile pair_tile(int tile, int tiles_m, int tiles_n, int tile_m, int tile_n)
+// Tiles of tile_m x tile_n walked in bands of `band` m-tiles so that pairs running together share B in L2.
+__device__ __forceinline__ PairTile pair_tile(int tile, int tiles_m, int tiles_n, int tile_m, int tile_n, int band_size = 4)
 {
-    const int per_band = BAND * tiles_n;
+    const int per_band = band_size * tiles_n;
     const int band = tile / per_band;
     const int in_band = tile - band * per_band;
-    const int band_rows = (tiles_m - band * BAND < BAND) ? tiles_m - band * BAND : BAND;
+    const int band_rows = (tiles_m - band * band_size < band_size) ? tiles_m - band * band_size : band_size;
     const int tn = in_band / band_rows;
-    const int tm = band * BAND + (in_band - tn * band_rows);
+    const int tm = band * band_size + (in_band - tn * band_rows);
     return {tm * tile_m, tn * tile_n};
 }
 
