@@ -212,6 +212,7 @@ int check_head(const void* X, int64_t ldx, const void* W, int64_t ldw, const int
     if (N < 0 || D < 1 || V < 1) return VELORA_ERR_INVALID_ARG;
     if (N > (1 << 30) || D > (1 << 30) || V > (1 << 30)) return VELORA_ERR_UNSUPPORTED;
     if (!valid_dtype(dtype)) return VELORA_ERR_UNSUPPORTED;
+    if (ceil_div64(N, 256) * ceil_div64(V, 256) > (1 << 30)) return VELORA_ERR_UNSUPPORTED;          // tiles are counted in 32 bits
     if (N == 0) return VELORA_OK;
     if (!X || !W || !target || ldx < D || ldw < D) return VELORA_ERR_INVALID_ARG;
     if (!elem_aligned(X, dtype) || !elem_aligned(W, dtype) || reinterpret_cast<uintptr_t>(target) % 8) return VELORA_ERR_ALIGNMENT;

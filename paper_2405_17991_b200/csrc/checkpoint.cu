@@ -90,8 +90,8 @@ template <> struct Raw8<float> {
         return top;
     }
 };
-// bf16 rows on any boundary: a lane loads the aligned 16 bytes that its first element lies in, its neighbour has the rest.  On the
-// matrix's first and last row (`edge`), whose aligned bytes may lie outside it, element by element.
+// bf16 rows on any boundary: a lane loads the aligned 16 bytes that its first element lies in, its neighbour has the rest.  Element by element
+// where the aligned bytes of a row may lie outside the matrix (`edge`: the first and last rows).
 struct Raw8Odd {
     uint4 w, over;
     __device__ __forceinline__ void load(const __nv_bfloat16* p, int left, bool edge, int lane)
@@ -152,7 +152,7 @@ checkpoint_store_vec_kernel(const T* X, int64_t ldx, int64_t N, int D, int8_t* Q
     for (RunWalk at(runs); at.row < N; at.next()) {
         const int col0 = at.run * (U * kSegment) + lane * 8, left0 = D - col0;
         const T* src = X + at.row * ldx + col0;
-        const bool edge = at.row == 0 || at.row == N - 1;
+        const bool edge = at.row * ldx < 8 || (N - 1 - at.row) * ldx < 8;      // fewer than 16 bytes of the matrix before or behind the row
         RAW raw[U];
 #pragma unroll
         for (int i = 0; i < U; ++i) raw[i].load(src + i * kSegment, left0 - i * kSegment, edge, lane);

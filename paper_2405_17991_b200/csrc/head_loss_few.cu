@@ -19,7 +19,7 @@ namespace {
 
 constexpr int W_BM = 128;                  // columns of the vocabulary in a tile
 constexpr int W_BK = 64;
-constexpr int W_SEGMENT = 16;              // k-blocks that an accumulator adds up
+constexpr int W_SEGMENT = 2;               // k-blocks that an accumulator adds up
 constexpr int W_THREADS = 192;
 constexpr int W_PITCH = 33;
 constexpr int W_STAGING_BYTES = 4 * 32 * W_PITCH * 4;

@@ -74,7 +74,7 @@ def equal_values(got: torch.Tensor, ref: np.ndarray):
     assert np.array_equal(np.nan_to_num(g), np.nan_to_num(ref))
 
 
-SIZES = [(1, 1), (1, 31), (3, 32), (2, 33), (5, 255), (4, 257), (7, 1000), (40, 264), (64, 4096), (33, 5461), (20000, 64), (3000, 520)]
+SIZES = [(1, 1), (3, 1), (20, 1), (9, 3), (1, 31), (3, 32), (2, 33), (5, 255), (4, 257), (7, 1000), (40, 264), (64, 4096), (33, 5461), (20000, 64), (3000, 520)]
 
 
 @pytest.mark.parametrize("rows", ["padded", "dense", "offset"])

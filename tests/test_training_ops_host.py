@@ -70,6 +70,7 @@ def test_head_refusals(b):
             assert f(**{name: v}) == b.ERR_INVALID_ARG, name
         for name in ("N", "V"):
             assert f(**{name: (1 << 30) + 1}) == b.ERR_UNSUPPORTED
+        assert f(N=1 << 29, V=1 << 29) == b.ERR_UNSUPPORTED
         assert f(dt=b.FP8_E4M3) == b.ERR_UNSUPPORTED
         assert f(X=odd) == b.ERR_ALIGNMENT
         assert f(t=P(0x10004)) == b.ERR_ALIGNMENT
