@@ -88,7 +88,9 @@ HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D, int64_t V,
         l.sum = take(n * static_cast<size_t>(l.ldx) * 4 * static_cast<size_t>(l.splits));
     } else {
         l.at_target = take(4 * n);
-        l.running = take(8 * n * (dtype == VELORA_BF16 ? 2 * static_cast<size_t>(ceil_div64(V, 256)) : 1));
+        // fp32: one of a row; bf16: one of each 128 columns (of 256 rounded up), of a tile for few tokens.
+        const size_t parts = dtype != VELORA_BF16 ? 1 : static_cast<size_t>(N <= kHeadFew ? ceil_div64(V, kHeadFewHeight) : 2 * ceil_div64(V, 256));
+        l.running = take(8 * n * parts);
     }
     l.x = take(n * static_cast<size_t>(l.ldx) * dtype_size(dtype));
     if (pack_w) l.w = take(pack_rows_bytes(V, D));
@@ -516,10 +518,11 @@ int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
     const int n = static_cast<int>(a.N);
     if (a.dtype == VELORA_BF16) {
         const HeadTile h = head_tile(a, l, 0, a.V);
-        rc = (a.N <= kHeadFew ? launch_head_few : launch_head_tiles)(a.ws + l.x, l.ldx, W, ldw, nullptr, 0, h, status, a.stream);
+        const bool few = a.N <= kHeadFew;
+        rc = (few ? launch_head_few : launch_head_tiles)(a.ws + l.x, l.ldx, W, ldw, nullptr, 0, h, status, a.stream);
         if (rc != VELORA_OK) return rc;
         return launch_chained(head_merge_kernel, dim3(static_cast<unsigned>(ceil_div64(a.N, 32))), kRowThreads, 0, a.stream, h.running,
-                              static_cast<int>(ceil_div64(a.V, 128)), n, h.live, reinterpret_cast<int*>(a.ws + l.order), h.target, h.at_target, loss, lse);
+                              static_cast<int>(ceil_div64(a.V, few ? head_few_height(a.V) : 128)), n, h.live, reinterpret_cast<int*>(a.ws + l.order), h.target, h.at_target, loss, lse);
     }
     float* piece = reinterpret_cast<float*>(a.ws + l.piece);
     for (int64_t v0 = 0; v0 < a.V; v0 += l.piece_cols) {

@@ -14,7 +14,7 @@ struct HeadLayout {
     size_t common;          // fp32: the largest |dloss| of a row with a target, a factor taken out of all of them (backward)
     size_t scale, lse;      // fp32[N]: what is left of the row's dloss, log sum exp (backward)
     size_t at_target;       // fp32[N]: logit of the target (forward)
-    size_t running;         // float2[N], or float2[128-column blocks][N]: maximum, and the sum of exponentials relative to it (forward)
+    size_t running;         // float2[N], or float2[parts of the vocabulary][N]: maximum, and the sum of exponentials relative to it (forward)
     size_t x;               // the rows of X, pitch ldx elements; zeros for rows without a target
     size_t w;               // W with a pitch that tensor maps take, where W's own is not
     size_t sum;             // fp32, pitch ldx: dX so far, `splits` partial sums (backward)
@@ -52,6 +52,8 @@ int launch_head_tiles(const void* x, int64_t ldx, const void* W, int64_t ldw, vo
 
 // The same for up to kHeadFew tokens.  (head_loss_few.cu)
 constexpr int kHeadFew = 128;
+constexpr int kHeadFewHeight = 64;                  // least height of its tiles
+int head_few_height(int64_t cols);                  // columns of the vocabulary in a tile: a row of `running` each
 int launch_head_few(const void* x, int64_t ldx, const void* W, int64_t ldw, void* G, int64_t ldg, const HeadTile& h, int* status, cudaStream_t stream);
 
 #ifdef __CUDACC__

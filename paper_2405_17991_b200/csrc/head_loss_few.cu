@@ -1,11 +1,11 @@
 // The logits of a linear head for few tokens (up to 128), used up where they come out of the tensor cores; roles and results as in
-// head_loss_tc.cu.  What bounds it is reading W once, so W's rows are the rows of the products: tiles of 128 columns of the vocabulary,
-// the tokens (rounded up to 32, 64 or 128) are the other side, and no tensor-core time goes into rows that are not there.  Single CTAs with up to
-// 200 KB of W in flight each; a CTA that has one tile more than another finds the memory less busy, so uneven shares cost little.
+// head_loss_tc.cu.  What bounds it is reading W once, so W's rows are the rows of the products: tiles of up to 128 columns of the vocabulary,
+// as high as shares the vocabulary out most evenly (32000: 112, 224 columns for a CTA that has two), the tokens (rounded up to 32, 64 or
+// 128) are the other side, and no tensor-core time goes into rows that are not there.  Single CTAs with up to 200 KB of W in flight each.
 //
 // Per CTA: warp 0 lane 0 TMA producer, warp 1 lane 0 MMA issuer, warps 2..5 epilogue (32 columns of the vocabulary each).  A lane of the
 // epilogue has one column for all tokens; 32 x 32 blocks are turned over through shared memory, and then it has one token for 32
-// columns.  Contractions are cut into segments of 1024 as in head_loss_tc.cu.  1 x 4096 of 32000: 51 us, 262 MB at 5.1 TB/s (71 us with the
+// columns.  Contractions are cut into segments as in head_loss_tc.cu, of 128 here: there is time for it.  1 x 4096 of 32000: 51 us, 262 MB at 5.1 TB/s (71 us with the
 // tokens as rows of 256).
 #include "gemm_tc.cuh"
 #include "head_loss.cuh"
@@ -44,7 +44,7 @@ __device__ __forceinline__ bool epilogue_any(bool p)
 
 template <bool GRADIENT, int NT>
 __global__ void __launch_bounds__(W_THREADS, 1)
-head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const HeadTile h, __nv_bfloat16* G, int64_t ldg,
+head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const HeadTile h, int height, __nv_bfloat16* G, int64_t ldg,
                 int* status)
 {
     typedef FewShape<NT> S;
@@ -62,7 +62,7 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
     static_assert(16 * S::kStages + 48 <= W_BARRIER_BYTES, "barriers");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int num_tiles = (h.cols + W_BM - 1) / W_BM, kblocks = (h.D + W_BK - 1) / W_BK;
+    const int num_tiles = (h.cols + height - 1) / height, kblocks = (h.D + W_BK - 1) / W_BK;
     const int segment = GRADIENT ? kblocks : W_SEGMENT;
 
     if (threadIdx.x == 0) {
@@ -99,9 +99,9 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
                 for (int kb = 0; kb < kblocks; ++kb, ++it) {
                     const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1u;
                     if (!mbar_wait(empty + 8 * s, ph ^ 1u, abort_flag)) { failed = true; break; }
-                    mbar_arrive_expect_tx(full + 8 * s, S::kStageBytes);
+                    mbar_arrive_expect_tx(full + 8 * s, static_cast<uint32_t>((height + NT) * W_BK * 2));
                     const uint32_t dst = base + s * S::kStageBytes;
-                    tma_load_2d(dst, &tmW, full + 8 * s, kb * W_BK, tile * W_BM);
+                    tma_load_2d(dst, &tmW, full + 8 * s, kb * W_BK, tile * height);                  // rows behind it: whatever was there, outputs that nobody reads
                     tma_load_2d(dst + W_BM * W_BK * 2, &tmX, full + 8 * s, kb * W_BK, 0);
                 }
             }
@@ -172,7 +172,7 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
                 if (lane == 0) mbar_arrive(tempty + 8 * acc);
             }
             if (GRADIENT ? failed : (failed = epilogue_any(failed))) break;      // behind it nobody reads the last tile's parts any more
-            const int v0 = tile * W_BM + quarter * 32, valid = min(32, h.cols - v0);      // this warp's columns; may be none
+            const int v0 = tile * height + quarter * 32, valid = min(min(32, height - quarter * 32), h.cols - v0);      // this warp's columns; may be none
 #pragma unroll
             for (int c = 0; c < NT / 32; ++c) {
                 const int row = 32 * c + lane;               // this lane's token behind the turn
@@ -202,10 +202,12 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
                         if (t == 2 * i + 1) y -= g;
                         w[i] = is ? pack_bf16x2(x, y) : 0u;
                     }
-                    // The pitch is a multiple of 256: columns past the piece's are there to be written.
+                    // The pitch is a multiple of 256 and the height of 16: columns past the piece's are there to be written, those of the next tile
+                    // are not touched.
                     uint4* dst = reinterpret_cast<uint4*>(G + row * ldg + v0);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) dst[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                    for (int i = 0; i < 4; ++i)
+                        if (8 * i < valid) dst[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
                 }
             }
             if (!GRADIENT) {
@@ -240,7 +242,7 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
 }
 
 template <bool GRADIENT, int NT>
-int launch_few(const CUtensorMap& tw, const CUtensorMap& tx, const HeadTile& h, void* G, int64_t ldg, int* status, int sm_count, cudaStream_t stream)
+int launch_few(const CUtensorMap& tw, const CUtensorMap& tx, const HeadTile& h, int height, void* G, int64_t ldg, int* status, int sm_count, cudaStream_t stream)
 {
     static DeviceOnce configured;
     int dev = 0;
@@ -250,12 +252,26 @@ int launch_few(const CUtensorMap& tw, const CUtensorMap& tx, const HeadTile& h, 
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(FewShape<NT>::kSmem)) != cudaSuccess) return VELORA_ERR_CUDA;
         configured.set(dev);
     }
-    const int tiles = (h.cols + W_BM - 1) / W_BM;
+    const int tiles = (h.cols + height - 1) / height;
     return launch_chained(kern, dim3(static_cast<unsigned>(tiles < sm_count ? tiles : sm_count)), W_THREADS, FewShape<NT>::kSmem, stream,
-                          tw, tx, h, static_cast<__nv_bfloat16*>(G), ldg, status);
+                          tw, tx, h, height, static_cast<__nv_bfloat16*>(G), ldg, status);
 }
 
 }  // namespace
+
+int head_few_height(int64_t cols)
+{
+    int best = W_BM;
+    int64_t most = 0;                                         // columns of the CTA that has the most of them, on 148 SMs
+    for (int t = W_BM; t >= kHeadFewHeight; t -= 16) {
+        const int64_t share = ceil_div64(ceil_div64(cols, t), 148) * t;
+        if (most == 0 || share < most) {
+            best = t;
+            most = share;
+        }
+    }
+    return best;
+}
 
 int launch_head_few(const void* x, int64_t ldx, const void* W, int64_t ldw, void* G, int64_t ldg, const HeadTile& h, int* status, cudaStream_t stream)
 {
@@ -264,14 +280,15 @@ int launch_head_few(const void* x, int64_t ldx, const void* W, int64_t ldw, void
     if (rc != VELORA_OK) return rc;
     const int nt = h.N <= 32 ? 32 : (h.N <= 64 ? 64 : 128);
     CUtensorMap tw, tx;
-    rc = make_tmap_bf16_2d(&tw, W, h.D, h.cols, ldw, W_BK, W_BM);
+    const int height = head_few_height(h.cols);
+    rc = make_tmap_bf16_2d(&tw, W, h.D, h.cols, ldw, W_BK, height);
     if (rc != VELORA_OK) return rc;
     rc = make_tmap_bf16_2d(&tx, x, h.D, h.N, ldx, W_BK, nt);
     if (rc != VELORA_OK) return rc;
 #define VELORA_FEW(GRAD)                                                                                      \
-    (nt == 32 ? launch_few<GRAD, 32>(tw, tx, h, G, ldg, status, di.sm_count, stream)                          \
-              : (nt == 64 ? launch_few<GRAD, 64>(tw, tx, h, G, ldg, status, di.sm_count, stream)              \
-                          : launch_few<GRAD, 128>(tw, tx, h, G, ldg, status, di.sm_count, stream)))
+    (nt == 32 ? launch_few<GRAD, 32>(tw, tx, h, height, G, ldg, status, di.sm_count, stream)                          \
+              : (nt == 64 ? launch_few<GRAD, 64>(tw, tx, h, height, G, ldg, status, di.sm_count, stream)              \
+                          : launch_few<GRAD, 128>(tw, tx, h, height, G, ldg, status, di.sm_count, stream)))
     return G ? VELORA_FEW(true) : VELORA_FEW(false);
 #undef VELORA_FEW
 }
