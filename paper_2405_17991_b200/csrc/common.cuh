@@ -153,6 +153,16 @@ int launch_gemm_simt(const void* A, int a_dtype, int64_t a_sm, int64_t a_sk,
 // Estimate of its time for fp32 operands, in microseconds.
 double gemm_simt_f32_us(int64_t Mdim, int64_t Ndim, int64_t Kdim, int sm_count);
 
+// The same for fp32, with the contraction cut into parts that go to a C each (C + part * part_stride; a part that gets nothing of a short
+// contraction is zeros): for products of few tiles whose result another kernel reads anyway.  No cluster, so no cluster launch.
+struct SimtParts {
+    int rows, cols, parts;                                      // of a tile; parts
+    double us;                                                  // estimate
+};
+SimtParts simt_parts(int64_t Mdim, int64_t Ndim, int64_t Kdim);
+int launch_gemm_simt_parts(const SimtParts& shape, const float* A, int64_t a_sm, int64_t a_sk, const float* B, int64_t b_sn, int64_t b_sk,
+                           float* C, int64_t ldc, int64_t part_stride, int beta, int64_t Mdim, int64_t Ndim, int64_t Kdim, cudaStream_t stream);
+
 // dW[o, m*Dsub + j] = beta*dW + (sum over `splits` partial P[s][o][m], fp32) * v[j].
 int launch_expand_p(const float* P, int splits, int64_t split_stride, int64_t ldp, const float* v,
                     int64_t O, int64_t D, int Dsub, void* dW, int dw_dtype, int64_t lddw, int beta,

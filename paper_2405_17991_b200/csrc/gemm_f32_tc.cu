@@ -559,7 +559,28 @@ int launch_shape(const F32Operand& A, const F32Operand& B, float* C, int64_t ldc
     return after_launch();
 }
 
+// By estimated time in microseconds, from what both forms take between 256 x 64, K = 64 and 12608 x 768, K = 768.  A k-block costs
+// nearly the same at both widths (24 products of no less than 97 cycles each), so tiles of 96 columns pay only where those of 192
+// leave pairs idle.  Measured, us, 192 / 96 / CUDA cores: 12608 x 768, K = 768: 97 / 142 / 373; 2048 x 768, K = 768: 39 / 34 / 94;
+// 3000 x 3000, K = 100: 31 / 40 / 55; 1280 x 440, K = 300: 21 / 19 / 19; 640 x 256, K = 256: 21 / 17 / 13.
+struct F32Estimate {
+    double us192, us96;
+};
+F32Estimate f32_estimate(int64_t Mdim, int64_t Ndim, int64_t Kdim, int sm_count)
+{
+    const int64_t kblocks = ceil_div64(Kdim, F_BK), tiles_m = ceil_div64(Mdim, 2 * F_BM), pairs = sm_count / 2 > 0 ? sm_count / 2 : 1;
+    return {6.0 + ceil_div64(tiles_m * ceil_div64(Ndim, 192), pairs) * (2.2 * kblocks + 4.5),
+            6.5 + ceil_div64(tiles_m * ceil_div64(Ndim, 96), pairs) * (1.95 * kblocks + 1.5)};
+}
+
 }  // namespace
+
+double gemm_f32_us(int64_t Mdim, int64_t Ndim, int64_t Kdim, int sm_count)
+{
+    const F32Estimate e = f32_estimate(Mdim, Ndim, Kdim, sm_count);
+    const double tc = e.us96 < e.us192 ? e.us96 : e.us192, simt = gemm_simt_f32_us(Mdim, Ndim, Kdim, sm_count);
+    return simt < tc ? simt : tc;
+}
 
 int launch_gemm_f32_tc(int kind, const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, int beta,
                        int64_t Mdim, int64_t Ndim, int64_t Kdim, int* status, cudaStream_t stream)
@@ -575,15 +596,9 @@ int launch_gemm_f32_tc(int kind, const void* A, int64_t lda, const void* B, int6
     const F32Operand b{static_cast<const float*>(B), ldb, aligned16(B) && ldb % 4 == 0 ? 1 : 0};
     const int m = static_cast<int>(Mdim), n = static_cast<int>(Ndim), k = static_cast<int>(Kdim);
     float* c = static_cast<float*>(C);
-    // By estimated time in microseconds, from what both forms take between 256 x 64, K = 64 and 12608 x 768, K = 768.  A k-block costs
-    // nearly the same at both widths (24 products of no less than 97 cycles each), so tiles of 96 columns pay only where those of 192
-    // leave pairs idle.  Measured, us, 192 / 96 / CUDA cores: 12608 x 768, K = 768: 97 / 142 / 373; 2048 x 768, K = 768: 39 / 34 / 94;
-    // 3000 x 3000, K = 100: 31 / 40 / 55; 1280 x 440, K = 300: 21 / 19 / 19; 640 x 256, K = 256: 21 / 17 / 13.
-    const int64_t kblocks = ceil_div64(Kdim, F_BK), tiles_m = ceil_div64(Mdim, 2 * F_BM), pairs = di.sm_count / 2 > 0 ? di.sm_count / 2 : 1;
-    const double us192 = 6.0 + ceil_div64(tiles_m * ceil_div64(Ndim, 192), pairs) * (2.2 * kblocks + 4.5);
-    const double us96 = 6.5 + ceil_div64(tiles_m * ceil_div64(Ndim, 96), pairs) * (1.95 * kblocks + 1.5);
-    const int bn = us96 < us192 ? 96 : 192;
-    if (0.95 * gemm_simt_f32_us(Mdim, Ndim, Kdim, di.sm_count) < (bn == 96 ? us96 : us192)) return VELORA_ERR_UNSUPPORTED;
+    const F32Estimate e = f32_estimate(Mdim, Ndim, Kdim, di.sm_count);
+    const int bn = e.us96 < e.us192 ? 96 : 192;
+    if (0.95 * gemm_simt_f32_us(Mdim, Ndim, Kdim, di.sm_count) < (bn == 96 ? e.us96 : e.us192)) return VELORA_ERR_UNSUPPORTED;
 #define VELORA_F32_CASE(AMN, BMN)                                                                             \
     return bn == 192 ? launch_shape<AMN, BMN, 192>(a, b, c, ldc, beta, m, n, k, status, di, stream)           \
                      : launch_shape<AMN, BMN, 96>(a, b, c, ldc, beta, m, n, k, status, di, stream)

@@ -138,13 +138,14 @@ __device__ __forceinline__ void put4(CT* __restrict__ C, int64_t ldc, int beta, 
 __host__ __device__ constexpr int slice_depth(int gm, int gn) { return gm * gn == 1 ? 32 : 16; }
 
 // GM groups of four rows and GN of four columns per thread, 64 apart: a tile of 64 * GM x 64 * GN.  gridDim.z = CTAs that
-// share a tile's contraction (a cluster; 64 x 64 tiles only).
-template <int GM, int GN, typename AT, typename BT, typename CT>
+// share a tile's contraction (a cluster; 64 x 64 tiles only), or, with PARTS, parts of the contraction that go to a C each, part_stride
+// elements apart.
+template <int GM, int GN, typename AT, typename BT, typename CT, bool PARTS = false>
 __global__ void __launch_bounds__(SG_THREADS, 2)
 gemm_simt_kernel(const AT* A, int64_t a_sm, int64_t a_sk, int a_mode,
                  const BT* B, int64_t b_sn, int64_t b_sk, int b_mode,
                  CT* __restrict__ C, int64_t ldc, int beta, int c_vec,
-                 int64_t Mdim, int64_t Ndim, int64_t Kdim, int64_t k_per_split)
+                 int64_t Mdim, int64_t Ndim, int64_t Kdim, int64_t k_per_split, int64_t part_stride)
 {
     constexpr int TM = 64 * GM, TN = 64 * GN, TK = slice_depth(GM, GN);
     __shared__ __align__(16) float As[2][TK][TM + 4];
@@ -163,7 +164,8 @@ gemm_simt_kernel(const AT* A, int64_t a_sm, int64_t a_sk, int a_mode,
         for (int j = 0; j < 2 * GN; ++j) acc[i][j] = 0ull;       // two zeros
 
     pdl_wait();
-    if (gridDim.z == 1) pdl_trigger();
+    if (PARTS || gridDim.z == 1) pdl_trigger();
+    if (PARTS) C += blockIdx.z * part_stride;
     float ra[Tile<AT, TM, TK>::E], rb[Tile<BT, TN, TK>::E];
     Tile<AT, TM, TK>::load(A, a_sm, a_sk, m0, Mdim, k_begin, k_end, a_mode, ra);
     Tile<BT, TN, TK>::load(B, b_sn, b_sk, n0, Ndim, k_begin, k_end, b_mode, rb);
@@ -205,7 +207,7 @@ gemm_simt_kernel(const AT* A, int64_t a_sm, int64_t a_sk, int a_mode,
         __syncthreads();
     }
 
-    if constexpr (GM * GN == 1) if (gridDim.z > 1) {
+    if constexpr (GM * GN == 1 && !PARTS) if (gridDim.z > 1) {
         namespace cg = cooperative_groups;
         cg::cluster_group cluster = cg::this_cluster();
         float* mine = &As[0][0][0];                             // 64 rows of TM + 4 floats: the slices have been used up
@@ -272,7 +274,7 @@ int launch_tiles(const void* A, int64_t a_sm, int64_t a_sk, int a_mode, const vo
     const int64_t k_per_split = ceil_div64(ceil_div64(Kdim, TK), splits) * TK;
     if (cudaLaunchKernelEx(&cfg, gemm_simt_kernel<GM, GN, AT, BT, CT>, static_cast<const AT*>(A), a_sm, a_sk, a_mode,
                            static_cast<const BT*>(B), b_sn, b_sk, b_mode, static_cast<CT*>(C), ldc, beta, c_vec, Mdim, Ndim, Kdim,
-                           k_per_split) != cudaSuccess) {
+                           k_per_split, static_cast<int64_t>(0)) != cudaSuccess) {
         cudaGetLastError();
         if (splits > 1)                                         // a refused cluster: the same tiles, one CTA each
             return launch_tiles<GM, GN, AT, BT, CT>(A, a_sm, a_sk, a_mode, B, b_sn, b_sk, b_mode, C, ldc, beta, c_vec, Mdim, Ndim, Kdim, 1, stream);
@@ -329,6 +331,35 @@ double gemm_simt_f32_us(int64_t Mdim, int64_t Ndim, int64_t Kdim, int sm_count)
     const int64_t ctas = ceil_div64(Mdim, t.rows) * ceil_div64(Ndim, t.cols) * t.splits;
     const double step = t.rows == 128 ? 0.22 : (t.cols == 128 ? 0.121 : 0.061);
     return (t.splits > 1 ? 9.0 : 5.0) + ceil_div64(ctas, 2 * static_cast<int64_t>(sm_count)) * step * ceil_div64(Kdim, t.splits);
+}
+
+// The fastest of the three tiles and up to 16 parts by estimated time: waves as above, half a microsecond a part for whoever adds them up.
+SimtParts simt_parts(int64_t Mdim, int64_t Ndim, int64_t Kdim)
+{
+    static const struct { int rows, cols; double step; } kTiles[] = {{64, 64, 0.061}, {64, 128, 0.121}, {128, 128, 0.22}};
+    SimtParts best{64, 64, 1, 0.0};
+    for (const auto& t : kTiles) {
+        const int64_t tiles = ceil_div64(Mdim, t.rows) * ceil_div64(Ndim, t.cols);
+        for (int parts = 1; parts <= 16 && (parts == 1 || Kdim >= 64 * parts); ++parts) {
+            const double us = 5.0 + ceil_div64(tiles * parts, 296) * t.step * ceil_div64(Kdim, parts) + 0.5 * (parts - 1);
+            if (best.us == 0.0 || us < best.us) best = SimtParts{t.rows, t.cols, parts, us};
+        }
+    }
+    return best;
+}
+
+int launch_gemm_simt_parts(const SimtParts& shape, const float* A, int64_t a_sm, int64_t a_sk, const float* B, int64_t b_sn, int64_t b_sk,
+                           float* C, int64_t ldc, int64_t part_stride, int beta, int64_t Mdim, int64_t Ndim, int64_t Kdim, cudaStream_t stream)
+{
+    if (Mdim <= 0 || Ndim <= 0) return VELORA_OK;
+    if (ceil_div64(Mdim, 64) > 65535) return VELORA_ERR_UNSUPPORTED;
+    const int a_mode = load_mode(A, VELORA_F32, a_sm, a_sk), b_mode = load_mode(B, VELORA_F32, b_sn, b_sk);
+    const int c_vec = aligned16(C) && ldc % 4 == 0 && part_stride % 4 == 0;
+    const dim3 grid(static_cast<unsigned>(ceil_div64(Ndim, shape.cols)), static_cast<unsigned>(ceil_div64(Mdim, shape.rows)), static_cast<unsigned>(shape.parts));
+    const int64_t k_per_part = ceil_div64(ceil_div64(Kdim, 32), shape.parts) * 32;             // whole slices of every tile
+#define VELORA_PARTS(GM, GN)                                                                                                                  launch_chained(gemm_simt_kernel<GM, GN, float, float, float, true>, grid, SG_THREADS, 0, stream, A, a_sm, a_sk, a_mode, B, b_sn, b_sk,                    b_mode, C, ldc, beta, c_vec, Mdim, Ndim, Kdim, k_per_part, part_stride)
+    return shape.rows == 128 ? VELORA_PARTS(2, 2) : (shape.cols == 128 ? VELORA_PARTS(1, 2) : VELORA_PARTS(1, 1));
+#undef VELORA_PARTS
 }
 
 int launch_gemm_simt(const void* A, int a_dtype, int64_t a_sm, int64_t a_sk,

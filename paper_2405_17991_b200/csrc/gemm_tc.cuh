@@ -41,6 +41,9 @@ int launch_gemm_tc(int kind, const void* A, int64_t lda, const void* B, int64_t 
 int launch_gemm_f32_tc(int kind, const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, int beta,
                        int64_t Mdim, int64_t Ndim, int64_t Kdim, int* status, cudaStream_t stream);
 
+// Estimate of an fp32 product's time in microseconds, tensor cores or CUDA cores.
+double gemm_f32_us(int64_t Mdim, int64_t Ndim, int64_t Kdim, int sm_count);
+
 // The same product with CTA pairs (tcgen05 cta_group::2, 256 x 256 tile per pair).  (gemm_tc2.cu)
 int launch_gemm_tc_pair(int kind, const void* A, int64_t lda, const void* B, int64_t ldb,
                         void* C, int c_dtype, int64_t ldc, int beta,

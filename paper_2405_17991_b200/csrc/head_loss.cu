@@ -20,7 +20,7 @@ constexpr int kPieceStep = 256;                     // pieces are multiples of t
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 int64_t round_up(int64_t x, int64_t to) { return ceil_div64(x, to) * to; }
 
-size_t piece_element(int dtype, bool backward) { return dtype == VELORA_BF16 && backward ? 2 : 4; }
+size_t piece_element(int dtype, bool backward) { return dtype == VELORA_BF16 && backward ? 2 : 4; }      // of one part
 
 // Pieces of equal width, as few as fit the room but for up to two more where those fill the last wave of tiles better.  What a piece
 // costs, in k-blocks of 256 x 256 tiles on 74 pairs: its products, and the sums of dX that each but the first reads and writes (about 9 k-blocks
@@ -49,9 +49,19 @@ int64_t room_wanted(int dtype, int64_t N, int64_t V)          // in columns
 
 // Parts of the contraction that dX's products are cut into, where its tiles are few: waves of units on 74 pairs, each its k-blocks and about
 // 4 more for its sums' way.
+// fp32 products of few tiles are cut into parts on the CUDA cores where that is estimated to be faster than either form of the whole
+// product: 64 x 768 of 1000, whose four products took 51 us of its 59 in clusters.
+int fp32_parts(int64_t M, int64_t N, int64_t K)
+{
+    if (M > 4096) return 1;                                     // the parts' sums would be large
+    const SimtParts p = simt_parts(M, N, K);
+    return p.parts > 1 && p.us < 0.9 * gemm_f32_us(M, N, K, 148) ? p.parts : 1;
+}
+
 int gradient_splits(int dtype, int64_t N, int64_t D, int64_t V)
 {
-    if (dtype != VELORA_BF16 || N <= kHeadFew) return 1;
+    if (dtype != VELORA_BF16) return fp32_parts(N, D, piece_width(N, D, V, room_wanted(dtype, N, V)));
+    if (N <= kHeadFew) return 1;
     const int64_t tiles = ceil_div64(N, 256) * ceil_div64(D, 256), kblocks = ceil_div64(piece_width(N, D, V, room_wanted(dtype, N, V)), 64);
     int best = 1;
     int64_t best_cost = 0;
@@ -98,19 +108,27 @@ HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D, int64_t V,
     return l;
 }
 
+int logit_parts(int dtype, int64_t N, int64_t D, int64_t V) { return dtype == VELORA_BF16 ? 1 : fp32_parts(N, piece_width(N, D, V, room_wanted(dtype, N, V)), D); }
+
 // As many columns a piece as there is room for.
 int head_layout(HeadLayout* l, bool backward, const HeadArgs& a)
 {
     const bool pack_w = a.dtype == VELORA_BF16 && !tc_operand_ok(a.W, a.ldw);
-    const size_t column = piece_element(a.dtype, backward) * static_cast<size_t>(a.N);
+    size_t column = piece_element(a.dtype, backward) * static_cast<size_t>(a.N);
     *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, backward ? gradient_splits(a.dtype, a.N, a.D, a.V) : 1);
-    if (l->splits > 1 && a.ws_bytes < l->piece + column * kPieceStep) *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, 1);
+    l->parts = logit_parts(a.dtype, a.N, a.D, a.V);
+    if (a.ws_bytes < l->piece + column * l->parts * kPieceStep) {             // less room than asked for: no partial sums
+        *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, 1);
+        l->parts = 1;
+    }
+    column *= static_cast<size_t>(l->parts);
     if (a.ws_bytes < l->piece) return VELORA_ERR_WORKSPACE;
     if (a.dtype == VELORA_BF16 && !backward) return VELORA_OK;
     const int64_t fit = static_cast<int64_t>((a.ws_bytes - l->piece) / column) / kPieceStep * kPieceStep;
     if (fit < kPieceStep) return VELORA_ERR_WORKSPACE;
     const int64_t want = room_wanted(a.dtype, a.N, a.V);
     l->piece_cols = piece_width(a.N, a.D, a.V, fit < want ? fit : want);
+    if (a.dtype != VELORA_BF16) return VELORA_OK;
     // In every piece, the last and narrower one too, each part has k-blocks.
     const int64_t last = a.V - (ceil_div64(a.V, l->piece_cols) - 1) * l->piece_cols;
     auto fills = [](int64_t cols, int parts) { const int64_t kb = ceil_div64(cols, 64); return ceil_div64(kb, ceil_div64(kb, parts)) == parts; };
@@ -295,10 +313,23 @@ __device__ __forceinline__ void write_loss(float* loss, float* lse, int n, int t
     lse[n] = target >= 0 ? l : 0.f;
 }
 
+// In a fixed order; up to 16, all under way at once.
+__device__ __forceinline__ float sum_of_parts(const float* p, int parts, int64_t stride)
+{
+    float x[16];
+#pragma unroll
+    for (int s = 0; s < 16; ++s) x[s] = s < parts ? p[s * stride] : 0.f;
+    float y = x[0];
+#pragma unroll
+    for (int s = 1; s < 16; ++s)
+        if (s < parts) y += x[s];
+    return y;
+}
+
 // A block per row takes the piece's maximum, then its exponentials, into what the pieces before have left; behind the last one the loss.  (A warp
 // per row: 29 us for 64 rows of 8000, 4 us here.)
 __global__ void __launch_bounds__(kRowThreads)
-head_stats_kernel(const float* logits, int64_t ld, int cols, int v0, const int* live, const int* order, const int* target, float* at_target,
+head_stats_kernel(float* logits, int64_t ld, int parts, int64_t part_stride, int cols, int v0, const int* live, const int* order, const int* target, float* at_target,
                   float2* running, int first, int last, float* loss, float* lse)
 {
     __shared__ float part[2][kRowThreads / 32];
@@ -309,10 +340,18 @@ head_stats_kernel(const float* logits, int64_t ld, int cols, int v0, const int* 
     float2 ms = make_float2(0.f, 1.f);
     float hit = 0.f;
     if (row < *live) {                                                // the same for the block
-        const float* l = logits + row * ld;
+        float* l = logits + row * ld;
         float m = -INFINITY;
+        if (parts > 1) {
+            for (int c = threadIdx.x; c < cols; c += kRowThreads) {
+                const float x = sum_of_parts(l + c, parts, part_stride);
+                l[c] = x;                                             // read again by this thread, the target's behind a barrier
+                m = fmaxf(m, x);
+            }
+        } else {
 #pragma unroll 4
-        for (int c = threadIdx.x; c < cols; c += kRowThreads) m = fmaxf(m, l[c]);
+            for (int c = threadIdx.x; c < cols; c += kRowThreads) m = fmaxf(m, l[c]);
+        }
         m = warp_max(m);
         if (lane == 0) part[0][warp] = m;
         __syncthreads();
@@ -388,7 +427,7 @@ head_merge_kernel(const float2* running, int parts, int N, const int* live, cons
 
 // Logits to their gradients, in place; a warp takes 128 columns of a row at a time, dealt over the blocks of its row.
 __global__ void __launch_bounds__(kRowThreads)
-head_gradient_kernel(float* logits, int64_t ld, int cols, int v0, const int* target, const float* scale, const float* lse)
+head_gradient_kernel(float* logits, int64_t ld, int parts, int64_t part_stride, int cols, int v0, const int* target, const float* scale, const float* lse)
 {
     pdl_wait();
     pdl_trigger();
@@ -400,7 +439,7 @@ head_gradient_kernel(float* logits, int64_t ld, int cols, int v0, const int* tar
     for (int c0 = (static_cast<int>(blockIdx.y) * (kRowThreads / 32) + warp) * 128; c0 < cols; c0 += static_cast<int>(gridDim.y) * (kRowThreads / 32) * 128) {
         float x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = is && c0 + lane + 32 * i < cols ? l[c0 + lane + 32 * i] : 0.f;
+        for (int i = 0; i < 4; ++i) x[i] = is && c0 + lane + 32 * i < cols ? sum_of_parts(l + c0 + lane + 32 * i, parts, part_stride) : 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int c = c0 + lane + 32 * i;
@@ -468,7 +507,8 @@ size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V
     if (N < 1) return kStatusBytes;
     const size_t front = head_front(backward, dtype, N, D, V, any_rows && dtype == VELORA_BF16, backward ? gradient_splits(dtype, N, D, V) : 1).piece;
     if (dtype == VELORA_BF16 && !backward) return front;
-    return front + up256(piece_element(dtype, backward) * static_cast<size_t>(N) * static_cast<size_t>(room_wanted(dtype, N, V)));
+    return front + up256(piece_element(dtype, backward) * static_cast<size_t>(logit_parts(dtype, N, D, V)) * static_cast<size_t>(N) *
+                         static_cast<size_t>(room_wanted(dtype, N, V)));
 }
 
 namespace {
@@ -483,6 +523,22 @@ int head_weights(const HeadArgs& a, const HeadLayout& l, const char** W, int64_t
     *W = a.ws + l.w;
     *ldw = pack_rows_pitch(a.D);
     return launch_pack_rows(&job, 1, a.stream);
+}
+
+// fp32 logits of a piece, in as many parts as it returns (up to the layout's).
+int fp32_logits(const HeadArgs& a, const HeadLayout& l, const char* w, int64_t ldw, int64_t cols, int* rc)
+{
+    const float* x = reinterpret_cast<const float*>(a.ws + l.x);
+    float* c = reinterpret_cast<float*>(a.ws + l.piece);
+    const int parts = l.parts > 1 ? fp32_parts(a.N, cols, a.D) : 1;
+    if (parts > 1 && parts <= l.parts) {
+        *rc = launch_gemm_simt_parts(simt_parts(a.N, cols, a.D), x, l.ldx, 1, reinterpret_cast<const float*>(w), ldw, 1, c, l.piece_cols,
+                                     a.N * l.piece_cols, 0, a.N, cols, a.D, a.stream);
+        return parts;
+    }
+    *rc = product(GEMM_NT_K_K, x, VELORA_F32, l.ldx, w, VELORA_F32, ldw, c, VELORA_F32, l.piece_cols, 0, a.N, cols, a.D,
+                  reinterpret_cast<int*>(a.ws), GemmMore{}, a.stream);
+    return 1;
 }
 
 HeadTile head_tile(const HeadArgs& a, const HeadLayout& l, int64_t v0, int64_t cols)
@@ -527,10 +583,10 @@ int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
     float* piece = reinterpret_cast<float*>(a.ws + l.piece);
     for (int64_t v0 = 0; v0 < a.V; v0 += l.piece_cols) {
         const int64_t cols = a.V - v0 < l.piece_cols ? a.V - v0 : l.piece_cols;
-        rc = product(GEMM_NT_K_K, a.ws + l.x, a.dtype, l.ldx, W + static_cast<size_t>(v0) * ldw * dtype_size(a.dtype), a.dtype, ldw, piece, VELORA_F32,
-                     l.piece_cols, 0, a.N, cols, a.D, status, GemmMore{}, a.stream);
+        const int64_t part_stride = a.N * l.piece_cols;
+        const int parts = fp32_logits(a, l, W + static_cast<size_t>(v0) * ldw * 4, ldw, cols, &rc);
         if (rc != VELORA_OK) return rc;
-        rc = launch_chained(head_stats_kernel, dim3(static_cast<unsigned>(a.N)), kRowThreads, 0, a.stream, piece, l.piece_cols, static_cast<int>(cols), static_cast<int>(v0),
+        rc = launch_chained(head_stats_kernel, dim3(static_cast<unsigned>(a.N)), kRowThreads, 0, a.stream, piece, l.piece_cols, parts, part_stride, static_cast<int>(cols), static_cast<int>(v0),
                             reinterpret_cast<int*>(a.ws + l.live), reinterpret_cast<int*>(a.ws + l.order), reinterpret_cast<int*>(a.ws + l.target),
                             reinterpret_cast<float*>(a.ws + l.at_target), reinterpret_cast<float2*>(a.ws + l.running), v0 == 0 ? 1 : 0,
                             v0 + cols == a.V ? 1 : 0, loss, lse);
@@ -567,11 +623,11 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
         if (a.dtype == VELORA_BF16) {
             rc = (a.N <= kHeadFew ? launch_head_few : launch_head_tiles)(a.ws + l.x, l.ldx, w, ldw, G, l.piece_cols, head_tile(a, l, v0, cols), status, a.stream);
         } else {
-            rc = product(GEMM_NT_K_K, a.ws + l.x, a.dtype, l.ldx, w, a.dtype, ldw, G, VELORA_F32, l.piece_cols, 0, a.N, cols, a.D, status, GemmMore{}, a.stream);
+            const int parts = fp32_logits(a, l, w, ldw, cols, &rc);
             if (rc != VELORA_OK) return rc;
             const int64_t blocks = ceil_div64(cols, 128 * (kRowThreads / 32));
             rc = launch_chained(head_gradient_kernel, dim3(static_cast<unsigned>(a.N), static_cast<unsigned>(blocks < 16 ? blocks : 16)), kRowThreads,
-                                0, a.stream, reinterpret_cast<float*>(G), l.piece_cols, static_cast<int>(cols), static_cast<int>(v0), reinterpret_cast<int*>(a.ws + l.target), reinterpret_cast<float*>(a.ws + l.scale),
+                                0, a.stream, reinterpret_cast<float*>(G), l.piece_cols, parts, a.N * l.piece_cols, static_cast<int>(cols), static_cast<int>(v0), reinterpret_cast<int*>(a.ws + l.target), reinterpret_cast<float*>(a.ws + l.scale),
                                 reinterpret_cast<float*>(a.ws + l.lse));
         }
         if (rc != VELORA_OK) return rc;
@@ -580,7 +636,13 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
             rc = product(GEMM_TN_MN_MN, G, a.dtype, l.piece_cols, a.ws + l.x, a.dtype, l.ldx, dw, dw_dtype, lddw, beta, cols, a.D, a.N, status, GemmMore{live, take_common ? common : nullptr, 1, 0, kBand}, a.stream);
             if (rc != VELORA_OK) return rc;
         }
-        if (dX) {
+        if (dX && a.dtype != VELORA_BF16 && l.splits > 1) {
+            SimtParts shape = simt_parts(a.N, a.D, l.piece_cols);
+            shape.parts = l.splits;
+            rc = launch_gemm_simt_parts(shape, reinterpret_cast<float*>(G), l.piece_cols, 1, reinterpret_cast<const float*>(w), 1, ldw,
+                                        reinterpret_cast<float*>(a.ws + l.sum), l.ldx, a.N * l.ldx, v0 > 0 ? 1 : 0, a.N, a.D, cols, a.stream);
+            if (rc != VELORA_OK) return rc;
+        } else if (dX) {
             rc = product(GEMM_NN_K_MN, G, a.dtype, l.piece_cols, w, a.dtype, ldw, a.ws + l.sum, VELORA_F32, l.ldx, v0 > 0 ? 1 : 0, a.N, a.D, cols, status,
                          GemmMore{live, nullptr, l.splits, a.N * l.ldx, kBand}, a.stream);
             if (rc != VELORA_OK) return rc;

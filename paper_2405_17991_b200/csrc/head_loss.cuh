@@ -20,7 +20,7 @@ struct HeadLayout {
     size_t sum;             // fp32, pitch ldx: dX so far, `splits` partial sums (backward)
     size_t piece;           // a piece of the vocabulary: logits or their gradient, pitch `piece_cols` elements
     int64_t ldx, piece_cols;
-    int splits;
+    int splits, parts;      // partial sums of dX; of the logits (fp32), one piece behind another
     size_t bytes;
 };
 

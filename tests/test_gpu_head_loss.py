@@ -96,7 +96,7 @@ def check_norm(got, ref, dtype, what):
         assert (got.double() - ref).norm() <= 2 ** 0.5 * 2.0 ** -8 * ref.norm(), what
 
 
-SIZES = [(1, 8, 1), (1, 64, 100), (2, 16, 33), (3, 72, 257), (65, 128, 1000), (300, 256, 2049), (257, 512, 4097), (1030, 264, 777), (129, 1024, 8192)]
+SIZES = [(1, 8, 1), (1, 64, 100), (2, 16, 33), (64, 768, 1000), (5, 1024, 3001), (200, 520, 2500), (3, 72, 257), (65, 128, 1000), (300, 256, 2049), (257, 512, 4097), (1030, 264, 777), (129, 1024, 8192)]
 
 
 @pytest.mark.parametrize("masked", ["none", "some", "all", "all but the last", "every other"])
