@@ -20,7 +20,6 @@ constexpr int kPieceStep = 256;                     // pieces are multiples of t
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 int64_t round_up(int64_t x, int64_t to) { return ceil_div64(x, to) * to; }
 
-size_t piece_element(int dtype, bool backward) { return dtype == VELORA_BF16 && backward ? 2 : 4; }      // of one part
 
 // Pieces of equal width, as few as fit the room but for up to two more where those fill the last wave of tiles better.  What a piece
 // costs, in k-blocks of 256 x 256 tiles on 74 pairs: its products, and the sums of dX that each but the first reads and writes (about 9 k-blocks
@@ -47,6 +46,13 @@ int64_t room_wanted(int dtype, int64_t N, int64_t V)          // in columns
     return least < all ? least : all;
 }
 
+// Up to 64 tokens the logits' gradients take two rows of bf16 each, the second what the first leaves: few of them do not average their
+// roundings out (one token: dX and dW off by up to 4e-3), and the products' tiles have the rows to spare.
+int gradient_rows(int dtype, int64_t N) { return dtype == VELORA_BF16 && N <= 64 ? 2 : 1; }
+
+// Bytes of a token and column of the piece, one part.
+size_t piece_element(int dtype, bool backward, int64_t N) { return dtype == VELORA_BF16 && backward ? 2 * static_cast<size_t>(gradient_rows(dtype, N)) : 4; }
+
 // Parts of the contraction that dX's products are cut into, where its tiles are few: waves of units on 74 pairs, each its k-blocks and about
 // 4 more for its sums' way.
 // fp32 products of few tiles are cut into parts on the CUDA cores where that is estimated to be faster than either form of the whole
@@ -61,7 +67,7 @@ int fp32_parts(int64_t M, int64_t N, int64_t K)
 int gradient_splits(int dtype, int64_t N, int64_t D, int64_t V)
 {
     if (dtype != VELORA_BF16) return fp32_parts(N, D, piece_width(N, D, V, room_wanted(dtype, N, V)));
-    if (N <= kHeadFew) return 1;
+    if (N <= kHeadFew) return gradient_rows(dtype, N);          // the rows' sums, one behind the other
     const int64_t tiles = ceil_div64(N, 256) * ceil_div64(D, 256), kblocks = ceil_div64(piece_width(N, D, V, room_wanted(dtype, N, V)), 64);
     int best = 1;
     int64_t best_cost = 0;
@@ -102,7 +108,8 @@ HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D, int64_t V,
         const size_t parts = dtype != VELORA_BF16 ? 1 : static_cast<size_t>(N <= kHeadFew ? ceil_div64(V, kHeadFewHeight) : 2 * ceil_div64(V, 256));
         l.running = take(8 * n * parts);
     }
-    l.x = take(n * static_cast<size_t>(l.ldx) * dtype_size(dtype));
+    l.rows = backward ? gradient_rows(dtype, N) : 1;
+    l.x = take(n * static_cast<size_t>(l.rows) * static_cast<size_t>(l.ldx) * dtype_size(dtype));
     if (pack_w) l.w = take(pack_rows_bytes(V, D));
     l.piece = at;
     return l;
@@ -114,11 +121,11 @@ int logit_parts(int dtype, int64_t N, int64_t D, int64_t V) { return dtype == VE
 int head_layout(HeadLayout* l, bool backward, const HeadArgs& a)
 {
     const bool pack_w = a.dtype == VELORA_BF16 && !tc_operand_ok(a.W, a.ldw);
-    size_t column = piece_element(a.dtype, backward) * static_cast<size_t>(a.N);
+    size_t column = piece_element(a.dtype, backward, a.N) * static_cast<size_t>(a.N);
     *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, backward ? gradient_splits(a.dtype, a.N, a.D, a.V) : 1);
     l->parts = logit_parts(a.dtype, a.N, a.D, a.V);
     if (a.ws_bytes < l->piece + column * l->parts * kPieceStep) {             // less room than asked for: no partial sums
-        *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, 1);
+        *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, backward ? gradient_rows(a.dtype, a.N) : 1);
         l->parts = 1;
     }
     column *= static_cast<size_t>(l->parts);
@@ -128,7 +135,7 @@ int head_layout(HeadLayout* l, bool backward, const HeadArgs& a)
     if (fit < kPieceStep) return VELORA_ERR_WORKSPACE;
     const int64_t want = room_wanted(a.dtype, a.N, a.V);
     l->piece_cols = piece_width(a.N, a.D, a.V, fit < want ? fit : want);
-    if (a.dtype != VELORA_BF16) return VELORA_OK;
+    if (a.dtype != VELORA_BF16 || l->rows > 1) return VELORA_OK;
     // In every piece, the last and narrower one too, each part has k-blocks.
     const int64_t last = a.V - (ceil_div64(a.V, l->piece_cols) - 1) * l->piece_cols;
     auto fills = [](int64_t cols, int parts) { const int64_t kb = ceil_div64(cols, 64); return ceil_div64(kb, ceil_div64(kb, parts)) == parts; };
@@ -145,7 +152,7 @@ struct RowsArgs {
     const float* dloss;             // backward only
     const float* lse;
     int take_common;                // whether a factor is taken out of the dloss
-    int N, V, D, rows_per_cta;
+    int N, V, D, rows_per_cta, copies;
     int* live;
     int* order;
     int* target_out;
@@ -238,14 +245,22 @@ head_rows_kernel(const RowsArgs a)
             const bool zero = code < 0;
             const T* src = static_cast<const T*>(a.X) + static_cast<int64_t>(b0 + i) * a.ldx;
             T* dst = static_cast<T*>(a.x_out) + static_cast<int64_t>(zero ? -1 - code : code) * a.ldx_out;
+            const int64_t copy = static_cast<int64_t>(a.N) * a.ldx_out;
             if (VEC) {
                 constexpr int per = 16 / sizeof(T);
                 const int chunks = a.D / per;                      // D is a multiple of 8
 #pragma unroll 4
-                for (int c = lane + 32 * blockIdx.y; c < chunks; c += 32 * gridDim.y)
-                    reinterpret_cast<uint4*>(dst)[c] = ld_stream_if(src + c * per, !zero);
+                for (int c = lane + 32 * blockIdx.y; c < chunks; c += 32 * gridDim.y) {
+                    const uint4 x = ld_stream_if(src + c * per, !zero);
+                    reinterpret_cast<uint4*>(dst)[c] = x;
+                    if (a.copies > 1) reinterpret_cast<uint4*>(dst + copy)[c] = x;
+                }
             } else {
-                for (int c = lane + 32 * blockIdx.y; c < a.ldx_out; c += 32 * gridDim.y) Elem<T>::store(dst + c, zero || c >= a.D ? 0.f : Elem<T>::load(src + c));
+                for (int c = lane + 32 * blockIdx.y; c < a.ldx_out; c += 32 * gridDim.y) {
+                    const float x = zero || c >= a.D ? 0.f : Elem<T>::load(src + c);
+                    Elem<T>::store(dst + c, x);
+                    if (a.copies > 1) Elem<T>::store(dst + copy + c, x);
+                }
             }
         }
         before += all;
@@ -278,6 +293,7 @@ int launch_rows(const HeadArgs& a, const HeadLayout& l, const float* lse, const 
     }
     r.x_out = a.ws + l.x;
     r.ldx_out = l.ldx;
+    r.copies = l.rows;
     r.status = reinterpret_cast<int*>(a.ws);
     // Eight rows a CTA (one a warp) as long as that leaves no more than four CTAs per SM.
     const int64_t most = static_cast<int64_t>(di.sm_count) * 4;
@@ -507,7 +523,7 @@ size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V
     if (N < 1) return kStatusBytes;
     const size_t front = head_front(backward, dtype, N, D, V, any_rows && dtype == VELORA_BF16, backward ? gradient_splits(dtype, N, D, V) : 1).piece;
     if (dtype == VELORA_BF16 && !backward) return front;
-    return front + up256(piece_element(dtype, backward) * static_cast<size_t>(logit_parts(dtype, N, D, V)) * static_cast<size_t>(N) *
+    return front + up256(piece_element(dtype, backward, N) * static_cast<size_t>(logit_parts(dtype, N, D, V)) * static_cast<size_t>(N) *
                          static_cast<size_t>(room_wanted(dtype, N, V)));
 }
 
@@ -575,7 +591,8 @@ int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
     if (a.dtype == VELORA_BF16) {
         const HeadTile h = head_tile(a, l, 0, a.V);
         const bool few = a.N <= kHeadFew;
-        rc = (few ? launch_head_few : launch_head_tiles)(a.ws + l.x, l.ldx, W, ldw, nullptr, 0, h, status, a.stream);
+        rc = few ? launch_head_few(a.ws + l.x, l.ldx, W, ldw, nullptr, 0, 0, h, status, a.stream)
+                 : launch_head_tiles(a.ws + l.x, l.ldx, W, ldw, nullptr, 0, h, status, a.stream);
         if (rc != VELORA_OK) return rc;
         return launch_chained(head_merge_kernel, dim3(static_cast<unsigned>(ceil_div64(a.N, 32))), kRowThreads, 0, a.stream, h.running,
                               static_cast<int>(ceil_div64(a.V, few ? head_few_height(a.V) : 128)), n, h.live, reinterpret_cast<int*>(a.ws + l.order), h.target, h.at_target, loss, lse);
@@ -605,7 +622,7 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
     int64_t ldw;
     rc = head_weights(a, l, &W, &ldw);
     if (rc != VELORA_OK) return rc;
-    // In bf16 the logits' gradients are rounded once, for the tensor cores: by half a step each.  A mean's 1 / count in all of them would be the same
+    // In bf16 the logits' gradients are rounded once (more than 64 tokens), for the tensor cores: by half a step each.  A mean's 1 / count in all of them would be the same
     // rounding again and again, which does not average out (relative error of dX and dW up to 4e-3 by the count alone); so the largest dloss
     // is taken out and multiplied back in fp32, wherever the product that writes dW takes a factor.
     const bool take_common = a.dtype == VELORA_BF16 && (!dW || dw_dtype == VELORA_BF16 || c_rows_vec(dW, lddw, sizeof(float)));
@@ -621,7 +638,9 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
         const int64_t cols = a.V - v0 < l.piece_cols ? a.V - v0 : l.piece_cols;
         const char* w = W + static_cast<size_t>(v0) * ldw * dtype_size(a.dtype);
         if (a.dtype == VELORA_BF16) {
-            rc = (a.N <= kHeadFew ? launch_head_few : launch_head_tiles)(a.ws + l.x, l.ldx, w, ldw, G, l.piece_cols, head_tile(a, l, v0, cols), status, a.stream);
+            const HeadTile h = head_tile(a, l, v0, cols);
+            rc = a.N <= kHeadFew ? launch_head_few(a.ws + l.x, l.ldx, w, ldw, G, l.piece_cols, l.rows > 1, h, status, a.stream)
+                                 : launch_head_tiles(a.ws + l.x, l.ldx, w, ldw, G, l.piece_cols, h, status, a.stream);
         } else {
             const int parts = fp32_logits(a, l, w, ldw, cols, &rc);
             if (rc != VELORA_OK) return rc;
@@ -633,7 +652,8 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
         if (rc != VELORA_OK) return rc;
         if (dW) {
             char* dw = static_cast<char*>(dW) + static_cast<size_t>(v0) * lddw * dtype_size(dw_dtype);
-            rc = product(GEMM_TN_MN_MN, G, a.dtype, l.piece_cols, a.ws + l.x, a.dtype, l.ldx, dw, dw_dtype, lddw, beta, cols, a.D, a.N, status, GemmMore{live, take_common ? common : nullptr, 1, 0, kBand}, a.stream);
+            rc = product(GEMM_TN_MN_MN, G, a.dtype, l.piece_cols, a.ws + l.x, a.dtype, l.ldx, dw, dw_dtype, lddw, beta, cols, a.D, a.N * l.rows, status,
+                         GemmMore{l.rows > 1 ? nullptr : live, take_common ? common : nullptr, 1, 0, kBand}, a.stream);
             if (rc != VELORA_OK) return rc;
         }
         if (dX && a.dtype != VELORA_BF16 && l.splits > 1) {
@@ -643,8 +663,8 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
                                         reinterpret_cast<float*>(a.ws + l.sum), l.ldx, a.N * l.ldx, v0 > 0 ? 1 : 0, a.N, a.D, cols, a.stream);
             if (rc != VELORA_OK) return rc;
         } else if (dX) {
-            rc = product(GEMM_NN_K_MN, G, a.dtype, l.piece_cols, w, a.dtype, ldw, a.ws + l.sum, VELORA_F32, l.ldx, v0 > 0 ? 1 : 0, a.N, a.D, cols, status,
-                         GemmMore{live, nullptr, l.splits, a.N * l.ldx, kBand}, a.stream);
+            rc = product(GEMM_NN_K_MN, G, a.dtype, l.piece_cols, w, a.dtype, ldw, a.ws + l.sum, VELORA_F32, l.ldx, v0 > 0 ? 1 : 0, a.N * l.rows, a.D, cols, status,
+                         l.rows > 1 ? GemmMore{} : GemmMore{live, nullptr, l.splits, a.N * l.ldx, kBand}, a.stream);
             if (rc != VELORA_OK) return rc;
         }
     }

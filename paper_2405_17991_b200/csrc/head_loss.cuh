@@ -20,6 +20,7 @@ struct HeadLayout {
     size_t sum;             // fp32, pitch ldx: dX so far, `splits` partial sums (backward)
     size_t piece;           // a piece of the vocabulary: logits or their gradient, pitch `piece_cols` elements
     int64_t ldx, piece_cols;
+    int rows;               // copies of the rows of X, and rows of the logits' gradients for each (backward)
     int splits, parts;      // partial sums of dX; of the logits (fp32), one piece behind another
     size_t bytes;
 };
@@ -50,11 +51,11 @@ struct HeadTile {
 // G == nullptr: statistics of bf16 x W^T; otherwise its gradient to G [N, ldg].  W: its row v0.  (head_loss_tc.cu)
 int launch_head_tiles(const void* x, int64_t ldx, const void* W, int64_t ldw, void* G, int64_t ldg, const HeadTile& h, int* status, cudaStream_t stream);
 
-// The same for up to kHeadFew tokens.  (head_loss_few.cu)
+// The same for up to kHeadFew tokens; `twice`: what the gradient's rounding to bf16 leaves of it goes to rows N .. 2 N - 1.  (head_loss_few.cu)
 constexpr int kHeadFew = 128;
 constexpr int kHeadFewHeight = 64;                  // least height of its tiles
 int head_few_height(int64_t cols);                  // columns of the vocabulary in a tile: a row of `running` each
-int launch_head_few(const void* x, int64_t ldx, const void* W, int64_t ldw, void* G, int64_t ldg, const HeadTile& h, int* status, cudaStream_t stream);
+int launch_head_few(const void* x, int64_t ldx, const void* W, int64_t ldw, void* G, int64_t ldg, int twice, const HeadTile& h, int* status, cudaStream_t stream);
 
 #ifdef __CUDACC__
 constexpr float kHeadLog2e = 1.4426950408889634f;

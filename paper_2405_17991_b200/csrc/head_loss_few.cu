@@ -5,8 +5,8 @@
 //
 // Per CTA: warp 0 lane 0 TMA producer, warp 1 lane 0 MMA issuer, warps 2..5 epilogue (32 columns of the vocabulary each).  A lane of the
 // epilogue has one column for all tokens; 32 x 32 blocks are turned over through shared memory, and then it has one token for 32
-// columns.  Contractions are cut into segments as in head_loss_tc.cu, of 128 here: there is time for it.  1 x 4096 of 32000: 51 us, 262 MB at 5.1 TB/s (71 us with the
-// tokens as rows of 256).
+// columns.  Contractions are cut into segments as in head_loss_tc.cu, of 512 here (of 128: 61 us).  1 x 4096 of 32000: the call 54 us, W
+// alone at the copy rate 41 (87 us with the tokens as rows of 256).
 #include "gemm_tc.cuh"
 #include "head_loss.cuh"
 #include "tc_common.cuh"
@@ -19,7 +19,7 @@ namespace {
 
 constexpr int W_BM = 128;                  // columns of the vocabulary in a tile
 constexpr int W_BK = 64;
-constexpr int W_SEGMENT = 2;               // k-blocks that an accumulator adds up
+constexpr int W_SEGMENT = 8;               // k-blocks that an accumulator adds up
 constexpr int W_THREADS = 192;
 constexpr int W_PITCH = 33;
 constexpr int W_STAGING_BYTES = 4 * 32 * W_PITCH * 4;
@@ -45,7 +45,7 @@ __device__ __forceinline__ bool epilogue_any(bool p)
 template <bool GRADIENT, int NT>
 __global__ void __launch_bounds__(W_THREADS, 1)
 head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const HeadTile h, int height, __nv_bfloat16* G, int64_t ldg,
-                int* status)
+                int twice, int* status)
 {
     typedef FewShape<NT> S;
     extern __shared__ uint8_t smem_raw[];
@@ -194,20 +194,27 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
                 } else if (row < h.N && valid > 0) {
                     const bool is = target >= 0;
                     const float g = is ? h.scale[row] : 0.f, z = is ? -h.lse[row] * kHeadLog2e : 0.f;
-                    uint32_t w[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float x = head_exp2(fmaf(mine[2 * i], kHeadLog2e, z)) * g, y = head_exp2(fmaf(mine[2 * i + 1], kHeadLog2e, z)) * g;
-                        if (t == 2 * i) x -= g;
-                        if (t == 2 * i + 1) y -= g;
-                        w[i] = is ? pack_bf16x2(x, y) : 0u;
-                    }
                     // The pitch is a multiple of 256 and the height of 16: columns past the piece's are there to be written, those of the next tile
                     // are not touched.
                     uint4* dst = reinterpret_cast<uint4*>(G + row * ldg + v0);
+                    uint4* rest = reinterpret_cast<uint4*>(G + (row + h.N) * ldg + v0);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (8 * i < valid) dst[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t w[4], r[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int j = 8 * i + 2 * k;
+                            float x = head_exp2(fmaf(mine[j], kHeadLog2e, z)) * g, y = head_exp2(fmaf(mine[j + 1], kHeadLog2e, z)) * g;
+                            if (t == j) x -= g;
+                            if (t == j + 1) y -= g;
+                            w[k] = is ? pack_bf16x2(x, y) : 0u;
+                            r[k] = is ? pack_bf16x2(x - bf16_lo(w[k]), y - bf16_hi(w[k])) : 0u;
+                        }
+                        if (8 * i < valid) {
+                            dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                            if (twice) rest[i] = make_uint4(r[0], r[1], r[2], r[3]);
+                        }
+                    }
                 }
             }
             if (!GRADIENT) {
@@ -242,7 +249,7 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
 }
 
 template <bool GRADIENT, int NT>
-int launch_few(const CUtensorMap& tw, const CUtensorMap& tx, const HeadTile& h, int height, void* G, int64_t ldg, int* status, int sm_count, cudaStream_t stream)
+int launch_few(const CUtensorMap& tw, const CUtensorMap& tx, const HeadTile& h, int height, void* G, int64_t ldg, int twice, int* status, int sm_count, cudaStream_t stream)
 {
     static DeviceOnce configured;
     int dev = 0;
@@ -254,7 +261,7 @@ int launch_few(const CUtensorMap& tw, const CUtensorMap& tx, const HeadTile& h, 
     }
     const int tiles = (h.cols + height - 1) / height;
     return launch_chained(kern, dim3(static_cast<unsigned>(tiles < sm_count ? tiles : sm_count)), W_THREADS, FewShape<NT>::kSmem, stream,
-                          tw, tx, h, height, static_cast<__nv_bfloat16*>(G), ldg, status);
+                          tw, tx, h, height, static_cast<__nv_bfloat16*>(G), ldg, twice, status);
 }
 
 }  // namespace
@@ -273,7 +280,7 @@ int head_few_height(int64_t cols)
     return best;
 }
 
-int launch_head_few(const void* x, int64_t ldx, const void* W, int64_t ldw, void* G, int64_t ldg, const HeadTile& h, int* status, cudaStream_t stream)
+int launch_head_few(const void* x, int64_t ldx, const void* W, int64_t ldw, void* G, int64_t ldg, int twice, const HeadTile& h, int* status, cudaStream_t stream)
 {
     DeviceInfo di;
     int rc = device_info(&di);
@@ -286,9 +293,9 @@ int launch_head_few(const void* x, int64_t ldx, const void* W, int64_t ldw, void
     rc = make_tmap_bf16_2d(&tx, x, h.D, h.N, ldx, W_BK, nt);
     if (rc != VELORA_OK) return rc;
 #define VELORA_FEW(GRAD)                                                                                      \
-    (nt == 32 ? launch_few<GRAD, 32>(tw, tx, h, height, G, ldg, status, di.sm_count, stream)                          \
-              : (nt == 64 ? launch_few<GRAD, 64>(tw, tx, h, height, G, ldg, status, di.sm_count, stream)              \
-                          : launch_few<GRAD, 128>(tw, tx, h, height, G, ldg, status, di.sm_count, stream)))
+    (nt == 32 ? launch_few<GRAD, 32>(tw, tx, h, height, G, ldg, twice, status, di.sm_count, stream)                          \
+              : (nt == 64 ? launch_few<GRAD, 64>(tw, tx, h, height, G, ldg, twice, status, di.sm_count, stream)              \
+                          : launch_few<GRAD, 128>(tw, tx, h, height, G, ldg, twice, status, di.sm_count, stream)))
     return G ? VELORA_FEW(true) : VELORA_FEW(false);
 #undef VELORA_FEW
 }

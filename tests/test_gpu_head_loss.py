@@ -4,7 +4,7 @@ Bounds, element by element, from the arithmetic (u = 2^-24; sums of K products o
 cores with truncation, K / 16 times into the accumulator; of fp32 numbers K roundings):
   logits   d = (K / 16 + 16) 2u max_v sum |x w|  (bf16),   K 2u max_v sum |x w|  (fp32)
   loss     2 d from the two logits' errors (log sum exp moves by no more than its arguments), exp and log: 2^-19 + 4u |lse|
-  G        g (p (2 d + 2^-18 + 4u |lse|)), and half a step of bf16, 2^-8 |G|, where it is stored so
+  G        g (p (2 d + 2^-18 + 4u |lse|)), and half a step of bf16, 2^-8 |G|, where it is stored so; 2^-16 |G| as two of them (up to 64 tokens)
   dX, dW   sum |error of G| |factor|, the products' sums like the logits', half a step of the output's type
 """
 import numpy as np
@@ -75,7 +75,7 @@ class Reference:
         p = torch.exp(l - lse[:, None])
         G = p * g[:, None]
         G.scatter_add_(1, t[:, None], -g[:, None])
-        rounding = half_step(dtype) if dtype == torch.bfloat16 else 4 * U
+        rounding = (half_step(dtype) if X.shape[0] > 64 else half_step(dtype) ** 2) if dtype == torch.bfloat16 else 4 * U
         dG = g.abs()[:, None] * p * (2 * d + 2.0 ** -18 + 4 * U * lse.abs())[:, None] + rounding * G.abs()
         self.dX, self.dW = G @ w, G.t() @ x
         self.dX_bound = dG @ w.abs() + sums(V, dtype) * (G.abs() @ w.abs())
@@ -90,13 +90,13 @@ def check(got, ref, bound, what, out_rounding):
     assert worst <= 1.0, "%s: %.3g times its bound" % (what, worst)
 
 
-def check_norm(got, ref, dtype, what):
-    """Two independent roundings to bf16 (of G, of the output), each at most half a step: their norms add in squares."""
+def check_norm(got, ref, dtype, what, tokens):
+    """Two independent roundings to bf16 (of G, of the output), each at most half a step: their norms add in squares.  One up to 64 tokens."""
     if dtype == torch.bfloat16 and ref.norm() > 0:
-        assert (got.double() - ref).norm() <= 2 ** 0.5 * 2.0 ** -8 * ref.norm(), what
+        assert (got.double() - ref).norm() <= (2 ** 0.5 if tokens > 64 else 1.01) * 2.0 ** -8 * ref.norm(), what
 
 
-SIZES = [(1, 8, 1), (1, 64, 100), (2, 16, 33), (64, 768, 1000), (5, 1024, 3001), (200, 520, 2500), (3, 72, 257), (65, 128, 1000), (300, 256, 2049), (257, 512, 4097), (1030, 264, 777), (129, 1024, 8192)]
+SIZES = [(1, 8, 1), (1, 64, 100), (2, 16, 33), (64, 768, 1000), (63, 128, 3000), (5, 1024, 3001), (200, 520, 2500), (3, 72, 257), (65, 128, 1000), (300, 256, 2049), (257, 512, 4097), (1030, 264, 777), (129, 1024, 8192)]
 
 
 @pytest.mark.parametrize("masked", ["none", "some", "all", "all but the last", "every other"])
@@ -115,8 +115,8 @@ def test_loss_and_gradients(vl, guard, N, D, V, dtype, masked):
     dX, dW = vl.velora_head_loss_backward(X, W, t, lse, dloss, guard.mat(N, D, dtype), guard.mat(V, D, dtype), ws=ws)
     check(dX, ref.dX, ref.dX_bound, "dX", half_step(dtype))
     check(dW, ref.dW, ref.dW_bound, "dW", half_step(dtype))
-    check_norm(dX, ref.dX, dtype, "dX")
-    check_norm(dW, ref.dW, dtype, "dW")
+    check_norm(dX, ref.dX, dtype, "dX", N)
+    check_norm(dW, ref.dW, dtype, "dW", N)
     assert bool((dX[~ref.live] == 0).all())
     assert vl.velora_workspace_status(ws) == 0
 
