@@ -130,11 +130,10 @@ struct Raw8Odd {
     }
 };
 
-__device__ __forceinline__ uint4 pack8(const float (&y)[8])
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&y)[8])
 {
-    return make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+    __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])));
 }
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&y)[8]) { __stcs(reinterpret_cast<uint4*>(p), pack8(y)); }
 __device__ __forceinline__ void store8(float* p, const float (&y)[8]) { store_f32x8(p, y); }
 
 // CTAs on an SM, by the registers that four segments in flight take.
@@ -212,16 +211,17 @@ checkpoint_store_elem_kernel(const T* X, int64_t ldx, int64_t N, int D, int8_t* 
 // the run, is written one element at a time.
 struct OddRun {
     uint32_t s;                                                 // bytes of a chunk that are the neighbour's
-    uint4 carried;                                              // the last lane's values of the segment before
+    uint4 carried = {0u, 0u, 0u, 0u};                           // of lane 0: the last lane's values of the segment before
     bool begun = false;
     __device__ __forceinline__ OddRun(const __nv_bfloat16* p) : s(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p) & 15)) {}
     // count: how many of this lane's eight there are; next: the same of the next segment's first lane, 0 behind the run's last.
-    __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&y)[8], int count, int next, int lane)
+    __device__ __forceinline__ void store(__nv_bfloat16* p, const uint4& v, int count, int next, int lane)
     {
-        const uint4 v = pack8(y);
-        uint4 before = make_uint4(__shfl_up_sync(0xffffffffu, v.x, 1), __shfl_up_sync(0xffffffffu, v.y, 1),
-                                  __shfl_up_sync(0xffffffffu, v.z, 1), __shfl_up_sync(0xffffffffu, v.w, 1));
-        if (lane == 0) before = carried;
+        const int from_lane = (lane + 31) & 31;
+        const uint4 turned = make_uint4(__shfl_sync(0xffffffffu, v.x, from_lane), __shfl_sync(0xffffffffu, v.y, from_lane),
+                                        __shfl_sync(0xffffffffu, v.z, from_lane), __shfl_sync(0xffffffffu, v.w, from_lane));
+        const uint4 before = lane == 0 ? carried : turned;
+        carried = turned;
         const int mine = static_cast<int>(16 - s) / 2;           // elements in the chunk
         const bool whole = (lane > 0 || begun || s == 0) && count >= mine;
         bool next_whole = __shfl_down_sync(0xffffffffu, static_cast<int>(whole), 1) != 0;
@@ -229,12 +229,12 @@ struct OddRun {
         if (whole) __stcs(reinterpret_cast<uint4*>(reinterpret_cast<char*>(p) - s), s == 0 ? v : shift_chunks(before, v, 16 - s));
         const int from = whole ? mine : 0, to = next_whole ? mine : count;
         if (from < to && count > 0) {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (e >= from && e < to && e < count) p[e] = __float2bfloat16_rn(y[e]);
+                if (e >= from && e < to && e < count)
+                    p[e] = __ushort_as_bfloat16(static_cast<unsigned short>(w[e >> 1] >> (16 * (e & 1))));
         }
-        carried = make_uint4(__shfl_sync(0xffffffffu, v.x, 31), __shfl_sync(0xffffffffu, v.y, 31), __shfl_sync(0xffffffffu, v.z, 31),
-                             __shfl_sync(0xffffffffu, v.w, 31));
         begun = true;
     }
 };
@@ -275,18 +275,20 @@ checkpoint_load_vec_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int64
         for (int i = 0; i < U; ++i) {
             const int left = left0 - i * kSegment;
             if (D - at.run * (U * kSegment) <= i * kSegment) break;            // for the whole warp
-            float y[8];
-            checkpoint_values(q[i], exponent[i], y);
             if constexpr (ODD) {
                 // The next segment's first lane has D - its first column left.
                 const int next = i + 1 < U ? D - at.run * (U * kSegment) - (i + 1) * kSegment : 0;
-                odd.store(dst + i * kSegment, y, min(max(left, 0), 8), min(max(next, 0), 8), lane);
-            } else if (left >= 8) {
-                store8(dst + i * kSegment, y);
-            } else if (left > 0) {
+                odd.store(dst + i * kSegment, checkpoint_values_bf16(q[i], exponent[i]), min(max(left, 0), 8), min(max(next, 0), 8), lane);
+            } else {
+                float y[8];                                   // before the branches: within them 107 us instead of 99 for 8192 x 11008
+                checkpoint_values(q[i], exponent[i], y);
+                if (left >= 8) {
+                    store8(dst + i * kSegment, y);
+                } else if (left > 0) {
 #pragma unroll
-                for (int e = 0; e < 7; ++e)
-                    if (e < left) Elem<T>::store(dst + i * kSegment + e, y[e]);
+                    for (int e = 0; e < 7; ++e)
+                        if (e < left) Elem<T>::store(dst + i * kSegment + e, y[e]);
+                }
             }
         }
     }

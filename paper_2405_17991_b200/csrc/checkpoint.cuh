@@ -60,6 +60,22 @@ __device__ __forceinline__ void checkpoint_values(const uint2& q, uint32_t expon
         y[4 * h + 3] = (__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7653)) - 8388736.f) * s;
     }
 }
+// The same in bf16, two at a time: the low seven bits b of a code as 128 + b, minus 128 or, with the sign bit, 256; exact, as is the product
+// with a power of two.
+__device__ __forceinline__ uint32_t checkpoint_values_bf16x2(uint32_t halves, uint32_t step)
+{
+    const uint32_t v = (halves & 0x007f007fu) | 0x43004300u, c = (halves & 0x00800080u) | 0x43004300u;
+    uint32_t q, r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(q) : "r"(v), "r"(c));
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(q), "r"(step));
+    return r;
+}
+__device__ __forceinline__ uint4 checkpoint_values_bf16(const uint2& q, uint32_t exponent)
+{
+    const uint32_t step = (exponent << 7) * 0x00010001u;             // 2^(E - 127) twice; infinite for E = 255, so that 0 becomes NaN
+    return make_uint4(checkpoint_values_bf16x2(__byte_perm(q.x, 0, 0x4140), step), checkpoint_values_bf16x2(__byte_perm(q.x, 0, 0x4342), step),
+                      checkpoint_values_bf16x2(__byte_perm(q.y, 0, 0x4140), step), checkpoint_values_bf16x2(__byte_perm(q.y, 0, 0x4342), step));
+}
 #endif
 
 }  // namespace velora
