@@ -113,3 +113,19 @@ def test_binding_refuses_shapes(b):
             call()
     with pytest.raises(ValueError):
         b.velora_checkpoint_load(torch.zeros((4, 64), dtype=torch.uint8), torch.zeros((4, 2), dtype=torch.uint8))
+
+
+def test_binding_refuses_tensors_of_another_device(b, monkeypatch):
+    """The kernels go to the current device's stream: a tensor of another device is refused before anything is launched."""
+    import torch
+
+    class Elsewhere:
+        device = "cuda:7"
+
+        def get_device(self):
+            return 7
+
+    monkeypatch.setattr(b, "_raw_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    with pytest.raises(ValueError, match="current device"):
+        b._here(Elsewhere())
