@@ -59,6 +59,7 @@ int launch_head_few(const void* x, int64_t ldx, const void* W, int64_t ldw, void
 
 #ifdef __CUDACC__
 constexpr float kHeadLog2e = 1.4426950408889634f;
+constexpr float kHeadLost = 0x1p-8f;                // rounding of a maximum times log2 e that a first-order term makes up for (to 4e-6 of the sum)
 __device__ __forceinline__ float head_exp2(float x)
 {
     float y;

@@ -186,14 +186,25 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
                 if (!GRADIENT) {
                     float m = -INFINITY, s = 0.f;
                     for (int i = 0; i < valid; ++i) m = fmaxf(m, mine[i]);
-                    const float ref = m == -INFINITY ? 0.f : m, c2 = ref * kHeadLog2e, lost = fmaf(ref, kHeadLog2e, -c2);
+                    const float ref = m == -INFINITY ? 0.f : m;
+                    float off = 0.f, c2 = ref * kHeadLog2e, lost = fmaf(ref, kHeadLog2e, -c2);
+                    if (fabsf(lost) > kHeadLost) {           // the maximum is taken off first, see head_loss_tc.cu
+                        off = ref;
+                        c2 = lost = 0.f;
+                    }
 #pragma unroll 8
-                    for (int i = 0; i < valid; ++i) s += head_exp2(fmaf(mine[i], kHeadLog2e, -c2));
+                    for (int i = 0; i < valid; ++i) s += head_exp2(fmaf(mine[i] - off, kHeadLog2e, -c2));
                     parts[quarter * NT + row] = make_float2(m, s * (1.f - lost * 0.69314718f));
                     if (t >= 0 && t < valid) h.at_target[row] = mine[t];
                 } else if (row < h.N && valid > 0) {
                     const bool is = target >= 0;
-                    const float g = is ? h.scale[row] : 0.f, z = is ? -h.lse[row] * kHeadLog2e : 0.f;
+                    const float g = is ? h.scale[row] : 0.f, lse = is ? h.lse[row] : 0.f;
+                    float off = 0.f, z = -lse * kHeadLog2e, lost = fmaf(-lse, kHeadLog2e, -z);
+                    if (fabsf(lost) > kHeadLost) {
+                        off = lse;
+                        z = lost = 0.f;
+                    }
+                    const float gp = g * (1.f + lost * 0.69314718f);
                     // The pitch is a multiple of 256 and the height of 16: columns past the piece's are there to be written, those of the next tile
                     // are not touched.
                     uint4* dst = reinterpret_cast<uint4*>(G + row * ldg + v0);
@@ -204,7 +215,7 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             const int j = 8 * i + 2 * k;
-                            float x = head_exp2(fmaf(mine[j], kHeadLog2e, z)) * g, y = head_exp2(fmaf(mine[j + 1], kHeadLog2e, z)) * g;
+                            float x = head_exp2(fmaf(mine[j] - off, kHeadLog2e, z)) * gp, y = head_exp2(fmaf(mine[j + 1] - off, kHeadLog2e, z)) * gp;
                             if (t == j) x -= g;
                             if (t == j + 1) y -= g;
                             w[k] = is ? pack_bf16x2(x, y) : 0u;

@@ -218,15 +218,6 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) m = fmaxf(m, __uint_as_float(l[c][i]));
-                // 2^(l log2 e - c) with c = m log2 e as rounded, in one multiply-add each; what c lost is put right in the sum.
-                const float ref = m == -INFINITY ? 0.f : m, c2 = ref * kHeadLog2e, lost = fmaf(ref, kHeadLog2e, -c2);
-                float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) s[i & 3] += head_exp2(fmaf(__uint_as_float(l[c][i]), kHeadLog2e, -c2));
-                const float sum = ((s[0] + s[1]) + (s[2] + s[3])) * (1.f - lost * 0.69314718f);
-                if (in) h.running[static_cast<int64_t>((t0.n0 >> 7) + half) * h.N + row] = make_float2(m, sum);
                 const bool hit = t >= 0 && t < 128;
                 if (__any_sync(0xffffffffu, hit)) {
                     float x = 0.f;
@@ -237,13 +228,40 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                             if (t == 32 * c + i) x = __uint_as_float(l[c][i]);
                     if (hit) h.at_target[row] = x;
                 }
+                // 2^(l log2 e - c) with c = m log2 e as rounded, in one multiply-add each; what c lost is put right in the sum, or, where it is
+                // more than a first-order term can (m beyond 10^5), m is taken off first.
+                const float ref = m == -INFINITY ? 0.f : m;
+                float c2 = ref * kHeadLog2e, lost = fmaf(ref, kHeadLog2e, -c2);
+                if (__any_sync(0xffffffffu, fabsf(lost) > kHeadLost)) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(__uint_as_float(l[c][i]) - ref);
+                    c2 = lost = 0.f;
+                }
+                float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) s[i & 3] += head_exp2(fmaf(__uint_as_float(l[c][i]), kHeadLog2e, -c2));
+                const float sum = ((s[0] + s[1]) + (s[2] + s[3])) * (1.f - lost * 0.69314718f);
+                if (in) h.running[static_cast<int64_t>((t0.n0 >> 7) + half) * h.N + row] = make_float2(m, sum);
             } else {
                 const bool is = in && h.target[row] >= 0;
-                const float g = is ? h.scale[row] : 0.f, z = is ? -h.lse[row] * kHeadLog2e : 0.f;
+                const float g = is ? h.scale[row] : 0.f, lse = is ? h.lse[row] : 0.f;
+                float z = -lse * kHeadLog2e, lost = fmaf(-lse, kHeadLog2e, -z);                    // as for the statistics
+                if (__any_sync(0xffffffffu, fabsf(lost) > kHeadLost)) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(__uint_as_float(l[c][i]) - lse);
+                    z = lost = 0.f;
+                }
+                const float gp = g * (1.f + lost * 0.69314718f);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(head_exp2(fmaf(__uint_as_float(l[c][i]), kHeadLog2e, z)) * g);
+                    for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(head_exp2(fmaf(__uint_as_float(l[c][i]), kHeadLog2e, z)) * gp);
                     if (__any_sync(0xffffffffu, t >= 32 * c && t < 32 * c + 32)) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i)

@@ -309,3 +309,32 @@ def test_captured_replayed_and_on_another_stream(vl, dtype):
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("power", [10, 20, 24, 30, 60, 100])
+@pytest.mark.parametrize("N", [3, 100, 200])
+def test_logits_of_any_size(vl, N, power, dtype):
+    """Logits 2^power (v - 50): each is exact, and the row's largest alone has a share in the sum, so loss and lse are exact as well.
+
+    The share itself, 1, is one in fp32, exp(0).  In bf16 it is 2^y (1 - y ln 2) with y, what the rounding of lse log2 e loses, up to 2^-8: off by
+    (y ln 2)^2 / 2 < 3.7e-6 and 2^-22 of the exponential, together below 2^-17."""
+    V, D = 100, 64
+    W = torch.randint(-7, 8, (V, D), device=DEV).to(dtype)
+    W[:, 0] = torch.arange(V, device=DEV) - 50
+    X = torch.zeros((N, D), device=DEV, dtype=dtype)
+    sign = torch.where(torch.arange(N, device=DEV) % 3 == 0, -1.0, 1.0)
+    X[:, 0] = sign * 2.0 ** power
+    top = torch.where(sign > 0, V - 1, 0)
+    t = torch.where(torch.arange(N, device=DEV) % 2 == 0, top, torch.randint(V, (N,), device=DEV))
+    loss, lse = vl.velora_head_loss(X, W, t)
+    logits = X.double() @ W.double().t()
+    assert torch.equal(lse.double(), logits.amax(1))
+    assert torch.equal(loss, lse - logits.gather(1, t[:, None])[:, 0].float())
+    dX, dW = vl.velora_head_loss_backward(X, W, t, lse, torch.ones(N, device=DEV))
+    share = 2.0 ** -17 if dtype == torch.bfloat16 else 0.0
+    of_top, of_target = (torch.nn.functional.one_hot(c, V).double() for c in (top, t))
+    ref, bound = (of_top - of_target) @ W.double(), share * of_top @ W.double().abs()
+    assert bool(((dX.double() - ref).abs() <= (1 + share) * (bound + half_step(dtype) * ref.abs())).all())
+    ref, bound = (of_top - of_target).t() @ X.double(), share * of_top.t() @ X.double().abs()
+    assert bool(((dW.double() - ref).abs() <= (1 + share) * (bound + half_step(dtype) * ref.abs())).all())
