@@ -338,3 +338,41 @@ def test_logits_of_any_size(vl, N, power, dtype):
     assert bool(((dX.double() - ref).abs() <= (1 + share) * (bound + half_step(dtype) * ref.abs())).all())
     ref, bound = (of_top - of_target).t() @ X.double(), share * of_top.t() @ X.double().abs()
     assert bool(((dW.double() - ref).abs() <= (1 + share) * (bound + half_step(dtype) * ref.abs())).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N,shift", [(100, 25), (150, 24)])
+def test_rows_past_32_bits(vl, N, shift, dtype):
+    """Pitches that put the last rows of X, W, dX and dW more than 2^31 elements behind the first."""
+    D, V = 64, 600
+    X, W, t, dloss = batch(N, D, V, dtype, 7, "some")
+    ref = Reference(X, W, t, dloss)
+
+    def far(rows, shift):
+        assert (rows - 1) << shift > 2 ** 31
+        return torch.empty_strided((rows, D), (1 << shift, 1), dtype=dtype, device=DEV)
+
+    x, w, dX, dW = far(N, shift), far(V, 22), far(N, shift), far(V, 22)
+    x.copy_(X)
+    w.copy_(W)
+    loss, lse = vl.velora_head_loss(x, w, t)
+    check(loss, ref.loss, ref.loss_bound, "loss", 0)
+    vl.velora_head_loss_backward(x, w, t, lse, dloss, dX, dW)
+    check(dX, ref.dX, ref.dX_bound, "dX", half_step(dtype))
+    check(dW, ref.dW, ref.dW_bound, "dW", half_step(dtype))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_more_than_2_to_31_logits_at_a_time(vl, dtype):
+    N, D, V = 2200000, 16, 1500
+    X, W, t, dloss = batch(N, D, V, dtype, 8, "some")
+    loss, lse = vl.velora_head_loss(X, W, t)
+    dX, dW = vl.velora_head_loss_backward(X, W, t, lse, dloss)
+    want, bound = 0.0, 0.0
+    for at in range(0, N, 1 << 17):
+        part = slice(at, at + (1 << 17))
+        ref = Reference(X[part], W, t[part], dloss[part])
+        check(loss[part], ref.loss, ref.loss_bound, "loss", 0)
+        check(dX[part], ref.dX, ref.dX_bound, "dX", half_step(dtype))
+        want, bound = want + ref.dW, bound + ref.dW_bound * (sums(N, dtype) / sums(1 << 17, dtype))
+    check(dW, want, bound, "dW", half_step(dtype))
