@@ -386,7 +386,7 @@ int velora_linear_step_host(const void* hX, const void* hdY, void* hY, void* hdX
  *                                  velora_weight_grad);  ws: velora_workspace_bytes(VELORA_OP_CHECKPOINT_WEIGHT_GRAD, N, D, O, 1) bytes,
  *                                  | VELORA_OP_F32 for an fp32 dY, | VELORA_OP_ANY_ROWS where the rows of a bf16 dY do not start on
  *                                  16-byte boundaries (without that room they run on the CUDA cores); initialised.  It holds Xhat in
- *                                  dY's type while the call runs.
+ *                                  dY's type while the call runs, which is all it must have room for, and some sums of the product.
  * N == 0 as in velora_compress and velora_weight_grad.  Any rows are taken; fastest are X and Xhat on 16-byte boundaries (bf16: any) with Q
  * on 8-byte ones.
  */

@@ -203,7 +203,8 @@ int check_checkpoint(const void* Q, int64_t ldq, const void* E, int64_t lde, int
     return VELORA_OK;
 }
 
-// Xhat in dY's type; behind it a packed copy of a bf16 dY whose rows TMA cannot address.
+// Xhat in dY's type; behind it, where there is room, a packed copy of a bf16 dY whose rows TMA cannot address and the sums of a product whose
+// last wave is cut (GemmMore::tail).
 size_t checkpoint_grad_bytes(int64_t N, int64_t D, int dtype) { return kStatusBytes + align256(static_cast<size_t>(N) * round_up8(D) * dtype_size(dtype)); }
 
 // ---- loss of a linear head ----
@@ -295,7 +296,8 @@ size_t velora_workspace_bytes(int op, int64_t N, int64_t D, int64_t O, int Dsub)
         case VELORA_OP_UPDATE_V: return update_v_workspace_bytes(Dsub);
         case VELORA_OP_Z8_CALIBRATE: return z8_calibrate_workspace_bytes(N, D, Dsub);
         case VELORA_OP_CHECKPOINT_WEIGHT_GRAD:
-            return O < 1 ? 0 : checkpoint_grad_bytes(N, D, dtype) + pack_bytes_if_ragged(N, O, any_rows && dtype == VELORA_BF16);
+            return O < 1 ? 0 : checkpoint_grad_bytes(N, D, dtype) + pack_bytes_if_ragged(N, O, any_rows && dtype == VELORA_BF16) +
+                                   (dtype == VELORA_BF16 ? gemm_tail_bytes(O, D, N, 148) : 0);
         case VELORA_OP_HEAD_LOSS: return O < 1 ? 0 : head_loss_bytes(false, dtype, N, D, O, any_rows);
         case VELORA_OP_HEAD_LOSS_BACKWARD: return O < 1 ? 0 : head_loss_bytes(true, dtype, N, D, O, any_rows);
         default: return 0;
@@ -659,7 +661,7 @@ int velora_checkpoint_load(const int8_t* Q, int64_t ldq, const uint8_t* E, int64
     if (N == 0) return VELORA_OK;
     if (!Xhat || ldxhat < D) return VELORA_ERR_INVALID_ARG;
     if (!elem_aligned(Xhat, x_dtype)) return VELORA_ERR_ALIGNMENT;
-    return launch_checkpoint_load(Q, ldq, E, lde, N, D, Xhat, x_dtype, ldxhat, static_cast<cudaStream_t>(stream));
+    return launch_checkpoint_load(Q, ldq, E, lde, N, D, Xhat, x_dtype, ldxhat, nullptr, static_cast<cudaStream_t>(stream));
 }
 
 int velora_checkpoint_weight_grad(const void* dY, int dy_dtype, int64_t N, int64_t O, int64_t lddy,
@@ -680,21 +682,29 @@ int velora_checkpoint_weight_grad(const void* dY, int dy_dtype, int64_t N, int64
     }
     if (!dY || lddy < O) return VELORA_ERR_INVALID_ARG;
     if (!elem_aligned(dY, dy_dtype)) return VELORA_ERR_ALIGNMENT;
-    const size_t used = checkpoint_grad_bytes(N, D, dy_dtype);
+    size_t used = checkpoint_grad_bytes(N, D, dy_dtype);
     if (!ws || ws_bytes < used) return VELORA_ERR_WORKSPACE;
     if (!aligned16(ws)) return VELORA_ERR_ALIGNMENT;
     Operand y{dY, lddy, N, O};
+    uint32_t* tail = nullptr;
     if (dy_dtype == VELORA_BF16) {
         Operand* ops[1] = {&y};
         rc = pack_operands(ops, 1, ws, ws_bytes, used, s);
         if (rc != VELORA_OK) return rc;
+        if (y.p != dY) used += align256(pack_rows_bytes(N, O));
+        DeviceInfo di;
+        rc = device_info(&di);
+        if (rc != VELORA_OK) return rc;
+        const size_t want = gemm_tail_bytes(O, D, N, di.sm_count);
+        if (want > 0 && ws_bytes >= used + want) tail = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + used);
     }
     char* xhat = static_cast<char*>(ws) + kStatusBytes;
     const int64_t ldxh = round_up8(D);
-    rc = launch_checkpoint_load(Q, ldq, E, lde, N, D, xhat, dy_dtype, ldxh, s);
+    static_assert(kLoadZeros * 4 == kTailHeader, "counts of the cut wave");
+    rc = launch_checkpoint_load(Q, ldq, E, lde, N, D, xhat, dy_dtype, ldxh, tail, s);
     if (rc != VELORA_OK) return rc;
     rc = launch_gemm_tc(GEMM_TN_MN_MN, y.p, y.ld, xhat, ldxh, dW, dw_dtype, lddw, beta, O, D, N, dy_dtype, static_cast<int*>(ws), s,
-                        GemmMore{nullptr, nullptr, 1, 0, 8});          // bands of 8 row blocks: 237 us for 8192 x 4096 to 4096, 241 in bands of 4
+                        GemmMore{nullptr, nullptr, 1, 0, 8, tail});          // bands of 8 row blocks: 237 us for 8192 x 4096 to 4096, 241 in bands of 4
     if (rc != VELORA_ERR_UNSUPPORTED) return rc;
     return launch_gemm_simt(dY, dy_dtype, 1, lddy, xhat, dy_dtype, 1, ldxh, dW, dw_dtype, lddw, beta, O, D, N, s);
 }

@@ -242,10 +242,11 @@ struct OddRun {
 // Rows of Q on 8-byte boundaries, rows of Xhat on 16-byte ones unless ODD.
 template <typename T, int U, bool ODD>
 __global__ void __launch_bounds__(kStreamThreads, kResidentLoad)
-checkpoint_load_vec_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int D, T* Xhat, int64_t ldx, int runs)
+checkpoint_load_vec_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int D, T* Xhat, int64_t ldx, int runs, uint32_t* zeros)
 {
     pdl_wait();
     pdl_trigger();
+    if (zeros && blockIdx.x == 0 && threadIdx.x < kLoadZeros) zeros[threadIdx.x] = 0u;
     const int lane = threadIdx.x & 31;
     for (RunWalk at(runs); at.row < N; at.next()) {
         const int col0 = at.run * (U * kSegment) + lane * 8, left0 = D - col0;
@@ -296,10 +297,11 @@ checkpoint_load_vec_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int64
 
 template <typename T>
 __global__ void __launch_bounds__(kStreamThreads)
-checkpoint_load_elem_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int D, T* Xhat, int64_t ldx, int runs)
+checkpoint_load_elem_kernel(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int D, T* Xhat, int64_t ldx, int runs, uint32_t* zeros)
 {
     pdl_wait();
     pdl_trigger();
+    if (zeros && blockIdx.x == 0 && threadIdx.x < kLoadZeros) zeros[threadIdx.x] = 0u;
     const int lane = threadIdx.x & 31;
     for (RunWalk at(runs); at.row < N; at.next()) {
         const int col0 = at.run * kSegment + lane;
@@ -354,24 +356,24 @@ int store_typed(const void* X, int64_t N, int64_t D, int64_t ldx, int8_t* Q, int
 }
 
 template <typename T>
-int load_typed(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int64_t D, void* Xhat, int64_t ldx, int sm_count, cudaStream_t stream)
+int load_typed(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int64_t D, void* Xhat, int64_t ldx, uint32_t* zeros, int sm_count, cudaStream_t stream)
 {
     const int d = static_cast<int>(D);
     T* x = static_cast<T*>(Xhat);
     if (reinterpret_cast<uintptr_t>(Q) % 8 == 0 && ldq % 8 == 0) {
         const int u = run_segments(N, D, sm_count), runs = static_cast<int>(ceil_div64(D, u * kSegment));
         const dim3 grid(grid_for(N * runs, sm_count, kResidentLoad));
-#define VELORA_LOAD(U) launch_chained(checkpoint_load_vec_kernel<T, U, false>, grid, kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, runs)
+#define VELORA_LOAD(U) launch_chained(checkpoint_load_vec_kernel<T, U, false>, grid, kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, runs, zeros)
         if (c_rows_vec(Xhat, ldx, sizeof(T))) return VELORA_BY_SEGMENTS(VELORA_LOAD);
 #undef VELORA_LOAD
         if constexpr (sizeof(T) == 2) {
-#define VELORA_LOAD(U) launch_chained(checkpoint_load_vec_kernel<T, U, true>, grid, kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, runs)
+#define VELORA_LOAD(U) launch_chained(checkpoint_load_vec_kernel<T, U, true>, grid, kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, runs, zeros)
             return VELORA_BY_SEGMENTS(VELORA_LOAD);
 #undef VELORA_LOAD
         }
     }
     const int runs = static_cast<int>(ceil_div64(D, kSegment));
-    return launch_chained(checkpoint_load_elem_kernel<T>, dim3(grid_for(N * runs, sm_count, kStreamCtasPerSm)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, runs);
+    return launch_chained(checkpoint_load_elem_kernel<T>, dim3(grid_for(N * runs, sm_count, kStreamCtasPerSm)), kStreamThreads, 0, stream, Q, ldq, E, lde, N, d, x, ldx, runs, zeros);
 }
 #undef VELORA_BY_SEGMENTS
 
@@ -386,13 +388,13 @@ int launch_checkpoint_store(const void* X, int x_dtype, int64_t N, int64_t D, in
                                   : store_typed<float>(X, N, D, ldx, Q, ldq, E, lde, di.sm_count, stream);
 }
 
-int launch_checkpoint_load(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int64_t D, void* Xhat, int x_dtype, int64_t ldx, cudaStream_t stream)
+int launch_checkpoint_load(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int64_t D, void* Xhat, int x_dtype, int64_t ldx, uint32_t* zeros, cudaStream_t stream)
 {
     DeviceInfo di;
     const int rc = device_info(&di);
     if (rc != VELORA_OK) return rc;
-    return x_dtype == VELORA_BF16 ? load_typed<__nv_bfloat16>(Q, ldq, E, lde, N, D, Xhat, ldx, di.sm_count, stream)
-                                  : load_typed<float>(Q, ldq, E, lde, N, D, Xhat, ldx, di.sm_count, stream);
+    return x_dtype == VELORA_BF16 ? load_typed<__nv_bfloat16>(Q, ldq, E, lde, N, D, Xhat, ldx, zeros, di.sm_count, stream)
+                                  : load_typed<float>(Q, ldq, E, lde, N, D, Xhat, ldx, zeros, di.sm_count, stream);
 }
 
 }  // namespace velora

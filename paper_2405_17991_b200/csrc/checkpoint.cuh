@@ -9,7 +9,9 @@ constexpr int kCheckpointBlock = 32;                // columns that share an exp
 constexpr uint32_t kCheckpointNaN = 255;            // exponent byte of a block that cannot be represented
 
 int launch_checkpoint_store(const void* X, int x_dtype, int64_t N, int64_t D, int64_t ldx, int8_t* Q, int64_t ldq, uint8_t* E, int64_t lde, cudaStream_t stream);
-int launch_checkpoint_load(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int64_t D, void* Xhat, int x_dtype, int64_t ldx, cudaStream_t stream);
+// zeros: NULL, or kLoadZeros words that become zero for the kernel behind it.
+constexpr int kLoadZeros = 64;
+int launch_checkpoint_load(const int8_t* Q, int64_t ldq, const uint8_t* E, int64_t lde, int64_t N, int64_t D, void* Xhat, int x_dtype, int64_t ldx, uint32_t* zeros, cudaStream_t stream);
 
 #ifdef __CUDACC__
 // E from the bits of a = max |x|.  a = m 2^k with 1 <= m < 2 is at most 127 * 2^(k - 6) where m <= 127 / 64, whose fraction's

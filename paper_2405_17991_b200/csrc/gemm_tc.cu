@@ -17,7 +17,7 @@ GemmShape gemm_shape(int64_t Mdim, int64_t Ndim, int64_t Kdim, int sm_count, boo
 {
     static const struct { int bn; double per_kblock; } kSingle[] = {{256, 0.43}, {192, 0.34}, {128, 0.28}, {64, 0.19}};
     const int64_t kblocks = ceil_div64(Kdim, BK), tiles_m = ceil_div64(Mdim, BM);
-    GemmShape best{true, 256, 1};
+    GemmShape best{true, 256, 1, 0.0};
     double best_us = static_cast<double>(ceil_div64(ceil_div64(Mdim, 256) * ceil_div64(Ndim, 256), sm_count / 2)) * (kblocks * 0.39 + 0.5) + 3.5;
     for (const auto& c : kSingle) {
         if (fused && c.bn != 256 && c.bn != 128) continue;
@@ -29,11 +29,25 @@ GemmShape gemm_shape(int64_t Mdim, int64_t Ndim, int64_t Kdim, int sm_count, boo
                               2.0 * c.bn / 256 + (s > 1 ? 2.5 + 1.5 * c.bn / 256 : 0.0);
             if (us < best_us - 0.2) {
                 best_us = us;
-                best = GemmShape{false, c.bn, s};
+                best = GemmShape{false, c.bn, s, 0.0};
             }
         }
     }
+    best.us = best_us;
     return best;
+}
+
+// Whole waves of pair tiles, the last one's parts, and what it takes to bring those together (14 us: their way through memory, and a last wave
+// that is half empty is faster than a full one).  X-hat from 8 bits and the product, us, uncut / cut: 8192 rows, 4096 x 4096: 200 / 190; 2816 x
+// 2048: 108 / 95; 2304 x 2304 (uncut in tiles of one CTA): 118 / 114; 16384 rows, 4096 x 4096: 410 / 378.  Where it is not taken: 4096 rows,
+// 4096 x 4096: 109 / 110; 2304 x 2304: 60 / 65.
+size_t gemm_tail_bytes(int64_t Mdim, int64_t Ndim, int64_t Kdim, int sm_count)
+{
+    const int64_t tiles = ceil_div64(Mdim, 256) * ceil_div64(Ndim, 256), kblocks = ceil_div64(Kdim, BK), pairs = sm_count / 2;
+    const int parts = gemm_tail_parts(tiles, kblocks, pairs);
+    if (parts < 2) return 0;
+    const double us = static_cast<double>(tiles / pairs) * (kblocks * 0.39 + 0.5) + ceil_div64(kblocks, parts) * 0.39 + 0.5 + 3.5 + 14.0;
+    return us < gemm_shape(Mdim, Ndim, Kdim, sm_count, false).us ? gemm_tail_room(tiles, parts, pairs) : 0;
 }
 
 bool tc_operand_ok(const void* p, int64_t ld_elems)
@@ -60,11 +74,11 @@ int launch_gemm_tc(int kind, const void* A, int64_t lda, const void* B, int64_t 
     int rc = device_info(&di);
     if (rc != VELORA_OK) return rc;
     GemmShape shape = gemm_shape(Mdim, Ndim, Kdim, di.sm_count, false);
-    if (more.splits > 1) return launch_gemm_tc_pair(kind, A, lda, B, ldb, C, c_dtype, ldc, beta, Mdim, Ndim, Kdim, in_dtype, status, stream, more);
+    if (more.splits > 1 || more.tail) return launch_gemm_tc_pair(kind, A, lda, B, ldb, C, c_dtype, ldc, beta, Mdim, Ndim, Kdim, in_dtype, status, stream, more);
     if (shape.pair) {
         const int prc = launch_gemm_tc_pair(kind, A, lda, B, ldb, C, c_dtype, ldc, beta, Mdim, Ndim, Kdim, in_dtype, status, stream, more);
         if (prc != VELORA_ERR_UNSUPPORTED) return prc;
-        shape = GemmShape{false, 256, 1};
+        shape = GemmShape{false, 256, 1, 0.0};
     }
     const bool a_mn = (kind == GEMM_TN_MN_MN);
     const bool b_mn = (kind != GEMM_NT_K_K);
@@ -119,7 +133,7 @@ int launch_linear_forward_tc(const void* X, int64_t ldx, const void* W, int64_t 
         if (shape.pair) {
             const int prc = launch_linear_forward_tc_pair(X, ldx, W, ldw, v, Y, ldy, Z, z_dtype, ldz, N, D, O, Dsub, status, stream);
             if (prc != VELORA_ERR_UNSUPPORTED) return prc;
-            shape = GemmShape{false, 256, 1};
+            shape = GemmShape{false, 256, 1, 0.0};
         }
         return launch_linear_forward_tc_single(shape, X, ldx, W, ldw, v, Y, ldy, Z, z_dtype, ldz, N, D, O, Dsub, status, stream);
     }

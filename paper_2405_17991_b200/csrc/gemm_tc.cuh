@@ -26,7 +26,16 @@ struct GemmMore {
     int splits = 1;
     int64_t split_stride = 0;
     int band = 4;           // row blocks whose tiles are walked together, on CTA pairs
+    // GEMM_TN_MN_MN on CTA pairs: room for the sums of a last wave whose tiles are cut over the contraction (tail_bytes), its first kTailHeader bytes
+    // zeros; NULL: no tile is cut.
+    void* tail = nullptr;
 };
+constexpr size_t kTailHeader = 256;
+// Into how many parts each tile of the last wave is cut (1: none); the room that takes.
+int gemm_tail_parts(int64_t tiles, int64_t kblocks, int64_t pairs);
+size_t gemm_tail_room(int64_t tiles, int parts, int64_t pairs);
+// Bytes of GemmMore::tail where cutting the last wave is estimated to pay, else 0.
+size_t gemm_tail_bytes(int64_t Mdim, int64_t Ndim, int64_t Kdim, int sm_count);
 
 // `status` (may be NULL) is a device word that a kernel sets to VELORA_ERR_TIMEOUT if one of its bounded
 // waits expires; nothing ever clears it but velora_workspace_init.
@@ -87,6 +96,7 @@ int make_tmap_bf16_chunks3d(CUtensorMap* map, const void* base, int64_t inner, i
 struct GemmShape {
     bool pair;
     int bn, splits;
+    double us;              // estimate
 };
 int launch_linear_forward_tc_single(const GemmShape& shape, const void* X, int64_t ldx, const void* W, int64_t ldw, const float* v,
                                     void* Y, int64_t ldy, void* Z, int z_dtype, int64_t ldz,

@@ -23,6 +23,10 @@
 // sub-token groups g with g % tiles_n == j.  These warps read X with plain 16-byte loads and share no
 // stage, no barrier and no producer work with the GEMM's pipeline (a second copy of the X tile fetched by the
 // TMA producer into a buffer of their own cost 4-9 % of the product's time).
+//
+// TAIL (GEMM_TN_MN_MN only): where the last wave of tiles leaves half of the pairs or more without one, its tiles are cut over the contraction
+// into as many parts as there are pairs for.  Each warp of the epilogue writes its part's sums, counts itself in, and the one that
+// counts in last adds all parts up in their order and stores the outputs, so nobody waits and the bits do not depend on who was last.
 #include <cooperative_groups.h>
 
 #include "gemm_fuse.cuh"
@@ -52,13 +56,16 @@ constexpr int P_STAGING_BYTES = 17 * 1024;           // behind the ring: output 
 static_assert(P_STAGING_BYTES >= 4 * kStageFloats * 4 && P_STAGING_BYTES >= 4 * kStoreBytes, "staging");
 constexpr size_t P_SMEM = 1024 + static_cast<size_t>(P_STAGES) * P_STAGE_BYTES + P_STAGING_BYTES + P_BARRIER_BYTES;
 constexpr size_t P_FUSE_SMEM = P_SMEM;
+constexpr int P_TAIL_PARTS = 8;                      // most: counted in four bits a warp
+constexpr int64_t P_TAIL_WARP = 32 * P_BN;           // sums of a warp: its rows, the pair's columns
 
-template <bool A_MN, bool B_MN, typename CT, int FUSE>
+template <bool A_MN, bool B_MN, typename CT, int FUSE, bool TAIL>
 __global__ void __launch_bounds__(FUSE ? P_FUSE_THREADS : P_THREADS, 1)
 gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                  const __grid_constant__ CUtensorMap tmC, CT* __restrict__ C, int64_t ldc, int beta, int Mdim, int Ndim, int Kdim,
-                 int all_tiles_m, int tiles_n, int c_vec, int* __restrict__ status, const GemmMore more, const FuseArgs fz)
+                 int all_tiles_m, int tiles_n, int c_vec, int* __restrict__ status, const GemmMore more, int parts, const FuseArgs fz)
 {
+    static_assert(!TAIL || (FUSE == 0 && A_MN && B_MN), "only weight gradients have a cut last wave");
     static_assert(FUSE == 0 || (!A_MN && !B_MN), "compress rides on the K-major forward GEMM only");
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
@@ -89,7 +96,19 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
     }
     const int num_tiles = tiles_m * tiles_n;
     const int kb_per_split = (kblocks + more.splits - 1) / more.splits;          // no part without k-blocks (host)
-    const int num_units = num_tiles * more.splits;           // all tiles of the first part, then of the second, ..
+    // All tiles of the first part, then of the second, ..; with TAIL the tiles of all waves but the last, then the parts of that one's.
+    const int whole = TAIL ? num_tiles - num_tiles % num_pairs : 0;
+    const int num_units = TAIL ? whole + (num_tiles - whole) * parts : num_tiles * more.splits;
+    struct Unit { int tile, part, kb0, kb1; };
+    auto unit_at = [&](int unit) -> Unit {
+        if (TAIL) {
+            if (unit < whole) return {unit, -1, 0, kblocks};
+            const int tile = (unit - whole) / parts, part = unit - whole - tile * parts, step = (kblocks + parts - 1) / parts;
+            return {whole + tile, part, part * step, min(kblocks, part * step + step)};
+        }
+        const int part = unit / num_tiles;
+        return {unit - part * num_tiles, part, part * kb_per_split, min(kblocks, part * kb_per_split + kb_per_split)};
+    };
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < P_STAGES; ++s) {
@@ -125,11 +144,11 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
             int started = 0;
             for (int unit = pair; unit < num_units && !failed; unit += num_pairs) {
                 if (FUSE) *tiles_started = ++started;          // the compress warps may take this tile's row block now
-                const int part = unit / num_tiles, kb0 = part * kb_per_split, kb1 = min(kblocks, kb0 + kb_per_split);
-                const PairTile t0 = pair_tile(unit - part * num_tiles, tiles_m, tiles_n, 2 * P_BM, P_BN, more.band);
+                const Unit u = unit_at(unit);
+                const PairTile t0 = pair_tile(u.tile, tiles_m, tiles_n, 2 * P_BM, P_BN, more.band);
                 const int m0 = t0.m0 + static_cast<int>(rank) * P_BM;
                 const int n0 = t0.n0 + static_cast<int>(rank) * (P_BN / 2);
-                for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                for (int kb = u.kb0; kb < u.kb1; ++kb, ++it) {
                     const uint32_t s = it % P_STAGES, ph = (it / P_STAGES) & 1u;
                     if (!mbar_wait(empty + 8 * s, ph ^ 1u, abort_flag)) { failed = true; break; }
                     const uint32_t lead_full = map_to_cta(full + 8 * s, 0);
@@ -177,11 +196,11 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
             uint32_t it = 0, t = 0;
             for (int unit = pair; unit < num_units && !failed; unit += num_pairs, ++t) {
                 const uint32_t acc = t & 1u, aph = (t >> 1) & 1u;
-                const int kb0 = unit / num_tiles * kb_per_split, kb1 = min(kblocks, kb0 + kb_per_split);
+                const Unit u = unit_at(unit);
                 if (!mbar_wait(tempty + 8 * acc, aph ^ 1u, abort_flag)) { failed = true; break; }
                 tc_fence_after_sync();
                 const uint32_t d_tmem = tmem_base + acc * P_BN;
-                for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                for (int kb = u.kb0; kb < u.kb1; ++kb, ++it) {
                     const uint32_t s = it % P_STAGES, ph = (it / P_STAGES) & 1u;
                     if (!mbar_wait(full + 8 * s, ph, abort_flag)) { failed = true; break; }
                     tc_fence_after_sync();
@@ -192,7 +211,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                                                  : umma_smem_desc(a_addr + j * 32, 16, 1024);
                         const uint64_t db = B_MN ? umma_smem_desc(b_addr + j * 2048, P_SLAB, 1024)
                                                  : umma_smem_desc(b_addr + j * 32, 16, 1024);
-                        umma_bf16_pair(d_tmem, da, db, idesc, kb != kb0 || j != 0);
+                        umma_bf16_pair(d_tmem, da, db, idesc, kb != u.kb0 || j != 0);
                     }
                     umma_commit_pair(empty + 8 * s);          // both CTAs may refill the stage
                 }
@@ -234,26 +253,15 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         const float alpha = more.alpha ? *more.alpha : 1.f;
         uint32_t t = 0;
         for (int unit = pair; unit < num_units && !failed; unit += num_pairs, ++t) {
-            const int part = unit / num_tiles;
-            const PairTile t0 = pair_tile(unit - part * num_tiles, tiles_m, tiles_n, 2 * P_BM, P_BN, more.band);
+            const Unit u = unit_at(unit);
+            const PairTile t0 = pair_tile(u.tile, tiles_m, tiles_n, 2 * P_BM, P_BN, more.band);
             const uint32_t acc = t & 1u, aph = (t >> 1) & 1u;
             if (!mbar_wait_warp(tfull + 8 * acc, aph, abort_flag, 256)) { failed = true; break; }
             tc_fence_after_sync();
             const int row = t0.m0 + static_cast<int>(rank) * P_BM + quarter * 32 + lane;
             const uint32_t taddr = tmem_base + acc * P_BN + (static_cast<uint32_t>(quarter * 32) << 16);
-            CT* crow = C + part * more.split_stride + static_cast<int64_t>(row) * ldc + t0.n0;
-#pragma unroll 1
-            for (int c = 0; c < P_BN / 32; c += 2) {            // 64 columns a step: two TMEM loads in flight
-                uint32_t r[2][32];
-                tmem_ld_32x32(taddr + c * 32, r[0]);
-                tmem_ld_32x32(taddr + c * 32 + 32, r[1]);
-                tmem_ld_wait();
-                if (c == P_BN / 32 - 2) {                       // accumulator fully read: hand it back
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(lead_tempty0 + 8 * acc);
-                }
-                if (more.alpha) scale_block(r, alpha);
+            CT* crow = C + (TAIL ? 0 : u.part * more.split_stride) + static_cast<int64_t>(row) * ldc + t0.n0;
+            auto put = [&](uint32_t (&r)[2][32], int c) {       // columns 32 c .. 32 c + 63 of the tile
                 const int valid = Ndim - (t0.n0 + c * 32);
                 if (sizeof(CT) == 2 && c_vec == C_TILES && (valid >= 64 || Ndim % 8 == 0)) {
                     if (row - lane < Mdim && valid > 0) store_block(&tmC, block, r, t0.n0 + c * 32, row - lane, lane);
@@ -268,6 +276,90 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                             store_rows_staged<CT>(crow - static_cast<int64_t>(lane) * ldc + (c + h) * 32, ldc, Mdim - (row - lane), valid - 32 * h,
                                                   r[h], beta, reinterpret_cast<float*>(staging) + quarter * kStageFloats, lane);
                 }
+            };
+            auto sums_of = [&](uint32_t (&r)[2][32], int c) {
+                tmem_ld_32x32(taddr + c * 32, r[0]);
+                tmem_ld_32x32(taddr + c * 32 + 32, r[1]);
+                tmem_ld_wait();
+            };
+            if (TAIL && u.part >= 0) {                          // the pair's last unit: the accumulator is not handed back
+                const int who = static_cast<int>(rank) * 4 + quarter;
+                uint32_t* count = static_cast<uint32_t*>(more.tail) + (u.tile - whole);
+                // This warp's sums of the tile's parts, one part behind another, four sums of a lane together.
+                float4* sums = reinterpret_cast<float4*>(static_cast<char*>(more.tail) + kTailHeader) +
+                               ((static_cast<int64_t>(u.tile - whole) * 8 + who) * parts * P_TAIL_WARP) / 4 + lane;
+                auto all_but_this = [&](uint32_t word) { return static_cast<int>(word >> (4 * who) & 15u) == parts - 1; };
+                uint32_t word = 0;
+                if (lane == 0) word = *static_cast<volatile uint32_t*>(count);
+                bool last = all_but_this(__shfl_sync(0xffffffffu, word, 0));
+                if (!last) {
+#pragma unroll 1
+                    for (int c = 0; c < P_BN / 32; c += 2) {
+                        uint32_t r[2][32];
+                        sums_of(r, c);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            sums[u.part * (P_TAIL_WARP / 4) + (c * 8 + i) * 32] =
+                                make_float4(__uint_as_float(r[i / 8][4 * (i % 8)]), __uint_as_float(r[i / 8][4 * (i % 8) + 1]),
+                                            __uint_as_float(r[i / 8][4 * (i % 8) + 2]), __uint_as_float(r[i / 8][4 * (i % 8) + 3]));
+                    }
+                    __threadfence();
+                    __syncwarp();
+                    if (lane == 0) word = atomicAdd(count, 1u << (4 * who));
+                    last = all_but_this(__shfl_sync(0xffffffffu, word, 0));
+                }
+                if (!last) continue;
+                __threadfence();
+#pragma unroll 1
+                for (int c = 0; c < P_BN / 32; c += 2) {
+                    uint32_t own[2][32], r[2][32];
+                    float4 x[16];
+                    int p = u.part == 0 ? 1 : 0;                // the first of the others; they are loaded one ahead
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = __ldcg(sums + p * (P_TAIL_WARP / 4) + (c * 8 + i) * 32);
+                    sums_of(own, c);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) r[h][i] = u.part == 0 ? own[h][i] : 0u;
+                    for (; p < parts; ++p) {
+                        if (p == u.part) {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) r[h][i] = __float_as_uint(__uint_as_float(r[h][i]) + __uint_as_float(own[h][i]));
+                            continue;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            uint32_t* y = &r[i / 8][4 * (i % 8)];
+                            y[0] = __float_as_uint(__uint_as_float(y[0]) + x[i].x);
+                            y[1] = __float_as_uint(__uint_as_float(y[1]) + x[i].y);
+                            y[2] = __float_as_uint(__uint_as_float(y[2]) + x[i].z);
+                            y[3] = __float_as_uint(__uint_as_float(y[3]) + x[i].w);
+                        }
+                        const int next = p + 1 == u.part ? p + 2 : p + 1;
+                        if (next < parts) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) x[i] = __ldcg(sums + next * (P_TAIL_WARP / 4) + (c * 8 + i) * 32);
+                        }
+                    }
+                    if (more.alpha) scale_block(r, alpha);
+                    put(r, c);
+                }
+                continue;
+            }
+#pragma unroll 1
+            for (int c = 0; c < P_BN / 32; c += 2) {            // 64 columns a step: two TMEM loads in flight
+                uint32_t r[2][32];
+                sums_of(r, c);
+                if (c == P_BN / 32 - 2) {                       // accumulator fully read: hand it back
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(lead_tempty0 + 8 * acc);
+                }
+                if (more.alpha) scale_block(r, alpha);
+                put(r, c);
             }
         }
         if (sizeof(CT) == 2 && c_vec == C_TILES && lane == 0) bulk_wait_all();
@@ -285,7 +377,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
     }
 }
 
-template <bool A_MN, bool B_MN, typename CT, int FUSE = 0>
+template <bool A_MN, bool B_MN, typename CT, int FUSE = 0, bool TAIL = false>
 int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, void* C, int64_t ldc, int beta,
                 int Mdim, int Ndim, int Kdim, int* status, int sm_count, cudaStream_t stream,
                 const FuseArgs fz = FuseArgs{}, const GemmMore& more = GemmMore{})
@@ -294,7 +386,7 @@ int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, void* C, int64_t l
     static DeviceOnce configured;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return VELORA_ERR_CUDA;
-    auto kern = gemm_pair_kernel<A_MN, B_MN, CT, FUSE>;
+    auto kern = gemm_pair_kernel<A_MN, B_MN, CT, FUSE, TAIL>;
     if (!configured.get(dev)) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes)) != cudaSuccess)
             return VELORA_ERR_CUDA;
@@ -304,6 +396,7 @@ int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, void* C, int64_t l
     const int64_t units = static_cast<int64_t>(tiles_m) * tiles_n * more.splits;
     int pairs = sm_count / 2;
     if (units < pairs) pairs = static_cast<int>(units);
+    const int parts = TAIL ? gemm_tail_parts(units, ceil_div64(Kdim, P_BK), pairs) : 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs), 1, 1);
     cfg.blockDim = dim3(FUSE ? P_FUSE_THREADS : P_THREADS, 1, 1);
@@ -319,7 +412,7 @@ int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, void* C, int64_t l
     int c_vec = c_rows_vec(C, ldc, sizeof(CT)) ? C_VECTORS : C_ELEMENTS;
     CUtensorMap tc = ta;
     if (sizeof(CT) == 2 && c_vec && !beta && more.splits == 1 && tc_operand_ok(C, ldc) && make_tmap_bf16_2d(&tc, C, Ndim, Mdim, ldc, 64, 32) == VELORA_OK) c_vec = C_TILES;
-    if (cudaLaunchKernelEx(&cfg, kern, ta, tb, tc, static_cast<CT*>(C), ldc, beta, Mdim, Ndim, Kdim, tiles_m, tiles_n, c_vec, status, more, fz) !=
+    if (cudaLaunchKernelEx(&cfg, kern, ta, tb, tc, static_cast<CT*>(C), ldc, beta, Mdim, Ndim, Kdim, tiles_m, tiles_n, c_vec, status, more, parts, fz) !=
         cudaSuccess) {
         cudaGetLastError();
         return VELORA_ERR_CUDA;
@@ -358,9 +451,23 @@ int launch_gemm_tc_pair(int kind, const void* A, int64_t lda, const void* B, int
                : launch_pair<AMN, BMN, float>(ta, tb, C, ldc, beta, m, n, k, status, di.sm_count, stream, FuseArgs{}, more)
     if (!a_mn && !b_mn) { VELORA_PAIR_CASE(false, false); }
     if (!a_mn && b_mn) { VELORA_PAIR_CASE(false, true); }
+    if (more.tail)
+        return c_dtype == VELORA_BF16
+                   ? launch_pair<true, true, __nv_bfloat16, 0, true>(ta, tb, C, ldc, beta, m, n, k, status, di.sm_count, stream, FuseArgs{}, more)
+                   : launch_pair<true, true, float, 0, true>(ta, tb, C, ldc, beta, m, n, k, status, di.sm_count, stream, FuseArgs{}, more);
     VELORA_PAIR_CASE(true, true);
 #undef VELORA_PAIR_CASE
 }
+
+int gemm_tail_parts(int64_t tiles, int64_t kblocks, int64_t pairs)
+{
+    const int64_t rest = pairs < 1 ? 0 : tiles % pairs;
+    if (tiles < pairs || rest == 0 || rest > static_cast<int64_t>(kTailHeader / 4)) return 1;
+    const int64_t parts = pairs / rest < P_TAIL_PARTS ? pairs / rest : P_TAIL_PARTS;
+    return static_cast<int>(ceil_div64(kblocks, ceil_div64(kblocks, parts)));              // none without k-blocks
+}
+
+size_t gemm_tail_room(int64_t tiles, int parts, int64_t pairs) { return kTailHeader + static_cast<size_t>(tiles % pairs * parts * 8 * P_TAIL_WARP * 4); }
 
 // Forward of the layer with compress fused in (see the kernel's header); returns VELORA_ERR_UNSUPPORTED
 // without launching when the device cannot hold the kernel's shared memory.

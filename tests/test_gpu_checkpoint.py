@@ -247,3 +247,34 @@ def test_weight_grad_refuses_a_workspace_without_room(vl):
     Q, E = vl.velora_checkpoint_store(X)
     with pytest.raises(vl.VeloraError):
         vl.velora_checkpoint_weight_grad(dY, Q, E, ws=vl.velora_workspace_alloc(256, DEV))
+
+
+@pytest.mark.parametrize("dw_dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N,D,O,padded", [(8200, 2304, 2304, True), (8200, 2303, 2305, False), (9001, 4096, 1300, True)])
+def test_weight_grad_whose_last_wave_is_cut(vl, guard, N, D, O, padded, dw_dtype):
+    """Tiles of 256 x 256 on 74 pairs: 81, 90, 96, so the last wave's 7, 16 or 22 are cut into 8, 4 or 3 parts of the contraction.  Whatever
+    stands in the workspace, twice the same bits, beta = 1, and the uncut product of a workspace without the room."""
+    X, dY = finite_inputs(N, D, O, torch.bfloat16, N + D + O)
+    Q, E = vl.velora_checkpoint_store(X)
+    ref = dY.double().t() @ vl.velora_checkpoint_load(Q, E, x_dtype=torch.float32).double()
+    size = vl.velora_workspace_bytes(vl.OP_CHECKPOINT_WEIGHT_GRAD, N, D, O, 1, not padded)
+    assert size > 256 + 2 * N * (D + 7) + (0 if padded else 2 * N * (O + 7)) + (10 << 20)
+    got = []
+    for fill in (0, 255):
+        ws = guard.workspace(vl, size)
+        ws[256:] = fill
+        dW = guard.mat(O, D, dw_dtype, ld=None if padded else D)
+        vl.velora_checkpoint_weight_grad(dY, Q, E, dW, ws=ws)
+        assert_matches(dW, ref.cpu().numpy(), TOL_GEMM, "dW", c=C_SUM)
+        vl.velora_checkpoint_weight_grad(dY, Q, E, dW, ws=ws)
+        assert vl.velora_workspace_status(ws) == 0
+        got.append(dW.clone())
+    assert torch.equal(got[0], got[1])
+    start = torch.randn((O, D), device=DEV).to(dw_dtype)
+    dW = guard.mat(O, D, dw_dtype, init=start)
+    vl.velora_checkpoint_weight_grad(dY, Q, E, dW, beta=1)
+    assert_matches(dW, (ref + start.double()).cpu().numpy(), TOL_GEMM, "dW, beta = 1", c=C_SUM)
+    less = guard.workspace(vl, size - 256)
+    dW = guard.mat(O, D, dw_dtype)
+    vl.velora_checkpoint_weight_grad(dY, Q, E, dW, ws=less)
+    assert_matches(dW, ref.cpu().numpy(), TOL_GEMM, "dW, uncut", c=C_SUM)
