@@ -407,7 +407,8 @@ int velora_checkpoint_weight_grad(const void* dY, int dy_dtype, int64_t N, int64
  *     G[n, v] = dloss[n] (exp(l[n, v] - lse[n]) - [v = target[n]]),   dX = G W,   dW = beta * dW + G^T X
  * (dX == NULL or dW == NULL: skipped).  `dtype`: X, W and dX; loss, lse, dloss: fp32 [N], dense; target: int64 [N], dense.  Logits,
  * their maxima and sums and the sums of dX and dW are fp32; where X and W are bf16, G is rounded to bf16 once for more than 64 tokens
- * and kept as two bf16 numbers for fewer.
+ * and kept as two bf16 numbers for fewer.  lse is rounded to fp32, so a token whose loss is small beside 2^-24 lse has a gradient
+ * of that relative error; both passes add bf16 logits up in the same order, also where the backward pass takes a slice of the tokens.
  *   - A token with target < 0 (padding, a prompt) has no part in it: loss, lse and its row of dX are 0, and nothing of its row of X,
  *     NaN or infinity included, nor its lse and dloss, reaches dW.  Such tokens cost no products.
  *   - A target >= V is no column: the token's loss is NaN, it has no part in the gradients, and the workspace's status

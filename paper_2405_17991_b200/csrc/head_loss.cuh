@@ -57,6 +57,10 @@ constexpr int kHeadFewHeight = 64;                  // least height of its tiles
 int head_few_height(int64_t cols);                  // columns of the vocabulary in a tile: a row of `running` each
 int launch_head_few(const void* x, int64_t ldx, const void* W, int64_t ldw, void* G, int64_t ldg, int twice, const HeadTile& h, int* status, cudaStream_t stream);
 
+// k-blocks of 64 whose products an accumulator of the tensor cores adds up; segments are added in registers, rounded to nearest.  The same for both
+// kernels and both passes: G's 1 - p of a token that the head is sure of has no other source than logits equal to those in lse.
+constexpr int kHeadSegment = 8;
+
 #ifdef __CUDACC__
 constexpr float kHeadLog2e = 1.4426950408889634f;
 constexpr float kHeadLost = 0x1p-8f;                // rounding of a maximum times log2 e that a first-order term makes up for (to 4e-6 of the sum)

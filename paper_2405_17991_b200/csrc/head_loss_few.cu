@@ -5,7 +5,7 @@
 //
 // Per CTA: warp 0 lane 0 TMA producer, warp 1 lane 0 MMA issuer, warps 2..5 epilogue (32 columns of the vocabulary each).  A lane of the
 // epilogue has one column for all tokens; 32 x 32 blocks are turned over through shared memory, and then it has one token for 32
-// columns.  Contractions are cut into segments as in head_loss_tc.cu, of 512 here (of 128: 61 us).  1 x 4096 of 32000: the call 54 us, W
+// columns.  Contractions are cut into segments as in head_loss_tc.cu (of 128 instead of 512: 61 us).  1 x 4096 of 32000: the call 54 us, W
 // alone at the copy rate 41 (87 us with the tokens as rows of 256).
 #include "gemm_tc.cuh"
 #include "head_loss.cuh"
@@ -19,7 +19,6 @@ namespace {
 
 constexpr int W_BM = 128;                  // columns of the vocabulary in a tile
 constexpr int W_BK = 64;
-constexpr int W_SEGMENT = 8;               // k-blocks that an accumulator adds up
 constexpr int W_THREADS = 192;
 constexpr int W_PITCH = 33;
 constexpr int W_STAGING_BYTES = 4 * 32 * W_PITCH * 4;
@@ -63,7 +62,6 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int num_tiles = (h.cols + height - 1) / height, kblocks = (h.D + W_BK - 1) / W_BK;
-    const int segment = GRADIENT ? kblocks : W_SEGMENT;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) {
@@ -123,12 +121,12 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
             constexpr uint32_t idesc = umma_idesc_bf16(W_BM, NT, false, false);
             uint32_t it = 0, seg = 0;
             for (int tile = blockIdx.x; tile < num_tiles && !failed; tile += gridDim.x) {
-                for (int k0 = 0; k0 < kblocks && !failed; k0 += segment, ++seg) {
+                for (int k0 = 0; k0 < kblocks && !failed; k0 += kHeadSegment, ++seg) {
                     const uint32_t acc = seg & 1u, aph = (seg >> 1) & 1u;
                     if (!mbar_wait(tempty + 8 * acc, aph ^ 1u, abort_flag)) { failed = true; break; }
                     tc_fence_after_sync();
                     const uint32_t d_tmem = tmem_base + acc * NT;
-                    const int k1 = min(kblocks, k0 + segment);
+                    const int k1 = min(kblocks, k0 + kHeadSegment);
                     for (int kb = k0; kb < k1; ++kb, ++it) {
                         const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1u;
                         if (!mbar_wait(full + 8 * s, ph, abort_flag)) { failed = true; break; }
@@ -155,7 +153,7 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
             for (int c = 0; c < NT / 32; ++c)
 #pragma unroll
                 for (int i = 0; i < 32; ++i) l[c][i] = 0u;
-            for (int k0 = 0; k0 < kblocks; k0 += segment, ++seg) {
+            for (int k0 = 0; k0 < kblocks; k0 += kHeadSegment, ++seg) {
                 const uint32_t acc = seg & 1u, aph = (seg >> 1) & 1u;
                 if (!mbar_wait_warp(tfull + 8 * acc, aph, abort_flag, 64)) { failed = true; *abort_flag = 1; break; }
                 tc_fence_after_sync();

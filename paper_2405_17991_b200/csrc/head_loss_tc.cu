@@ -3,11 +3,13 @@
 //   HEAD_GRADIENT  G[n, v] = g[n] (exp(l[n, v] - lse[n]) - [v = t[n]]) in bf16
 // l = X W^T, bf16 operands K-major, 256 x 256 logits a pair (tcgen05 cta_group::2; the pipeline is that of gemm_tc2.cu).
 //
-// The tensor cores add with truncation, 16 products at a time: over D = 4096 that shrinks a logit by some 5e-6 of itself, and a loss with
-// it (1.5e-6 against 64 bits for 4096 tokens of 32000 columns; fp32 multiply-adds: 3.1e-7).  So for the statistics a tile's contraction
-// is cut into segments of 1024, each into an accumulator of its own (two, alternating), and the epilogue adds the segments up in registers,
-// rounded to nearest: eight warps with 128 sums a thread (3.5e-7; segments of 2048: 7.3e-7).  The next segment's products run meanwhile;
-// 8192 x 4096 of 32000: 1615 us, 1577 in one segment.  The gradient's logits take one: what they lose is below G's rounding.
+// The tensor cores add with truncation, 16 products at a time: over D = 4096 that shrinks a logit by some 5e-6 of itself.  So a tile's
+// contraction is cut into segments of 512 (kHeadSegment), each into an accumulator of its own (two, alternating), and the epilogue adds the segments
+// up in registers, rounded to nearest: eight warps with 128 sums a thread.  The next segment's products run meanwhile.  Error of the loss
+// in norm, 8192 x 4096 of 32000 columns: 7.1e-8 (segments of 1024: 1.3e-7).  Both passes do it: G = g (exp(l - lse) - 1) of a target whose share is
+// near one has what its l and the l in lse differ by divided by 1 - p (one accumulator in the backward pass alone, D = 4096: rows of dX off by 1.4e-2 in
+// the median at a loss of 1e-3 to 1e-2, by 0.3 below; now 1.9e-3 and 3.7e-3, the latter by lse's rounding to fp32).  8192 x 4096 of 32000, forward and
+// backward: 1467 + 5130 us, 1418 + 5040 with segments of 1024 and one accumulator.
 //
 // Bound by the power limit and by what the operands' way from L2 costs of it: the same launch in bands of 4 row blocks 1728 us, 8: 1643, 16: 1615 (W
 // crosses HBM twice, X stays in L2), 32: 1689.
@@ -31,7 +33,6 @@ namespace {
 constexpr int H_BM = 128;                  // rows per CTA (256 per pair)
 constexpr int H_BN = 256;                  // columns per pair; half of them staged by each CTA
 constexpr int H_BK = 64;
-constexpr int H_SEGMENT = 16;              // k-blocks that an accumulator adds up for the statistics
 constexpr int H_BAND = 16;                 // row blocks that are walked together
 constexpr int H_STAGES = 6;
 constexpr int H_A_BYTES = H_BM * H_BK * 2;
@@ -67,7 +68,6 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int kblocks = (h.D + H_BK - 1) / H_BK;
-    const int segment = ROLE == HEAD_STATS ? H_SEGMENT : kblocks;
     const int live = *h.live;
     const int tiles_m = (live + 2 * H_BM - 1) / (2 * H_BM);          // rows without a target are not computed
     const int tiles_n = (h.cols + H_BN - 1) / H_BN;
@@ -140,12 +140,12 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
             constexpr uint32_t idesc = umma_idesc_bf16(2 * H_BM, H_BN, false, false);
             uint32_t it = 0, seg = 0;
             for (int tile = pair; tile < num_tiles && !failed; tile += num_pairs) {
-                for (int k0 = 0; k0 < kblocks && !failed; k0 += segment, ++seg) {
+                for (int k0 = 0; k0 < kblocks && !failed; k0 += kHeadSegment, ++seg) {
                     const uint32_t acc = seg & 1u, aph = (seg >> 1) & 1u;
                     if (!mbar_wait(tempty + 8 * acc, aph ^ 1u, abort_flag)) { failed = true; break; }
                     tc_fence_after_sync();
                     const uint32_t d_tmem = tmem_base + acc * H_BN;
-                    const int k1 = min(kblocks, k0 + segment);
+                    const int k1 = min(kblocks, k0 + kHeadSegment);
                     for (int kb = k0; kb < k1; ++kb, ++it) {
                         const uint32_t s = it % H_STAGES, ph = (it / H_STAGES) & 1u;
                         if (!mbar_wait(full + 8 * s, ph, abort_flag)) { failed = true; break; }
@@ -173,27 +173,25 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
             const int row0 = t0.m0 + static_cast<int>(rank) * H_BM + quarter * 32, row = row0 + lane;
             const int col0 = t0.n0 + half * 128, valid = h.cols - col0;
             uint32_t l[4][32];                               // fp32 bits
-            if (ROLE == HEAD_STATS) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) l[c][i] = 0u;
-            }
-            for (int k0 = 0; k0 < kblocks; k0 += segment, ++seg) {
+            for (int k0 = 0; k0 < kblocks; k0 += kHeadSegment, ++seg) {
                 const uint32_t acc = seg & 1u, aph = (seg >> 1) & 1u;
                 if (!mbar_wait_warp(tfull + 8 * acc, aph, abort_flag, 256)) { failed = true; break; }
                 tc_fence_after_sync();
                 const uint32_t taddr = tmem_base + acc * H_BN + half * 128 + (static_cast<uint32_t>(quarter * 32) << 16);
-                if (ROLE == HEAD_STATS) {
+                if (k0 > 0) {                                // 16 columns a step: the sums leave few registers
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t r[32];
-                        tmem_ld_32x32(taddr + c * 32, r);
+                    for (int c = 0; c < 16; c += 2) {
+                        uint32_t r[2][8];
+                        tmem_ld_32x8(taddr + c * 8, r[0]);
+                        tmem_ld_32x8(taddr + c * 8 + 8, r[1]);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(__uint_as_float(l[c][i]) + __uint_as_float(r[i]));
+                        for (int i = 0; i < 16; ++i) {
+                            uint32_t& y = l[c / 4][c % 4 * 8 + i];
+                            y = __float_as_uint(__uint_as_float(y) + __uint_as_float(r[i / 8][i % 8]));
+                        }
                     }
-                } else {                                     // one segment
+                } else {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_ld_32x32(taddr + c * 32, l[c]);
                     tmem_ld_wait();
