@@ -372,17 +372,14 @@ head_stats_kernel(float* logits, int64_t ld, int parts, int64_t part_stride, int
         if (lane == 0) part[0][warp] = m;
         __syncthreads();
         for (int w = 0; w < kRowThreads / 32; ++w) m = fmaxf(m, part[0][w]);
-        float before = 0.f;
-        if (!first) {
-            const float2 old = running[row];
-            const float both = fmaxf(m, old.x);
-            before = old.y * expf(old.x - both);
-            m = both;
-            hit = at_target[row];
-        }
+        const float2 old = first ? make_float2(-INFINITY, 0.f) : running[row];
+        if (!first) hit = at_target[row];
+        m = fmaxf(m, old.x);
+        const float ref = m == -INFINITY ? 0.f : m;                  // nothing but minus infinities so far: their sum is 0
+        const float before = old.y * expf(old.x - ref);
         float s = 0.f;
 #pragma unroll 4
-        for (int c = threadIdx.x; c < cols; c += kRowThreads) s += expf(l[c] - m);
+        for (int c = threadIdx.x; c < cols; c += kRowThreads) s += expf(l[c] - ref);
         s = warp_sum(s);
         if (lane == 0) part[1][warp] = s;
         __syncthreads();
