@@ -289,6 +289,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                 float4* sums = reinterpret_cast<float4*>(static_cast<char*>(more.tail) + kTailHeader) +
                                ((static_cast<int64_t>(u.tile - whole) * 8 + who) * parts * P_TAIL_WARP) / 4 + lane;
                 auto all_but_this = [&](uint32_t word) { return static_cast<int>(word >> (4 * who) & 15u) == parts - 1; };
+                // Lane 0 reads and counts for the warp: its fences stand between the warp's accesses (ordered by __syncwarp) and the count's.
                 uint32_t word = 0;
                 if (lane == 0) word = *static_cast<volatile uint32_t*>(count);
                 bool last = all_but_this(__shfl_sync(0xffffffffu, word, 0));
@@ -303,13 +304,16 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                                 make_float4(__uint_as_float(r[i / 8][4 * (i % 8)]), __uint_as_float(r[i / 8][4 * (i % 8) + 1]),
                                             __uint_as_float(r[i / 8][4 * (i % 8) + 2]), __uint_as_float(r[i / 8][4 * (i % 8) + 3]));
                     }
-                    __threadfence();
                     __syncwarp();
-                    if (lane == 0) word = atomicAdd(count, 1u << (4 * who));
+                    if (lane == 0) {
+                        __threadfence();
+                        word = atomicAdd(count, 1u << (4 * who));
+                    }
                     last = all_but_this(__shfl_sync(0xffffffffu, word, 0));
                 }
                 if (!last) continue;
-                __threadfence();
+                if (lane == 0) __threadfence();
+                __syncwarp();
 #pragma unroll 1
                 for (int c = 0; c < P_BN / 32; c += 2) {
                     uint32_t own[2][32], r[2][32];
