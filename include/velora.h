@@ -95,7 +95,7 @@ typedef enum {
     VELORA_OP_CHECKPOINT_WEIGHT_GRAD = 8,
     VELORA_OP_HEAD_LOSS = 9,              /* O: the vocabulary; Dsub is not used (1) */
     VELORA_OP_HEAD_LOSS_BACKWARD = 10,    /* the same */
-    /* added to one of these three: operands in fp32 */
+    /* added to one of these three: operands in fp32 (0 bytes with the others, which have one size for both types) */
     VELORA_OP_F32 = 512,
     /* added to one of the layer's, the explicit gradient's or the last three: with room for copies of operands on odd rows */
     VELORA_OP_ANY_ROWS = 256

@@ -284,8 +284,9 @@ size_t velora_workspace_bytes(int op, int64_t N, int64_t D, int64_t O, int Dsub)
 {
     if (N < 0 || D < 1 || Dsub < 1 || Dsub > D || Dsub > VELORA_MAX_DSUB) return 0;
     const bool any_rows = (op & VELORA_OP_ANY_ROWS) != 0;
-    const int dtype = (op & VELORA_OP_F32) != 0 ? VELORA_F32 : VELORA_BF16;
-    switch (op & ~(VELORA_OP_ANY_ROWS | VELORA_OP_F32)) {
+    const int dtype = (op & VELORA_OP_F32) != 0 ? VELORA_F32 : VELORA_BF16, plain = op & ~(VELORA_OP_ANY_ROWS | VELORA_OP_F32);
+    if (dtype == VELORA_F32 && plain < VELORA_OP_CHECKPOINT_WEIGHT_GRAD) return 0;       // those have one size for both types
+    switch (plain) {
         case VELORA_OP_INIT_V: return init_v_workspace_bytes(Dsub);
         case VELORA_OP_WEIGHT_GRAD_FACTORED: return O < 1 ? 0 : factored_bytes(N, D, O, Dsub, true);
         case VELORA_OP_LINEAR_BACKWARD_FACTORED:
