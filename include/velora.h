@@ -120,6 +120,7 @@ const char* velora_status_string(int status);
  * With op | VELORA_OP_ANY_ROWS the figure includes, where D or O is no multiple of 8, room for aligned copies of the
  * bf16 operands of that width (X and W of the forward, dY and W of the backward): worth it for rows that are not
  * 16-byte aligned, which run on the CUDA cores without it, and for nothing else (padded rows and fp32 never use it).
+ * The checkpoint gradient's dY and the head's W have that room at any width, since a view of any width may start on an odd boundary.
  */
 size_t velora_workspace_bytes(int op, int64_t N, int64_t D, int64_t O, int Dsub);
 

@@ -191,7 +191,8 @@ def velora_status_string(status: int) -> str:
 
 def velora_workspace_bytes(op: int, N: int, D: int, O: int, Dsub: int, any_rows: bool = True) -> int:
     """Bytes that ``op`` needs.  ``any_rows``: with room for aligned copies of bf16 operands where D or O is no multiple of 8 and
-    the rows may lie as torch.empty leaves them, without padding; False where they are padded to 16 bytes, or fp32."""
+    the rows may lie as torch.empty leaves them, without padding (of the checkpoint gradient's dY and the head's W at any width); False
+    where they are padded to 16 bytes, or fp32."""
     return int(lib().velora_workspace_bytes(op | OP_ANY_ROWS if any_rows else op, N, D, O, Dsub))
 
 

@@ -297,7 +297,7 @@ size_t velora_workspace_bytes(int op, int64_t N, int64_t D, int64_t O, int Dsub)
         case VELORA_OP_UPDATE_V: return update_v_workspace_bytes(Dsub);
         case VELORA_OP_Z8_CALIBRATE: return z8_calibrate_workspace_bytes(N, D, Dsub);
         case VELORA_OP_CHECKPOINT_WEIGHT_GRAD:
-            return O < 1 ? 0 : checkpoint_grad_bytes(N, D, dtype) + pack_bytes_if_ragged(N, O, any_rows && dtype == VELORA_BF16) +
+            return O < 1 ? 0 : checkpoint_grad_bytes(N, D, dtype) + (any_rows && dtype == VELORA_BF16 && packable(N, O) ? align256(pack_rows_bytes(N, O)) : 0) +
                                    (dtype == VELORA_BF16 ? gemm_tail_bytes(O, D, N, 148) : 0);
         case VELORA_OP_HEAD_LOSS: return O < 1 ? 0 : head_loss_bytes(false, dtype, N, D, O, any_rows);
         case VELORA_OP_HEAD_LOSS_BACKWARD: return O < 1 ? 0 : head_loss_bytes(true, dtype, N, D, O, any_rows);

@@ -28,3 +28,11 @@ def test_fp32_flag_where_it_belongs(b, name):
     size, op = b.lib().velora_workspace_bytes, getattr(b, name)
     assert size(op | b.OP_F32, 300, 64, 40, 1) > 256
     assert size(op | 1024, 300, 64, 40, 1) == 0
+
+
+@pytest.mark.parametrize("O", [40, 2056, 45])
+def test_room_for_any_rows_of_the_checkpoint_gradient(b, O):
+    """A bf16 dY may be a view on odd boundaries whatever its width: with the flag there is room for its packed copy, N rows of O rounded up to 8."""
+    size, op, N, D = b.lib().velora_workspace_bytes, b.OP_CHECKPOINT_WEIGHT_GRAD, 300, 64
+    assert size(op | b.OP_ANY_ROWS, N, D, O, 1) - size(op, N, D, O, 1) >= 2 * N * (-(-O // 8) * 8)
+    assert size(op | b.OP_F32 | b.OP_ANY_ROWS, N, D, O, 1) == size(op | b.OP_F32, N, D, O, 1)
