@@ -140,8 +140,27 @@ def _stream(stream) -> int:
     return _raw_stream(_raw_device())
 
 
-def velora_workspace_alloc(nbytes: int, device) -> torch.Tensor:
-    """Device workspace of at least ``nbytes`` with its status header zeroed."""
+def _lend(t: torch.Tensor) -> None:
+    """The current stream may still read ``t``, which belongs to another, when it is let go."""
+    t.record_stream(torch.cuda.current_stream(t.device))
+
+
+def _on(stream, call, *args):
+    """``call``, which has something to allocate, with ``stream`` as the current stream.  The allocator gives memory that was let go to whoever asks next on
+    the same stream, so what a call makes for itself (its workspace is let go when it returns, its kernels run later) has to belong to theirs."""
+    with torch.cuda.stream(stream):
+        out = call(*args)
+    for t in out if isinstance(out, tuple) else (out,):
+        if t is not None:
+            _lend(t)
+    return out
+
+
+def velora_workspace_alloc(nbytes: int, device, stream=None) -> torch.Tensor:
+    """Device workspace of at least ``nbytes`` with its status header zeroed, for calls on ``stream`` (the current one)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return velora_workspace_alloc(nbytes, device)
     ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
     velora_workspace_init(ws)
     return ws
@@ -202,6 +221,8 @@ def _odd_rows(t: torch.Tensor, ptr: int, ld: int) -> bool:
 
 def velora_init_v(X: torch.Tensor, Dsub: int, v: Optional[torch.Tensor] = None,
                   ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    if stream is not None and (v is None or ws is None):
+        return _on(stream, velora_init_v, X, Dsub, v, ws)
     xp, ldx = _mat(X, "X")
     N, D = X.shape
     if v is None:
@@ -229,6 +250,8 @@ def velora_init_v_static(X: torch.Tensor, Dsub: int, v: torch.Tensor, stream=Non
 
 def velora_compress(X: torch.Tensor, v: torch.Tensor, Z: Optional[torch.Tensor] = None,
                     z_dtype=torch.float32, stream=None) -> torch.Tensor:
+    if stream is not None and Z is None:
+        return _on(stream, velora_compress, X, v, Z, z_dtype)
     xp, ldx = _mat(X, "X")
     N, D = X.shape
     Dsub = v.shape[0]
@@ -242,6 +265,8 @@ def velora_compress(X: torch.Tensor, v: torch.Tensor, Z: Optional[torch.Tensor] 
 
 def velora_reconstruct(Z: torch.Tensor, v: torch.Tensor, D: int, Xhat: Optional[torch.Tensor] = None,
                        x_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    if stream is not None and Xhat is None:
+        return _on(stream, velora_reconstruct, Z, v, D, Xhat, x_dtype)
     zp, ldz = _mat(Z, "Z")
     N = Z.shape[0]
     Dsub = v.shape[0]
@@ -256,6 +281,8 @@ def velora_reconstruct(Z: torch.Tensor, v: torch.Tensor, D: int, Xhat: Optional[
 def velora_weight_grad(dY: torch.Tensor, Z: torch.Tensor, v: torch.Tensor, D: int,
                        dW: Optional[torch.Tensor] = None, dw_dtype=None, beta: int = 0, mode: int = WG_FACTORED,
                        ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    if stream is not None and (dW is None or ws is None):
+        return _on(stream, velora_weight_grad, dY, Z, v, D, dW, dw_dtype, beta, mode, ws)
     yp, lddy = _mat(dY, "dY")
     zp, ldz = _mat(Z, "Z")
     N, O = dY.shape
@@ -276,6 +303,8 @@ def velora_weight_grad(dY: torch.Tensor, Z: torch.Tensor, v: torch.Tensor, D: in
 def velora_linear_forward(X: torch.Tensor, W: torch.Tensor, v: torch.Tensor,
                           Y: Optional[torch.Tensor] = None, Z: Optional[torch.Tensor] = None,
                           z_dtype=torch.float32, ws: Optional[torch.Tensor] = None, stream=None):
+    if stream is not None and (Y is None or Z is None or ws is None):
+        return _on(stream, velora_linear_forward, X, W, v, Y, Z, z_dtype, ws)
     xp, ldx = _mat(X, "X")
     wp, ldw = _mat(W, "W")
     N, D = X.shape
@@ -303,6 +332,8 @@ def velora_linear_backward(dY: torch.Tensor, W: torch.Tensor, Z: torch.Tensor, v
                            dX: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None,
                            need_dX: bool = True, need_dW: bool = True, dw_dtype=None, beta: int = 0,
                            mode: int = WG_FACTORED, ws: Optional[torch.Tensor] = None, stream=None):
+    if stream is not None and (ws is None or (need_dX and dX is None) or (need_dW and dW is None)):
+        return _on(stream, velora_linear_backward, dY, W, Z, v, dX, dW, need_dX, need_dW, dw_dtype, beta, mode, ws)
     yp, lddy = _mat(dY, "dY")
     wp, ldw = _mat(W, "W")
     zp, ldz = _mat(Z, "Z")
@@ -330,6 +361,8 @@ def velora_linear_backward(dY: torch.Tensor, W: torch.Tensor, Z: torch.Tensor, v
 def velora_dense_product(kind: int, A: torch.Tensor, B: torch.Tensor, C: Optional[torch.Tensor] = None,
                          c_dtype=None, beta: int = 0, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """C = beta * C + op(A) op(B): the plain products of the layer (PRODUCT_A_BT, PRODUCT_A_B, PRODUCT_AT_B)."""
+    if stream is not None and (C is None or ws is None):
+        return _on(stream, velora_dense_product, kind, A, B, C, c_dtype, beta, ws)
     ap, lda = _mat(A, "A")
     bp, ldb = _mat(B, "B")
     Mdim, Kdim = (A.shape[1], A.shape[0]) if kind == PRODUCT_AT_B else (A.shape[0], A.shape[1])
@@ -350,6 +383,8 @@ def velora_dense_product(kind: int, A: torch.Tensor, B: torch.Tensor, C: Optiona
 def velora_z8_calibrate(X: torch.Tensor, v: torch.Tensor, headroom: float = 2.0, ws: Optional[torch.Tensor] = None,
                         stream=None):
     """Scale of the 8-bit Z store from a batch: returns (zscale[1], v_store = v / zscale, v_load = v * zscale)."""
+    if stream is not None:
+        return _on(stream, velora_z8_calibrate, X, v, headroom, ws)
     xp, ldx = _mat(X, "X")
     N, D = X.shape
     Dsub = v.shape[0]
@@ -401,6 +436,8 @@ def velora_linear_step_host(hX: torch.Tensor, hdY: torch.Tensor, W: torch.Tensor
 def velora_subtoken_sum(X: torch.Tensor, Dsub: int, s: Optional[torch.Tensor] = None,
                         ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Un-normalised sub-token sum of this rank's shard (add the ranks' sums, then velora_normalize_v)."""
+    if stream is not None and (s is None or ws is None):
+        return _on(stream, velora_subtoken_sum, X, Dsub, s, ws)
     N, D = X.shape
     xp, ldx = (_mat(X, "X") if N > 0 else (None, D))
     if s is None:
@@ -416,6 +453,8 @@ def velora_subtoken_sum(X: torch.Tensor, Dsub: int, s: Optional[torch.Tensor] = 
 def velora_update_v(X: torch.Tensor, Dsub: int, rho: float, a: torch.Tensor, v: torch.Tensor,
                     ws: Optional[torch.Tensor] = None, stream=None) -> None:
     """Running-average variant: a <- (1 - rho) a + rho * (mean sub-token of X), v <- a / ||a||, in place, no sync."""
+    if stream is not None and ws is None:
+        return _on(stream, velora_update_v, X, Dsub, rho, a, v, ws)
     xp, ldx = _mat(X, "X")
     N, D = X.shape
     if ws is None:
@@ -427,6 +466,8 @@ def velora_update_v(X: torch.Tensor, Dsub: int, rho: float, a: torch.Tensor, v: 
 
 def velora_normalize_v(s: torch.Tensor, v: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
                        stream=None) -> torch.Tensor:
+    if stream is not None and (v is None or ws is None):
+        return _on(stream, velora_normalize_v, s, v, ws)
     Dsub = s.shape[0]
     if v is None:
         v = torch.empty_like(s)
@@ -440,6 +481,8 @@ def velora_normalize_v(s: torch.Tensor, v: Optional[torch.Tensor] = None, ws: Op
 def velora_weight_grad_p(dY: torch.Tensor, Z: torch.Tensor, D: int, Dsub: int, P: Optional[torch.Tensor] = None,
                          beta: int = 0, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """P[O, M] = beta * P + dY^T Z in fp32: the weight gradient before its expansion by v."""
+    if stream is not None and (P is None or ws is None):
+        return _on(stream, velora_weight_grad_p, dY, Z, D, Dsub, P, beta, ws)
     N, O = dY.shape
     M = num_subtokens(D, Dsub)
     yp, lddy = (_mat(dY, "dY") if N > 0 else (None, O))
@@ -458,6 +501,8 @@ def velora_weight_grad_p(dY: torch.Tensor, Z: torch.Tensor, D: int, Dsub: int, P
 def velora_expand_p(P: torch.Tensor, v: torch.Tensor, D: int, dW: Optional[torch.Tensor] = None,
                     dw_dtype=torch.bfloat16, beta: int = 0, stream=None) -> torch.Tensor:
     """dW[o, m*Dsub + j] = beta * dW + P[o, m] v[j]."""
+    if stream is not None and dW is None:
+        return _on(stream, velora_expand_p, P, v, D, dW, dw_dtype, beta)
     O = P.shape[0]
     Dsub = v.shape[0]
     pp, ldp = _mat(P, "P")
@@ -491,6 +536,8 @@ def _codes(Q: torch.Tensor, E: torch.Tensor):
 def velora_checkpoint_store(X: torch.Tensor, Q: Optional[torch.Tensor] = None, E: Optional[torch.Tensor] = None, stream=None):
     """X in 8 bits: codes Q (int8 [N, D]) and block exponents E (uint8 [N, ceil(D / 32)]).  Rows of those allocated here start on
     16-byte boundaries, where velora_checkpoint_weight_grad is fastest."""
+    if stream is not None and Q is None:
+        return _on(stream, velora_checkpoint_store, X, Q, E)
     xp, ldx = _mat(X, "X")
     N, D = X.shape
     blocks = -(-D // CHECKPOINT_BLOCK)
@@ -511,6 +558,8 @@ def velora_checkpoint_store(X: torch.Tensor, Q: Optional[torch.Tensor] = None, E
 
 def velora_checkpoint_load(Q: torch.Tensor, E: torch.Tensor, Xhat: Optional[torch.Tensor] = None,
                            x_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    if stream is not None and Xhat is None:
+        return _on(stream, velora_checkpoint_load, Q, E, Xhat, x_dtype)
     qp, ldq, ep, lde = _codes(Q, E)
     N, D = Q.shape
     if Xhat is None:
@@ -529,6 +578,8 @@ def velora_checkpoint_load(Q: torch.Tensor, E: torch.Tensor, Xhat: Optional[torc
 def velora_checkpoint_weight_grad(dY: torch.Tensor, Q: torch.Tensor, E: torch.Tensor, dW: Optional[torch.Tensor] = None,
                                   dw_dtype=None, beta: int = 0, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """dW = beta * dW + dY^T Xhat with the input kept in 8 bits (velora_checkpoint_store)."""
+    if stream is not None and (dW is None or ws is None):
+        return _on(stream, velora_checkpoint_weight_grad, dY, Q, E, dW, dw_dtype, beta, ws)
     yp, lddy = _mat(dY, "dY")
     qp, ldq, ep, lde = _codes(Q, E)
     N, O = dY.shape
@@ -573,6 +624,8 @@ def velora_head_loss(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, los
                      lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
     """Cross entropy of every token under the linear head W, without the logits: (loss, lse), both fp32 [N].  Tokens with
     target < 0 have none."""
+    if stream is not None and (loss is None or lse is None or ws is None):
+        return _on(stream, velora_head_loss, X, W, target, loss, lse, ws)
     xp, ldx, wp, ldw = _head(X, W)
     N, D = X.shape
     V = W.shape[0]
@@ -594,6 +647,8 @@ def velora_head_loss_backward(X: torch.Tensor, W: torch.Tensor, target: torch.Te
                               dX: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None, need_dX: bool = True,
                               need_dW: bool = True, dw_dtype=None, beta: int = 0, ws: Optional[torch.Tensor] = None, stream=None):
     """(dX, dW) of velora_head_loss, given the gradient of every token's loss and the lse it returned."""
+    if stream is not None and (ws is None or (need_dX and dX is None) or (need_dW and dW is None)):
+        return _on(stream, velora_head_loss_backward, X, W, target, lse, dloss, dX, dW, need_dX, need_dW, dw_dtype, beta, ws)
     xp, ldx, wp, ldw = _head(X, W)
     N, D = X.shape
     V = W.shape[0]
