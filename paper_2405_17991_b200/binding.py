@@ -522,6 +522,14 @@ def _here(*tensors) -> None:
             raise ValueError("tensors must be on the current device (%s), got one on %s" % (current, t.device))
 
 
+def _room(ws: torch.Tensor):
+    """Address and size of a workspace."""
+    _here(ws)
+    if not ws.is_contiguous():
+        raise ValueError("a workspace must be contiguous")
+    return ws.data_ptr(), ws.numel()
+
+
 def _codes(Q: torch.Tensor, E: torch.Tensor):
     if Q.dtype != torch.int8 or E.dtype != torch.uint8:
         raise ValueError("Q must be int8 and E uint8")
@@ -598,7 +606,7 @@ def velora_checkpoint_weight_grad(dY: torch.Tensor, Q: torch.Tensor, E: torch.Te
         op = OP_CHECKPOINT_WEIGHT_GRAD | (OP_F32 if dY.dtype == torch.float32 else 0)
         ws = velora_workspace_alloc(velora_workspace_bytes(op, N, D, O, 1, _odd_rows(dY, yp, lddy)), dY.device)
     rc = lib().velora_checkpoint_weight_grad(yp, _dt(dY), N, O, lddy, qp, ldq, ep, lde, D, wp, _dt(dW), lddw, beta,
-                                             ws.data_ptr(), ws.numel(), _stream(stream))
+                                             *_room(ws), _stream(stream))
     _check(rc, "velora_checkpoint_weight_grad")
     return dW
 
@@ -638,7 +646,7 @@ def velora_head_loss(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, los
     _here(X, W, target, loss, lse)
     if ws is None:
         ws = _head_workspace(OP_HEAD_LOSS, X, W, wp, ldw)
-    rc = lib().velora_head_loss(xp, ldx, wp, ldw, tp, lp, sp, _dt(X), N, D, V, ws.data_ptr(), ws.numel(), _stream(stream))
+    rc = lib().velora_head_loss(xp, ldx, wp, ldw, tp, lp, sp, _dt(X), N, D, V, *_room(ws), _stream(stream))
     _check(rc, "velora_head_loss")
     return loss, lse
 
@@ -667,6 +675,6 @@ def velora_head_loss_backward(X: torch.Tensor, W: torch.Tensor, target: torch.Te
     if ws is None:
         ws = _head_workspace(OP_HEAD_LOSS_BACKWARD, X, W, wp, ldw)
     rc = lib().velora_head_loss_backward(xp, ldx, wp, ldw, tp, sp, gp, dxp, lddx, dwp, _dt(dW) if need_dW else F32, lddw, beta,
-                                         _dt(X), N, D, V, ws.data_ptr(), ws.numel(), _stream(stream))
+                                         _dt(X), N, D, V, *_room(ws), _stream(stream))
     _check(rc, "velora_head_loss_backward")
     return dX, dW
