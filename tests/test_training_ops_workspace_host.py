@@ -9,11 +9,14 @@ def b(monkeypatch):
 
     class Library:
         def __getattr__(self, name):
-            raise AssertionError("reached %s" % name)
+            def call(*args):
+                raise AssertionError("reached %s" % name)
+            return call
 
     monkeypatch.setattr(binding, "lib", lambda: Library())
     monkeypatch.setattr(binding, "_mat", lambda t, name: (t.data_ptr(), t.stride(0)))
     monkeypatch.setattr(binding, "_tokens", lambda t, n, dtype, name: t.data_ptr())
+    monkeypatch.setattr(binding, "_stream", lambda s: 0)
     monkeypatch.setattr(binding, "_raw_device", lambda: 0)
     monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
     return binding
