@@ -100,3 +100,16 @@ def test_backward_pass_of_a_slice_of_the_tokens(vl, step, dtype):
         ref = SureReference(X[s], W, t[s], dloss[s], n, dtype == torch.bfloat16)
         dX, _ = vl.velora_head_loss_backward(X[s], W, t[s], lse[s].contiguous(), dloss[s].contiguous(), need_dW=False)
         check_rows(dX, ref.dX, ref.dX_bound, "dX")
+
+
+@pytest.mark.parametrize("D", [64, 500, 576, 4096])
+def test_every_kernel_forms_the_same_logits(vl, D):
+    """With one column lse is the logit itself, so its bits are to be seen: the kernel for more than 128 tokens, those for up to 128, 64 and 32."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(D)
+    N = 1200
+    X, W = torch.randn((N, D), generator=g, device=DEV).bfloat16(), torch.randn((1, D), generator=g, device=DEV).bfloat16()
+    t = torch.zeros(N, dtype=torch.int64, device=DEV)
+    whole = vl.velora_head_loss(X, W, t)[1]
+    for step in (200, 100, 60, 30, 1):
+        assert torch.equal(torch.cat([vl.velora_head_loss(X[i:i + step], W, t[i:i + step])[1] for i in range(0, N, step)]), whole)
