@@ -408,16 +408,19 @@ int velora_checkpoint_weight_grad(const void* dY, int dy_dtype, int64_t N, int64
  *     G[n, v] = dloss[n] (exp(l[n, v] - lse[n]) - [v = target[n]]),   dX = G W,   dW = beta * dW + G^T X
  * (dX == NULL or dW == NULL: skipped).  `dtype`: X, W and dX; loss, lse, dloss: fp32 [N], dense; target: int64 [N], dense.  Logits,
  * their maxima and sums and the sums of dX and dW are fp32; where X and W are bf16, G is rounded to bf16 once for more than 64 tokens
- * and kept as two bf16 numbers for fewer.  lse is rounded to fp32, so a token whose loss is small beside 2^-24 lse has a gradient
- * of that relative error; both passes add bf16 logits up in the same order, also where the backward pass takes a slice of the tokens.
+ * and kept as two bf16 numbers for fewer.  Both passes add a bf16 logit up in the same order, also where the backward
+ * pass takes a slice of the forward pass's tokens.  What is left is lse's rounding to fp32: G[n, target[n]] is off by some 2^-24 |lse[n]| dloss[n], which
+ * counts for a token whose loss is as small as that.
  *   - A token with target < 0 (padding, a prompt) has no part in it: loss, lse and its row of dX are 0, and nothing of its row of X,
- *     NaN or infinity included, nor its lse and dloss, reaches dW.  Such tokens cost no products.
+ *     NaN or infinity included, nor its lse and dloss, reaches dW.  Such tokens cost no products where they
+ *     make up whole tiles of 256 (bf16, more than 128 tokens, sizes that run on CTA pairs); elsewhere zeros are multiplied for them.
  *   - A target >= V is no column: the token's loss is NaN, it has no part in the gradients, and the workspace's status
  *     word says VELORA_ERR_INVALID_ARG (velora_workspace_status) until velora_workspace_init.
  *   - N == 0: the loss writes nothing, the backward pass dW = beta * dW.
  * ws: velora_workspace_bytes(VELORA_OP_HEAD_LOSS or VELORA_OP_HEAD_LOSS_BACKWARD, N, D, V, 1) bytes (| VELORA_OP_F32 for fp32,
  * | VELORA_OP_ANY_ROWS for bf16 rows of W that are not 16-byte aligned), initialised.  It holds a piece of the vocabulary of the logits or
- * their gradients; a call also runs in less, in smaller pieces (of 256 columns at least), and the order of dX's sums goes by them.
+ * their gradients: 128 MB, or what 1024 columns take where that is more (all columns where there are fewer), in several parts for fp32 and
+ * few tokens; a call also runs in less, in smaller pieces (of 256 columns at least), and the order of dX's sums goes by them.
  */
 int velora_head_loss(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* target, float* loss, float* lse,
                      int dtype, int64_t N, int64_t D, int64_t V, void* ws, size_t ws_bytes, void* stream);

@@ -357,7 +357,9 @@ int launch_gemm_simt_parts(const SimtParts& shape, const float* A, int64_t a_sm,
     const int c_vec = aligned16(C) && ldc % 4 == 0 && part_stride % 4 == 0;
     const dim3 grid(static_cast<unsigned>(ceil_div64(Ndim, shape.cols)), static_cast<unsigned>(ceil_div64(Mdim, shape.rows)), static_cast<unsigned>(shape.parts));
     const int64_t k_per_part = ceil_div64(ceil_div64(Kdim, 32), shape.parts) * 32;             // whole slices of every tile
-#define VELORA_PARTS(GM, GN)                                                                                                                  launch_chained(gemm_simt_kernel<GM, GN, float, float, float, true>, grid, SG_THREADS, 0, stream, A, a_sm, a_sk, a_mode, B, b_sn, b_sk,                    b_mode, C, ldc, beta, c_vec, Mdim, Ndim, Kdim, k_per_part, part_stride)
+#define VELORA_PARTS(GM, GN)                                                                                                                \
+    launch_chained(gemm_simt_kernel<GM, GN, float, float, float, true>, grid, SG_THREADS, 0, stream, A, a_sm, a_sk, a_mode, B, b_sn, b_sk, \
+                   b_mode, C, ldc, beta, c_vec, Mdim, Ndim, Kdim, k_per_part, part_stride)
     return shape.rows == 128 ? VELORA_PARTS(2, 2) : (shape.cols == 128 ? VELORA_PARTS(1, 2) : VELORA_PARTS(1, 1));
 #undef VELORA_PARTS
 }

@@ -38,8 +38,8 @@ GemmShape gemm_shape(int64_t Mdim, int64_t Ndim, int64_t Kdim, int sm_count, boo
 }
 
 // Whole waves of pair tiles, the last one's parts, and what it takes to bring those together (14 us: their way through memory, and a last wave
-// that is half empty is faster than a full one).  X-hat from 8 bits and the product, us, uncut / cut: 8192 rows, 4096 x 4096: 200 / 190; 2816 x
-// 2048: 108 / 95; 2304 x 2304 (uncut in tiles of one CTA): 118 / 114; 16384 rows, 4096 x 4096: 410 / 378.  Where it is not taken: 4096 rows,
+// that is half empty is faster than a full one).  X-hat from 8 bits and the product, us, uncut / cut: 8192 rows, 4096 x 4096: 201 / 196; 2816 x
+// 2048: 114 / 98; 2304 x 2304 (uncut in tiles of one CTA): 101 / 89; 16384 rows, 4096 x 4096: 449 / 403.  Where it is not taken: 4096 rows,
 // 4096 x 4096: 109 / 110; 2304 x 2304: 60 / 65.
 size_t gemm_tail_bytes(int64_t Mdim, int64_t Ndim, int64_t Kdim, int sm_count)
 {

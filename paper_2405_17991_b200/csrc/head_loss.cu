@@ -13,13 +13,14 @@ namespace velora {
 namespace {
 
 constexpr int kRowThreads = 256;
-constexpr int64_t kPieceElements = 1 << 26;         // logits that exist at a time where the workspace has the room: 128 MB in bf16 (fp32: half as many)
-constexpr int kBand = 8;                            // of the gradients' products: the operands are larger than L2 (backward pass of 8192 x 4096 of 32000: 5.38 ms in bands of 4, 5.26)
+// Logits that exist at a time where the workspace has the room: 128 MB in bf16 (fp32: half as many), but never fewer than 1024 columns of them.
+constexpr int64_t kPieceElements = 1 << 26;
+// Of the gradients' products: the operands are larger than L2 (backward pass of 8192 x 4096 of 32000: 5.38 ms in bands of 4, 5.26 in bands of 8).
+constexpr int kBand = 8;
 constexpr int kPieceStep = 256;                     // pieces are multiples of this
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 int64_t round_up(int64_t x, int64_t to) { return ceil_div64(x, to) * to; }
-
 
 // Pieces of equal width, as few as fit the room but for up to two more where those fill the last wave of tiles better.  What a piece
 // costs, in k-blocks of 256 x 256 tiles on 74 pairs: its products, and the sums of dX that each but the first reads and writes (about 9 k-blocks
@@ -53,8 +54,6 @@ int gradient_rows(int dtype, int64_t N) { return dtype == VELORA_BF16 && N <= 64
 // Bytes of a token and column of the piece, one part.
 size_t piece_element(int dtype, bool backward, int64_t N) { return dtype == VELORA_BF16 && backward ? 2 * static_cast<size_t>(gradient_rows(dtype, N)) : 4; }
 
-// Parts of the contraction that dX's products are cut into, where its tiles are few: waves of units on 74 pairs, each its k-blocks and about
-// 4 more for its sums' way.
 // fp32 products of few tiles are cut into parts on the CUDA cores where that is estimated to be faster than either form of the whole
 // product: 64 x 768 of 1000, whose four products took 51 us of its 59 in clusters.
 int fp32_parts(int64_t M, int64_t N, int64_t K)
@@ -64,6 +63,8 @@ int fp32_parts(int64_t M, int64_t N, int64_t K)
     return p.parts > 1 && p.us < 0.9 * gemm_f32_us(M, N, K, 148) ? p.parts : 1;
 }
 
+// Parts of the contraction that dX's products are cut into, where its tiles are few: waves of units on 74 pairs, each its k-blocks and about
+// 4 more for its sums' way.
 int gradient_splits(int dtype, int64_t N, int64_t D, int64_t V)
 {
     if (dtype != VELORA_BF16) return fp32_parts(N, D, piece_width(N, D, V, room_wanted(dtype, N, V)));
@@ -592,7 +593,8 @@ int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
                  : launch_head_tiles(a.ws + l.x, l.ldx, W, ldw, nullptr, 0, h, status, a.stream);
         if (rc != VELORA_OK) return rc;
         return launch_chained(head_merge_kernel, dim3(static_cast<unsigned>(ceil_div64(a.N, 32))), kRowThreads, 0, a.stream, h.running,
-                              static_cast<int>(ceil_div64(a.V, few ? head_few_height(a.V) : 128)), n, h.live, reinterpret_cast<int*>(a.ws + l.order), h.target, h.at_target, loss, lse);
+                              static_cast<int>(ceil_div64(a.V, few ? head_few_height(a.V) : 128)), n, h.live,
+                              reinterpret_cast<int*>(a.ws + l.order), h.target, h.at_target, loss, lse);
     }
     float* piece = reinterpret_cast<float*>(a.ws + l.piece);
     for (int64_t v0 = 0; v0 < a.V; v0 += l.piece_cols) {
@@ -600,7 +602,8 @@ int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
         const int64_t part_stride = a.N * l.piece_cols;
         const int parts = fp32_logits(a, l, W + static_cast<size_t>(v0) * ldw * 4, ldw, cols, &rc);
         if (rc != VELORA_OK) return rc;
-        rc = launch_chained(head_stats_kernel, dim3(static_cast<unsigned>(a.N)), kRowThreads, 0, a.stream, piece, l.piece_cols, parts, part_stride, static_cast<int>(cols), static_cast<int>(v0),
+        rc = launch_chained(head_stats_kernel, dim3(static_cast<unsigned>(a.N)), kRowThreads, 0, a.stream, piece, l.piece_cols, parts,
+                            part_stride, static_cast<int>(cols), static_cast<int>(v0),
                             reinterpret_cast<int*>(a.ws + l.live), reinterpret_cast<int*>(a.ws + l.order), reinterpret_cast<int*>(a.ws + l.target),
                             reinterpret_cast<float*>(a.ws + l.at_target), reinterpret_cast<float2*>(a.ws + l.running), v0 == 0 ? 1 : 0,
                             v0 + cols == a.V ? 1 : 0, loss, lse);
@@ -619,9 +622,9 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
     int64_t ldw;
     rc = head_weights(a, l, &W, &ldw);
     if (rc != VELORA_OK) return rc;
-    // In bf16 the logits' gradients are rounded once (more than 64 tokens), for the tensor cores: by half a step each.  A mean's 1 / count in all of them would be the same
-    // rounding again and again, which does not average out (relative error of dX and dW up to 4e-3 by the count alone); so the largest dloss
-    // is taken out and multiplied back in fp32, wherever the product that writes dW takes a factor.
+    // In bf16 the logits' gradients are rounded once (more than 64 tokens), for the tensor cores: by half a step each.  A mean's 1 / count in
+    // all of them would be the same rounding again and again, which does not average out (relative error of dX and dW up to 4e-3 by the
+    // count alone); so the largest dloss is taken out and multiplied back in fp32, wherever the product that writes dW takes a factor.
     const bool take_common = a.dtype == VELORA_BF16 && (!dW || dw_dtype == VELORA_BF16 || c_rows_vec(dW, lddw, sizeof(float)));
     rc = launch_rows(a, l, lse, dloss, take_common);
     if (rc != VELORA_OK) return rc;
@@ -643,7 +646,8 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
             if (rc != VELORA_OK) return rc;
             const int64_t blocks = ceil_div64(cols, 128 * (kRowThreads / 32));
             rc = launch_chained(head_gradient_kernel, dim3(static_cast<unsigned>(a.N), static_cast<unsigned>(blocks < 16 ? blocks : 16)), kRowThreads,
-                                0, a.stream, reinterpret_cast<float*>(G), l.piece_cols, parts, a.N * l.piece_cols, static_cast<int>(cols), static_cast<int>(v0), reinterpret_cast<int*>(a.ws + l.target), reinterpret_cast<float*>(a.ws + l.scale),
+                                0, a.stream, reinterpret_cast<float*>(G), l.piece_cols, parts, a.N * l.piece_cols, static_cast<int>(cols),
+                                static_cast<int>(v0), reinterpret_cast<int*>(a.ws + l.target), reinterpret_cast<float*>(a.ws + l.scale),
                                 reinterpret_cast<float*>(a.ws + l.lse));
         }
         if (rc != VELORA_OK) return rc;

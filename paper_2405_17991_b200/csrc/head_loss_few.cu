@@ -1,7 +1,8 @@
 // The logits of a linear head for few tokens (up to 128), used up where they come out of the tensor cores; roles and results as in
 // head_loss_tc.cu.  What bounds it is reading W once, so W's rows are the rows of the products: tiles of up to 128 columns of the vocabulary,
 // as high as shares the vocabulary out most evenly (32000: 112, 224 columns for a CTA that has two), the tokens (rounded up to 32, 64 or
-// 128) are the other side, and no tensor-core time goes into rows that are not there.  Single CTAs with up to 200 KB of W in flight each.
+// 128) are the other side, and no tensor-core time goes into rows that are not there.  Single CTAs with 160 KB of W in flight each (128 for more than
+// 32 tokens, 96 for more than 64).
 //
 // Per CTA: warp 0 lane 0 TMA producer, warp 1 lane 0 MMA issuer, warps 2..5 epilogue (32 columns of the vocabulary each).  A lane of the
 // epilogue has one column for all tokens; 32 x 32 blocks are turned over through shared memory, and then it has one token for 32

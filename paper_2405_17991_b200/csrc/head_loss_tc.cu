@@ -9,10 +9,10 @@
 // in norm, 8192 x 4096 of 32000 columns: 7.1e-8 (segments of 1024: 1.3e-7).  Both passes do it: G = g (exp(l - lse) - 1) of a target whose share is
 // near one has what its l and the l in lse differ by divided by 1 - p (one accumulator in the backward pass alone, D = 4096: rows of dX off by 1.4e-2 in
 // the median at a loss of 1e-3 to 1e-2, by 0.3 below; now 1.9e-3 and 3.7e-3, the latter by lse's rounding to fp32).  8192 x 4096 of 32000, forward and
-// backward: 1467 + 5130 us, 1418 + 5040 with segments of 1024 and one accumulator.
+// backward: 1470 to 1520 + 5130 to 5310 us, 1420 to 1470 + 5040 to 5230 with segments of 1024 and one accumulator.
 //
-// Bound by the power limit and by what the operands' way from L2 costs of it: the same launch in bands of 4 row blocks 1728 us, 8: 1643, 16: 1615 (W
-// crosses HBM twice, X stays in L2), 32: 1689.
+// Bound by the power limit and by what the operands' way from L2 costs of it: the statistics of 8192 x 4096 of 32000 (with segments of
+// 1024) in bands of 4 row blocks 1728 us, 8: 1643, 16: 1615 (W crosses HBM twice, X stays in L2), 32: 1689.
 //
 // Roles per CTA (320 threads): warp 0 lane 0 TMA producer, warp 1 lane 0 MMA issuer (leader only), warps 2..9 epilogue: TMEM lanes
 // 32 * (w % 4) .., columns 128 * (w >= 6) ...  Barriers as in gemm_tc2.cu.  Every wait is bounded; both CTAs reach the closing
