@@ -409,7 +409,7 @@ int velora_checkpoint_weight_grad(const void* dY, int dy_dtype, int64_t N, int64
  * (dX == NULL or dW == NULL: skipped).  `dtype`: X, W and dX; loss, lse, dloss: fp32 [N], dense; target: int64 [N], dense.  Logits,
  * their maxima and sums and the sums of dX and dW are fp32; where X and W are bf16, G is rounded to bf16 once for more than 64 tokens
  * and kept as two bf16 numbers for fewer.  Both passes add a bf16 logit up in the same order, also where the backward
- * pass takes a slice of the forward pass's tokens.  What is left is lse's rounding to fp32: G[n, target[n]] is off by some 2^-24 |lse[n]| dloss[n], which
+ * pass takes a slice of the forward pass's tokens (an fp32 one as the number of tokens and the room say: equal to fp32 rounding).  What is left is lse's rounding to fp32: G[n, target[n]] is off by some 2^-24 |lse[n]| dloss[n], which
  * counts for a token whose loss is as small as that.
  *   - A token with target < 0 (padding, a prompt) has no part in it: loss, lse and its row of dX are 0, and nothing of its row of X,
  *     NaN or infinity included, nor its lse and dloss, reaches dW.  Such tokens cost no products where they
