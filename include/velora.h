@@ -95,9 +95,12 @@ typedef enum {
     VELORA_OP_CHECKPOINT_WEIGHT_GRAD = 8,
     VELORA_OP_HEAD_LOSS = 9,              /* O: the vocabulary; Dsub is not used (1) */
     VELORA_OP_HEAD_LOSS_BACKWARD = 10,    /* the same */
-    /* added to one of these three: operands in fp32 (0 bytes with the others, which have one size for both types) */
+    VELORA_OP_HEAD_DISTILL = 11,          /* O: the vocabulary; Dsub: K, the entries of a token */
+    VELORA_OP_HEAD_DISTILL_BACKWARD = 12, /* the same */
+    VELORA_OP_LAYER_NORM_BACKWARD = 13,   /* O and Dsub are not used (1) */
+    /* added to one of these six: operands in fp32 (0 bytes with the others, which have one size for both types) */
     VELORA_OP_F32 = 512,
-    /* added to one of the layer's, the explicit gradient's or the last three: with room for copies of operands on odd rows */
+    /* added to one of the layer's, the explicit gradient's, the checkpoint's or the head's: with room for copies of operands on odd rows */
     VELORA_OP_ANY_ROWS = 256
 } velora_op;
 
@@ -132,7 +135,7 @@ size_t velora_workspace_bytes(int op, int64_t N, int64_t D, int64_t O, int Dsub)
  * allocating a workspace.  velora_workspace_status synchronises `stream`, reads the flag and returns
  * VELORA_OK or VELORA_ERR_TIMEOUT; outputs of a call that raised the flag are undefined.  (The two other
  * values are VELORA_ERR_DEGENERATE_V, which velora_update_v leaves there instead of synchronising, and
- * VELORA_ERR_INVALID_ARG, left by velora_head_loss and its backward pass for a target that is no column of W.)
+ * VELORA_ERR_INVALID_ARG, left by velora_head_loss, velora_head_distill and their backward passes for a target or an entry that is no column of W.)
  * The paper has no counterpart: this is run-time hygiene of the implementation.
  */
 int velora_workspace_init(void* ws, size_t ws_bytes, void* stream);
@@ -427,6 +430,58 @@ int velora_head_loss(const void* X, int64_t ldx, const void* W, int64_t ldw, con
 int velora_head_loss_backward(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* target,
                               const float* lse, const float* dloss, void* dX, int64_t lddx, void* dW, int dw_dtype, int64_t lddw, int beta,
                               int dtype, int64_t N, int64_t D, int64_t V, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Distillation: the same head, taught by a teacher's top logits instead of one target.  A teacher (a larger model, run beforehand) leaves for every token
+ * K columns index[n, k] of the vocabulary and its logits there, teacher[n, k].  With the temperature T,
+ *     l[n, v] = sum_d X[n, d] W[v, d] / T,      lse[n] = log sum_v exp l[n, v],
+ *     p[n, k] = exp(teacher[n, k] / T - s[n]),  s[n] = log sum_k exp(teacher[n, k] / T), or teacher_lse[n] where that is not NULL
+ *     loss[n] = sum_k p[n, k] (log p[n, k] - l[n, index[n, k]] + lse[n])
+ * which is the divergence of the student from the teacher's K likeliest columns; with teacher_lse, the log sum of exp(logit / T) over the teacher's whole
+ * vocabulary, they keep their true shares, which then add up to less than one.  Backward pass, given dloss[n] and the lse that the forward pass returned:
+ *     G[n, v] = dloss[n] / T (exp(l[n, v] - lse[n]) sum_k p[n, k] - sum_{k: index[n, k] = v} p[n, k]),   dX = G W,   dW = beta * dW + G^T X
+ * (the T^2 that is often put in front of such a loss belongs into dloss).  Neither pass has a gradient for the teacher.  Nothing of [N, V] exists.
+ * index: int64 [N, K], ldi; teacher: fp32 or bf16 (t_dtype) [N, K], ldt; teacher_lse: fp32 [N], dense, or NULL; 1 <= K <= VELORA_DISTILL_MAX_K; T finite,
+ * above 0 (1 / T finite, too).  The other arguments, their types, sums and roundings as in velora_head_loss.
+ *   - An entry with index < 0 is none: lists may be shorter than K.  The same column twice counts twice.  A logit of minus infinity has no share.
+ *   - A token with no entry, or whose logits are all minus infinity, has no part in it, as a token without a target in velora_head_loss.
+ *   - An index >= V is no column: the token's loss is NaN, it has no part in the gradients, and the workspace's status
+ *     word says VELORA_ERR_INVALID_ARG (velora_workspace_status) until velora_workspace_init.
+ *   - A NaN or plus infinity among a token's logits makes its loss and gradients NaN, as one in X does.
+ *   - N == 0: the loss writes nothing, the backward pass dW = beta * dW.
+ * ws: velora_workspace_bytes(VELORA_OP_HEAD_DISTILL or VELORA_OP_HEAD_DISTILL_BACKWARD, N, D, V, K) bytes, flags as in velora_head_loss; besides that
+ * operation's, it holds the lists in the order of their columns (8 bytes an entry, in the forward pass 12) and 2 bytes a token and 128 columns.
+ */
+#define VELORA_DISTILL_MAX_K 1024
+int velora_head_distill(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* index, int64_t ldi,
+                        const void* teacher, int t_dtype, int64_t ldt, const float* teacher_lse, float temperature, int K, float* loss, float* lse,
+                        int dtype, int64_t N, int64_t D, int64_t V, void* ws, size_t ws_bytes, void* stream);
+int velora_head_distill_backward(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* index, int64_t ldi,
+                                 const void* teacher, int t_dtype, int64_t ldt, const float* teacher_lse, float temperature, int K,
+                                 const float* lse, const float* dloss, void* dX, int64_t lddx, void* dW, int dw_dtype, int64_t lddw, int beta,
+                                 int dtype, int64_t N, int64_t D, int64_t V, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Layer norm of the rows in front of a layer, with the residual added on the way, and its gradients:
+ *     H = X + R, rounded to the rows' type (R == NULL: H = X),   m[n] = mean_d H,   r[n] = 1 / sqrt(mean_d (H - m)^2 + eps)
+ *     Y = (H - m) r weight + bias        (weight == NULL: ones; bias == NULL: zeros)
+ * Backward pass, given the gradients dY of Y and, where H is handed on to another layer, dH of H (NULL: none), xhat = (H - m) r, c = dY weight:
+ *     dX = dH + r (c - mean_d c - xhat mean_d (c xhat)),    dweight = beta * dweight + sum_n dY xhat,    dbias = beta * dbias + sum_n dY
+ * dX is the gradient of X and of R.  (dX, dweight or dbias NULL: skipped.)  beta is 0 or 1.
+ * `dtype` (bf16 or f32): X, R, H, Y, dY, dH, dX, [N, D] with pitches of their own; p_dtype: weight and bias, dw_dtype: dweight and dbias, [D], dense.
+ * mean, rstd: fp32 [N], m and r for the backward pass (velora_layer_norm: NULL where there is none; H may be NULL, too).  eps >= 0, finite.
+ * Statistics, sums and products are fp32, every output is rounded once; the variance is taken about the mean; sums have a fixed order.  Squares of H - m
+ * must stay in fp32's range; an infinity or a NaN makes its row NaN.
+ * H or Y may lie where X or R does, dX where dY, dH or H does (the same address and pitch; nothing else may overlap).
+ * ws of the backward pass: velora_workspace_bytes(VELORA_OP_LAYER_NORM_BACKWARD, N, D, 1, 1) bytes, for dweight and dbias (NULL without both).
+ * N == 0: nothing is written, but dweight = beta * dweight, dbias = beta * dbias.
+ */
+int velora_layer_norm(const void* X, int64_t ldx, const void* R, int64_t ldr, const void* weight, const void* bias, int p_dtype, float eps,
+                      void* H, int64_t ldh, void* Y, int64_t ldy, float* mean, float* rstd, int dtype, int64_t N, int64_t D, void* stream);
+int velora_layer_norm_backward(const void* dY, int64_t lddy, const void* H, int64_t ldh, const float* mean, const float* rstd,
+                               const void* weight, int p_dtype, const void* dH, int64_t lddh, void* dX, int64_t lddx,
+                               void* dweight, void* dbias, int dw_dtype, int beta,
+                               int dtype, int64_t N, int64_t D, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

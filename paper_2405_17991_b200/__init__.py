@@ -18,5 +18,7 @@ from .binding import (  # noqa: F401
     velora_host_step_staging_bytes, velora_linear_step_host,
     velora_checkpoint_store, velora_checkpoint_load, velora_checkpoint_weight_grad, OP_CHECKPOINT_WEIGHT_GRAD, OP_F32, CHECKPOINT_BLOCK,
     velora_head_loss, velora_head_loss_backward, OP_HEAD_LOSS, OP_HEAD_LOSS_BACKWARD,
+    OP_HEAD_DISTILL, OP_HEAD_DISTILL_BACKWARD, OP_LAYER_NORM_BACKWARD,
 )
+from .training_ops import velora_head_distill, velora_head_distill_backward, velora_layer_norm, velora_layer_norm_backward  # noqa: F401
 from .memory_model import saved_activation_bytes  # noqa: F401

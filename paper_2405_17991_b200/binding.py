@@ -23,7 +23,8 @@ WG_FACTORED, WG_EXPLICIT = 0, 1
 PRODUCT_A_BT, PRODUCT_A_B, PRODUCT_AT_B = 0, 1, 2
 (OP_INIT_V, OP_WEIGHT_GRAD_FACTORED, OP_WEIGHT_GRAD_EXPLICIT, OP_LINEAR_FORWARD,
  OP_LINEAR_BACKWARD_FACTORED, OP_LINEAR_BACKWARD_EXPLICIT, OP_UPDATE_V, OP_Z8_CALIBRATE,
- OP_CHECKPOINT_WEIGHT_GRAD, OP_HEAD_LOSS, OP_HEAD_LOSS_BACKWARD) = range(11)
+ OP_CHECKPOINT_WEIGHT_GRAD, OP_HEAD_LOSS, OP_HEAD_LOSS_BACKWARD, OP_HEAD_DISTILL, OP_HEAD_DISTILL_BACKWARD,
+ OP_LAYER_NORM_BACKWARD) = range(14)
 OP_ANY_ROWS = 256                                    # see velora_workspace_bytes
 OP_F32 = 512
 CHECKPOINT_BLOCK = 32
@@ -64,6 +65,13 @@ SIGNATURES = {
     "velora_head_loss": (_int, [_p, _i64, _p, _i64, _p, _p, _p, _int, _i64, _i64, _i64, _p, _sz, _p]),
     "velora_head_loss_backward": (_int, [_p, _i64, _p, _i64, _p, _p, _p, _p, _i64, _p, _int, _i64, _int,
                                          _int, _i64, _i64, _i64, _p, _sz, _p]),
+    "velora_head_distill": (_int, [_p, _i64, _p, _i64, _p, _i64, _p, _int, _i64, _p, ctypes.c_float, _int, _p, _p,
+                                   _int, _i64, _i64, _i64, _p, _sz, _p]),
+    "velora_head_distill_backward": (_int, [_p, _i64, _p, _i64, _p, _i64, _p, _int, _i64, _p, ctypes.c_float, _int, _p, _p,
+                                            _p, _i64, _p, _int, _i64, _int, _int, _i64, _i64, _i64, _p, _sz, _p]),
+    "velora_layer_norm": (_int, [_p, _i64, _p, _i64, _p, _p, _int, ctypes.c_float, _p, _i64, _p, _i64, _p, _p, _int, _i64, _i64, _p]),
+    "velora_layer_norm_backward": (_int, [_p, _i64, _p, _i64, _p, _p, _p, _int, _p, _i64, _p, _i64, _p, _p, _int, _int,
+                                          _int, _i64, _i64, _p, _sz, _p]),
 }
 
 
@@ -678,3 +686,11 @@ def velora_head_loss_backward(X: torch.Tensor, W: torch.Tensor, target: torch.Te
                                          _dt(X), N, D, V, *_room(ws), _stream(stream))
     _check(rc, "velora_head_loss_backward")
     return dX, dW
+
+
+def __getattr__(name: str):
+    """Entry points that are bound in a module of their own are reached here as well."""
+    if name in SIGNATURES:
+        from . import training_ops
+        return getattr(training_ops, name)
+    raise AttributeError("module %r has no attribute %r" % (__name__, name))

@@ -4,6 +4,7 @@
 #include "common.cuh"
 #include "gemm_tc.cuh"
 #include "head_loss.cuh"
+#include "layer_norm.cuh"
 
 namespace velora {
 
@@ -220,6 +221,37 @@ int check_head(const void* X, int64_t ldx, const void* W, int64_t ldw, const int
     return VELORA_OK;
 }
 
+int check_teacher(const Teacher& t, int64_t N, int64_t V)
+{
+    if (t.K < 1 || !(t.temperature > 0.f) || !(t.temperature <= 3.4e38f) || !(1.f / t.temperature <= 3.4e38f)) return VELORA_ERR_INVALID_ARG;
+    if (t.K > VELORA_DISTILL_MAX_K) return VELORA_ERR_UNSUPPORTED;
+    if (!valid_dtype(t.t_dtype)) return VELORA_ERR_UNSUPPORTED;
+    if (N == 0) return VELORA_OK;
+    if (!t.logits || t.ldi < t.K || t.ldt < t.K) return VELORA_ERR_INVALID_ARG;
+    if (!elem_aligned(t.logits, t.t_dtype) || !elem_aligned(t.lse, VELORA_F32)) return VELORA_ERR_ALIGNMENT;
+    return VELORA_OK;
+}
+
+// ---- layer norm ----
+int check_norm(int dtype, int p_dtype, const void* w, const void* b, int64_t N, int64_t D)
+{
+    if (N < 0 || D < 1) return VELORA_ERR_INVALID_ARG;
+    if (D > (1 << 30) || N > (static_cast<int64_t>(1) << 40)) return VELORA_ERR_UNSUPPORTED;
+    if (!valid_dtype(dtype) || ((w || b) && !valid_dtype(p_dtype))) return VELORA_ERR_UNSUPPORTED;
+    if ((w && !elem_aligned(w, p_dtype)) || (b && !elem_aligned(b, p_dtype))) return VELORA_ERR_ALIGNMENT;
+    return VELORA_OK;
+}
+
+// A matrix that must be there, or (`may`) may be NULL.
+int check_rows(const void* p, int64_t ld, int dtype, int64_t D, bool may)
+{
+    if (!p) return may ? VELORA_OK : VELORA_ERR_INVALID_ARG;
+    if (ld < D) return VELORA_ERR_INVALID_ARG;
+    return elem_aligned(p, dtype) ? VELORA_OK : VELORA_ERR_ALIGNMENT;
+}
+
+size_t norm_grad_bytes(int64_t N, int64_t D) { return kStatusBytes + align256(2 * static_cast<size_t>(norm_slices(N)) * static_cast<size_t>(D) * sizeof(float)); }
+
 }  // namespace
 }  // namespace velora
 
@@ -282,9 +314,13 @@ const char* velora_status_string(int status)
 
 size_t velora_workspace_bytes(int op, int64_t N, int64_t D, int64_t O, int Dsub)
 {
-    if (N < 0 || D < 1 || Dsub < 1 || Dsub > D || Dsub > VELORA_MAX_DSUB) return 0;
     const bool any_rows = (op & VELORA_OP_ANY_ROWS) != 0;
     const int dtype = (op & VELORA_OP_F32) != 0 ? VELORA_F32 : VELORA_BF16, plain = op & ~(VELORA_OP_ANY_ROWS | VELORA_OP_F32);
+    if (plain == VELORA_OP_HEAD_DISTILL || plain == VELORA_OP_HEAD_DISTILL_BACKWARD) {         // Dsub: the entries of a token
+        if (N < 0 || D < 1 || O < 1 || Dsub < 1 || Dsub > VELORA_DISTILL_MAX_K) return 0;
+        return head_loss_bytes(plain == VELORA_OP_HEAD_DISTILL_BACKWARD, dtype, N, D, O, any_rows, Dsub);
+    }
+    if (N < 0 || D < 1 || Dsub < 1 || Dsub > D || Dsub > VELORA_MAX_DSUB) return 0;
     if (dtype == VELORA_F32 && plain < VELORA_OP_CHECKPOINT_WEIGHT_GRAD) return 0;       // those have one size for both types
     switch (plain) {
         case VELORA_OP_INIT_V: return init_v_workspace_bytes(Dsub);
@@ -301,6 +337,7 @@ size_t velora_workspace_bytes(int op, int64_t N, int64_t D, int64_t O, int Dsub)
                                    (dtype == VELORA_BF16 ? gemm_tail_bytes(O, D, N, 148) : 0);
         case VELORA_OP_HEAD_LOSS: return O < 1 ? 0 : head_loss_bytes(false, dtype, N, D, O, any_rows);
         case VELORA_OP_HEAD_LOSS_BACKWARD: return O < 1 ? 0 : head_loss_bytes(true, dtype, N, D, O, any_rows);
+        case VELORA_OP_LAYER_NORM_BACKWARD: return norm_grad_bytes(N, D);
         default: return 0;
     }
 }
@@ -720,34 +757,114 @@ int velora_head_loss(const void* X, int64_t ldx, const void* W, int64_t ldw, con
     if (!elem_aligned(loss, VELORA_F32) || !elem_aligned(lse, VELORA_F32)) return VELORA_ERR_ALIGNMENT;
     if (!ws) return VELORA_ERR_WORKSPACE;
     if (!aligned16(ws)) return VELORA_ERR_ALIGNMENT;
-    return launch_head_loss(HeadArgs{X, ldx, W, ldw, target, dtype, N, D, V, static_cast<char*>(ws), ws_bytes, static_cast<cudaStream_t>(stream)}, loss, lse);
+    return launch_head_loss(HeadArgs{X, ldx, W, ldw, target, dtype, N, D, V, static_cast<char*>(ws), ws_bytes, static_cast<cudaStream_t>(stream), nullptr}, loss, lse);
+}
+
+static int head_backward(const HeadArgs& a, const float* lse, const float* dloss, void* dX, int64_t lddx, void* dW, int dw_dtype, int64_t lddw, int beta)
+{
+    if (dW) {
+        if (!valid_dtype(dw_dtype)) return VELORA_ERR_UNSUPPORTED;
+        if (lddw < a.D || (beta != 0 && beta != 1)) return VELORA_ERR_INVALID_ARG;
+        if (!elem_aligned(dW, dw_dtype)) return VELORA_ERR_ALIGNMENT;
+    }
+    if (a.N == 0) {
+        if (!dW || beta) return VELORA_OK;
+        const size_t es = dtype_size(dw_dtype);
+        return cudaMemset2DAsync(dW, static_cast<size_t>(lddw) * es, 0, static_cast<size_t>(a.D) * es,
+                                 static_cast<size_t>(a.V), a.stream) == cudaSuccess ? VELORA_OK : VELORA_ERR_CUDA;
+    }
+    if (!lse || !dloss || (dX && lddx < a.D)) return VELORA_ERR_INVALID_ARG;
+    if (!elem_aligned(lse, VELORA_F32) || !elem_aligned(dloss, VELORA_F32) || (dX && !elem_aligned(dX, a.dtype))) return VELORA_ERR_ALIGNMENT;
+    if (!a.ws) return VELORA_ERR_WORKSPACE;
+    if (!aligned16(a.ws)) return VELORA_ERR_ALIGNMENT;
+    if (!dX && !dW) return VELORA_OK;
+    return launch_head_loss_backward(a, lse, dloss, dX, lddx, dW, dw_dtype, lddw, beta);
 }
 
 int velora_head_loss_backward(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* target,
                               const float* lse, const float* dloss, void* dX, int64_t lddx, void* dW, int dw_dtype, int64_t lddw, int beta,
                               int dtype, int64_t N, int64_t D, int64_t V, void* ws, size_t ws_bytes, void* stream)
 {
-    int rc = check_head(X, ldx, W, ldw, target, dtype, N, D, V);
+    const int rc = check_head(X, ldx, W, ldw, target, dtype, N, D, V);
     if (rc != VELORA_OK) return rc;
-    if (dW) {
-        if (!valid_dtype(dw_dtype)) return VELORA_ERR_UNSUPPORTED;
-        if (lddw < D || (beta != 0 && beta != 1)) return VELORA_ERR_INVALID_ARG;
-        if (!elem_aligned(dW, dw_dtype)) return VELORA_ERR_ALIGNMENT;
-    }
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (N == 0) {
-        if (!dW || beta) return VELORA_OK;
-        const size_t es = dtype_size(dw_dtype);
-        return cudaMemset2DAsync(dW, static_cast<size_t>(lddw) * es, 0, static_cast<size_t>(D) * es,
-                                 static_cast<size_t>(V), s) == cudaSuccess ? VELORA_OK : VELORA_ERR_CUDA;
-    }
-    if (!lse || !dloss || (dX && lddx < D)) return VELORA_ERR_INVALID_ARG;
-    if (!elem_aligned(lse, VELORA_F32) || !elem_aligned(dloss, VELORA_F32) || (dX && !elem_aligned(dX, dtype))) return VELORA_ERR_ALIGNMENT;
+    return head_backward(HeadArgs{X, ldx, W, ldw, target, dtype, N, D, V, static_cast<char*>(ws), ws_bytes, static_cast<cudaStream_t>(stream), nullptr},
+                         lse, dloss, dX, lddx, dW, dw_dtype, lddw, beta);
+}
+
+int velora_head_distill(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* index, int64_t ldi, const void* teacher, int t_dtype,
+                        int64_t ldt, const float* teacher_lse, float temperature, int K, float* loss, float* lse,
+                        int dtype, int64_t N, int64_t D, int64_t V, void* ws, size_t ws_bytes, void* stream)
+{
+    int rc = check_head(X, ldx, W, ldw, index, dtype, N, D, V);
+    if (rc != VELORA_OK) return rc;
+    const Teacher t{index, ldi, teacher, t_dtype, ldt, teacher_lse, temperature, K};
+    rc = check_teacher(t, N, V);
+    if (rc != VELORA_OK) return rc;
+    if (N == 0) return VELORA_OK;
+    if (!loss || !lse) return VELORA_ERR_INVALID_ARG;
+    if (!elem_aligned(loss, VELORA_F32) || !elem_aligned(lse, VELORA_F32)) return VELORA_ERR_ALIGNMENT;
     if (!ws) return VELORA_ERR_WORKSPACE;
     if (!aligned16(ws)) return VELORA_ERR_ALIGNMENT;
-    if (!dX && !dW) return VELORA_OK;
-    return launch_head_loss_backward(HeadArgs{X, ldx, W, ldw, target, dtype, N, D, V, static_cast<char*>(ws), ws_bytes, s}, lse, dloss, dX, lddx,
-                                     dW, dw_dtype, lddw, beta);
+    return launch_head_loss(HeadArgs{X, ldx, W, ldw, nullptr, dtype, N, D, V, static_cast<char*>(ws), ws_bytes, static_cast<cudaStream_t>(stream), &t}, loss, lse);
+}
+
+int velora_head_distill_backward(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* index, int64_t ldi, const void* teacher, int t_dtype,
+                                 int64_t ldt, const float* teacher_lse, float temperature, int K, const float* lse, const float* dloss,
+                                 void* dX, int64_t lddx, void* dW, int dw_dtype, int64_t lddw, int beta,
+                                 int dtype, int64_t N, int64_t D, int64_t V, void* ws, size_t ws_bytes, void* stream)
+{
+    int rc = check_head(X, ldx, W, ldw, index, dtype, N, D, V);
+    if (rc != VELORA_OK) return rc;
+    const Teacher t{index, ldi, teacher, t_dtype, ldt, teacher_lse, temperature, K};
+    rc = check_teacher(t, N, V);
+    if (rc != VELORA_OK) return rc;
+    return head_backward(HeadArgs{X, ldx, W, ldw, nullptr, dtype, N, D, V, static_cast<char*>(ws), ws_bytes, static_cast<cudaStream_t>(stream), &t},
+                         lse, dloss, dX, lddx, dW, dw_dtype, lddw, beta);
+}
+
+int velora_layer_norm(const void* X, int64_t ldx, const void* R, int64_t ldr, const void* weight, const void* bias, int p_dtype, float eps,
+                      void* H, int64_t ldh, void* Y, int64_t ldy, float* mean, float* rstd, int dtype, int64_t N, int64_t D, void* stream)
+{
+    int rc = check_norm(dtype, p_dtype, weight, bias, N, D);
+    if (rc != VELORA_OK) return rc;
+    if (!(eps >= 0.f) || !(eps <= 3.4e38f)) return VELORA_ERR_INVALID_ARG;
+    if (N == 0) return VELORA_OK;
+    if ((rc = check_rows(X, ldx, dtype, D, false)) != VELORA_OK || (rc = check_rows(R, ldr, dtype, D, true)) != VELORA_OK ||
+        (rc = check_rows(H, ldh, dtype, D, true)) != VELORA_OK || (rc = check_rows(Y, ldy, dtype, D, false)) != VELORA_OK) return rc;
+    if ((mean && !elem_aligned(mean, VELORA_F32)) || (rstd && !elem_aligned(rstd, VELORA_F32))) return VELORA_ERR_ALIGNMENT;
+    return launch_layer_norm(NormArgs{X, ldx, R, ldr, weight, bias, p_dtype, eps, H, ldh, Y, ldy, mean, rstd, dtype, N, static_cast<int>(D)},
+                             static_cast<cudaStream_t>(stream));
+}
+
+int velora_layer_norm_backward(const void* dY, int64_t lddy, const void* H, int64_t ldh, const float* mean, const float* rstd, const void* weight, int p_dtype,
+                               const void* dH, int64_t lddh, void* dX, int64_t lddx, void* dweight, void* dbias, int dw_dtype, int beta,
+                               int dtype, int64_t N, int64_t D, void* ws, size_t ws_bytes, void* stream)
+{
+    int rc = check_norm(dtype, p_dtype, weight, nullptr, N, D);
+    if (rc != VELORA_OK) return rc;
+    if (dweight || dbias) {
+        if (!valid_dtype(dw_dtype)) return VELORA_ERR_UNSUPPORTED;
+        if (beta != 0 && beta != 1) return VELORA_ERR_INVALID_ARG;
+        if ((dweight && !elem_aligned(dweight, dw_dtype)) || (dbias && !elem_aligned(dbias, dw_dtype))) return VELORA_ERR_ALIGNMENT;
+    }
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (N == 0) {                                            /* empty sums */
+        const size_t bytes = static_cast<size_t>(D) * dtype_size(dw_dtype);
+        if (!beta && dweight && cudaMemsetAsync(dweight, 0, bytes, s) != cudaSuccess) return VELORA_ERR_CUDA;
+        if (!beta && dbias && cudaMemsetAsync(dbias, 0, bytes, s) != cudaSuccess) return VELORA_ERR_CUDA;
+        return VELORA_OK;
+    }
+    if ((rc = check_rows(dY, lddy, dtype, D, false)) != VELORA_OK || (rc = check_rows(H, ldh, dtype, D, false)) != VELORA_OK ||
+        (rc = check_rows(dH, lddh, dtype, D, true)) != VELORA_OK || (rc = check_rows(dX, lddx, dtype, D, true)) != VELORA_OK) return rc;
+    if (!mean || !rstd) return VELORA_ERR_INVALID_ARG;
+    if (!elem_aligned(mean, VELORA_F32) || !elem_aligned(rstd, VELORA_F32)) return VELORA_ERR_ALIGNMENT;
+    if (dweight || dbias) {
+        if (!ws || ws_bytes < norm_grad_bytes(N, D)) return VELORA_ERR_WORKSPACE;
+        if (!aligned16(ws)) return VELORA_ERR_ALIGNMENT;
+    }
+    if (!dX && !dweight && !dbias) return VELORA_OK;
+    return launch_layer_norm_backward(NormGradArgs{dY, lddy, H, ldh, mean, rstd, weight, p_dtype, dH, lddh, dX, lddx, dweight, dbias, dw_dtype, beta, dtype, N,
+                                                   static_cast<int>(D), reinterpret_cast<float*>(static_cast<char*>(ws) + kStatusBytes)}, s);
 }
 
 }  // extern "C"

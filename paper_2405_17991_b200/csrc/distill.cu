@@ -1,0 +1,303 @@
+// Distillation into a linear head from a teacher's top logits: what it takes beside the head's own kernels.  With T the temperature, l = X W^T / T and
+// lse its log sum exp, and a teacher's K columns i and logits t of a token,
+//   p[n, k] = exp(t[n, k] / T - s[n]),  s[n] = log sum_k exp(t[n, k] / T)  or as given
+//   loss[n] = sum_k p (log p - (l[n, i] - lse)),    G[n, v] = g[n] / T (exp(l - lse) sum_k p - sum_{k: i = v} p)
+// A token's entries are put in the order of their columns once a call (distill_lists_kernel), and where every 128 columns' entries start is noted:
+// the kernels that have a row of logits in registers, 128 columns of it at a time, find what belongs there with one look and turn only those
+// values over through shared memory.  The logits' gradients are complete before they are rounded, so G of a student that agrees with its
+// teacher is the rounded difference and not the difference of roundings.
+#include "head_loss.cuh"
+
+namespace velora {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr unsigned long long kLast = ~0ull;               // sorts behind every entry
+
+struct ListsArgs {
+    Teacher t;
+    int64_t* mark;                                         // 0: has entries; -1: has none; V: one of them is no column
+    Entry* entries;
+    unsigned short* starts;
+    float* mass;
+    int N, V, pitch, size;                                 // size: K rounded up to a power of two
+    float inverse_t;
+};
+
+__device__ __forceinline__ float teacher_logit(const Teacher& t, int64_t at)
+{
+    return t.t_dtype == VELORA_BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(t.logits)[at]) : static_cast<const float*>(t.logits)[at];
+}
+
+// A warp a token: probabilities, a bitonic sort of (column, place in the list) in shared memory, starts by bisection.
+__global__ void __launch_bounds__(kThreads)
+distill_lists_kernel(const ListsArgs a)
+{
+    extern __shared__ unsigned long long keys_of_warps[];
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    unsigned long long* key = keys_of_warps + warp * a.size;
+    float* p = reinterpret_cast<float*>(keys_of_warps + warps * a.size) + warp * a.size;
+    const int K = a.t.K;
+    for (int n = blockIdx.x * warps + warp; n < a.N; n += gridDim.x * warps) {
+        bool bad = false, some = false;
+        float m = -INFINITY;
+        int count = 0;
+        for (int k = lane; k < a.size; k += 32) {
+            const int64_t i = k < K ? a.t.index[n * a.t.ldi + k] : -1;
+            const bool is = i >= 0 && i < a.V;
+            const float u = is ? teacher_logit(a.t, n * a.t.ldt + k) * a.inverse_t : -INFINITY;
+            bad |= i >= a.V;
+            some |= is && u != -INFINITY;                  // a NaN is something
+            m = fmaxf(m, u);
+            p[k] = u;
+            key[k] = is ? static_cast<unsigned long long>(i) << 32 | static_cast<unsigned>(k) : kLast;
+            count += is;
+        }
+        bad = __any_sync(0xffffffffu, bad);
+        some = __any_sync(0xffffffffu, some) && !bad;
+        count = __reduce_add_sync(0xffffffffu, count);
+        if (lane == 0) a.mark[n] = bad ? a.V : (some ? 0 : -1);
+        if (!some) continue;                               // for the warp; nobody reads its entries
+        float s = 0.f, scale = 1.f;
+        if (a.t.lse) {
+            m = a.t.lse[n];
+            for (int k = lane; k < K; k += 32) s += p[k] = p[k] == -INFINITY ? 0.f : expf(p[k] - m);
+        } else {
+            m = warp_max(m);
+            for (int k = lane; k < K; k += 32) s += p[k] = expf(p[k] - m);
+            scale = 1.f / warp_sum(s);
+            s = 0.f;
+            for (int k = lane; k < K; k += 32) s += p[k] *= scale;
+        }
+        s = warp_sum(s);
+        if (lane == 0) a.mass[n] = s;
+        __syncwarp();
+        for (int run = 2; run <= a.size; run *= 2)
+            for (int step = run / 2; step > 0; step /= 2) {
+                for (int i = lane; i < a.size / 2; i += 32) {
+                    const int x = 2 * i - (i & (step - 1)), y = x + step;
+                    const unsigned long long kx = key[x], ky = key[y];
+                    if ((kx > ky) == ((x & run) == 0)) {
+                        key[x] = ky;
+                        key[y] = kx;
+                    }
+                }
+                __syncwarp();
+            }
+        Entry* out = a.entries + static_cast<int64_t>(n) * K;
+        for (int j = lane; j < count; j += 32) out[j] = Entry{static_cast<int>(key[j] >> 32), p[static_cast<unsigned>(key[j])]};
+        unsigned short* starts = a.starts + static_cast<int64_t>(n) * a.pitch;
+        for (int b = lane; b < a.pitch; b += 32) {
+            const unsigned long long from = static_cast<unsigned long long>(b) * kEntryColumns << 32;
+            int lo = 0, hi = count;
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                if (key[mid] < from) lo = mid + 1; else hi = mid;
+            }
+            starts[b] = static_cast<unsigned short>(lo);
+        }
+        __syncwarp();
+    }
+}
+
+// fp32: a block per row takes the piece's maximum and its exponentials into what the pieces before have left, and notes the entries' logits.
+__global__ void __launch_bounds__(kThreads)
+distill_stats_kernel(float* logits, int64_t ld, int parts, int64_t part_stride, const HeadTile h, int first)
+{
+    __shared__ float part[2][kWarps];
+    pdl_wait();
+    pdl_trigger();
+    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (row >= *h.live) return;                            // the same for the block
+    float* l = logits + row * ld;
+    float m = -INFINITY;
+    for (int c = threadIdx.x; c < h.cols; c += kThreads) {
+        const float x = sum_of_parts(l + c, parts, part_stride) * h.e.inverse_t;
+        l[c] = x;                                          // read again by this thread, the entries' behind a barrier
+        m = fmaxf(m, x);
+    }
+    m = warp_max(m);
+    if (lane == 0) part[0][warp] = m;
+    __syncthreads();
+    for (int w = 0; w < kWarps; ++w) m = fmaxf(m, part[0][w]);
+    const float2 old = first ? make_float2(-INFINITY, 0.f) : h.running[row];
+    m = fmaxf(m, old.x);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float s = 0.f;
+#pragma unroll 4
+    for (int c = threadIdx.x; c < h.cols; c += kThreads) s += expf(l[c] - ref);
+    s = warp_sum(s);
+    if (lane == 0) part[1][warp] = s;
+    const int n = h.e.order[row];
+    const unsigned short* starts = h.e.starts + static_cast<int64_t>(n) * h.e.pitch;
+    const Entry* entries = h.e.entries + static_cast<int64_t>(n) * h.e.K;
+    for (int j = starts[h.v0 / kEntryColumns] + threadIdx.x; j < starts[(h.v0 + h.cols + kEntryColumns - 1) / kEntryColumns]; j += kThreads)
+        h.e.at[static_cast<int64_t>(n) * h.e.K + j] = l[entries[j].column - h.v0];
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = old.y * expf(old.x - ref);
+        for (int w = 0; w < kWarps; ++w) s += part[1][w];
+        h.running[row] = make_float2(m, s);
+    }
+}
+
+// fp32: logits to their gradients, in place; a warp takes 128 columns of a row at a time.
+__global__ void __launch_bounds__(kThreads)
+distill_gradient_kernel(float* logits, int64_t ld, int parts, int64_t part_stride, const HeadTile h)
+{
+    pdl_wait();
+    pdl_trigger();
+    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float* l = logits + row * ld;
+    const bool is = h.target[row] >= 0;
+    const int n = h.e.order[row];
+    const float g = h.scale[row] * h.e.inverse_t, z = h.lse[row], q = is ? g * h.e.mass[n] : 0.f;
+    const unsigned short* starts = h.e.starts + static_cast<int64_t>(n) * h.e.pitch;
+    const Entry* entries = h.e.entries + static_cast<int64_t>(n) * h.e.K;
+    for (int c0 = (static_cast<int>(blockIdx.y) * kWarps + warp) * kEntryColumns; c0 < h.cols; c0 += static_cast<int>(gridDim.y) * kWarps * kEntryColumns) {
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = is && c0 + lane + 32 * i < h.cols ? sum_of_parts(l + c0 + lane + 32 * i, parts, part_stride) : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = is ? q * expf(x[i] * h.e.inverse_t - z) : 0.f;
+        if (is) {
+            const int b = (h.v0 + c0) / kEntryColumns;
+            for (int j = starts[b]; j < starts[b + 1]; ++j) {
+                const Entry e = entries[j];
+                const int c = e.column - h.v0 - c0 - lane;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (c == 32 * i) x[i] -= g * e.p;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c0 + lane + 32 * i < h.cols) l[c0 + lane + 32 * i] = x[i];
+    }
+}
+
+// A block takes 32 rows: eight slices of their parts, then the eight together; then a warp four rows' entries.
+__global__ void __launch_bounds__(kThreads)
+distill_merge_kernel(const HeadTile h, int parts, float* loss, float* lse)
+{
+    __shared__ float2 slice[kWarps][32];
+    __shared__ float sums[32];
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row0 = blockIdx.x * 32;
+    const int live = *h.live;
+    float m = -INFINITY, s = 0.f;
+    if (row0 + lane < live) {
+        for (int p0 = warp; p0 < parts; p0 += kWarps * 8) {                   // eight loads in flight
+            float2 x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int p = p0 + kWarps * i;
+                x[i] = p < parts ? h.running[static_cast<int64_t>(p) * h.N + row0 + lane] : make_float2(-INFINITY, 0.f);
+            }
+            float both = m;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) both = x[i].x > both ? x[i].x : (x[i].x == x[i].x ? both : x[i].x);      // a NaN stays one
+            const float ref = both == -INFINITY ? 0.f : both;
+            s *= expf(m - ref);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += x[i].y * expf(x[i].x - ref);
+            m = both;
+        }
+    }
+    slice[warp][lane] = make_float2(m, s);
+    __syncthreads();
+    if (warp == 0) {
+        m = -INFINITY;
+        bool nan = false;
+        for (int w = 0; w < kWarps; ++w) {
+            m = fmaxf(m, slice[w][lane].x);
+            nan |= slice[w][lane].x != slice[w][lane].x;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        s = nan ? __int_as_float(0x7fc00000) : 0.f;
+        for (int w = 0; w < kWarps; ++w) s += slice[w][lane].y * expf(slice[w][lane].x - ref);
+        sums[lane] = m + logf(s);
+    }
+    __syncthreads();
+    for (int r = warp; r < 32 && row0 + r < h.N; r += kWarps) {
+        const int row = row0 + r, n = h.e.order[row], mark = h.target[row];
+        float y = 0.f;
+        if (mark >= 0) {
+            const int count = h.e.starts[static_cast<int64_t>(n) * h.e.pitch + h.e.pitch - 1];
+            const int64_t first = static_cast<int64_t>(n) * h.e.K;
+            for (int j = lane; j < count; j += 32) {
+                const float p = h.e.entries[first + j].p;
+                if (p != 0.f) y += p * (logf(p) - (h.e.at[first + j] - sums[r]));      // p log p is 0 there, whatever the student's logit
+            }
+            y = warp_sum(y);
+        }
+        if (lane == 0) {
+            loss[n] = mark == -2 ? __int_as_float(0x7fc00000) : y;
+            lse[n] = mark >= 0 ? sums[r] : 0.f;
+        }
+    }
+}
+
+}  // namespace
+
+Entries distill_entries(const HeadArgs& a, const HeadLayout& l)
+{
+    Entries e{};
+    e.entries = reinterpret_cast<const Entry*>(a.ws + l.entries);
+    e.starts = reinterpret_cast<const unsigned short*>(a.ws + l.starts);
+    e.mass = reinterpret_cast<const float*>(a.ws + l.mass);
+    e.order = reinterpret_cast<const int*>(a.ws + l.order);
+    e.at = reinterpret_cast<float*>(a.ws + l.at_entries);
+    e.K = a.teacher->K;
+    e.pitch = entry_pitch(a.V);
+    e.inverse_t = 1.f / a.teacher->temperature;
+    return e;
+}
+
+int launch_distill_lists(const HeadArgs& a, const HeadLayout& l)
+{
+    DeviceInfo di;
+    const int rc = device_info(&di);
+    if (rc != VELORA_OK) return rc;
+    const Entries e = distill_entries(a, l);
+    ListsArgs args{};
+    args.t = *a.teacher;
+    args.mark = reinterpret_cast<int64_t*>(a.ws + l.mark);
+    args.entries = const_cast<Entry*>(e.entries);
+    args.starts = const_cast<unsigned short*>(e.starts);
+    args.mass = const_cast<float*>(e.mass);
+    args.N = static_cast<int>(a.N);
+    args.V = static_cast<int>(a.V);
+    args.pitch = e.pitch;
+    args.size = 1;
+    while (args.size < a.teacher->K) args.size *= 2;
+    args.inverse_t = e.inverse_t;
+    const int warps = args.size <= 256 ? kWarps : 2;       // 24 KB of keys and probabilities at most
+    const int64_t ctas = ceil_div64(a.N, warps), most = static_cast<int64_t>(di.sm_count) * 8;
+    return launch_chained(distill_lists_kernel, dim3(static_cast<unsigned>(ctas < most ? ctas : most)), 32 * warps,
+                          static_cast<size_t>(warps) * args.size * 12, a.stream, args);
+}
+
+int launch_distill_stats(float* logits, int64_t ld, int parts, int64_t part_stride, const HeadTile& h, bool first, cudaStream_t stream)
+{
+    return launch_chained(distill_stats_kernel, dim3(static_cast<unsigned>(h.N)), kThreads, 0, stream, logits, ld, parts, part_stride, h, first ? 1 : 0);
+}
+
+int launch_distill_gradient(float* logits, int64_t ld, int parts, int64_t part_stride, const HeadTile& h, cudaStream_t stream)
+{
+    const int64_t blocks = ceil_div64(h.cols, kEntryColumns * kWarps);
+    return launch_chained(distill_gradient_kernel, dim3(static_cast<unsigned>(h.N), static_cast<unsigned>(blocks < 16 ? blocks : 16)), kThreads, 0,
+                          stream, logits, ld, parts, part_stride, h);
+}
+
+int launch_distill_merge(const HeadTile& h, int parts, float* loss, float* lse, cudaStream_t stream)
+{
+    return launch_chained(distill_merge_kernel, dim3(static_cast<unsigned>(ceil_div64(h.N, 32))), kThreads, 0, stream, h, parts, loss, lse);
+}
+
+}  // namespace velora

@@ -83,7 +83,7 @@ int gradient_splits(int dtype, int64_t N, int64_t D, int64_t V)
 }
 
 // The arrays in front of the piece; bf16 needs none for the forward pass.
-HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool pack_w, int splits)
+HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool pack_w, int splits, int K)
 {
     HeadLayout l{};
     const size_t n = static_cast<size_t>(N);
@@ -112,6 +112,14 @@ HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D, int64_t V,
     l.rows = backward ? gradient_rows(dtype, N) : 1;
     l.x = take(n * static_cast<size_t>(l.rows) * static_cast<size_t>(l.ldx) * dtype_size(dtype));
     if (pack_w) l.w = take(pack_rows_bytes(V, D));
+    if (K > 0) {
+        const size_t k = n * static_cast<size_t>(K);
+        l.mark = take(8 * n);
+        l.entries = take(sizeof(Entry) * k);
+        l.starts = take(2 * n * static_cast<size_t>(entry_pitch(V)));
+        l.mass = take(4 * n);
+        if (!backward) l.at_entries = take(4 * k);
+    }
     l.piece = at;
     return l;
 }
@@ -122,11 +130,12 @@ int logit_parts(int dtype, int64_t N, int64_t D, int64_t V) { return dtype == VE
 int head_layout(HeadLayout* l, bool backward, const HeadArgs& a)
 {
     const bool pack_w = a.dtype == VELORA_BF16 && !tc_operand_ok(a.W, a.ldw);
+    const int K = a.teacher ? a.teacher->K : 0;
     size_t column = piece_element(a.dtype, backward, a.N) * static_cast<size_t>(a.N);
-    *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, backward ? gradient_splits(a.dtype, a.N, a.D, a.V) : 1);
+    *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, backward ? gradient_splits(a.dtype, a.N, a.D, a.V) : 1, K);
     l->parts = logit_parts(a.dtype, a.N, a.D, a.V);
     if (a.ws_bytes < l->piece + column * l->parts * kPieceStep) {             // less room than asked for: no partial sums
-        *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, backward ? gradient_rows(a.dtype, a.N) : 1);
+        *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, backward ? gradient_rows(a.dtype, a.N) : 1, K);
         l->parts = 1;
     }
     column *= static_cast<size_t>(l->parts);
@@ -277,7 +286,7 @@ int launch_rows(const HeadArgs& a, const HeadLayout& l, const float* lse, const 
     RowsArgs r{};
     r.X = a.X;
     r.ldx = a.ldx;
-    r.target = a.target;
+    r.target = a.teacher ? reinterpret_cast<const int64_t*>(a.ws + l.mark) : a.target;
     r.N = static_cast<int>(a.N);
     r.V = static_cast<int>(a.V);
     r.D = static_cast<int>(a.D);
@@ -309,38 +318,12 @@ int launch_rows(const HeadArgs& a, const HeadLayout& l, const float* lse, const 
                : launch_chained(head_rows_kernel<float, false>, grid, kRowThreads, 0, a.stream, r);
 }
 
-__device__ __forceinline__ float warp_max(float x)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-    return x;
-}
-__device__ __forceinline__ float warp_sum(float x)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
-}
-
 // A row's loss and log sum exp to where its token is.
 __device__ __forceinline__ void write_loss(float* loss, float* lse, int n, int target, float m, float s, float at_target)
 {
     const float l = m + logf(s);
     loss[n] = target >= 0 ? l - at_target : (target == -1 ? 0.f : __int_as_float(0x7fc00000));
     lse[n] = target >= 0 ? l : 0.f;
-}
-
-// In a fixed order; up to 16, all under way at once.
-__device__ __forceinline__ float sum_of_parts(const float* p, int parts, int64_t stride)
-{
-    float x[16];
-#pragma unroll
-    for (int s = 0; s < 16; ++s) x[s] = s < parts ? p[s * stride] : 0.f;
-    float y = x[0];
-#pragma unroll
-    for (int s = 1; s < 16; ++s)
-        if (s < parts) y += x[s];
-    return y;
 }
 
 // A block per row takes the piece's maximum, then its exponentials, into what the pieces before have left; behind the last one the loss.  (A warp
@@ -516,10 +499,10 @@ int product(int kind, const void* A, int a_dtype, int64_t lda, const void* B, in
 
 }  // namespace
 
-size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool any_rows)
+size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool any_rows, int K)
 {
     if (N < 1) return kStatusBytes;
-    const size_t front = head_front(backward, dtype, N, D, V, any_rows && dtype == VELORA_BF16, backward ? gradient_splits(dtype, N, D, V) : 1).piece;
+    const size_t front = head_front(backward, dtype, N, D, V, any_rows && dtype == VELORA_BF16, backward ? gradient_splits(dtype, N, D, V) : 1, K).piece;
     if (dtype == VELORA_BF16 && !backward) return front;
     return front + up256(piece_element(dtype, backward, N) * static_cast<size_t>(logit_parts(dtype, N, D, V)) * static_cast<size_t>(N) *
                          static_cast<size_t>(room_wanted(dtype, N, V)));
@@ -568,6 +551,7 @@ HeadTile head_tile(const HeadArgs& a, const HeadLayout& l, int64_t v0, int64_t c
     h.D = static_cast<int>(a.D);
     h.cols = static_cast<int>(cols);
     h.v0 = static_cast<int>(v0);
+    if (a.teacher) h.e = distill_entries(a, l);
     return h;
 }
 
@@ -582,6 +566,10 @@ int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
     int64_t ldw;
     rc = head_weights(a, l, &W, &ldw);
     if (rc != VELORA_OK) return rc;
+    if (a.teacher) {
+        rc = launch_distill_lists(a, l);
+        if (rc != VELORA_OK) return rc;
+    }
     rc = launch_rows(a, l, nullptr, nullptr, false);
     if (rc != VELORA_OK) return rc;
     int* status = reinterpret_cast<int*>(a.ws);
@@ -592,8 +580,9 @@ int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
         rc = few ? launch_head_few(a.ws + l.x, l.ldx, W, ldw, nullptr, 0, 0, h, status, a.stream)
                  : launch_head_tiles(a.ws + l.x, l.ldx, W, ldw, nullptr, 0, h, status, a.stream);
         if (rc != VELORA_OK) return rc;
-        return launch_chained(head_merge_kernel, dim3(static_cast<unsigned>(ceil_div64(a.N, 32))), kRowThreads, 0, a.stream, h.running,
-                              static_cast<int>(ceil_div64(a.V, few ? head_few_height(a.V) : 128)), n, h.live,
+        const int parts = static_cast<int>(ceil_div64(a.V, few ? head_few_height(a.V) : 128));
+        if (a.teacher) return launch_distill_merge(h, parts, loss, lse, a.stream);
+        return launch_chained(head_merge_kernel, dim3(static_cast<unsigned>(ceil_div64(a.N, 32))), kRowThreads, 0, a.stream, h.running, parts, n, h.live,
                               reinterpret_cast<int*>(a.ws + l.order), h.target, h.at_target, loss, lse);
     }
     float* piece = reinterpret_cast<float*>(a.ws + l.piece);
@@ -602,6 +591,11 @@ int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
         const int64_t part_stride = a.N * l.piece_cols;
         const int parts = fp32_logits(a, l, W + static_cast<size_t>(v0) * ldw * 4, ldw, cols, &rc);
         if (rc != VELORA_OK) return rc;
+        if (a.teacher) {
+            rc = launch_distill_stats(piece, l.piece_cols, parts, part_stride, head_tile(a, l, v0, cols), v0 == 0, a.stream);
+            if (rc != VELORA_OK) return rc;
+            continue;
+        }
         rc = launch_chained(head_stats_kernel, dim3(static_cast<unsigned>(a.N)), kRowThreads, 0, a.stream, piece, l.piece_cols, parts,
                             part_stride, static_cast<int>(cols), static_cast<int>(v0),
                             reinterpret_cast<int*>(a.ws + l.live), reinterpret_cast<int*>(a.ws + l.order), reinterpret_cast<int*>(a.ws + l.target),
@@ -609,7 +603,7 @@ int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
                             v0 + cols == a.V ? 1 : 0, loss, lse);
         if (rc != VELORA_OK) return rc;
     }
-    return VELORA_OK;
+    return a.teacher ? launch_distill_merge(head_tile(a, l, 0, a.V), 1, loss, lse, a.stream) : VELORA_OK;
 }
 
 int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* dloss, void* dX, int64_t lddx,
@@ -626,6 +620,10 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
     // all of them would be the same rounding again and again, which does not average out (relative error of dX and dW up to 4e-3 by the
     // count alone); so the largest dloss is taken out and multiplied back in fp32, wherever the product that writes dW takes a factor.
     const bool take_common = a.dtype == VELORA_BF16 && (!dW || dw_dtype == VELORA_BF16 || c_rows_vec(dW, lddw, sizeof(float)));
+    if (a.teacher) {
+        rc = launch_distill_lists(a, l);
+        if (rc != VELORA_OK) return rc;
+    }
     rc = launch_rows(a, l, lse, dloss, take_common);
     if (rc != VELORA_OK) return rc;
     int* status = reinterpret_cast<int*>(a.ws);
@@ -645,7 +643,10 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
             const int parts = fp32_logits(a, l, w, ldw, cols, &rc);
             if (rc != VELORA_OK) return rc;
             const int64_t blocks = ceil_div64(cols, 128 * (kRowThreads / 32));
-            rc = launch_chained(head_gradient_kernel, dim3(static_cast<unsigned>(a.N), static_cast<unsigned>(blocks < 16 ? blocks : 16)), kRowThreads,
+            if (a.teacher)
+                rc = launch_distill_gradient(reinterpret_cast<float*>(G), l.piece_cols, parts, a.N * l.piece_cols, head_tile(a, l, v0, cols), a.stream);
+            else
+                rc = launch_chained(head_gradient_kernel, dim3(static_cast<unsigned>(a.N), static_cast<unsigned>(blocks < 16 ? blocks : 16)), kRowThreads,
                                 0, a.stream, reinterpret_cast<float*>(G), l.piece_cols, parts, a.N * l.piece_cols, static_cast<int>(cols),
                                 static_cast<int>(v0), reinterpret_cast<int*>(a.ws + l.target), reinterpret_cast<float*>(a.ws + l.scale),
                                 reinterpret_cast<float*>(a.ws + l.lse));

@@ -18,11 +18,26 @@ struct HeadLayout {
     size_t x;               // the rows of X, pitch ldx elements; zeros for rows without a target
     size_t w;               // W with a pitch that tensor maps take, where W's own is not
     size_t sum;             // fp32, pitch ldx: dX so far, `splits` partial sums (backward)
+    // Distillation, by token: a target for the arrays above, entries and their probabilities in the order of their columns, where each 128
+    // columns' entries start, the probabilities' sum, the entries' logits (forward)
+    size_t mark, entries, starts, mass, at_entries;
     size_t piece;           // a piece of the vocabulary: logits or their gradient, pitch `piece_cols` elements
     int64_t ldx, piece_cols;
     int rows;               // copies of the rows of X, and rows of the logits' gradients for each (backward)
     int splits, parts;      // partial sums of dX; of the logits (fp32), one piece behind another
     size_t bytes;
+};
+
+// What a teacher says of the next token: K columns and logits a token (distill.cu).
+struct Teacher {
+    const int64_t* index;
+    int64_t ldi;
+    const void* logits;
+    int t_dtype;
+    int64_t ldt;
+    const float* lse;               // NULL: of the K entries
+    float temperature;
+    int K;
 };
 
 struct HeadArgs {
@@ -36,7 +51,25 @@ struct HeadArgs {
     char* ws;
     size_t ws_bytes;
     cudaStream_t stream;
+    const Teacher* teacher;         // NULL: a target a token
 };
+
+// An entry of a teacher's list: the column and its probability.
+struct Entry {
+    int column;
+    float p;
+};
+constexpr int kEntryColumns = 128;                  // of `starts`: entries of columns 128 b .. are entries[starts[b]] .. before entries[starts[b + 1]]
+struct Entries {
+    const Entry* entries;                           // [token][K], in the order of their columns
+    const unsigned short* starts;                   // [token][pitch]
+    const float* mass;                              // [token]
+    const int* order;                               // token of a row
+    float* at;                                      // [token][K]: logits over the temperature (forward)
+    int K, pitch;
+    float inverse_t;                                // 1 / temperature
+};
+inline int entry_pitch(int64_t V) { return static_cast<int>(ceil_div64(V, kEntryColumns)) + 1; }
 
 // A product's worth of logits, columns v0 .. v0 + cols of the vocabulary; arrays as in HeadLayout.
 struct HeadTile {
@@ -47,6 +80,7 @@ struct HeadTile {
     float* at_target;
     float2* running;
     int N, D, cols, v0;
+    Entries e;                      // entries == nullptr: a target a row
 };
 // G == nullptr: statistics of bf16 x W^T; otherwise its gradient to G [N, ldg].  W: its row v0.  (head_loss_tc.cu)
 int launch_head_tiles(const void* x, int64_t ldx, const void* W, int64_t ldw, void* G, int64_t ldg, const HeadTile& h, int* status, cudaStream_t stream);
@@ -70,10 +104,70 @@ __device__ __forceinline__ float head_exp2(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float warp_max(float x)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+    return x;
+}
+__device__ __forceinline__ float warp_sum(float x)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+
+// In a fixed order; up to 16, all under way at once.
+__device__ __forceinline__ float sum_of_parts(const float* p, int parts, int64_t stride)
+{
+    float x[16];
+#pragma unroll
+    for (int s = 0; s < 16; ++s) x[s] = s < parts ? p[s * stride] : 0.f;
+    float y = x[0];
+#pragma unroll
+    for (int s = 1; s < 16; ++s)
+        if (s < parts) y += x[s];
+    return y;
+}
+
+constexpr int kNoColumn = 1 << 30;
+// The entries of a row that lie in some columns from `first` on, one after the other.
+struct EntryWalk {
+    const Entry* list;
+    int j, end, first, column;                      // column: of entry j, from `first` on; kNoColumn behind the last
+    float p;
+    __device__ __forceinline__ void start(const Entries& e, int token, int from, int columns)
+    {
+        const unsigned short* s = e.starts + static_cast<int64_t>(token) * e.pitch;
+        list = e.entries + static_cast<int64_t>(token) * e.K;
+        j = s[from / kEntryColumns];
+        end = s[(from + columns - 1) / kEntryColumns + 1];      // some of them may lie behind
+        first = from;
+        load();
+        while (column < 0) next();                  // of the same 128 columns, but in front
+    }
+    __device__ __forceinline__ void none() { list = nullptr; j = end = 0; column = kNoColumn; }
+    __device__ __forceinline__ void load()
+    {
+        column = kNoColumn;
+        if (j < end) {
+            const Entry e = list[j];
+            column = e.column - first;
+            p = e.p;
+        }
+    }
+    __device__ __forceinline__ void next() { ++j; load(); }
+};
 #endif
 
 // What velora_workspace_bytes reports.
-size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool any_rows);
+size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool any_rows, int K = 0);      // K > 0: distillation
+// Distillation's own kernels (distill.cu).
+Entries distill_entries(const HeadArgs& a, const HeadLayout& l);
+int launch_distill_lists(const HeadArgs& a, const HeadLayout& l);
+int launch_distill_stats(float* logits, int64_t ld, int parts, int64_t part_stride, const HeadTile& h, bool first, cudaStream_t stream);
+int launch_distill_gradient(float* logits, int64_t ld, int parts, int64_t part_stride, const HeadTile& h, cudaStream_t stream);
+int launch_distill_merge(const HeadTile& h, int parts, float* loss, float* lse, cudaStream_t stream);
 int launch_head_loss(const HeadArgs& a, float* loss, float* lse);
 int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* dloss, void* dX, int64_t lddx,
                               void* dW, int dw_dtype, int64_t lddw, int beta);

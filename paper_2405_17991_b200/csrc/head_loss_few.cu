@@ -42,7 +42,7 @@ __device__ __forceinline__ bool epilogue_any(bool p)
     return any != 0;
 }
 
-template <bool GRADIENT, int NT>
+template <bool GRADIENT, bool LISTS, int NT>
 __global__ void __launch_bounds__(W_THREADS, 1)
 head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const HeadTile h, int height, __nv_bfloat16* G, int64_t ldg,
                 int twice, int* status)
@@ -177,11 +177,16 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
                 const int row = 32 * c + lane;               // this lane's token behind the turn
                 __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) block[i * W_PITCH + lane] = __uint_as_float(l[c][i]);
+                for (int i = 0; i < 32; ++i) block[i * W_PITCH + lane] = LISTS ? __uint_as_float(l[c][i]) * h.e.inverse_t : __uint_as_float(l[c][i]);
                 __syncwarp();
                 if (32 * c >= h.N) break;                    // for all epilogue warps
                 const int target = row < h.N ? h.target[row] : -1, t = target - h.v0 - v0;
-                const float* mine = block + lane * W_PITCH;
+                float* mine = block + lane * W_PITCH;
+                EntryWalk walk;
+                if (LISTS) {
+                    walk.none();
+                    if (target >= 0 && valid > 0) walk.start(h.e, h.e.order[row], h.v0 + v0, valid);
+                }
                 if (!GRADIENT) {
                     float m = -INFINITY, s = 0.f;
                     for (int i = 0; i < valid; ++i) m = fmaxf(m, mine[i]);
@@ -194,16 +199,25 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
 #pragma unroll 8
                     for (int i = 0; i < valid; ++i) s += head_exp2(fmaf(mine[i] - off, kHeadLog2e, -c2));
                     parts[quarter * NT + row] = make_float2(m, s * (1.f - lost * 0.69314718f));
-                    if (t >= 0 && t < valid) h.at_target[row] = mine[t];
+                    if (LISTS) {
+                        for (; walk.column < valid; walk.next()) h.e.at[walk.list - h.e.entries + walk.j] = mine[walk.column];
+                    } else if (t >= 0 && t < valid) {
+                        h.at_target[row] = mine[t];
+                    }
                 } else if (row < h.N && valid > 0) {
                     const bool is = target >= 0;
-                    const float g = is ? h.scale[row] : 0.f, lse = is ? h.lse[row] : 0.f;
+                    const float g = is ? (LISTS ? h.scale[row] * h.e.inverse_t : h.scale[row]) : 0.f, lse = is ? h.lse[row] : 0.f;
                     float off = 0.f, z = -lse * kHeadLog2e, lost = fmaf(-lse, kHeadLog2e, -z);
                     if (fabsf(lost) > kHeadLost) {
                         off = lse;
                         z = lost = 0.f;
                     }
-                    const float gp = g * (1.f + lost * 0.69314718f);
+                    const float mass = LISTS ? (is ? h.e.mass[h.e.order[row]] : 0.f) : 1.f;
+                    const float gp = (LISTS ? g * mass : g) * (1.f + lost * 0.69314718f);
+                    if (LISTS) {                             // complete before they are rounded
+                        for (int i = 0; i < valid; ++i) mine[i] = head_exp2(fmaf(mine[i] - off, kHeadLog2e, z)) * gp;
+                        for (; walk.column < valid; walk.next()) mine[walk.column] -= g * walk.p;
+                    }
                     // The pitch is a multiple of 256 and the height of 16: columns past the piece's are there to be written, those of the next tile
                     // are not touched.
                     uint4* dst = reinterpret_cast<uint4*>(G + row * ldg + v0);
@@ -214,9 +228,13 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             const int j = 8 * i + 2 * k;
-                            float x = head_exp2(fmaf(mine[j] - off, kHeadLog2e, z)) * gp, y = head_exp2(fmaf(mine[j + 1] - off, kHeadLog2e, z)) * gp;
-                            if (t == j) x -= g;
-                            if (t == j + 1) y -= g;
+                            float x = mine[j], y = mine[j + 1];
+                            if (!LISTS) {
+                                x = head_exp2(fmaf(x - off, kHeadLog2e, z)) * gp;
+                                y = head_exp2(fmaf(y - off, kHeadLog2e, z)) * gp;
+                                if (t == j) x -= g;
+                                if (t == j + 1) y -= g;
+                            }
                             w[k] = is ? pack_bf16x2(x, y) : 0u;
                             r[k] = is ? pack_bf16x2(x - bf16_lo(w[k]), y - bf16_hi(w[k])) : 0u;
                         }
@@ -258,13 +276,13 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
     }
 }
 
-template <bool GRADIENT, int NT>
+template <bool GRADIENT, bool LISTS, int NT>
 int launch_few(const CUtensorMap& tw, const CUtensorMap& tx, const HeadTile& h, int height, void* G, int64_t ldg, int twice, int* status, int sm_count, cudaStream_t stream)
 {
     static DeviceOnce configured;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return VELORA_ERR_CUDA;
-    auto kern = head_few_kernel<GRADIENT, NT>;
+    auto kern = head_few_kernel<GRADIENT, LISTS, NT>;
     if (!configured.get(dev)) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(FewShape<NT>::kSmem)) != cudaSuccess) return VELORA_ERR_CUDA;
         configured.set(dev);
@@ -302,11 +320,12 @@ int launch_head_few(const void* x, int64_t ldx, const void* W, int64_t ldw, void
     if (rc != VELORA_OK) return rc;
     rc = make_tmap_bf16_2d(&tx, x, h.D, h.N, ldx, W_BK, nt);
     if (rc != VELORA_OK) return rc;
-#define VELORA_FEW(GRAD)                                                                                      \
-    (nt == 32 ? launch_few<GRAD, 32>(tw, tx, h, height, G, ldg, twice, status, di.sm_count, stream)                          \
-              : (nt == 64 ? launch_few<GRAD, 64>(tw, tx, h, height, G, ldg, twice, status, di.sm_count, stream)              \
-                          : launch_few<GRAD, 128>(tw, tx, h, height, G, ldg, twice, status, di.sm_count, stream)))
-    return G ? VELORA_FEW(true) : VELORA_FEW(false);
+#define VELORA_FEW(GRAD, LISTS)                                                                                      \
+    (nt == 32 ? launch_few<GRAD, LISTS, 32>(tw, tx, h, height, G, ldg, twice, status, di.sm_count, stream)                          \
+              : (nt == 64 ? launch_few<GRAD, LISTS, 64>(tw, tx, h, height, G, ldg, twice, status, di.sm_count, stream)              \
+                          : launch_few<GRAD, LISTS, 128>(tw, tx, h, height, G, ldg, twice, status, di.sm_count, stream)))
+    if (h.e.entries) return G ? VELORA_FEW(true, true) : VELORA_FEW(false, true);
+    return G ? VELORA_FEW(true, false) : VELORA_FEW(false, false);
 #undef VELORA_FEW
 }
 

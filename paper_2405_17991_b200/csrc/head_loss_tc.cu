@@ -1,6 +1,7 @@
 // The logits of a linear head on CTA pairs, used up where they come out of the tensor cores:
 //   HEAD_STATS     per row and 128 columns the maximum and the sum of exponentials relative to it, and the target's logit
 //   HEAD_GRADIENT  G[n, v] = g[n] (exp(l[n, v] - lse[n]) - [v = t[n]]) in bf16
+//   DISTILL_STATS, DISTILL_GRADIENT  the same of logits over a temperature, with a list of columns and probabilities for a target (distill.cu)
 // l = X W^T, bf16 operands K-major, 256 x 256 logits a pair (tcgen05 cta_group::2; the pipeline is that of gemm_tc2.cu).
 //
 // The tensor cores add with truncation, 16 products at a time: over D = 4096 that shrinks a logit by some 5e-6 of itself.  So a tile's
@@ -43,13 +44,14 @@ constexpr int H_STAGING_BYTES = H_EPILOGUE_WARPS * kStoreBytes;
 constexpr int H_BARRIER_BYTES = 256;
 constexpr size_t H_SMEM = 1024 + static_cast<size_t>(H_STAGES) * H_STAGE_BYTES + H_STAGING_BYTES + H_BARRIER_BYTES;
 
-enum HeadRole { HEAD_STATS = 0, HEAD_GRADIENT = 1 };
+enum HeadRole { HEAD_STATS = 0, HEAD_GRADIENT = 1, DISTILL_STATS = 2, DISTILL_GRADIENT = 3 };
 
 template <int ROLE>
 __global__ void __launch_bounds__(H_THREADS, 1)
 head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmG,
                  const HeadTile h, int* __restrict__ status)
 {
+    constexpr bool STORES = ROLE == HEAD_GRADIENT || ROLE == DISTILL_GRADIENT, LISTS = ROLE == DISTILL_STATS || ROLE == DISTILL_GRADIENT;
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t rank = cluster.block_rank();              // 0 = leader
@@ -86,7 +88,7 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
         fence_mbar_init();
         prefetch_tensormap(&tmX);
         prefetch_tensormap(&tmW);
-        if (ROLE == HEAD_GRADIENT) prefetch_tensormap(&tmG);
+        if (STORES) prefetch_tensormap(&tmG);
     }
     if (warp == 1) {
         tmem_alloc_pair(smem_u32(tmem_slot), 2 * H_BN);
@@ -173,6 +175,11 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
             const int row0 = t0.m0 + static_cast<int>(rank) * H_BM + quarter * 32, row = row0 + lane;
             const int col0 = t0.n0 + half * 128, valid = h.cols - col0;
             uint32_t l[4][32];                               // fp32 bits
+            EntryWalk walk;                                  // its first entry is on its way while the products run
+            if (LISTS) {
+                walk.none();
+                if (row < h.N && valid > 0 && h.target[row] >= 0) walk.start(h.e, h.e.order[row], h.v0 + col0, 128);
+            }
             for (int k0 = 0; k0 < kblocks; k0 += kHeadSegment, ++seg) {
                 const uint32_t acc = seg & 1u, aph = (seg >> 1) & 1u;
                 if (!mbar_wait_warp(tfull + 8 * acc, aph, abort_flag, 256)) { failed = true; break; }
@@ -202,8 +209,16 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
             }
             if (failed || valid <= 0) continue;
             const bool in = row < h.N;
-            const int t = in ? h.target[row] - h.v0 - col0 : -1;                // in this warp's columns: 0 .. 127
-            if (ROLE == HEAD_STATS) {
+            if (LISTS && h.e.inverse_t != 1.f) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(__uint_as_float(l[c][i]) * h.e.inverse_t);
+            }
+            // Entries: this lane's 32 values through the warp's block of shared memory, a column of it that only this lane touches.
+            float* turn = reinterpret_cast<float*>(smem_raw + (block - raw)) + lane;
+            const int t = !LISTS && in ? h.target[row] - h.v0 - col0 : -1;                // in this warp's columns: 0 .. 127
+            if (!STORES) {
                 if (valid < 128) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
@@ -216,8 +231,17 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) m = fmaxf(m, __uint_as_float(l[c][i]));
-                const bool hit = t >= 0 && t < 128;
-                if (__any_sync(0xffffffffu, hit)) {
+                if (LISTS && __any_sync(0xffffffffu, walk.column != kNoColumn)) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (__any_sync(0xffffffffu, walk.column < 32 * c + 32)) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) turn[32 * i] = __uint_as_float(l[c][i]);
+                            for (; walk.column < 32 * c + 32; walk.next()) h.e.at[walk.list - h.e.entries + walk.j] = turn[32 * (walk.column - 32 * c)];
+                        }
+                }
+                const bool hit = !LISTS && t >= 0 && t < 128;
+                if (!LISTS && __any_sync(0xffffffffu, hit)) {
                     float x = 0.f;
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
@@ -246,7 +270,7 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                 if (in) h.running[static_cast<int64_t>((t0.n0 >> 7) + half) * h.N + row] = make_float2(m, sum);
             } else {
                 const bool is = in && h.target[row] >= 0;
-                const float g = is ? h.scale[row] : 0.f, lse = is ? h.lse[row] : 0.f;
+                const float g = is ? (LISTS ? h.scale[row] * h.e.inverse_t : h.scale[row]) : 0.f, lse = is ? h.lse[row] : 0.f;
                 float z = -lse * kHeadLog2e, lost = fmaf(-lse, kHeadLog2e, -z);                    // as for the statistics
                 if (__any_sync(0xffffffffu, fabsf(lost) > kHeadLost)) {
 #pragma unroll
@@ -255,12 +279,25 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                         for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(__uint_as_float(l[c][i]) - lse);
                     z = lost = 0.f;
                 }
-                const float gp = g * (1.f + lost * 0.69314718f);
+                const float mass = LISTS ? (is ? h.e.mass[h.e.order[row]] : 0.f) : 1.f;
+                const float gp = (LISTS ? g * mass : g) * (1.f + lost * 0.69314718f);
+                if (LISTS && __any_sync(0xffffffffu, walk.column != kNoColumn)) {
+                    if (lane == 0) bulk_wait_read();         // the last tile's outputs are out of the block
+                    __syncwarp();
+                }
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(head_exp2(fmaf(__uint_as_float(l[c][i]), kHeadLog2e, z)) * gp);
-                    if (__any_sync(0xffffffffu, t >= 32 * c && t < 32 * c + 32)) {
+                    if (LISTS) {
+                        if (__any_sync(0xffffffffu, walk.column < 32 * c + 32)) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) turn[32 * i] = __uint_as_float(l[c][i]);
+                            for (; walk.column < 32 * c + 32; walk.next()) turn[32 * (walk.column - 32 * c)] -= g * walk.p;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(turn[32 * i]);
+                        }
+                    } else if (__any_sync(0xffffffffu, t >= 32 * c && t < 32 * c + 32)) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             if (t == 32 * c + i) l[c][i] = __float_as_uint(__uint_as_float(l[c][i]) - g);
@@ -276,7 +313,7 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                         store_block(&tmG, block, *reinterpret_cast<uint32_t(*)[2][32]>(&l[2 * b]), col0 + 64 * b, row0, lane);
             }
         }
-        if (ROLE == HEAD_GRADIENT && !failed) {
+        if (STORES && !failed) {
             // Zeros for the row blocks that no tile has: a block of them, stored as often as it takes.
             if (lane == 0) bulk_wait_read();
             __syncwarp();
@@ -290,7 +327,7 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                 for (int i = blockIdx.x * H_EPILOGUE_WARPS + (warp - 2); i < blocks; i += gridDim.x * H_EPILOGUE_WARPS)
                     tma_store_2d(&tmG, block, i % blocks_n * 64, (first + i / blocks_n) * 32);
         }
-        if (ROLE == HEAD_GRADIENT && lane == 0) bulk_wait_all();
+        if (STORES && lane == 0) bulk_wait_all();
         if (failed) *abort_flag = 1;
     }
     if (failed && status) atomicExch(status, VELORA_ERR_TIMEOUT);
@@ -353,9 +390,11 @@ int launch_head_tiles(const void* x, int64_t ldx, const void* W, int64_t ldw, vo
     if (G) {
         rc = make_tmap_bf16_2d(&tg, G, ldg, h.N, ldg, 64, 32);              // whole pitch: columns past the piece's are written as well
         if (rc != VELORA_OK) return rc;
-        return launch_role<HEAD_GRADIENT>(tx, tw, tg, h, status, di.sm_count, stream);
+        return h.e.entries ? launch_role<DISTILL_GRADIENT>(tx, tw, tg, h, status, di.sm_count, stream)
+                           : launch_role<HEAD_GRADIENT>(tx, tw, tg, h, status, di.sm_count, stream);
     }
-    return launch_role<HEAD_STATS>(tx, tw, tg, h, status, di.sm_count, stream);
+    return h.e.entries ? launch_role<DISTILL_STATS>(tx, tw, tg, h, status, di.sm_count, stream)
+                       : launch_role<HEAD_STATS>(tx, tw, tg, h, status, di.sm_count, stream);
 }
 
 }  // namespace velora
