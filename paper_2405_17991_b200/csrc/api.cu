@@ -250,7 +250,7 @@ int check_rows(const void* p, int64_t ld, int dtype, int64_t D, bool may)
     return elem_aligned(p, dtype) ? VELORA_OK : VELORA_ERR_ALIGNMENT;
 }
 
-size_t norm_grad_bytes(int64_t N, int64_t D) { return kStatusBytes + align256(2 * static_cast<size_t>(norm_slices(N)) * static_cast<size_t>(D) * sizeof(float)); }
+size_t norm_grad_bytes(int64_t N, int64_t D) { return kStatusBytes + align256(2 * static_cast<size_t>(norm_slices(N)) * static_cast<size_t>(norm_pitch(D)) * sizeof(float)); }
 
 }  // namespace
 }  // namespace velora

@@ -1,185 +1,211 @@
-// Layer norm of rows, with a residual added in front, and its gradients.
-//   h = x + r (rounded to the rows' type),  m = mean h,  s = 1 / sqrt(mean (h - m)^2 + eps),  xhat = (h - m) s,  y = xhat w + b
-//   c = dy w,  dx = dh + s (c - mean c - xhat mean(c xhat)),  dw = sum_n dy xhat,  db = sum_n dy
-// Statistics and sums are fp32; the variance is taken about the mean.
-#include "layer_norm.cuh"
+// Layer norm of rows, with a residual added in front.
+//   h = x + r (rounded to the rows' type),  m = mean h,  s = 1 / sqrt(mean (h - m)^2 + eps),  y = (h - m) s w + b
+// Bound by HBM: x (and r) once in, y (and h) once out.  A row is held in the registers of a warp (up to 1024 columns) or of a block while its mean and its
+// variance about the mean are taken; blocks walk over rows, the weights stay in registers, and the next rows are on their way to shared memory meanwhile.
+// A warp takes its own columns' mean and squares about it, and the block puts those together (n, sum and squares of each warp), so that a row costs one
+// barrier and nothing is lost to a mean that is large beside the deviation.
+#include "layer_norm_rows.cuh"
 
 namespace velora {
 
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kWarps = kThreads / 32;
+struct Rows {
+    int stages;                                                // rows on their way or in use
+    int stage_bytes;                                           // of a row (of a block's, or of a warp's)
+    bool wide;                                                 // weights on 16-byte boundaries
+};
 
-__device__ __forceinline__ float load_param(const void* p, int dtype, int d, float none)
+template <typename T, int WARPS, int C, bool VEC, int BLOCKS>
+__global__ void __launch_bounds__((RowShape<WARPS, C>::kThreads), BLOCKS)
+norm_rows_kernel(const NormArgs a, const Rows rows)
 {
-    if (!p) return none;
-    return dtype == VELORA_BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[d]) : static_cast<const float*>(p)[d];
-}
-__device__ __forceinline__ void store_param(void* p, int dtype, int d, float x, int beta)
-{
-    if (dtype == VELORA_BF16) {
-        __nv_bfloat16* q = static_cast<__nv_bfloat16*>(p) + d;
-        *q = __float2bfloat16_rn(beta ? __bfloat162float(*q) + x : x);
-    } else {
-        float* q = static_cast<float*>(p) + d;
-        *q = beta ? *q + x : x;
-    }
-}
-
-// Sums over the block, the same in every thread.
-__device__ __forceinline__ float2 block_sum(float x, float y, float2* part)
-{
+    typedef RowShape<WARPS, C> S;
+    constexpr int P = S::kPerRow;
+    extern __shared__ __align__(16) char ring[];
+    __shared__ float4 part[2][WARPS];                          // sum, squares about the warp's mean, that mean, number of columns
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = threadIdx.x % P;
+    const int D = a.D;
+    const float inverse = 1.f / static_cast<float>(D);
+    // This thread's columns, this warp's.
+    int mine = 0;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        x += __shfl_xor_sync(0xffffffffu, x, o);
-        y += __shfl_xor_sync(0xffffffffu, y, o);
-    }
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = make_float2(x, y);
-    __syncthreads();
-    float2 s = make_float2(0.f, 0.f);
-    for (int w = 0; w < kWarps; ++w) {
-        s.x += part[w].x;
-        s.y += part[w].y;
-    }
-    return s;
-}
-
-template <typename T> __device__ __forceinline__ float rounded(float x) { T t; Elem<T>::store(&t, x); return Elem<T>::load(&t); }
-
-// A block per row, three times over it.
-template <typename T>
-__global__ void __launch_bounds__(kThreads)
-norm_any_kernel(const NormArgs a)
-{
-    __shared__ float2 part[kWarps];
+    for (int c = 0; c < C; ++c) mine += min(8, max(0, chunk_left<VEC, P>(c, t, D)));
+    const int count = __reduce_add_sync(0xffffffffu, mine);
+    const float n_warp = static_cast<float>(count), inverse_warp = count > 0 ? 1.f / n_warp : 0.f;
     pdl_wait();
     pdl_trigger();
-    const float inverse = 1.f / static_cast<float>(a.D);
-    for (int64_t n = blockIdx.x; n < a.N; n += gridDim.x) {
-        const T* x = static_cast<const T*>(a.X) + n * a.ldx;
-        const T* r = a.R ? static_cast<const T*>(a.R) + n * a.ldr : nullptr;
-        T* h = a.H ? static_cast<T*>(a.H) + n * a.ldh : nullptr;
+
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * S::kRows + (WARPS == 1 ? warp : 0), step = static_cast<int64_t>(gridDim.x) * S::kRows;
+    const T* X = static_cast<const T*>(a.X);
+    const T* R = static_cast<const T*>(a.R);
+    constexpr int kShare = Share<T, C>::kWords * P * 16;
+    char* own = ring + (WARPS == 1 ? warp * rows.stages * rows.stage_bytes : 0) + t * 16;
+    const uint32_t own_at = static_cast<uint32_t>(__cvta_generic_to_shared(own));
+    auto fetch = [&](int64_t n, int slot) {
+        if (n < a.N) {
+            Share<T, C>::template copy<P>(own_at + slot * rows.stage_bytes, X + n * a.ldx, D, t);
+            if (R) Share<T, C>::template copy<P>(own_at + slot * rows.stage_bytes + kShare, R + n * a.ldr, D, t);
+        }
+        copies_commit();                                       // a row that is not there is an empty one
+    };
+    if (VEC)
+        for (int s = 0; s < rows.stages - 1; ++s) fetch(first + s * step, s);
+    float w[C][8], b[C][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        load_params<VEC, P>(w[c], a.w, a.p_dtype, rows.wide, c, t, D, 1.f);
+        load_params<VEC, P>(b[c], a.b, a.p_dtype, rows.wide, c, t, D, 0.f);
+    }
+    int slot = 0, buffer = 0;
+    for (int64_t n = first; n < a.N; n += step, slot = slot + 1 == rows.stages ? 0 : slot + 1, buffer ^= 1) {
+        float x[C][8];
+        if (VEC) {
+            fetch(n + (rows.stages - 1) * step, slot == 0 ? rows.stages - 1 : slot - 1);
+            copies_wait(rows.stages - 1);
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                if (chunk_left<VEC, P>(c, t, D) > 0) {          // else nothing was copied
+
+                    Share<T, C>::template load<P>(x[c], own + slot * rows.stage_bytes, c);
+                    if (R) {
+                        float r[8];
+                        Share<T, C>::template load<P>(r, own + slot * rows.stage_bytes + kShare, c);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[c][e] = rounded<T>(x[c][e] + r[e]);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[c][e] = 0.f;
+                }
+            }
+        } else {
+            const T* p = X + n * a.ldx + t;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int left = chunk_left<VEC, P>(c, t, D);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[c][e] = e < left ? Elem<T>::load(p + (c * 8 + e) * P) : 0.f;
+            }
+            if (R) {
+                const T* q = R + n * a.ldr + t;
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    const int left = chunk_left<VEC, P>(c, t, D);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e < left) x[c][e] = rounded<T>(x[c][e] + Elem<T>::load(q + (c * 8 + e) * P));
+                }
+            }
+        }
+        float sum = 0.f;                                       // columns that are not there hold zeros
+#pragma unroll
+        for (int c = 0; c < C; ++c) sum += sum8(x[c]);
+        sum = lanes_sum(sum);
+        const float m_warp = sum * inverse_warp;
+        float squares = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int left = chunk_left<VEC, P>(c, t, D);
+            if (left < 8) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e >= left) x[c][e] = m_warp;
+            }
+            float q[2] = {0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = x[c][e] - m_warp;
+                q[e & 1] = fmaf(d, d, q[e & 1]);
+            }
+            squares += q[0] + q[1];
+        }
+        squares = lanes_sum(squares);
+        float m = m_warp;
+        if (WARPS > 1) {
+            if (lane == 0) part[buffer][warp] = make_float4(sum, squares, m_warp, n_warp);
+            __syncthreads();                                   // the other buffer's readers are past the barrier before
+            float all = 0.f;
+#pragma unroll 4
+            for (int i = 0; i < WARPS; ++i) all += part[buffer][i].x;
+            m = all * inverse;
+            squares = 0.f;
+#pragma unroll 2
+            for (int i = 0; i < WARPS; ++i) {                  // few in registers at a time
+
+                const float4 v = part[buffer][i];
+                squares += fmaf(v.w * (v.z - m), v.z - m, v.y);
+            }
+        }
+        const float s = 1.f / sqrtf(squares * inverse + a.eps);
         T* y = static_cast<T*>(a.Y) + n * a.ldy;
-        auto value = [&](int d) { return r ? rounded<T>(Elem<T>::load(x + d) + Elem<T>::load(r + d)) : Elem<T>::load(x + d); };
-        float sum = 0.f;
-        for (int d = threadIdx.x; d < a.D; d += kThreads) sum += value(d);
-        const float m = block_sum(sum, 0.f, part).x * inverse;
-        sum = 0.f;
-        for (int d = threadIdx.x; d < a.D; d += kThreads) {
-            const float c = value(d) - m;
-            sum += c * c;
+        T* h = a.H ? static_cast<T*>(a.H) + n * a.ldh : nullptr;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float o[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = fmaf((x[c][e] - m) * s, w[c][e], b[c][e]);
+            const int left = chunk_left<VEC, P>(c, t, D), col = column_of<VEC, P>(c, 0, t);
+            if (VEC) {
+                if (left > 0) {
+                    if (h) store_chunk(h + col, x[c], left);
+                    store_chunk(y + col, o, left);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e < left) {
+                        if (h) Elem<T>::store(h + col + e * P, x[c][e]);
+                        Elem<T>::store(y + col + e * P, o[e]);
+                    }
+            }
         }
-        const float s = 1.f / sqrtf(block_sum(sum, 0.f, part).x * inverse + a.eps);
-        for (int d = threadIdx.x; d < a.D; d += kThreads) {
-            const float v = value(d);
-            if (h) Elem<T>::store(h + d, v);
-            Elem<T>::store(y + d, (v - m) * s * load_param(a.w, a.p_dtype, d, 1.f) + load_param(a.b, a.p_dtype, d, 0.f));
-        }
-        if (threadIdx.x == 0) {
+        if (t == 0) {
             if (a.mean) a.mean[n] = m;
             if (a.rstd) a.rstd[n] = s;
         }
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads)
-norm_grad_any_kernel(const NormGradArgs a)
+template <typename T, int WARPS, int C, bool VEC, int BLOCKS>
+int launch_rows(const NormArgs& a, int sm_count, cudaStream_t stream)
 {
-    __shared__ float2 part[kWarps];
-    pdl_wait();
-    pdl_trigger();
-    const float inverse = 1.f / static_cast<float>(a.D);
-    for (int64_t n = blockIdx.x; n < a.N; n += gridDim.x) {
-        const T* dy = static_cast<const T*>(a.dY) + n * a.lddy;
-        const T* h = static_cast<const T*>(a.H) + n * a.ldh;
-        const T* dh = a.dH ? static_cast<const T*>(a.dH) + n * a.lddh : nullptr;
-        T* dx = static_cast<T*>(a.dX) + n * a.lddx;
-        const float m = a.mean[n], s = a.rstd[n];
-        float sum = 0.f, along = 0.f;
-        for (int d = threadIdx.x; d < a.D; d += kThreads) {
-            const float c = Elem<T>::load(dy + d) * load_param(a.w, a.p_dtype, d, 1.f);
-            sum += c;
-            along += c * ((Elem<T>::load(h + d) - m) * s);
-        }
-        const float2 t = block_sum(sum, along, part);
-        const float mean_c = t.x * inverse, mean_cx = t.y * inverse;
-        for (int d = threadIdx.x; d < a.D; d += kThreads) {
-            const float c = Elem<T>::load(dy + d) * load_param(a.w, a.p_dtype, d, 1.f);
-            const float g = s * (c - mean_c - (Elem<T>::load(h + d) - m) * s * mean_cx);
-            Elem<T>::store(dx + d, dh ? Elem<T>::load(dh + d) + g : g);
-        }
+    typedef RowShape<WARPS, C> S;
+    static DeviceOnce configured;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return VELORA_ERR_CUDA;
+    constexpr int kBudget = 216 * 1024 / BLOCKS;               // shared memory of a block, so that BLOCKS of them fit
+    auto kern = norm_rows_kernel<T, WARPS, C, VEC, BLOCKS>;
+    if (!configured.get(dev)) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBudget) != cudaSuccess) return VELORA_ERR_CUDA;
+        configured.set(dev);
     }
+    Rows rows{};
+    rows.stage_bytes = Share<T, C>::kWords * S::kPerRow * 16 * (a.R ? 2 : 1);
+    const int fit = kBudget / (rows.stage_bytes * S::kRows);
+    rows.stages = fit < 2 ? 2 : (fit > 4 ? 4 : fit);
+    static_assert(2 * Share<T, C>::kWords * S::kPerRow * 16 * S::kRows * 2 <= kBudget, "two rows of both operands");
+    rows.wide = aligned16(a.w) && aligned16(a.b);
+    const int64_t blocks = ceil_div64(a.N, S::kRows), most = static_cast<int64_t>(sm_count) * BLOCKS;
+    return launch_chained(kern, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), S::kThreads,
+                          VEC ? static_cast<size_t>(rows.stages) * rows.stage_bytes * S::kRows : 0, stream, a, rows);
 }
 
-// Sums over a slice of the rows: a thread a column.
-template <typename T>
-__global__ void __launch_bounds__(kThreads)
-norm_columns_kernel(const NormGradArgs a, int slices)
+template <typename T, bool VEC>
+int launch_held(const NormArgs& a, int sm_count, cudaStream_t stream)
 {
-    pdl_wait();
-    pdl_trigger();
-    const int d = blockIdx.x * kThreads + threadIdx.x, slice = blockIdx.y;
-    if (d >= a.D) return;
-    const int64_t n0 = a.N * slice / slices, n1 = a.N * (slice + 1) / slices;
-    float dw = 0.f, db = 0.f;
-    for (int64_t n = n0; n < n1; ++n) {
-        const float dy = Elem<T>::load(static_cast<const T*>(a.dY) + n * a.lddy + d);
-        dw += dy * ((Elem<T>::load(static_cast<const T*>(a.H) + n * a.ldh + d) - a.mean[n]) * a.rstd[n]);
-        db += dy;
-    }
-    a.partials[static_cast<int64_t>(slice) * a.D + d] = dw;
-    a.partials[static_cast<int64_t>(slices + slice) * a.D + d] = db;
+    if (a.D <= 256) return launch_rows<T, 1, 1, VEC, 4>(a, sm_count, stream);
+    if (a.D <= 512) return launch_rows<T, 1, 2, VEC, 3>(a, sm_count, stream);
+    if (a.D <= 768) return launch_rows<T, 1, 3, VEC, 2>(a, sm_count, stream);
+    if (a.D <= 1024) return launch_rows<T, 1, 4, VEC, sizeof(T) == 2 ? 2 : 1>(a, sm_count, stream);
+    if (a.D <= 2048) return launch_rows<T, 4, 2, VEC, 6>(a, sm_count, stream);
+    if (a.D <= 4096) return launch_rows<T, 8, 2, VEC, 3>(a, sm_count, stream);
+    if (a.D <= 6144) return launch_rows<T, 8, 3, VEC, 2>(a, sm_count, stream);
+    if (a.D <= 8192) return launch_rows<T, 16, 2, VEC, 1>(a, sm_count, stream);
+    return launch_rows<T, 16, 3, VEC, 1>(a, sm_count, stream);
 }
 
-// The slices' sums in a fixed order: a block takes 32 columns of dw or db, a warp every eighth slice.
-__global__ void __launch_bounds__(256)
-norm_slices_kernel(const float* partials, int slices, int D, void* dw, void* db, int dtype, int beta)
-{
-    __shared__ float part[8][32];
-    pdl_wait();
-    pdl_trigger();
-    void* out = blockIdx.y ? db : dw;
-    if (!out) return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = blockIdx.x * 32 + lane;
-    const float* p = partials + static_cast<int64_t>(blockIdx.y) * slices * D + d;
-    float s = 0.f;
-    if (d < D)
-#pragma unroll 8
-        for (int i = warp; i < slices; i += 8) s += p[static_cast<int64_t>(i) * D];
-    part[warp][lane] = s;
-    __syncthreads();
-    if (warp != 0 || d >= D) return;
-    s = 0.f;
-    for (int w = 0; w < 8; ++w) s += part[w][lane];
-    store_param(out, dtype, d, s, beta);
-}
-
-template <typename T>
-int norm_any(const NormArgs& a, int sm_count, cudaStream_t stream)
-{
-    const int64_t most = static_cast<int64_t>(sm_count) * 4;
-    return launch_chained(norm_any_kernel<T>, dim3(static_cast<unsigned>(a.N < most ? a.N : most)), kThreads, 0, stream, a);
-}
-
-template <typename T>
-int norm_grad_any(const NormGradArgs& a, int sm_count, cudaStream_t stream)
-{
-    if (a.dw || a.db) {                                       // first: dX may lie where dY or H does
-        const int slices = static_cast<int>(norm_slices(a.N));
-        int rc = launch_chained(norm_columns_kernel<T>, dim3(static_cast<unsigned>(ceil_div64(a.D, kThreads)), static_cast<unsigned>(slices)), kThreads, 0,
-                                stream, a, slices);
-        if (rc != VELORA_OK) return rc;
-        rc = launch_chained(norm_slices_kernel, dim3(static_cast<unsigned>(ceil_div64(a.D, 32)), 2), 256, 0, stream, a.partials, slices, a.D, a.dw, a.db,
-                            a.dw_dtype, a.beta);
-        if (rc != VELORA_OK) return rc;
-    }
-    if (!a.dX) return VELORA_OK;
-    const int64_t most = static_cast<int64_t>(sm_count) * 4;
-    return launch_chained(norm_grad_any_kernel<T>, dim3(static_cast<unsigned>(a.N < most ? a.N : most)), kThreads, 0, stream, a);
-}
+bool rows_vec(const void* p, int64_t ld, int dtype) { return !p || (aligned16(p) && ld * static_cast<int64_t>(dtype_size(dtype)) % 16 == 0); }
 
 }  // namespace
 
@@ -188,15 +214,11 @@ int launch_layer_norm(const NormArgs& a, cudaStream_t stream)
     DeviceInfo di;
     const int rc = device_info(&di);
     if (rc != VELORA_OK) return rc;
-    return a.dtype == VELORA_BF16 ? norm_any<__nv_bfloat16>(a, di.sm_count, stream) : norm_any<float>(a, di.sm_count, stream);
-}
-
-int launch_layer_norm_backward(const NormGradArgs& a, cudaStream_t stream)
-{
-    DeviceInfo di;
-    const int rc = device_info(&di);
-    if (rc != VELORA_OK) return rc;
-    return a.dtype == VELORA_BF16 ? norm_grad_any<__nv_bfloat16>(a, di.sm_count, stream) : norm_grad_any<float>(a, di.sm_count, stream);
+    if (a.D > 12288) return launch_layer_norm_any(a, di.sm_count, stream);
+    const bool vec = rows_vec(a.X, a.ldx, a.dtype) && rows_vec(a.R, a.ldr, a.dtype) && rows_vec(a.H, a.ldh, a.dtype) && rows_vec(a.Y, a.ldy, a.dtype);
+    if (a.dtype == VELORA_BF16)
+        return vec ? launch_held<__nv_bfloat16, true>(a, di.sm_count, stream) : launch_held<__nv_bfloat16, false>(a, di.sm_count, stream);
+    return vec ? launch_held<float, true>(a, di.sm_count, stream) : launch_held<float, false>(a, di.sm_count, stream);
 }
 
 }  // namespace velora

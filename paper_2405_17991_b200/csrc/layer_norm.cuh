@@ -45,12 +45,42 @@ struct NormGradArgs {
     int dtype;
     int64_t N;
     int D;
-    float* partials;                // [2][slices][D]: sums of some rows each, for dw and for db
+    float* partials;                // [2][slices][norm_pitch(D)]: sums of some rows each, for dw and for db
 };
 
+#ifdef __CUDACC__
+__host__ __device__
+#endif
+inline int64_t norm_pitch(int64_t D) { return (D + 7) / 8 * 8; }
 // Rows of `partials`, at most.
 constexpr int kNormSlices = 296;
 inline int64_t norm_slices(int64_t N) { return N < kNormSlices ? N : kNormSlices; }
+
+// Rows of any length (layer_norm_any.cu).
+int launch_layer_norm_any(const NormArgs& a, int sm_count, cudaStream_t stream);
+int launch_layer_norm_backward_any(const NormGradArgs& a, int sm_count, cudaStream_t stream);
+// dw and db = beta .. + the sums of `partials` over so many slices.
+int launch_norm_slices(const NormGradArgs& a, int slices, cudaStream_t stream);
+
+#ifdef __CUDACC__
+__device__ __forceinline__ float load_param(const void* p, int dtype, int d, float none)
+{
+    if (!p) return none;
+    return dtype == VELORA_BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[d]) : static_cast<const float*>(p)[d];
+}
+__device__ __forceinline__ void store_param(void* p, int dtype, int d, float x, int beta)
+{
+    if (dtype == VELORA_BF16) {
+        __nv_bfloat16* q = static_cast<__nv_bfloat16*>(p) + d;
+        *q = __float2bfloat16_rn(beta ? __bfloat162float(*q) + x : x);
+    } else {
+        float* q = static_cast<float*>(p) + d;
+        *q = beta ? *q + x : x;
+    }
+}
+
+template <typename T> __device__ __forceinline__ float rounded(float x) { T t; Elem<T>::store(&t, x); return Elem<T>::load(&t); }
+#endif
 
 int launch_layer_norm(const NormArgs& a, cudaStream_t stream);
 int launch_layer_norm_backward(const NormGradArgs& a, cudaStream_t stream);
