@@ -10,19 +10,20 @@ namespace velora {
 
 namespace {
 
-struct Rows {
-    int stages;                                                // rows on their way or in use
-    int stage_bytes;                                           // of a row (of a block's, or of a warp's)
-    bool wide;                                                 // weights on 16-byte boundaries
-};
+// 1 / sqrt(v): the approximation and one step of Newton's method, where that has a meaning.
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const float r = rsqrtf(v), e = fmaf(-v * r, r, 1.f);
+    return v > 1e-37f && v < 1e37f ? fmaf(0.5f * r, e, r) : 1.f / sqrtf(v);
+}
 
 template <typename T, int WARPS, int C, bool VEC, int BLOCKS>
 __global__ void __launch_bounds__((RowShape<WARPS, C>::kThreads), BLOCKS)
-norm_rows_kernel(const NormArgs a, const Rows rows)
+norm_rows_kernel(const NormArgs a, const Ring ring)
 {
     typedef RowShape<WARPS, C> S;
-    constexpr int P = S::kPerRow;
-    extern __shared__ __align__(16) char ring[];
+    constexpr int P = S::kPerRow, kShare = kShareBytes<T, WARPS, C, VEC>;
+    extern __shared__ __align__(16) char ring_bytes[];
     __shared__ float4 part[2][WARPS];                          // sum, squares about the warp's mean, that mean, number of columns
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = threadIdx.x % P;
     const int D = a.D;
@@ -31,134 +32,105 @@ norm_rows_kernel(const NormArgs a, const Rows rows)
     int mine = 0;
 #pragma unroll
     for (int c = 0; c < C; ++c) mine += min(8, max(0, chunk_left<VEC, P>(c, t, D)));
-    const int count = __reduce_add_sync(0xffffffffu, mine);
-    const float n_warp = static_cast<float>(count), inverse_warp = count > 0 ? 1.f / n_warp : 0.f;
+    const float n_warp = static_cast<float>(__reduce_add_sync(0xffffffffu, mine)), inverse_warp = n_warp > 0.f ? 1.f / n_warp : 0.f;
     pdl_wait();
     pdl_trigger();
 
     const int64_t first = static_cast<int64_t>(blockIdx.x) * S::kRows + (WARPS == 1 ? warp : 0), step = static_cast<int64_t>(gridDim.x) * S::kRows;
-    const T* X = static_cast<const T*>(a.X);
-    const T* R = static_cast<const T*>(a.R);
-    constexpr int kShare = Share<T, C>::kWords * P * 16;
-    char* own = ring + (WARPS == 1 ? warp * rows.stages * rows.stage_bytes : 0) + t * 16;
-    const uint32_t own_at = static_cast<uint32_t>(__cvta_generic_to_shared(own));
+    const RowSource<T, WARPS, C, VEC> X{static_cast<const T*>(a.X), a.ldx}, R{static_cast<const T*>(a.R), a.ldr};
+    const bool residual = a.R != nullptr;
+    char* slots = ring_bytes + (WARPS == 1 ? warp * ring.stages * ring.stage_bytes : 0);
+    const uint32_t slots_at = static_cast<uint32_t>(__cvta_generic_to_shared(slots));
     auto fetch = [&](int64_t n, int slot) {
         if (n < a.N) {
-            Share<T, C>::template copy<P>(own_at + slot * rows.stage_bytes, X + n * a.ldx, D, t);
-            if (R) Share<T, C>::template copy<P>(own_at + slot * rows.stage_bytes + kShare, R + n * a.ldr, D, t);
+            const int at = slot * ring.stage_bytes;
+            X.copy(slots + at, slots_at + at, n, D, t);
+            if (residual) R.copy(slots + at + kShare, slots_at + at + kShare, n, D, t);
         }
         copies_commit();                                       // a row that is not there is an empty one
     };
-    if (VEC)
-        for (int s = 0; s < rows.stages - 1; ++s) fetch(first + s * step, s);
-    float w[C][8], b[C][8];
+    for (int s = 0; s < ring.stages - 1; ++s) fetch(first + s * step, s);
+    F2 w[C][4], b[C][4];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        load_params<VEC, P>(w[c], a.w, a.p_dtype, rows.wide, c, t, D, 1.f);
-        load_params<VEC, P>(b[c], a.b, a.p_dtype, rows.wide, c, t, D, 0.f);
+        load_params<VEC, P>(w[c], a.w, a.p_dtype, ring.wide, c, t, D, 1.f);
+        load_params<VEC, P>(b[c], a.b, a.p_dtype, ring.wide, c, t, D, 0.f);
     }
     int slot = 0, buffer = 0;
-    for (int64_t n = first; n < a.N; n += step, slot = slot + 1 == rows.stages ? 0 : slot + 1, buffer ^= 1) {
-        float x[C][8];
+    for (int64_t n = first; n < a.N; n += step, slot = slot + 1 == ring.stages ? 0 : slot + 1, buffer ^= 1) {
+        const int before = slot == 0 ? ring.stages - 1 : slot - 1;
         if (VEC) {
-            fetch(n + (rows.stages - 1) * step, slot == 0 ? rows.stages - 1 : slot - 1);
-            copies_wait(rows.stages - 1);
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                if (chunk_left<VEC, P>(c, t, D) > 0) {          // else nothing was copied
-
-                    Share<T, C>::template load<P>(x[c], own + slot * rows.stage_bytes, c);
-                    if (R) {
-                        float r[8];
-                        Share<T, C>::template load<P>(r, own + slot * rows.stage_bytes + kShare, c);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[c][e] = rounded<T>(x[c][e] + r[e]);
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[c][e] = 0.f;
-                }
-            }
+            fetch(n + (ring.stages - 1) * step, before);
+            copies_wait(ring.stages - 1);
         } else {
-            const T* p = X + n * a.ldx + t;
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const int left = chunk_left<VEC, P>(c, t, D);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[c][e] = e < left ? Elem<T>::load(p + (c * 8 + e) * P) : 0.f;
-            }
-            if (R) {
-                const T* q = R + n * a.ldr + t;
-#pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    const int left = chunk_left<VEC, P>(c, t, D);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (e < left) x[c][e] = rounded<T>(x[c][e] + Elem<T>::load(q + (c * 8 + e) * P));
-                }
-            }
+            copies_wait(ring.stages - 2);
+            row_barrier<WARPS>();
+            fetch(n + (ring.stages - 1) * step, before);
         }
+        const char* row = slots + slot * ring.stage_bytes;
+        T* h = a.H ? static_cast<T*>(a.H) + n * a.ldh : nullptr;
+        F2 x[C][4];
         float sum = 0.f;                                       // columns that are not there hold zeros
 #pragma unroll
-        for (int c = 0; c < C; ++c) sum += sum8(x[c]);
-        sum = lanes_sum(sum);
+        for (int c = 0; c < C; ++c) {
+            const int left = chunk_left<VEC, P>(c, t, D);
+            if (left > 0) {                                    // else nothing was copied
+                X.load(x[c], row, n, c, t, left);
+                if (residual) {
+                    F2 r[4];
+                    R.load(r, row + kShare, n, c, t, left);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        x[c][i] = add(x[c][i], r[i]);
+                        if (sizeof(T) == 2) x[c][i] = of_bf16(to_bf16(x[c][i]));
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[c][i] = f2(0.f, 0.f);
+            }
+            sum += sum8(x[c][0], x[c][1], x[c][2], x[c][3]);
+        }
+        sum = lanes_sum<32>(sum);
         const float m_warp = sum * inverse_warp;
-        float squares = 0.f;
+        const F2 minus_warp = f2(-m_warp, -m_warp);
+        F2 q[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int left = chunk_left<VEC, P>(c, t, D);
             if (left < 8) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e >= left) x[c][e] = m_warp;
+                for (int i = 0; i < 4; ++i) {
+                    const float2 v = parts(x[c][i]);
+                    x[c][i] = f2(2 * i < left ? v.x : m_warp, 2 * i + 1 < left ? v.y : m_warp);
+                }
             }
-            float q[2] = {0.f, 0.f};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float d = x[c][e] - m_warp;
-                q[e & 1] = fmaf(d, d, q[e & 1]);
+            for (int i = 0; i < 4; ++i) {
+                const F2 d = add(x[c][i], minus_warp);
+                q[i & 1] = fma(d, d, q[i & 1]);
             }
-            squares += q[0] + q[1];
         }
-        squares = lanes_sum(squares);
-        float m = m_warp;
+        const float2 both = parts(add(q[0], q[1]));
+        float squares = lanes_sum<32>(both.x + both.y), m = m_warp;
         if (WARPS > 1) {
             if (lane == 0) part[buffer][warp] = make_float4(sum, squares, m_warp, n_warp);
             __syncthreads();                                   // the other buffer's readers are past the barrier before
-            float all = 0.f;
-#pragma unroll 4
-            for (int i = 0; i < WARPS; ++i) all += part[buffer][i].x;
-            m = all * inverse;
-            squares = 0.f;
-#pragma unroll 2
-            for (int i = 0; i < WARPS; ++i) {                  // few in registers at a time
-
-                const float4 v = part[buffer][i];
-                squares += fmaf(v.w * (v.z - m), v.z - m, v.y);
-            }
+            const float4 v = part[buffer][lane % WARPS];
+            m = lanes_sum<WARPS>(v.x) * inverse;
+            squares = lanes_sum<WARPS>(fmaf(v.w * (v.z - m), v.z - m, v.y));
         }
-        const float s = 1.f / sqrtf(squares * inverse + a.eps);
+        const float s = inverse_root(fmaf(squares, inverse, a.eps));
+        const F2 minus_m = f2(-m, -m), scale = f2(s, s);
         T* y = static_cast<T*>(a.Y) + n * a.ldy;
-        T* h = a.H ? static_cast<T*>(a.H) + n * a.ldh : nullptr;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            float o[8];
+            const int left = chunk_left<VEC, P>(c, t, D);
+            if (h) store_chunk<T, VEC, P>(h, x[c], c, t, left);
+            F2 o[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = fmaf((x[c][e] - m) * s, w[c][e], b[c][e]);
-            const int left = chunk_left<VEC, P>(c, t, D), col = column_of<VEC, P>(c, 0, t);
-            if (VEC) {
-                if (left > 0) {
-                    if (h) store_chunk(h + col, x[c], left);
-                    store_chunk(y + col, o, left);
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e < left) {
-                        if (h) Elem<T>::store(h + col + e * P, x[c][e]);
-                        Elem<T>::store(y + col + e * P, o[e]);
-                    }
-            }
+            for (int i = 0; i < 4; ++i) o[i] = fma(mul(add(x[c][i], minus_m), scale), w[c][i], b[c][i]);
+            store_chunk<T, VEC, P>(y, o, c, t, left);
         }
         if (t == 0) {
             if (a.mean) a.mean[n] = m;
@@ -175,20 +147,21 @@ int launch_rows(const NormArgs& a, int sm_count, cudaStream_t stream)
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return VELORA_ERR_CUDA;
     constexpr int kBudget = 216 * 1024 / BLOCKS;               // shared memory of a block, so that BLOCKS of them fit
+    constexpr int kShare = kShareBytes<T, WARPS, C, VEC>;
+    static_assert(2 * 2 * kShare * S::kRows <= kBudget, "two rows of both operands");
     auto kern = norm_rows_kernel<T, WARPS, C, VEC, BLOCKS>;
     if (!configured.get(dev)) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBudget) != cudaSuccess) return VELORA_ERR_CUDA;
         configured.set(dev);
     }
-    Rows rows{};
-    rows.stage_bytes = Share<T, C>::kWords * S::kPerRow * 16 * (a.R ? 2 : 1);
-    const int fit = kBudget / (rows.stage_bytes * S::kRows);
-    rows.stages = fit < 2 ? 2 : (fit > 4 ? 4 : fit);
-    static_assert(2 * Share<T, C>::kWords * S::kPerRow * 16 * S::kRows * 2 <= kBudget, "two rows of both operands");
-    rows.wide = aligned16(a.w) && aligned16(a.b);
+    Ring ring{};
+    ring.stage_bytes = kShare * (a.R ? 2 : 1);
+    const int fit = kBudget / (ring.stage_bytes * S::kRows);
+    ring.stages = fit > 4 ? 4 : fit;
+    ring.wide = aligned16(a.w) && aligned16(a.b);
     const int64_t blocks = ceil_div64(a.N, S::kRows), most = static_cast<int64_t>(sm_count) * BLOCKS;
     return launch_chained(kern, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), S::kThreads,
-                          VEC ? static_cast<size_t>(rows.stages) * rows.stage_bytes * S::kRows : 0, stream, a, rows);
+                          static_cast<size_t>(ring.stages) * ring.stage_bytes * S::kRows, stream, a, ring);
 }
 
 template <typename T, bool VEC>
@@ -204,8 +177,6 @@ int launch_held(const NormArgs& a, int sm_count, cudaStream_t stream)
     if (a.D <= 8192) return launch_rows<T, 16, 2, VEC, 1>(a, sm_count, stream);
     return launch_rows<T, 16, 3, VEC, 1>(a, sm_count, stream);
 }
-
-bool rows_vec(const void* p, int64_t ld, int dtype) { return !p || (aligned16(p) && ld * static_cast<int64_t>(dtype_size(dtype)) % 16 == 0); }
 
 }  // namespace
 
