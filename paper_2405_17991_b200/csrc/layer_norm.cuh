@@ -59,6 +59,9 @@ inline int64_t norm_slices(int64_t N) { return N < kNormSlices ? N : kNormSlices
 // Rows of any length (layer_norm_any.cu).
 int launch_layer_norm_any(const NormArgs& a, int sm_count, cudaStream_t stream);
 int launch_layer_norm_backward_any(const NormGradArgs& a, int sm_count, cudaStream_t stream);
+// Rows that do not all start on 16-byte boundaries (layer_norm_odd.cu, layer_norm_backward_odd.cu).
+int launch_layer_norm_odd(const NormArgs& a, int sm_count, cudaStream_t stream);
+int launch_layer_norm_backward_odd(const NormGradArgs& a, int sm_count, cudaStream_t stream);
 // dw and db = beta .. + the sums of `partials` over so many slices.
 int launch_norm_slices(const NormGradArgs& a, int slices, cudaStream_t stream);
 

@@ -8,223 +8,220 @@ namespace velora {
 
 namespace {
 
-template <typename T, int WARPS, int C, bool VEC, int BLOCKS>
-__global__ void __launch_bounds__((RowShape<WARPS, C>::kThreads), BLOCKS)
-norm_grad_rows_kernel(const NormGradArgs a, const Ring ring)
+// TEAM: the warps that have a row, so that a block of 256 threads has 8 / TEAM at a time; 0: the whole block has one.  KEEP: xhat and c stay in registers between the row's sums and dx; else dy and h are read from shared memory again.
+template <typename T, int C, int STAGES, bool MORE, int TEAM, bool KEEP, int THREADS, int BLOCKS>
+__global__ void __launch_bounds__(THREADS, BLOCKS)
+norm_grad_rows_kernel(const NormGradArgs a, bool wide)
 {
-    typedef RowShape<WARPS, C> S;
-    constexpr int P = S::kPerRow, kShare = kShareBytes<T, WARPS, C, VEC>;
-    constexpr bool kHold = C <= 3;                             // weights in registers
-    constexpr bool kKeep = C <= 2;                             // xhat and c between the row's sums and dx; else from shared memory again
+    constexpr int E = Word<T>::E, kTeams = TEAM ? 8 / TEAM : 1, kLanes = TEAM ? TEAM : kWarpLanes<THREADS>;
     extern __shared__ __align__(16) char ring_bytes[];
-    __shared__ float2 part[2][WARPS];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = threadIdx.x % P;
-    const int D = a.D;
+    __shared__ float2 part[2][kTeams * kLanes];
+    const int P = TEAM ? 32 * TEAM : blockDim.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int mine = TEAM ? warp / (TEAM ? TEAM : 1) : 0, t = TEAM ? threadIdx.x % (TEAM ? 32 * TEAM : 1) : threadIdx.x;       // team of the block, thread of the team
+    const int D = a.D, share = C * P * 16, stage = share * (MORE ? 3 : 2), ring_end = STAGES * stage;
+    const bool last = ((C - 1) * P + t) * E < D;               // the last word is there
     const float inverse = 1.f / static_cast<float>(D);
+    if (!TEAM && threadIdx.x < 2 * kLanes) part[threadIdx.x / kLanes][threadIdx.x % kLanes] = make_float2(0.f, 0.f);     // warps that are not there
     pdl_wait();
     pdl_trigger();
 
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * S::kRows + (WARPS == 1 ? warp : 0), step = static_cast<int64_t>(gridDim.x) * S::kRows;
-    const RowSource<T, WARPS, C, VEC> dY{static_cast<const T*>(a.dY), a.lddy}, H{static_cast<const T*>(a.H), a.ldh}, dH{static_cast<const T*>(a.dH), a.lddh};
-    const bool more = a.dH && a.dX;
-    char* slots = ring_bytes + (WARPS == 1 ? warp * ring.stages * ring.stage_bytes : 0);
-    const uint32_t slots_at = static_cast<uint32_t>(__cvta_generic_to_shared(slots));
-    auto fetch = [&](int64_t n, int slot) {
-        if (n < a.N) {
-            const int at = slot * ring.stage_bytes;
-            dY.copy(slots + at, slots_at + at, n, D, t);
-            H.copy(slots + at + kShare, slots_at + at + kShare, n, D, t);
-            if (more) dH.copy(slots + at + 2 * kShare, slots_at + at + 2 * kShare, n, D, t);
-        }
-        copies_commit();                                       // a row that is not there is an empty one
+    const int64_t team = static_cast<int64_t>(blockIdx.x) * kTeams + mine, teams = static_cast<int64_t>(gridDim.x) * kTeams;
+    const int64_t each = a.N / teams, over = a.N % teams, first = each * team + (team < over ? team : over), rows = each + (team < over ? 1 : 0);
+    const T* dy_at = static_cast<const T*>(a.dY) + first * a.lddy + t * E;
+    const T* h_at = static_cast<const T*>(a.H) + first * a.ldh + t * E;
+    const T* dh_at = MORE ? static_cast<const T*>(a.dH) + first * a.lddh + t * E : nullptr;
+    T* dx_at = a.dX ? static_cast<T*>(a.dX) + first * a.lddx + t * E : nullptr;
+    const float* mean_at = a.mean + first;
+    const float* rstd_at = a.rstd + first;
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(ring_bytes)) + mine * ring_end + t * 16;
+    auto fetch = [&](int at) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (c < C - 1 || last) {
+                copy_word(ring + at + c * P * 16, dy_at + c * P * E);
+                copy_word(ring + at + share + c * P * 16, h_at + c * P * E);
+                if (MORE) copy_word(ring + at + 2 * share + c * P * 16, dh_at + c * P * E);
+            }
+        dy_at += a.lddy;
+        h_at += a.ldh;
+        if (MORE) dh_at += a.lddh;
     };
-    for (int s = 0; s < ring.stages - 1; ++s) fetch(first + s * step, s);
-    F2 w[kHold ? C : 1][4], dw[C][4], db[C][4];
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) {
+        if (s < rows) fetch(s * stage);
+        copies_commit();
+    }
+    F2 w[C][E / 2], dw[C][E / 2], db[C][E / 2];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        if (kHold) load_params<VEC, P>(w[kHold ? c : 0], a.w, a.p_dtype, ring.wide, c, t, D, 1.f);
+        if (c < C - 1 || last) load_columns<E>(w[c], a.w, a.p_dtype, wide, (c * P + t) * E, 1.f);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) dw[c][i] = db[c][i] = f2(0.f, 0.f);
+        for (int i = 0; i < E / 2; ++i) dw[c][i] = db[c][i] = f2(0.f);
     }
-    float m_next = first < a.N ? a.mean[first] : 0.f, s_next = first < a.N ? a.rstd[first] : 0.f;
-    int slot = 0, buffer = 0;
-    for (int64_t n = first; n < a.N; n += step, slot = slot + 1 == ring.stages ? 0 : slot + 1, buffer ^= 1) {
-        const float s = s_next;
-        const F2 minus_m = f2(-m_next, -m_next), scale = f2(s, s);
-        if (n + step < a.N) {
-            m_next = a.mean[n + step];
-            s_next = a.rstd[n + step];
+    float m_next = rows > 0 ? mean_at[0] : 0.f, s_next = rows > 0 ? rstd_at[0] : 0.f;
+    if (!TEAM) __syncthreads();
+    int at = 0, turn = 0;
+    for (int64_t row = 0; row < rows; ++row) {
+        const F2 minus_m = f2(-m_next), scale = f2(s_next);
+        if (row + 1 < rows) {
+            m_next = mean_at[row + 1];
+            s_next = rstd_at[row + 1];
         }
-        const int before = slot == 0 ? ring.stages - 1 : slot - 1;
-        if (VEC) {
-            fetch(n + (ring.stages - 1) * step, before);
-            copies_wait(ring.stages - 1);
-        } else {
-            copies_wait(ring.stages - 2);
-            row_barrier<WARPS>();
-            fetch(n + (ring.stages - 1) * step, before);
-        }
-        const char* row = slots + slot * ring.stage_bytes;
-        F2 kept_x[kKeep ? C : 1][4], kept_c[kKeep ? C : 1][4];
-        F2 sum2 = f2(0.f, 0.f), along2 = f2(0.f, 0.f);
+        if (row + STAGES - 1 < rows) fetch(at == 0 ? ring_end - stage : at - stage);
+        copies_commit();
+        copies_wait<STAGES - 1>();
+        const uint32_t here = ring + at;
+        at = at == ring_end - stage ? 0 : at + stage;
+        F2 kept_x[KEEP ? C : 1][E / 2], kept_c[KEEP ? C : 1][E / 2];
+        F2 sums = f2(0.f), along = f2(0.f);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int left = chunk_left<VEC, P>(c, t, D);
-            if (left <= 0) continue;                           // columns behind the row's end within a chunk are zeros of dy
-            F2 dy[4], h[4], now[4];
-            dY.load(dy, row, n, c, t, left);
-            H.load(h, row + kShare, n, c, t, left);
-            if (!kHold) load_params<VEC, P>(now, a.w, a.p_dtype, ring.wide, c, t, D, 1.f);
+        for (int c = 0; c < C; ++c)
+            if (c < C - 1 || last) {
+                Word<T> dy, h;
+                dy.load(here + c * P * 16);
+                h.load(here + share + c * P * 16);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const F2 xhat = mul(add(h[i], minus_m), scale), g = mul(dy[i], kHold ? w[kHold ? c : 0][i] : now[i]);
-                dw[c][i] = fma(dy[i], xhat, dw[c][i]);
-                db[c][i] = add(db[c][i], dy[i]);
-                sum2 = add(sum2, g);
-                along2 = fma(g, xhat, along2);
-                if (kKeep) {
-                    kept_x[c][i] = xhat;
-                    kept_c[c][i] = g;
+                for (int i = 0; i < E / 2; ++i) {
+                    const F2 xhat = mul(add(h.x[i], minus_m), scale), g = mul(dy.x[i], w[c][i]);
+                    dw[c][i] = fma(dy.x[i], xhat, dw[c][i]);
+                    db[c][i] = add(db[c][i], dy.x[i]);
+                    sums = add(sums, g);
+                    along = fma(g, xhat, along);
+                    if (KEEP) {
+                        kept_x[KEEP ? c : 0][i] = xhat;
+                        kept_c[KEEP ? c : 0][i] = g;
+                    }
                 }
             }
+        if (!dx_at) continue;
+        float s1 = warp_total(sum(sums)), s2 = warp_total(sum(along));
+        if (TEAM != 1) {
+            if (lane == 0) part[turn][warp] = make_float2(s1, s2);
+            if (TEAM) asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "n"(32 * TEAM) : "memory");
+            else __syncthreads();                              // the other half's readers are past the barrier before
+            const float2 v = part[turn][mine * kLanes + lane % kLanes];
+            turn ^= 1;
+            s1 = warps_total<kLanes>(v.x);
+            s2 = warps_total<kLanes>(v.y);
         }
-        if (!a.dX) continue;
-        const float2 u = parts(sum2), v = parts(along2);
-        float sum = lanes_sum<32>(u.x + u.y), along = lanes_sum<32>(v.x + v.y);
-        if (WARPS > 1) {
-            if (lane == 0) part[buffer][warp] = make_float2(sum, along);
-            __syncthreads();                                   // the other buffer's readers are past the barrier before
-            const float2 p = part[buffer][lane % WARPS];
-            sum = lanes_sum<WARPS>(p.x);
-            along = lanes_sum<WARPS>(p.y);
-        }
-        const F2 minus_sum = f2(-sum * inverse, -sum * inverse), minus_along = f2(-along * inverse, -along * inverse);
-        T* dx = static_cast<T*>(a.dX) + n * a.lddx;
+        const F2 minus_sum = f2(-s1 * inverse), minus_along = f2(-s2 * inverse);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int left = chunk_left<VEC, P>(c, t, D);
-            if (left <= 0) continue;
-            F2 o[4];
-            if (!kKeep) {
-                F2 dy[4], h[4], now[4];
-                dY.load(dy, row, n, c, t, left);
-                H.load(h, row + kShare, n, c, t, left);
-                if (!kHold) load_params<VEC, P>(now, a.w, a.p_dtype, ring.wide, c, t, D, 1.f);
+        for (int c = 0; c < C; ++c)
+            if (c < C - 1 || last) {
+                Word<T> o;
+                if (KEEP) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const F2 xhat = mul(add(h[i], minus_m), scale), g = mul(dy[i], kHold ? w[kHold ? c : 0][i] : now[i]);
-                    o[i] = mul(add(fma(xhat, minus_along, g), minus_sum), scale);
+                    for (int i = 0; i < E / 2; ++i) o.x[i] = mul(add(fma(kept_x[KEEP ? c : 0][i], minus_along, kept_c[KEEP ? c : 0][i]), minus_sum), scale);
+                } else {
+                    Word<T> dy, h;
+                    dy.load(here + c * P * 16);
+                    h.load(here + share + c * P * 16);
+#pragma unroll
+                    for (int i = 0; i < E / 2; ++i) {
+                        const F2 xhat = mul(add(h.x[i], minus_m), scale), g = mul(dy.x[i], w[c][i]);
+                        o.x[i] = mul(add(fma(xhat, minus_along, g), minus_sum), scale);
+                    }
                 }
-            } else {
+                if (MORE) {
+                    Word<T> dh;
+                    dh.load(here + 2 * share + c * P * 16);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = mul(add(fma(kept_x[kKeep ? c : 0][i], minus_along, kept_c[kKeep ? c : 0][i]), minus_sum), scale);
+                    for (int i = 0; i < E / 2; ++i) o.x[i] = add(o.x[i], dh.x[i]);
+                }
+                o.store(dx_at + c * P * E);
             }
-            if (more) {
-                F2 dh[4];
-                dH.load(dh, row + 2 * kShare, n, c, t, left);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = add(o[i], dh[i]);
-            }
-            store_chunk<T, VEC, P>(dx, o, c, t, left);
-        }
+        dx_at += a.lddx;
     }
     if (!a.dw && !a.db) return;
     const bool alone = gridDim.x == 1;
     float* out_w = a.partials + static_cast<int64_t>(blockIdx.x) * norm_pitch(D);
     float* out_b = out_w + static_cast<int64_t>(gridDim.x) * norm_pitch(D);
     auto put = [&](bool bias, int d, float x) {
-        if (alone) {
-            if (bias ? a.db : a.dw) store_param(bias ? a.db : a.dw, a.dw_dtype, d, x, a.beta);
-        } else {
-            (bias ? out_b : out_w)[d] = x;
-        }
+        if (!alone) (bias ? out_b : out_w)[d] = x;
+        else if (bias ? a.db : a.dw) store_param(bias ? a.db : a.dw, a.dw_dtype, d, x, a.beta);
     };
-    if (WARPS == 1) {                                          // the eight warps' sums, through the ring's room
-        copies_wait(0);
+    if (TEAM) {                                                // the teams' sums, through the ring's room
+        copies_wait<0>();
         float* sums = reinterpret_cast<float*>(ring_bytes);
+        constexpr int kColumns = C * 32 * TEAM * E;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
             __syncthreads();
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < E / 2; ++i) {
                     const float2 v = parts(which ? db[c][i] : dw[c][i]);
-                    float* p = sums + warp * S::kColumns;
-                    p[column_of<VEC, P>(c, 2 * i, t)] = v.x;
-                    p[column_of<VEC, P>(c, 2 * i + 1, t)] = v.y;
+                    *reinterpret_cast<float2*>(sums + mine * kColumns + (c * P + t) * E + 2 * i) = v;
                 }
             __syncthreads();
-            for (int d = threadIdx.x; d < D; d += S::kThreads) {
+            for (int d = threadIdx.x; d < D; d += THREADS) {
                 float x = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x += sums[i * S::kColumns + d];
+                for (int i = 0; i < kTeams; ++i) x += sums[i * kColumns + d];
                 put(which != 0, d, x);
             }
         }
         return;
     }
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int left = chunk_left<VEC, P>(c, t, D);
-        if (!alone) {
-            const int room = VEC && left > 0 ? 8 : left;       // the pitch is a multiple of eight
-            store_chunk<float, VEC, P>(out_w, dw[c], c, t, room);
-            store_chunk<float, VEC, P>(out_b, db[c], c, t, room);
-        } else {
+    for (int c = 0; c < C; ++c)
+        if (c < C - 1 || last)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e < left) {
-                    put(false, column_of<VEC, P>(c, e, t), e & 1 ? parts(dw[c][e >> 1]).y : parts(dw[c][e >> 1]).x);
-                    put(true, column_of<VEC, P>(c, e, t), e & 1 ? parts(db[c][e >> 1]).y : parts(db[c][e >> 1]).x);
+            for (int i = 0; i < E / 2; ++i) {
+                const int d = (c * P + t) * E + 2 * i;
+                const float2 u = parts(dw[c][i]), v = parts(db[c][i]);
+                if (!alone) {
+                    *reinterpret_cast<float2*>(out_w + d) = u;
+                    *reinterpret_cast<float2*>(out_b + d) = v;
+                } else {
+                    put(false, d, u.x);
+                    put(false, d + 1, u.y);
+                    put(true, d, v.x);
+                    put(true, d + 1, v.y);
                 }
-        }
-    }
+            }
 }
 
-template <typename T, int WARPS, int C, bool VEC, int BLOCKS>
+template <typename T, int C, bool MORE, int TEAM, bool KEEP, int THREADS, int BLOCKS>
 int launch_rows(const NormGradArgs& a, int sm_count, cudaStream_t stream)
 {
-    typedef RowShape<WARPS, C> S;
+    constexpr int kTeams = TEAM ? 8 / TEAM : 1;
+    // Rows of a full block on their way or in use: two, up to four of them, in the share of an SM's shared memory that BLOCKS leave.
+    constexpr int kRow = C * THREADS * 16 * (MORE ? 3 : 2), kFit = 216 * 1024 / BLOCKS / kRow, kStages = kFit > 4 ? 4 : kFit;
+    static_assert(kStages >= 2, "two rows");
     static DeviceOnce configured;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return VELORA_ERR_CUDA;
-    constexpr int kBudget = 216 * 1024 / BLOCKS;               // shared memory of a block, so that BLOCKS of them fit
-    constexpr int kShare = kShareBytes<T, WARPS, C, VEC>;
-    static_assert(2 * 3 * kShare * S::kRows <= kBudget, "two rows of three operands");
-    auto kern = norm_grad_rows_kernel<T, WARPS, C, VEC, BLOCKS>;
+    auto kern = norm_grad_rows_kernel<T, C, kStages, MORE, TEAM, KEEP, THREADS, BLOCKS>;
     if (!configured.get(dev)) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBudget) != cudaSuccess) return VELORA_ERR_CUDA;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kStages * kRow) != cudaSuccess) return VELORA_ERR_CUDA;
         configured.set(dev);
     }
-    Ring ring{};
-    ring.stage_bytes = kShare * (a.dH && a.dX ? 3 : 2);
-    const int fit = kBudget / (ring.stage_bytes * S::kRows);
-    ring.stages = fit > 4 ? 4 : fit;
-    ring.wide = aligned16(a.w);
-    size_t smem = static_cast<size_t>(ring.stages) * ring.stage_bytes * S::kRows;
-    if (WARPS == 1 && smem < 8 * sizeof(float) * S::kColumns) smem = 8 * sizeof(float) * S::kColumns;
-    int64_t blocks = ceil_div64(a.N, S::kRows);
+    static_assert(TEAM == 0 || kStages * kRow >= C * THREADS * Word<T>::E * 4, "room for the teams' sums");
+    const int threads = TEAM ? THREADS : row_threads(row_words(a.D, a.dtype), C);
+    int64_t blocks = ceil_div64(a.N, kTeams);
     const int64_t most = static_cast<int64_t>(sm_count) * BLOCKS < kNormSlices ? static_cast<int64_t>(sm_count) * BLOCKS : kNormSlices;
     if (blocks > most) blocks = most;
-    const int rc = launch_chained(kern, dim3(static_cast<unsigned>(blocks)), S::kThreads, smem, stream, a, ring);
+    const int rc = launch_chained(kern, dim3(static_cast<unsigned>(blocks)), threads, static_cast<size_t>(kStages) * kRow / THREADS * threads, stream, a,
+                                  aligned16(a.w));
     if (rc != VELORA_OK || blocks == 1 || (!a.dw && !a.db)) return rc;
     return launch_norm_slices(a, static_cast<int>(blocks), stream);
 }
 
-template <typename T, bool VEC>
-int launch_held(const NormGradArgs& a, int sm_count, cudaStream_t stream)
+template <typename T, bool MORE>
+int launch_words(const NormGradArgs& a, int sm_count, cudaStream_t stream)
 {
-    constexpr int kPair = sizeof(T) == 2 ? 2 : 1;              // blocks where two rows of three operands take half of an SM's shared memory, or all of it
-    if (a.D <= 256) return launch_rows<T, 1, 1, VEC, 2>(a, sm_count, stream);
-    if (a.D <= 512) return launch_rows<T, 1, 2, VEC, kPair>(a, sm_count, stream);
-    if (a.D <= 768) return launch_rows<T, 1, 3, VEC, kPair>(a, sm_count, stream);
-    if (a.D <= 1024) return launch_rows<T, 4, 1, VEC, 2>(a, sm_count, stream);
-    if (a.D <= 2048) return launch_rows<T, 4, 2, VEC, 2>(a, sm_count, stream);
-    if (a.D <= 4096) return launch_rows<T, 8, 2, VEC, kPair>(a, sm_count, stream);
-    if (a.D <= 6144) return launch_rows<T, 8, 3, VEC, kPair>(a, sm_count, stream);
-    if (a.D <= 8192) return launch_rows<T, 16, 2, VEC, 1>(a, sm_count, stream);
-    if (sizeof(T) == 2) return launch_rows<__nv_bfloat16, 16, 3, VEC, 1>(a, sm_count, stream);
+    const int words = row_words(a.D, a.dtype);
+    if (words <= 32) return launch_rows<T, 1, MORE, 1, true, 256, 2>(a, sm_count, stream);
+    if (words <= 64) return launch_rows<T, 2, MORE, 1, true, 256, 2>(a, sm_count, stream);
+    if (words <= 96) return launch_rows<T, 3, MORE, 1, false, 256, 2>(a, sm_count, stream);
+    if (words <= 128) return launch_rows<T, 2, MORE, 2, true, 256, 2>(a, sm_count, stream);
+    if (words <= 256) return launch_rows<T, 2, MORE, 4, true, 256, 2>(a, sm_count, stream);
+    if (words <= 512) return launch_rows<T, 2, MORE, 0, true, 256, 2>(a, sm_count, stream);
+    if (words <= 768) return launch_rows<T, 3, MORE, 0, false, 256, 2>(a, sm_count, stream);
+    if (words <= 1024) return launch_rows<T, 2, MORE, 0, true, 512, 1>(a, sm_count, stream);
+    if (words <= 1536) return launch_rows<T, 3, MORE, 0, false, 512, 1>(a, sm_count, stream);
     return launch_layer_norm_backward_any(a, sm_count, stream);
 }
 
@@ -235,12 +232,13 @@ int launch_layer_norm_backward(const NormGradArgs& a, cudaStream_t stream)
     DeviceInfo di;
     const int rc = device_info(&di);
     if (rc != VELORA_OK) return rc;
-    if (a.D > 12288) return launch_layer_norm_backward_any(a, di.sm_count, stream);
-    const bool vec = rows_vec(a.dY, a.lddy, a.dtype) && rows_vec(a.H, a.ldh, a.dtype) && rows_vec(a.dX ? a.dH : nullptr, a.lddh, a.dtype) &&
-                     rows_vec(a.dX, a.lddx, a.dtype);
+    const void* dH = a.dX ? a.dH : nullptr;
+    const bool vec = a.D * static_cast<int64_t>(dtype_size(a.dtype)) % 16 == 0 && rows_vec(a.dY, a.lddy, a.dtype) && rows_vec(a.H, a.ldh, a.dtype) &&
+                     rows_vec(dH, a.lddh, a.dtype) && rows_vec(a.dX, a.lddx, a.dtype);
+    if (!vec) return launch_layer_norm_backward_odd(a, di.sm_count, stream);
     if (a.dtype == VELORA_BF16)
-        return vec ? launch_held<__nv_bfloat16, true>(a, di.sm_count, stream) : launch_held<__nv_bfloat16, false>(a, di.sm_count, stream);
-    return vec ? launch_held<float, true>(a, di.sm_count, stream) : launch_held<float, false>(a, di.sm_count, stream);
+        return dH ? launch_words<__nv_bfloat16, true>(a, di.sm_count, stream) : launch_words<__nv_bfloat16, false>(a, di.sm_count, stream);
+    return dH ? launch_words<float, true>(a, di.sm_count, stream) : launch_words<float, false>(a, di.sm_count, stream);
 }
 
 }  // namespace velora
