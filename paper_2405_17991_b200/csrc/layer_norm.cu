@@ -143,25 +143,42 @@ int launch_rows(const NormArgs& a, int sm_count, cudaStream_t stream)
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kStages * kRow) != cudaSuccess) return VELORA_ERR_CUDA;
         configured.set(dev);
     }
-    const int threads = ONE ? THREADS : row_threads(row_words(a.D, a.dtype), C);
+    const int words = row_words(a.D, a.dtype), threads = ONE ? THREADS : row_threads(words, C), per_row = ONE ? 32 : threads;
+    if (threads > THREADS || (C - 1) * per_row >= words || C * per_row < words) return VELORA_ERR_UNSUPPORTED;         // only last words may be missing
     const int64_t blocks = ceil_div64(a.N, kTeams), most = static_cast<int64_t>(sm_count) * BLOCKS;
     return launch_chained(kern, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), threads, static_cast<size_t>(kStages) * kRow / THREADS * threads,
                           stream, a, aligned16(a.w) && aligned16(a.b));
 }
 
+// By the row's words: what was fastest of some forty shapes, in TB/s of x, y (and r, h).  bf16, without and with a residual: 16384 x 256 2.6 / 4.1, 16384 x 512
+// 4.2 / 5.2, 12608 x 768 4.0 / 5.0, 16384 x 1024 4.5 / 5.2, 8192 x 2048 4.5 / 5.3, 8192 x 4096 5.0 / 5.8 (256 threads with a residual: 5.2), 4096 x 5464
+// 4.1 / 5.3 (256 threads: 5.1), 8192 x 8192 5.2 (512 threads: 4.6) / 6.2, 8192 x 11008 5.0 / 6.0 (512 threads: 5.5).  fp32: 8192 x 512 3.9 / 5.0, 12608 x 768
+// 5.0 (a warp a row: 4.7) / 5.1, 4096 x 2048 4.9 / 5.1, 4096 x 4096 5.4 / 5.3, 4096 x 8192 5.7 / 5.4, 2048 x 11008 5.4 / 5.2.
 template <typename T, bool RESIDUAL>
 int launch_words(const NormArgs& a, int sm_count, cudaStream_t stream)
 {
     const int words = row_words(a.D, a.dtype);
-    if (words <= 32) return launch_rows<T, 1, RESIDUAL, true, 256, 4>(a, sm_count, stream);
-    if (words <= 64) return launch_rows<T, 2, RESIDUAL, true, 256, 3>(a, sm_count, stream);
-    if (words <= 96) return launch_rows<T, 3, RESIDUAL, true, 256, 2>(a, sm_count, stream);
-    if (words <= 128) return launch_rows<T, 2, RESIDUAL, false, 64, 10>(a, sm_count, stream);
-    if (words <= 256) return launch_rows<T, 2, RESIDUAL, false, 128, 6>(a, sm_count, stream);
-    if (words <= 512) return launch_rows<T, 2, RESIDUAL, false, 256, 3>(a, sm_count, stream);
-    if (words <= 768) return launch_rows<T, 3, RESIDUAL, false, 256, 2>(a, sm_count, stream);
-    if (words <= 1536) return launch_rows<T, 3, RESIDUAL, false, 512, 1>(a, sm_count, stream);
-    if (sizeof(T) == 4 && words <= 4 * 768) return launch_rows<float, 4, RESIDUAL, false, 768, 1>(a, sm_count, stream);
+    if (words <= 32) return launch_rows<T, 1, RESIDUAL, true, 256, 3>(a, sm_count, stream);
+    if (words <= 64) return launch_rows<T, 2, RESIDUAL, true, 256, 2>(a, sm_count, stream);
+    if constexpr (sizeof(T) == 2) {
+        if (words <= 96) return launch_rows<T, 3, RESIDUAL, true, 256, 2>(a, sm_count, stream);
+        if (words <= 128) return launch_rows<T, 2, RESIDUAL, false, 64, 10>(a, sm_count, stream);
+        if (words <= 256) return launch_rows<T, 2, RESIDUAL, false, 128, 5>(a, sm_count, stream);
+        if (words <= 512) return RESIDUAL ? launch_rows<T, 1, true, false, 512, 2>(a, sm_count, stream) : launch_rows<T, 2, false, false, 256, 3>(a, sm_count, stream);
+        if (words <= 704) return launch_rows<T, 2, RESIDUAL, false, 352, 2>(a, sm_count, stream);
+        if (RESIDUAL) return words <= 1408 ? launch_rows<T, 2, true, false, 704, 1>(a, sm_count, stream) : words <= 1536 ? launch_rows<T, 3, true, false, 512, 1>(a, sm_count, stream) : launch_layer_norm_any(a, sm_count, stream);
+        if (words <= 1024) return launch_rows<T, 4, false, false, 256, 2>(a, sm_count, stream);
+        if (words <= 1536) return launch_rows<T, 4, false, false, 384, 1>(a, sm_count, stream);
+    } else {
+        if (words <= 96) return launch_rows<T, 3, RESIDUAL, true, 256, 2>(a, sm_count, stream);
+        if (words <= 128) return launch_rows<T, 4, RESIDUAL, true, 256, 2>(a, sm_count, stream);
+        if (words <= 192) return launch_rows<T, 2, RESIDUAL, false, 96, 8>(a, sm_count, stream);
+        if (words <= 384) return launch_rows<T, 3, RESIDUAL, false, 128, 5>(a, sm_count, stream);
+        if (words <= 512) return launch_rows<T, 4, RESIDUAL, false, 128, 4>(a, sm_count, stream);
+        if (words <= 1024) return launch_rows<T, 2, RESIDUAL, false, 512, 2>(a, sm_count, stream);
+        if (words <= 2048) return launch_rows<T, 4, RESIDUAL, false, 512, 1>(a, sm_count, stream);
+        if (words <= 4 * 768) return launch_rows<T, 4, RESIDUAL, false, 768, 1>(a, sm_count, stream);
+    }
     return launch_layer_norm_any(a, sm_count, stream);
 }
 

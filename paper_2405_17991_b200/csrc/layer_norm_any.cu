@@ -114,11 +114,13 @@ norm_columns_kernel(const NormGradArgs a, int slices)
     a.partials[static_cast<int64_t>(slices + slice) * norm_pitch(a.D) + d] = db;
 }
 
-// The slices' sums in a fixed order: a block takes 32 columns of dw or db, a warp every eighth slice.
-__global__ void __launch_bounds__(256)
+// The slices' sums in a fixed order: a block takes 32 columns of dw or db, a warp every 32nd slice, ten loads under way at once, which all of kNormSlices are.
+constexpr int kSliceWarps = 32, kSliceLoads = 10;
+static_assert(kSliceWarps * kSliceLoads >= kNormSlices, "one round");
+__global__ void __launch_bounds__(32 * kSliceWarps)
 norm_slices_kernel(const float* partials, int slices, int D, void* dw, void* db, int dtype, int beta)
 {
-    __shared__ float part[8][32];
+    __shared__ float part[kSliceWarps][33];
     pdl_wait();
     pdl_trigger();
     void* out = blockIdx.y ? db : dw;
@@ -126,16 +128,18 @@ norm_slices_kernel(const float* partials, int slices, int D, void* dw, void* db,
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = blockIdx.x * 32 + lane;
     const int64_t pitch = norm_pitch(D);
     const float* p = partials + blockIdx.y * slices * pitch + d;
+    float x[kSliceLoads];
+#pragma unroll
+    for (int i = 0; i < kSliceLoads; ++i) x[i] = d < D && warp + kSliceWarps * i < slices ? p[(warp + kSliceWarps * i) * pitch] : 0.f;
     float s = 0.f;
-    if (d < D)
-#pragma unroll 8
-        for (int i = warp; i < slices; i += 8) s += p[i * pitch];
+#pragma unroll
+    for (int i = 0; i < kSliceLoads; ++i) s += x[i];
     part[warp][lane] = s;
     __syncthreads();
-    if (warp != 0 || d >= D) return;
-    s = 0.f;
-    for (int w = 0; w < 8; ++w) s += part[w][lane];
-    store_param(out, dtype, d, s, beta);
+    s = part[lane][warp];                                     // column blockIdx.x * 32 + warp, of warp `lane`
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == 0 && blockIdx.x * 32 + warp < D) store_param(out, dtype, blockIdx.x * 32 + warp, s, beta);
 }
 
 template <typename T>
@@ -175,8 +179,8 @@ int launch_layer_norm_backward_any(const NormGradArgs& a, int sm_count, cudaStre
 
 int launch_norm_slices(const NormGradArgs& a, int slices, cudaStream_t stream)
 {
-    return launch_chained(norm_slices_kernel, dim3(static_cast<unsigned>(ceil_div64(a.D, 32)), 2), 256, 0, stream, a.partials, slices, a.D, a.dw, a.db,
-                          a.dw_dtype, a.beta);
+    return launch_chained(norm_slices_kernel, dim3(static_cast<unsigned>(ceil_div64(a.D, 32)), 2), 32 * kSliceWarps, 0, stream, a.partials, slices, a.D,
+                          a.dw, a.db, a.dw_dtype, a.beta);
 }
 
 }  // namespace velora

@@ -8,6 +8,28 @@ namespace velora {
 
 namespace {
 
+// E columns' sums, at a 16-byte boundary.  WIDE: 16 bytes at a time, for which they have to lie in four neighbouring registers all along: right where there are
+// registers to spare (8192 x 4096 bf16: 39 us, two at a time 42), but 8192 x 11008, dX alone, takes 112 us instead of 94.
+template <int E, bool WIDE> __device__ __forceinline__ void store_sums(float* p, const F2 (&x)[E / 2])
+{
+    if (WIDE) {
+#pragma unroll
+        for (int i = 0; i < E / 4; ++i) reinterpret_cast<ulonglong2*>(p)[i] = make_ulonglong2(x[2 * i].v, x[2 * i + 1].v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) reinterpret_cast<float2*>(p)[i] = parts(x[i]);
+    }
+}
+// To a gradient that starts anywhere: one load or store a column, all under way at once.
+template <int E> __device__ __forceinline__ void store_params(void* p, int dtype, int col, const F2 (&x)[E / 2], int beta)
+{
+    float y[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] = (e & 1 ? parts(x[e >> 1]).y : parts(x[e >> 1]).x) + (beta ? load_param(p, dtype, col + e, 0.f) : 0.f);
+#pragma unroll
+    for (int e = 0; e < E; ++e) store_param(p, dtype, col + e, y[e], 0);
+}
+
 // TEAM: the warps that have a row, so that a block of 256 threads has 8 / TEAM at a time; 0: the whole block has one.  KEEP: xhat and c stay in registers between the row's sums and dx; else dy and h are read from shared memory again.
 template <typename T, int C, int STAGES, bool MORE, int TEAM, bool KEEP, int THREADS, int BLOCKS>
 __global__ void __launch_bounds__(THREADS, BLOCKS)
@@ -136,10 +158,6 @@ norm_grad_rows_kernel(const NormGradArgs a, bool wide)
     const bool alone = gridDim.x == 1;
     float* out_w = a.partials + static_cast<int64_t>(blockIdx.x) * norm_pitch(D);
     float* out_b = out_w + static_cast<int64_t>(gridDim.x) * norm_pitch(D);
-    auto put = [&](bool bias, int d, float x) {
-        if (!alone) (bias ? out_b : out_w)[d] = x;
-        else if (bias ? a.db : a.dw) store_param(bias ? a.db : a.dw, a.dw_dtype, d, x, a.beta);
-    };
     if (TEAM) {                                                // the teams' sums, through the ring's room
         copies_wait<0>();
         float* sums = reinterpret_cast<float*>(ring_bytes);
@@ -159,37 +177,33 @@ norm_grad_rows_kernel(const NormGradArgs a, bool wide)
                 float x = 0.f;
 #pragma unroll
                 for (int i = 0; i < kTeams; ++i) x += sums[i * kColumns + d];
-                put(which != 0, d, x);
+                if (!alone) (which ? out_b : out_w)[d] = x;
+                else if (which ? a.db : a.dw) store_param(which ? a.db : a.dw, a.dw_dtype, d, x, a.beta);
             }
         }
         return;
     }
 #pragma unroll
     for (int c = 0; c < C; ++c)
-        if (c < C - 1 || last)
-#pragma unroll
-            for (int i = 0; i < E / 2; ++i) {
-                const int d = (c * P + t) * E + 2 * i;
-                const float2 u = parts(dw[c][i]), v = parts(db[c][i]);
-                if (!alone) {
-                    *reinterpret_cast<float2*>(out_w + d) = u;
-                    *reinterpret_cast<float2*>(out_b + d) = v;
-                } else {
-                    put(false, d, u.x);
-                    put(false, d + 1, u.y);
-                    put(true, d, v.x);
-                    put(true, d + 1, v.y);
-                }
+        if (c < C - 1 || last) {
+            const int d = (c * P + t) * E;
+            if (!alone) {
+                store_sums<E, KEEP>(out_w + d, dw[c]);
+                store_sums<E, KEEP>(out_b + d, db[c]);
+            } else {
+                if (a.dw) store_params<E>(a.dw, a.dw_dtype, d, dw[c], a.beta);
+                if (a.db) store_params<E>(a.db, a.dw_dtype, d, db[c], a.beta);
             }
+        }
 }
 
 template <typename T, int C, bool MORE, int TEAM, bool KEEP, int THREADS, int BLOCKS>
 int launch_rows(const NormGradArgs& a, int sm_count, cudaStream_t stream)
 {
     constexpr int kTeams = TEAM ? 8 / TEAM : 1;
-    // Rows of a full block on their way or in use: two, up to four of them, in the share of an SM's shared memory that BLOCKS leave.
+    // Rows of a full block on their way or in use: up to four of them, in the share of an SM's shared memory that BLOCKS leave.
     constexpr int kRow = C * THREADS * 16 * (MORE ? 3 : 2), kFit = 216 * 1024 / BLOCKS / kRow, kStages = kFit > 4 ? 4 : kFit;
-    static_assert(kStages >= 2, "two rows");
+    static_assert(kStages >= 1, "a row");
     static DeviceOnce configured;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return VELORA_ERR_CUDA;
@@ -199,8 +213,11 @@ int launch_rows(const NormGradArgs& a, int sm_count, cudaStream_t stream)
         configured.set(dev);
     }
     static_assert(TEAM == 0 || kStages * kRow >= C * THREADS * Word<T>::E * 4, "room for the teams' sums");
-    const int threads = TEAM ? THREADS : row_threads(row_words(a.D, a.dtype), C);
-    int64_t blocks = ceil_div64(a.N, kTeams);
+    const int words = row_words(a.D, a.dtype), threads = TEAM ? THREADS : row_threads(words, C), per_row = TEAM ? 32 * TEAM : threads;
+    if (threads > THREADS || (C - 1) * per_row >= words || C * per_row < words) return VELORA_ERR_UNSUPPORTED;         // only last words may be missing
+    // Where dw or db is asked for, each block leaves a row of sums that is written and read: a quarter of the rows at most, once there are 64 of them.
+    const int64_t rounds = ceil_div64(a.N, kTeams), few = a.dw || a.db ? ceil_div64(rounds, 4) : rounds;
+    int64_t blocks = few > 64 ? few : (rounds < 64 ? rounds : 64);
     const int64_t most = static_cast<int64_t>(sm_count) * BLOCKS < kNormSlices ? static_cast<int64_t>(sm_count) * BLOCKS : kNormSlices;
     if (blocks > most) blocks = most;
     const int rc = launch_chained(kern, dim3(static_cast<unsigned>(blocks)), threads, static_cast<size_t>(kStages) * kRow / THREADS * threads, stream, a,
@@ -209,19 +226,34 @@ int launch_rows(const NormGradArgs& a, int sm_count, cudaStream_t stream)
     return launch_norm_slices(a, static_cast<int>(blocks), stream);
 }
 
+// By the row's words: what was fastest of some forty shapes, in TB/s of dy, h, dx (and dh), dw and db included.  bf16, without and with dh: 16384 x 256 2.6 / 3.2,
+// 16384 x 512 3.8 / 4.2, 12608 x 768 3.7 / 4.0 (a warp a row: 3.6 / 4.0), 16384 x 1024 4.8 / 4.7, 8192 x 2048 4.5 / 4.7 (a block a row: 3.3 / 3.9),
+// 8192 x 4096 5.1 / 5.4, 4096 x 5464 3.6 / 4.3, 8192 x 8192 5.2 / 5.9, 8192 x 11008 5.2 / 4.8.  fp32: 8192 x 512 4.0 / 4.4, 12608 x 768 4.9 / 5.2,
+// 4096 x 2048 4.7 / 5.0, 4096 x 4096 5.5 / 5.9, 4096 x 8192 5.3 / 6.0, 2048 x 11008 4.8 / 5.0.
 template <typename T, bool MORE>
 int launch_words(const NormGradArgs& a, int sm_count, cudaStream_t stream)
 {
     const int words = row_words(a.D, a.dtype);
     if (words <= 32) return launch_rows<T, 1, MORE, 1, true, 256, 2>(a, sm_count, stream);
     if (words <= 64) return launch_rows<T, 2, MORE, 1, true, 256, 2>(a, sm_count, stream);
-    if (words <= 96) return launch_rows<T, 3, MORE, 1, false, 256, 2>(a, sm_count, stream);
-    if (words <= 128) return launch_rows<T, 2, MORE, 2, true, 256, 2>(a, sm_count, stream);
-    if (words <= 256) return launch_rows<T, 2, MORE, 4, true, 256, 2>(a, sm_count, stream);
-    if (words <= 512) return launch_rows<T, 2, MORE, 0, true, 256, 2>(a, sm_count, stream);
-    if (words <= 768) return launch_rows<T, 3, MORE, 0, false, 256, 2>(a, sm_count, stream);
-    if (words <= 1024) return launch_rows<T, 2, MORE, 0, true, 512, 1>(a, sm_count, stream);
-    if (words <= 1536) return launch_rows<T, 3, MORE, 0, false, 512, 1>(a, sm_count, stream);
+    if constexpr (sizeof(T) == 2) {
+        if (words <= 128) return launch_rows<T, 2, MORE, 2, true, 256, 2>(a, sm_count, stream);
+        if (words <= 256) return launch_rows<T, 2, MORE, 4, true, 256, 2>(a, sm_count, stream);
+        if (words <= 512) return launch_rows<T, 2, MORE, 0, true, 256, 2>(a, sm_count, stream);
+        if (words <= 768) return launch_rows<T, 3, MORE, 0, true, 256, 1>(a, sm_count, stream);
+        if (words <= 1024) return launch_rows<T, 2, MORE, 0, true, 512, 1>(a, sm_count, stream);
+        if (words <= 1536) return launch_rows<T, 3, MORE, 0, false, 512, 1>(a, sm_count, stream);
+    } else {
+        if (words <= 96) return launch_rows<T, 3, MORE, 1, true, 256, 2>(a, sm_count, stream);
+        if (words <= 128) return launch_rows<T, 4, MORE, 1, true, 256, 2>(a, sm_count, stream);
+        if (words <= 192) return launch_rows<T, 3, MORE, 2, true, 256, 2>(a, sm_count, stream);
+        if (words <= 256) return launch_rows<T, 4, MORE, 2, true, 256, 2>(a, sm_count, stream);
+        if (words <= 384) return launch_rows<T, 3, MORE, 4, true, 256, 2>(a, sm_count, stream);
+        if (words <= 512) return launch_rows<T, 4, MORE, 4, true, 256, 2>(a, sm_count, stream);
+        if (words <= 1024) return launch_rows<T, 3, MORE, 0, true, 512, 1>(a, sm_count, stream);
+        if (words <= 2048) return launch_rows<T, 4, MORE, 0, true, 512, 1>(a, sm_count, stream);
+        if (words <= 6 * 512) return launch_rows<T, 6, MORE, 0, false, 512, 1>(a, sm_count, stream);
+    }
     return launch_layer_norm_backward_any(a, sm_count, stream);
 }
 

@@ -79,18 +79,14 @@ def velora_head_distill_backward(X: torch.Tensor, W: torch.Tensor, index: torch.
     return dX, dW
 
 
-def _rows_like(t: Optional[torch.Tensor], X: torch.Tensor, name: str):
-    """Address and pitch of a matrix like X; None: there is none."""
-    if t is None:
-        return None, X.shape[1]
+def _rows_like(t: torch.Tensor, X: torch.Tensor, name: str):
+    """Address and pitch of a matrix like X."""
     if t.shape != X.shape or t.dtype != X.dtype:
         raise ValueError("%s must have the rows' shape and type" % name)
     return b._mat(t, name)
 
 
-def _columns(t: Optional[torch.Tensor], D: int, name: str):
-    if t is None:
-        return None
+def _columns(t: torch.Tensor, D: int, name: str) -> int:
     if t.ndim != 1 or t.shape[0] != D or not t.is_cuda or not t.is_contiguous():
         raise ValueError("%s must be a contiguous CUDA tensor with one element per column" % name)
     return t.data_ptr()
@@ -103,34 +99,51 @@ def velora_layer_norm(X: torch.Tensor, weight: Optional[torch.Tensor] = None, bi
     where nothing is added."""
     if stream is not None and (Y is None or mean is None or rstd is None or (residual is not None and H is None)):
         return b._on(stream, velora_layer_norm, X, weight, bias, eps, residual, Y, H, mean, rstd)
-    if X.ndim != 2:
-        raise ValueError("X must be a 2-d CUDA tensor")
-    N, D = X.shape
-    if residual is None and H is not None and H is not X:
-        raise ValueError("H is X where nothing is added")
-    if weight is not None and bias is not None and weight.dtype != bias.dtype:
-        raise ValueError("weight and bias must have one type")
     xp, ldx = b._mat(X, "X")
-    rp, ldr = _rows_like(residual, X, "residual")
+    N, D = X.shape
+    given = [X]                                               # what is made here needs no look
+    rp, ldr, hp, ldh, wp, bp, p_dtype = None, D, None, D, None, None, b.F32
+    if residual is not None:
+        rp, ldr = _rows_like(residual, X, "residual")
+        given.append(residual)
+        if H is None:
+            H = torch.empty_like(X, memory_format=torch.contiguous_format)
+            hp = H.data_ptr()
+        else:
+            hp, ldh = _rows_like(H, X, "H")
+            given.append(H)
+    elif H is None or H is X:
+        H = X
+    else:
+        raise ValueError("H is X where nothing is added")
+    if weight is not None:
+        wp, p_dtype = _columns(weight, D, "weight"), b._dt(weight)
+        given.append(weight)
+    if bias is not None:
+        if weight is not None and weight.dtype != bias.dtype:
+            raise ValueError("weight and bias must have one type")
+        bp, p_dtype = _columns(bias, D, "bias"), b._dt(bias)
+        given.append(bias)
     if Y is None:
-        Y = torch.empty((N, D), dtype=X.dtype, device=X.device)
+        Y = torch.empty_like(X, memory_format=torch.contiguous_format)
+        yp, ldy = Y.data_ptr(), D
+    else:
+        yp, ldy = _rows_like(Y, X, "Y")
+        given.append(Y)
     if mean is None:
         mean = torch.empty(N, dtype=torch.float32, device=X.device)
+        mp = mean.data_ptr()
+    else:
+        mp = b._tokens(mean, N, torch.float32, "mean")
+        given.append(mean)
     if rstd is None:
         rstd = torch.empty(N, dtype=torch.float32, device=X.device)
-    yp, ldy = _rows_like(Y, X, "Y")
-    if residual is None:
-        H, hp, ldh = X, None, D
+        sp = rstd.data_ptr()
     else:
-        if H is None:
-            H = torch.empty((N, D), dtype=X.dtype, device=X.device)
-        hp, ldh = _rows_like(H, X, "H")
-    wp, bp = _columns(weight, D, "weight"), _columns(bias, D, "bias")
-    mp, sp = b._tokens(mean, N, torch.float32, "mean"), b._tokens(rstd, N, torch.float32, "rstd")
-    b._here(*(t for t in (X, Y, H, mean, rstd, residual, weight, bias) if t is not None))
-    params = weight if weight is not None else bias
-    rc = b.lib().velora_layer_norm(xp, ldx, rp, ldr, wp, bp, b.F32 if params is None else b._dt(params), eps, hp, ldh, yp, ldy, mp, sp, b._dt(X), N, D,
-                                 b._stream(stream))
+        sp = b._tokens(rstd, N, torch.float32, "rstd")
+        given.append(rstd)
+    b._here(*given)
+    rc = b.lib().velora_layer_norm(xp, ldx, rp, ldr, wp, bp, p_dtype, eps, hp, ldh, yp, ldy, mp, sp, b._dt(X), N, D, b._stream(stream))
     b._check(rc, "velora_layer_norm")
     return Y, H, mean, rstd
 
@@ -142,33 +155,55 @@ def velora_layer_norm_backward(dY: torch.Tensor, H: torch.Tensor, mean: torch.Te
     """(dX, dweight, dbias) of velora_layer_norm, given what it returned and the gradients of Y and, where H went on to another layer, of H."""
     if stream is not None and ((need_dX and dX is None) or (need_dweight and dweight is None) or (need_dbias and dbias is None) or ws is None):
         return b._on(stream, velora_layer_norm_backward, dY, H, mean, rstd, weight, dH, dX, dweight, dbias, need_dX, need_dweight, need_dbias,
-                   dw_dtype, beta, ws)
-    if H.ndim != 2:
-        raise ValueError("H must be a 2-d CUDA tensor")
-    N, D = H.shape
-    if beta and ((need_dweight and dweight is None) or (need_dbias and dbias is None)):
-        raise ValueError("beta = 1 adds to a dweight and a dbias that are passed in")
+                     dw_dtype, beta, ws)
     hp, ldh = b._mat(H, "H")
+    N, D = H.shape
     yp, lddy = _rows_like(dY, H, "dY")
-    gp, lddh = _rows_like(dH, H, "dH")
-    kind = dw_dtype or (weight.dtype if weight is not None else torch.float32)
-    if need_dX and dX is None:
-        dX = torch.empty((N, D), dtype=H.dtype, device=H.device)
-    if need_dweight and dweight is None:
-        dweight = torch.empty(D, dtype=dbias.dtype if need_dbias and dbias is not None else kind, device=H.device)
-    if need_dbias and dbias is None:
-        dbias = torch.empty(D, dtype=dweight.dtype if need_dweight else kind, device=H.device)
-    dX, dweight, dbias = dX if need_dX else None, dweight if need_dweight else None, dbias if need_dbias else None
+    mp, sp = b._tokens(mean, N, torch.float32, "mean"), b._tokens(rstd, N, torch.float32, "rstd")
+    given = [dY, H, mean, rstd]                               # what is made here needs no look
+    wp, p_dtype, gp, lddh, xp, lddx, dwp, dbp = None, b.F32, None, D, None, D, None, None
+    if weight is not None:
+        wp, p_dtype = _columns(weight, D, "weight"), b._dt(weight)
+        given.append(weight)
+    if dH is not None:
+        gp, lddh = _rows_like(dH, H, "dH")
+        given.append(dH)
+    if not need_dX:
+        dX = None
+    elif dX is None:
+        dX = torch.empty_like(H, memory_format=torch.contiguous_format)
+        xp = dX.data_ptr()
+    else:
+        xp, lddx = _rows_like(dX, H, "dX")
+        given.append(dX)
+    dweight, dbias = dweight if need_dweight else None, dbias if need_dbias else None
     if dweight is not None and dbias is not None and dweight.dtype != dbias.dtype:
         raise ValueError("dweight and dbias must have one type")
-    xp, lddx = _rows_like(dX, H, "dX")
-    wp, dwp, dbp = _columns(weight, D, "weight"), _columns(dweight, D, "dweight"), _columns(dbias, D, "dbias")
-    mp, sp = b._tokens(mean, N, torch.float32, "mean"), b._tokens(rstd, N, torch.float32, "rstd")
-    b._here(*(t for t in (dY, H, mean, rstd, weight, dH, dX, dweight, dbias) if t is not None))
-    sums = dweight if dweight is not None else dbias
+    if (need_dweight and dweight is None) or (need_dbias and dbias is None):
+        if beta:
+            raise ValueError("beta = 1 adds to a dweight and a dbias that are passed in")
+        kind = dweight.dtype if dweight is not None else dbias.dtype if dbias is not None else dw_dtype or (torch.float32 if weight is None else weight.dtype)
+    if need_dweight:
+        if dweight is None:
+            dweight = torch.empty(D, dtype=kind, device=H.device)
+            dwp = dweight.data_ptr()
+        else:
+            dwp = _columns(dweight, D, "dweight")
+            given.append(dweight)
+    if need_dbias:
+        if dbias is None:
+            dbias = torch.empty(D, dtype=kind, device=H.device)
+            dbp = dbias.data_ptr()
+        else:
+            dbp = _columns(dbias, D, "dbias")
+            given.append(dbias)
+    b._here(*given)
+    sums, room = dweight if need_dweight else dbias, (None, 0)
     if ws is None and sums is not None:
         ws = b.velora_workspace_alloc(b.velora_workspace_bytes(b.OP_LAYER_NORM_BACKWARD, N, D, 1, 1, False), H.device)
-    rc = b.lib().velora_layer_norm_backward(yp, lddy, hp, ldh, mp, sp, wp, b.F32 if weight is None else b._dt(weight), gp, lddh, xp, lddx, dwp, dbp,
-                                          b.F32 if sums is None else b._dt(sums), beta, b._dt(H), N, D, *((None, 0) if ws is None else b._room(ws)), b._stream(stream))
+    if ws is not None:
+        room = b._room(ws)
+    rc = b.lib().velora_layer_norm_backward(yp, lddy, hp, ldh, mp, sp, wp, p_dtype, gp, lddh, xp, lddx, dwp, dbp,
+                                            b.F32 if sums is None else b._dt(sums), beta, b._dt(H), N, D, *room, b._stream(stream))
     b._check(rc, "velora_layer_norm_backward")
     return dX, dweight, dbias

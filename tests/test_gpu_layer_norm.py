@@ -135,6 +135,17 @@ def test_norm_and_gradients(vl, guard, N, D, dtype, residual):
     run(vl, guard, p, residual, dtype, ld=D)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("residual", [False, True])
+def test_widths_around_every_multiple_of_a_warps_words(vl, guard, dtype, residual):
+    """Rows of 32 n - 1, 32 n and 32 n + 1 words of 16 bytes, up to the longest that is held and beyond."""
+    words = torch.finfo(dtype).bits // 8
+    per = 16 // words
+    for n in list(range(1, 16)) + list(range(16, 98, 3)):
+        for w in (32 * n - 1, 32 * n, 32 * n + 1):
+            run(vl, guard, batch(2, w * per, dtype, w), residual, dtype)
+
+
 def test_more_rows_than_slices_or_blocks(vl, guard):
     for N, D in ((20011, 24), (5003, 264), (3001, 1320)):
         run(vl, guard, batch(N, D, torch.bfloat16, 3), True, torch.bfloat16)

@@ -210,7 +210,8 @@ def seen(monkeypatch):
         r.lent += 1
 
     monkeypatch.setattr(torch.cuda, "stream", stream_context)
-    monkeypatch.setattr(torch, "empty", recording(torch.empty))
+    for name in ("empty", "empty_like"):
+        monkeypatch.setattr(torch, name, recording(getattr(torch, name)))
     monkeypatch.setattr(b, "lib", lambda: Library())
     monkeypatch.setattr(b, "_mat", lambda t, name: (t.data_ptr(), t.stride(0)))
     monkeypatch.setattr(b, "_tokens", lambda t, n, dtype, name: t.data_ptr())
