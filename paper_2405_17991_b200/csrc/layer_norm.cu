@@ -10,13 +10,6 @@ namespace velora {
 
 namespace {
 
-// 1 / sqrt(v): the approximation and one step of Newton's method, where that has a meaning.
-__device__ __forceinline__ float inverse_root(float v)
-{
-    const float r = rsqrtf(v), e = fmaf(-v * r, r, 1.f);
-    return v > 1e-37f && v < 1e37f ? fmaf(0.5f * r, e, r) : 1.f / sqrtf(v);
-}
-
 template <typename T, int C, int STAGES, bool RESIDUAL, bool ONE, int THREADS, int BLOCKS>
 __global__ void __launch_bounds__(THREADS, BLOCKS)
 norm_rows_kernel(const NormArgs a, bool wide)

@@ -55,6 +55,14 @@ inline int64_t norm_pitch(int64_t D) { return (D + 7) / 8 * 8; }
 // Rows of `partials`, at most.
 constexpr int kNormSlices = 296;
 inline int64_t norm_slices(int64_t N) { return N < kNormSlices ? N : kNormSlices; }
+// Blocks of `teams` rows at a time, up to `most`.  Where dw or db is asked for, each leaves a row of sums that is written and read: then one for four rows at
+// the most, once there are 64 of them.
+inline int64_t norm_grad_blocks(const NormGradArgs& a, int teams, int64_t most)
+{
+    const int64_t rounds = ceil_div64(a.N, teams), few = a.dw || a.db ? ceil_div64(rounds, 4) : rounds, blocks = few > 64 ? few : (rounds < 64 ? rounds : 64);
+    if (most > kNormSlices) most = kNormSlices;
+    return blocks < most ? blocks : most;
+}
 
 // Rows of any length (layer_norm_any.cu).
 int launch_layer_norm_any(const NormArgs& a, int sm_count, cudaStream_t stream);

@@ -114,32 +114,53 @@ norm_columns_kernel(const NormGradArgs a, int slices)
     a.partials[static_cast<int64_t>(slices + slice) * norm_pitch(a.D) + d] = db;
 }
 
-// The slices' sums in a fixed order: a block takes 32 columns of dw or db, a warp every 32nd slice, ten loads under way at once, which all of kNormSlices are.
-constexpr int kSliceWarps = 32, kSliceLoads = 10;
-static_assert(kSliceWarps * kSliceLoads >= kNormSlices, "one round");
-__global__ void __launch_bounds__(32 * kSliceWarps)
+// The slices' sums in a fixed order: a block takes 32 V columns of dw or db, a warp every WARPS-th slice, LOADS of them under way at once.  Two shapes:
+// eight warps of two columns a lane for up to 160 slices, which are one round (64 x 4096: 1.7 us, 32 warps 4.0); 32 warps of one for more (behind the kernel
+// that writes them, 296 x 4096: 5.1 us for both together, 7.7 with eight warps).
+template <int WARPS, int LOADS, int V>
+__global__ void __launch_bounds__(32 * WARPS)
 norm_slices_kernel(const float* partials, int slices, int D, void* dw, void* db, int dtype, int beta)
 {
-    __shared__ float part[kSliceWarps][33];
+    __shared__ float part[WARPS][32 * V];
     pdl_wait();
     pdl_trigger();
     void* out = blockIdx.y ? db : dw;
     if (!out) return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = blockIdx.x * 32 + lane;
-    const int64_t pitch = norm_pitch(D);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = (blockIdx.x * 32 + lane) * V;
+    const int64_t pitch = norm_pitch(D);                      // a multiple of eight
     const float* p = partials + blockIdx.y * slices * pitch + d;
-    float x[kSliceLoads];
+    float2 s = make_float2(0.f, 0.f);
+    for (int first = warp; first < slices; first += WARPS * LOADS) {
+        float2 x[LOADS];
 #pragma unroll
-    for (int i = 0; i < kSliceLoads; ++i) x[i] = d < D && warp + kSliceWarps * i < slices ? p[(warp + kSliceWarps * i) * pitch] : 0.f;
-    float s = 0.f;
+        for (int i = 0; i < LOADS; ++i) {
+            const bool is = d < D && first + WARPS * i < slices;
+            const float* q = p + (first + WARPS * i) * pitch;
+            if (V == 2) x[i] = is ? *reinterpret_cast<const float2*>(q) : make_float2(0.f, 0.f);
+            else x[i].x = is ? *q : 0.f;
+        }
 #pragma unroll
-    for (int i = 0; i < kSliceLoads; ++i) s += x[i];
-    part[warp][lane] = s;
+        for (int i = 0; i < LOADS; ++i) {
+            s.x += x[i].x;
+            if (V == 2) s.y += x[i].y;
+        }
+    }
+    if (V == 2) *reinterpret_cast<float2*>(&part[warp][2 * lane]) = s;
+    else part[warp][lane] = s.x;
     __syncthreads();
-    s = part[lane][warp];                                     // column blockIdx.x * 32 + warp, of warp `lane`
+    const int c = blockIdx.x * 32 * V + threadIdx.x;
+    if (threadIdx.x >= 32 * V || c >= D) return;
+    float t[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (lane == 0 && blockIdx.x * 32 + warp < D) store_param(out, dtype, blockIdx.x * 32 + warp, s, beta);
+    for (int w = 0; w < WARPS; ++w) t[w & 3] += part[w][threadIdx.x];
+    store_param(out, dtype, c, (t[0] + t[1]) + (t[2] + t[3]), beta);
+}
+
+template <int WARPS, int LOADS, int V>
+int launch_slices(const NormGradArgs& a, int slices, cudaStream_t stream)
+{
+    return launch_chained(norm_slices_kernel<WARPS, LOADS, V>, dim3(static_cast<unsigned>(ceil_div64(a.D, 32 * V)), 2), 32 * WARPS, 0, stream, a.partials,
+                          slices, a.D, a.dw, a.db, a.dw_dtype, a.beta);
 }
 
 template <typename T>
@@ -179,8 +200,7 @@ int launch_layer_norm_backward_any(const NormGradArgs& a, int sm_count, cudaStre
 
 int launch_norm_slices(const NormGradArgs& a, int slices, cudaStream_t stream)
 {
-    return launch_chained(norm_slices_kernel, dim3(static_cast<unsigned>(ceil_div64(a.D, 32)), 2), 32 * kSliceWarps, 0, stream, a.partials, slices, a.D,
-                          a.dw, a.db, a.dw_dtype, a.beta);
+    return slices <= 160 ? launch_slices<8, 20, 2>(a, slices, stream) : launch_slices<32, 10, 1>(a, slices, stream);
 }
 
 }  // namespace velora

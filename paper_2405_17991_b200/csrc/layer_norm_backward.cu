@@ -1,7 +1,7 @@
 // Gradients of a layer norm.
 //   xhat = (h - m) s,  c = dy w,  dx = dh + s (c - mean c - xhat mean(c xhat)),  dw = sum_n dy xhat,  db = sum_n dy
 // Bound by HBM: dy, h (and dh) once in, dx once out.  Rows are dealt out and fetched as in layer_norm.cu.  A thread adds its columns of dw and db up in
-// registers from row to row; a block's go to its row of `partials`, and a second kernel adds those up in order.  (One block: it writes dw and db itself.)
+// registers from row to row; a block's go to its row of `partials`, and a second kernel adds those up in order.
 #include "layer_norm_rows.cuh"
 
 namespace velora {
@@ -20,16 +20,6 @@ template <int E, bool WIDE> __device__ __forceinline__ void store_sums(float* p,
         for (int i = 0; i < E / 2; ++i) reinterpret_cast<float2*>(p)[i] = parts(x[i]);
     }
 }
-// To a gradient that starts anywhere: one load or store a column, all under way at once.
-template <int E> __device__ __forceinline__ void store_params(void* p, int dtype, int col, const F2 (&x)[E / 2], int beta)
-{
-    float y[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) y[e] = (e & 1 ? parts(x[e >> 1]).y : parts(x[e >> 1]).x) + (beta ? load_param(p, dtype, col + e, 0.f) : 0.f);
-#pragma unroll
-    for (int e = 0; e < E; ++e) store_param(p, dtype, col + e, y[e], 0);
-}
-
 // TEAM: the warps that have a row, so that a block of 256 threads has 8 / TEAM at a time; 0: the whole block has one.  KEEP: xhat and c stay in registers between the row's sums and dx; else dy and h are read from shared memory again.
 template <typename T, int C, int STAGES, bool MORE, int TEAM, bool KEEP, int THREADS, int BLOCKS>
 __global__ void __launch_bounds__(THREADS, BLOCKS)
@@ -155,7 +145,6 @@ norm_grad_rows_kernel(const NormGradArgs a, bool wide)
         dx_at += a.lddx;
     }
     if (!a.dw && !a.db) return;
-    const bool alone = gridDim.x == 1;
     float* out_w = a.partials + static_cast<int64_t>(blockIdx.x) * norm_pitch(D);
     float* out_b = out_w + static_cast<int64_t>(gridDim.x) * norm_pitch(D);
     if (TEAM) {                                                // the teams' sums, through the ring's room
@@ -177,8 +166,7 @@ norm_grad_rows_kernel(const NormGradArgs a, bool wide)
                 float x = 0.f;
 #pragma unroll
                 for (int i = 0; i < kTeams; ++i) x += sums[i * kColumns + d];
-                if (!alone) (which ? out_b : out_w)[d] = x;
-                else if (which ? a.db : a.dw) store_param(which ? a.db : a.dw, a.dw_dtype, d, x, a.beta);
+                (which ? out_b : out_w)[d] = x;
             }
         }
         return;
@@ -187,13 +175,8 @@ norm_grad_rows_kernel(const NormGradArgs a, bool wide)
     for (int c = 0; c < C; ++c)
         if (c < C - 1 || last) {
             const int d = (c * P + t) * E;
-            if (!alone) {
-                store_sums<E, KEEP>(out_w + d, dw[c]);
-                store_sums<E, KEEP>(out_b + d, db[c]);
-            } else {
-                if (a.dw) store_params<E>(a.dw, a.dw_dtype, d, dw[c], a.beta);
-                if (a.db) store_params<E>(a.db, a.dw_dtype, d, db[c], a.beta);
-            }
+            store_sums<E, KEEP>(out_w + d, dw[c]);
+            store_sums<E, KEEP>(out_b + d, db[c]);
         }
 }
 
@@ -215,14 +198,10 @@ int launch_rows(const NormGradArgs& a, int sm_count, cudaStream_t stream)
     static_assert(TEAM == 0 || kStages * kRow >= C * THREADS * Word<T>::E * 4, "room for the teams' sums");
     const int words = row_words(a.D, a.dtype), threads = TEAM ? THREADS : row_threads(words, C), per_row = TEAM ? 32 * TEAM : threads;
     if (threads > THREADS || (C - 1) * per_row >= words || C * per_row < words) return VELORA_ERR_UNSUPPORTED;         // only last words may be missing
-    // Where dw or db is asked for, each block leaves a row of sums that is written and read: a quarter of the rows at most, once there are 64 of them.
-    const int64_t rounds = ceil_div64(a.N, kTeams), few = a.dw || a.db ? ceil_div64(rounds, 4) : rounds;
-    int64_t blocks = few > 64 ? few : (rounds < 64 ? rounds : 64);
-    const int64_t most = static_cast<int64_t>(sm_count) * BLOCKS < kNormSlices ? static_cast<int64_t>(sm_count) * BLOCKS : kNormSlices;
-    if (blocks > most) blocks = most;
+    const int64_t blocks = norm_grad_blocks(a, kTeams, sm_count * BLOCKS);
     const int rc = launch_chained(kern, dim3(static_cast<unsigned>(blocks)), threads, static_cast<size_t>(kStages) * kRow / THREADS * threads, stream, a,
                                   aligned16(a.w));
-    if (rc != VELORA_OK || blocks == 1 || (!a.dw && !a.db)) return rc;
+    if (rc != VELORA_OK || (!a.dw && !a.db)) return rc;
     return launch_norm_slices(a, static_cast<int>(blocks), stream);
 }
 

@@ -124,6 +124,12 @@ template <int BEHIND> __device__ __forceinline__ void copies_wait()          // 
     asm volatile("cp.async.wait_group %0;" ::"n"(BEHIND) : "memory");
 }
 
+// 1 / sqrt(v): the approximation and one step of Newton's method, where that has a meaning.
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const float r = rsqrtf(v), e = fmaf(-v * r, r, 1.f);
+    return v > 1e-37f && v < 1e37f ? fmaf(0.5f * r, e, r) : 1.f / sqrtf(v);
+}
 __device__ __forceinline__ float warp_total(float x)
 {
 #pragma unroll

@@ -146,6 +146,14 @@ def test_widths_around_every_multiple_of_a_warps_words(vl, guard, dtype, residua
             run(vl, guard, batch(2, w * per, dtype, w), residual, dtype)
 
 
+@pytest.mark.parametrize("residual", [False, True])
+def test_odd_widths_around_every_tier(vl, guard, residual):
+    for D in (31, 33, 255, 257, 511, 513, 1023, 1025, 2047, 2049, 2559, 2561, 4095, 4097, 5631, 5633, 7167, 7169, 8191, 8193, 10239, 10241, 12287, 12289):
+        run(vl, guard, batch(5, D, torch.bfloat16, D), residual, torch.bfloat16, ld=D)
+        if D % 4 == 1:
+            run(vl, guard, batch(3, D, torch.float32, D), residual, torch.float32, ld=D)
+
+
 def test_more_rows_than_slices_or_blocks(vl, guard):
     for N, D in ((20011, 24), (5003, 264), (3001, 1320)):
         run(vl, guard, batch(N, D, torch.bfloat16, 3), True, torch.bfloat16)
