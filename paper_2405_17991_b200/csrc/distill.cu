@@ -14,15 +14,13 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr unsigned long long kLast = ~0ull;               // sorts behind every entry
-
 struct ListsArgs {
     Teacher t;
     int64_t* mark;                                         // 0: has entries; -1: has none; V: one of them is no column
     Entry* entries;
     unsigned short* starts;
     float* mass;
-    int N, V, pitch, size;                                 // size: K rounded up to a power of two
+    int N, V, pitch, size, shift;                          // size: K rounded up to a power of two, 2^shift
     float inverse_t;
 };
 
@@ -31,17 +29,22 @@ __device__ __forceinline__ float teacher_logit(const Teacher& t, int64_t at)
     return t.t_dtype == VELORA_BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(t.logits)[at]) : static_cast<const float*>(t.logits)[at];
 }
 
-// A warp a token: probabilities, a bitonic sort of (column, place in the list) in shared memory, starts by bisection.
+// A warp a token: probabilities, the entries' order by (column, place in the list), where every 128 columns' entries start.  KEY holds both (32 bits where they
+// fit).  Up to 64 entries are put in order by counting, for each, the smaller ones, 64 comparisons that wait for nothing (bitonic steps through shared memory
+// one after the other: 8192 lists of 64 22 us instead of 16); starts by a search a lane and a walk along its share of the columns, by searches for longer lists,
+// of which one lane might have them all to walk along.
+template <typename KEY, bool FEW>
 __global__ void __launch_bounds__(kThreads)
 distill_lists_kernel(const ListsArgs a)
 {
-    extern __shared__ unsigned long long keys_of_warps[];
+    constexpr KEY kLast = ~static_cast<KEY>(0);               // sorts behind every entry; none is as large
+    extern __shared__ __align__(16) char room[];
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    unsigned long long* key = keys_of_warps + warp * a.size;
-    float* p = reinterpret_cast<float*>(keys_of_warps + warps * a.size) + warp * a.size;
-    const int K = a.t.K;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, K = a.t.K;
+    KEY* key = reinterpret_cast<KEY*>(room) + warp * a.size;
+    float* p = reinterpret_cast<float*>(room + static_cast<size_t>(warps) * a.size * sizeof(KEY)) + warp * a.size;
+    KEY* sorted = FEW ? reinterpret_cast<KEY*>(room + static_cast<size_t>(warps) * a.size * (sizeof(KEY) + 4)) + warp * a.size : key;
     for (int n = blockIdx.x * warps + warp; n < a.N; n += gridDim.x * warps) {
         bool bad = false, some = false;
         float m = -INFINITY;
@@ -54,7 +57,7 @@ distill_lists_kernel(const ListsArgs a)
             some |= is && u != -INFINITY;                  // a NaN is something
             m = fmaxf(m, u);
             p[k] = u;
-            key[k] = is ? static_cast<unsigned long long>(i) << 32 | static_cast<unsigned>(k) : kLast;
+            key[k] = is ? static_cast<KEY>(i) << a.shift | static_cast<unsigned>(k) : kLast;
             count += is;
         }
         bad = __any_sync(0xffffffffu, bad);
@@ -62,41 +65,66 @@ distill_lists_kernel(const ListsArgs a)
         count = __reduce_add_sync(0xffffffffu, count);
         if (lane == 0) a.mark[n] = bad ? a.V : (some ? 0 : -1);
         if (!some) continue;                               // for the warp; nobody reads its entries
-        float s = 0.f, scale = 1.f;
+        float s = 0.f;
         if (a.t.lse) {
             m = a.t.lse[n];
             for (int k = lane; k < K; k += 32) s += p[k] = p[k] == -INFINITY ? 0.f : expf(p[k] - m);
         } else {
             m = warp_max(m);
             for (int k = lane; k < K; k += 32) s += p[k] = expf(p[k] - m);
-            scale = 1.f / warp_sum(s);
+            const float scale = 1.f / warp_sum(s);
             s = 0.f;
             for (int k = lane; k < K; k += 32) s += p[k] *= scale;
         }
         s = warp_sum(s);
         if (lane == 0) a.mass[n] = s;
         __syncwarp();
-        for (int run = 2; run <= a.size; run *= 2)
-            for (int step = run / 2; step > 0; step /= 2) {
-                for (int i = lane; i < a.size / 2; i += 32) {
-                    const int x = 2 * i - (i & (step - 1)), y = x + step;
-                    const unsigned long long kx = key[x], ky = key[y];
-                    if ((kx > ky) == ((x & run) == 0)) {
-                        key[x] = ky;
-                        key[y] = kx;
-                    }
-                }
-                __syncwarp();
-            }
         Entry* out = a.entries + static_cast<int64_t>(n) * K;
-        for (int j = lane; j < count; j += 32) out[j] = Entry{static_cast<int>(key[j] >> 32), p[static_cast<unsigned>(key[j])]};
+        const unsigned place = (1u << a.shift) - 1u;
+        if (FEW) {
+            for (int k = lane; k < a.size; k += 32) {
+                const KEY mine = key[k];
+                int rank = 0;
+#pragma unroll 8
+                for (int j = 0; j < a.size; ++j) rank += key[j] < mine;
+                if (mine != kLast) {
+                    sorted[rank] = mine;
+                    out[rank] = Entry{static_cast<int>(mine >> a.shift), p[k]};
+                }
+            }
+        } else {
+            for (int run = 2; run <= a.size; run *= 2)
+                for (int step = run / 2; step > 0; step /= 2) {
+                    for (int i = lane; i < a.size / 2; i += 32) {
+                        const int x = 2 * i - (i & (step - 1)), y = x + step;
+                        const KEY kx = key[x], ky = key[y];
+                        if ((kx > ky) == ((x & run) == 0)) {
+                            key[x] = ky;
+                            key[y] = kx;
+                        }
+                    }
+                    __syncwarp();
+                }
+            for (int j = lane; j < count; j += 32) out[j] = Entry{static_cast<int>(key[j] >> a.shift), p[static_cast<unsigned>(key[j]) & place]};
+        }
+        for (int j = count + lane; j < K; j += 32) out[j] = Entry{0, 0.f};                  // none
+        __syncwarp();
         unsigned short* starts = a.starts + static_cast<int64_t>(n) * a.pitch;
-        for (int b = lane; b < a.pitch; b += 32) {
-            const unsigned long long from = static_cast<unsigned long long>(b) * kEntryColumns << 32;
-            int lo = 0, hi = count;
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                if (key[mid] < from) lo = mid + 1; else hi = mid;
+        const int share = FEW ? (a.pitch + 31) / 32 : 1, step = FEW ? 1 : 32, first = lane * share, behind = FEW ? min(a.pitch, first + share) : a.pitch;
+        int lo = 0;
+        for (int b = first; b < behind; b += step) {
+            const KEY from = static_cast<KEY>(b) * kEntryColumns << a.shift;
+            // The last start is behind all entries: its key may not fit.
+            if (b == a.pitch - 1) lo = count;
+            else if (FEW && b > first) {
+                while (lo < count && sorted[lo] < from) ++lo;
+            } else {
+                lo = 0;
+                int hi = count;
+                while (lo < hi) {
+                    const int mid = (lo + hi) / 2;
+                    if (sorted[mid] < from) lo = mid + 1; else hi = mid;
+                }
             }
             starts[b] = static_cast<unsigned short>(lo);
         }
@@ -180,65 +208,86 @@ distill_gradient_kernel(float* logits, int64_t ld, int parts, int64_t part_strid
     }
 }
 
-// A block takes 32 rows: eight slices of their parts, then the eight together; then a warp four rows' entries.
-__global__ void __launch_bounds__(kThreads)
-distill_merge_kernel(const HeadTile h, int parts, float* loss, float* lse)
+__device__ __forceinline__ float2 merged(float2 a, float2 b)          // (maximum, sum of exponentials relative to it); a NaN stays one
 {
-    __shared__ float2 slice[kWarps][32];
-    __shared__ float sums[32];
+    const float m = a.x > b.x ? a.x : (a.x == a.x ? b.x : a.x), ref = m == -INFINITY ? 0.f : m;
+    return make_float2(m, a.y * expf(a.x - ref) + b.y * expf(b.x - ref));
+}
+
+// A block takes up to 32 rows: its threads are shared out over rows and slices of their parts, 16 loads in flight each, a warp puts a row's slices together; then
+// a warp takes two rows' entries.  Few rows have that many more slices.
+constexpr int kMergeThreads = 512, kMergeWarps = kMergeThreads / 32;
+__global__ void __launch_bounds__(kMergeThreads)
+distill_merge_kernel(const HeadTile h, int parts, int rows, float* loss, float* lse)          // rows: a power of two
+{
+    __shared__ float2 slice[kMergeThreads];
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row0 = blockIdx.x * 32;
-    const int live = *h.live;
-    float m = -INFINITY, s = 0.f;
-    if (row0 + lane < live) {
-        for (int p0 = warp; p0 < parts; p0 += kWarps * 8) {                   // eight loads in flight
-            float2 x[8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row0 = blockIdx.x * rows, slices = kMergeThreads / rows;
+    const int live = *h.live, mine = row0 + static_cast<int>(threadIdx.x) % rows;
+    float2 ms = make_float2(-INFINITY, 0.f);
+    if (mine < live) {
+        const float2* p = h.running + mine;
+        for (int p0 = static_cast<int>(threadIdx.x) / rows; p0 < parts; p0 += slices * 16) {
+            float2 x[16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int p = p0 + kWarps * i;
-                x[i] = p < parts ? h.running[static_cast<int64_t>(p) * h.N + row0 + lane] : make_float2(-INFINITY, 0.f);
+            for (int i = 0; i < 16; ++i) x[i] = p0 + slices * i < parts ? p[static_cast<int64_t>(p0 + slices * i) * h.N] : make_float2(-INFINITY, 0.f);
+            float m = ms.x;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m = x[i].x > m ? x[i].x : (x[i].x == x[i].x ? m : x[i].x);      // a NaN stays one
+            const float ref = m == -INFINITY ? 0.f : m;
+            float s = ms.y * expf(ms.x - ref);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s += x[i].y * expf(x[i].x - ref);
+            ms = make_float2(m, s);
+        }
+    }
+    slice[static_cast<int>(threadIdx.x) % rows * slices + static_cast<int>(threadIdx.x) / rows] = ms;
+    // What the entries need, on its way meanwhile.
+    int token[2], mark[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = warp + kMergeWarps * i;
+        mark[i] = -3;
+        if (r < rows && row0 + r < h.N) {
+            mark[i] = h.target[row0 + r];
+            token[i] = h.e.order[row0 + r];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (mark[i] == -3) continue;                           // for the warp
+        const int r = warp + kMergeWarps * i;
+        float y = 0.f, z = 0.f;
+        if (mark[i] >= 0) {
+            const Entry* entries = h.e.entries + static_cast<int64_t>(token[i]) * h.e.K;
+            const float* at = h.e.at + static_cast<int64_t>(token[i]) * h.e.K;
+            Entry e[2];
+            float l[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const bool is = lane + 32 * k < h.e.K;
+                e[k].p = is ? entries[lane + 32 * k].p : 0.f;
+                l[k] = is ? at[lane + 32 * k] : 0.f;
             }
-            float both = m;
+            ms = make_float2(-INFINITY, 0.f);
+            for (int k = lane; k < slices; k += 32) ms = merged(ms, slice[r * slices + k]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) both = x[i].x > both ? x[i].x : (x[i].x == x[i].x ? both : x[i].x);      // a NaN stays one
-            const float ref = both == -INFINITY ? 0.f : both;
-            s *= expf(m - ref);
+            for (int o = 16; o > 0; o >>= 1) ms = merged(ms, make_float2(__shfl_xor_sync(0xffffffffu, ms.x, o), __shfl_xor_sync(0xffffffffu, ms.y, o)));
+            z = ms.x + logf(ms.y);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += x[i].y * expf(x[i].x - ref);
-            m = both;
-        }
-    }
-    slice[warp][lane] = make_float2(m, s);
-    __syncthreads();
-    if (warp == 0) {
-        m = -INFINITY;
-        bool nan = false;
-        for (int w = 0; w < kWarps; ++w) {
-            m = fmaxf(m, slice[w][lane].x);
-            nan |= slice[w][lane].x != slice[w][lane].x;
-        }
-        const float ref = m == -INFINITY ? 0.f : m;
-        s = nan ? __int_as_float(0x7fc00000) : 0.f;
-        for (int w = 0; w < kWarps; ++w) s += slice[w][lane].y * expf(slice[w][lane].x - ref);
-        sums[lane] = m + logf(s);
-    }
-    __syncthreads();
-    for (int r = warp; r < 32 && row0 + r < h.N; r += kWarps) {
-        const int row = row0 + r, n = h.e.order[row], mark = h.target[row];
-        float y = 0.f;
-        if (mark >= 0) {
-            const int count = h.e.starts[static_cast<int64_t>(n) * h.e.pitch + h.e.pitch - 1];
-            const int64_t first = static_cast<int64_t>(n) * h.e.K;
-            for (int j = lane; j < count; j += 32) {
-                const float p = h.e.entries[first + j].p;
-                if (p != 0.f) y += p * (logf(p) - (h.e.at[first + j] - sums[r]));      // p log p is 0 there, whatever the student's logit
+            for (int k = 0; k < 2; ++k)
+                if (e[k].p != 0.f) y += e[k].p * (logf(e[k].p) - (l[k] - z));              // p log p is 0 there, whatever the student's logit
+            for (int k = lane + 64; k < h.e.K; k += 32) {
+                const float p = entries[k].p;
+                if (p != 0.f) y += p * (logf(p) - (at[k] - z));
             }
             y = warp_sum(y);
         }
         if (lane == 0) {
-            loss[n] = mark == -2 ? __int_as_float(0x7fc00000) : y;
-            lse[n] = mark >= 0 ? sums[r] : 0.f;
+            loss[token[i]] = mark[i] == -2 ? __int_as_float(0x7fc00000) : y;
+            lse[token[i]] = z;
         }
     }
 }
@@ -275,12 +324,19 @@ int launch_distill_lists(const HeadArgs& a, const HeadLayout& l)
     args.V = static_cast<int>(a.V);
     args.pitch = e.pitch;
     args.size = 1;
-    while (args.size < a.teacher->K) args.size *= 2;
+    while (args.size < a.teacher->K) {
+        args.size *= 2;
+        ++args.shift;
+    }
     args.inverse_t = e.inverse_t;
     const int warps = args.size <= 256 ? kWarps : 2;       // 24 KB of keys and probabilities at most
     const int64_t ctas = ceil_div64(a.N, warps), most = static_cast<int64_t>(di.sm_count) * 8;
-    return launch_chained(distill_lists_kernel, dim3(static_cast<unsigned>(ctas < most ? ctas : most)), 32 * warps,
-                          static_cast<size_t>(warps) * args.size * 12, a.stream, args);
+    const dim3 grid(static_cast<unsigned>(ctas < most ? ctas : most));
+    const size_t keys = static_cast<size_t>(warps) * args.size;
+    const bool narrow = a.V <= (static_cast<int64_t>(1) << (32 - args.shift)) - 1;              // columns and places below 2^32 - 2^shift
+    if (!narrow) return launch_chained(distill_lists_kernel<unsigned long long, false>, grid, 32 * warps, keys * 12, a.stream, args);
+    return args.size <= 64 ? launch_chained(distill_lists_kernel<unsigned, true>, grid, 32 * warps, keys * 12, a.stream, args)
+                           : launch_chained(distill_lists_kernel<unsigned, false>, grid, 32 * warps, keys * 8, a.stream, args);
 }
 
 int launch_distill_stats(float* logits, int64_t ld, int parts, int64_t part_stride, const HeadTile& h, bool first, cudaStream_t stream)
@@ -297,7 +353,9 @@ int launch_distill_gradient(float* logits, int64_t ld, int parts, int64_t part_s
 
 int launch_distill_merge(const HeadTile& h, int parts, float* loss, float* lse, cudaStream_t stream)
 {
-    return launch_chained(distill_merge_kernel, dim3(static_cast<unsigned>(ceil_div64(h.N, 32))), kThreads, 0, stream, h, parts, loss, lse);
+    int rows = 1;
+    while (rows < 32 && rows < h.N) rows *= 2;
+    return launch_chained(distill_merge_kernel, dim3(static_cast<unsigned>(ceil_div64(h.N, rows))), kMergeThreads, 0, stream, h, parts, rows, loss, lse);
 }
 
 }  // namespace velora

@@ -131,32 +131,71 @@ __device__ __forceinline__ float sum_of_parts(const float* p, int parts, int64_t
 }
 
 constexpr int kNoColumn = 1 << 30;
-// The entries of a row that lie in some columns from `first` on, one after the other.
+// The entries of a row that lie in some columns from `first` on, one after the other; the one behind the current is on its way.
 struct EntryWalk {
     const Entry* list;
-    int j, end, first, column;                      // column: of entry j, from `first` on; kNoColumn behind the last
-    float p;
+    int j, end, first;
+    int column, next_column;                        // from `first` on; kNoColumn behind the last
+    float p, next_p;
+    __device__ __forceinline__ void fetch(int at)
+    {
+        next_column = kNoColumn;
+        if (at < end) {
+            const Entry e = list[at];
+            next_column = e.column - first;
+            next_p = e.p;
+        }
+    }
+    __device__ __forceinline__ void next()
+    {
+        ++j;
+        column = next_column;
+        p = next_p;
+        fetch(j + 1);
+    }
+    // Entries j0 .. before j1 of a token's list, the first of which is not in front of column `from`.
+    __device__ __forceinline__ void begin(const Entries& e, int token, int j0, int j1, int from)
+    {
+        list = e.entries + static_cast<int64_t>(token) * e.K;
+        j = j0;
+        end = j1;
+        first = from;
+        fetch(j);
+        column = next_column;
+        p = next_p;
+        fetch(j + 1);
+    }
     __device__ __forceinline__ void start(const Entries& e, int token, int from, int columns)
     {
         const unsigned short* s = e.starts + static_cast<int64_t>(token) * e.pitch;
-        list = e.entries + static_cast<int64_t>(token) * e.K;
-        j = s[from / kEntryColumns];
-        end = s[(from + columns - 1) / kEntryColumns + 1];      // some of them may lie behind
-        first = from;
-        load();
+        begin(e, token, s[from / kEntryColumns], s[(from + columns - 1) / kEntryColumns + 1], from);      // some of them may lie behind
         while (column < 0) next();                  // of the same 128 columns, but in front
     }
-    __device__ __forceinline__ void none() { list = nullptr; j = end = 0; column = kNoColumn; }
-    __device__ __forceinline__ void load()
+    __device__ __forceinline__ void none()
     {
-        column = kNoColumn;
-        if (j < end) {
-            const Entry e = list[j];
-            column = e.column - first;
-            p = e.p;
+        list = nullptr;
+        j = end = 0;
+        column = next_column = kNoColumn;
+    }
+};
+// Where a row's entries of a tile's 128 columns are; looked up a tile ahead in two steps, since each waits for memory.
+struct EntryPlace {
+    int token;                                      // negative: the row has no part in it
+    int j, end;
+    __device__ __forceinline__ void find_token(const Entries& e, const int* target, int row, bool is)
+    {
+        token = -1;
+        if (is && target[row] >= 0) token = e.order[row];
+    }
+    __device__ __forceinline__ void find_entries(const Entries& e, int column)
+    {
+        j = end = 0;
+        if (token >= 0) {
+            const unsigned short* s = e.starts + static_cast<int64_t>(token) * e.pitch + column / kEntryColumns;
+            j = s[0];
+            end = s[1];
         }
     }
-    __device__ __forceinline__ void next() { ++j; load(); }
 };
 #endif
 

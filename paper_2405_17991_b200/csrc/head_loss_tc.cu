@@ -170,15 +170,33 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
         const uint32_t lead_tempty = map_to_cta(tempty, 0);
         const uint32_t block = staging + (warp - 2) * kStoreBytes;
         uint32_t seg = 0;
+        EntryPlace ahead;                                    // of the tile that comes next
+        if (LISTS && pair < num_tiles) {
+            const PairTile t0 = pair_tile(pair, tiles_m, tiles_n, 2 * H_BM, H_BN, H_BAND);
+            const int row = t0.m0 + static_cast<int>(rank) * H_BM + quarter * 32 + lane, col0 = t0.n0 + half * 128;
+            ahead.find_token(h.e, h.target, row, row < h.N && col0 < h.cols);
+            ahead.find_entries(h.e, h.v0 + col0);
+        }
         for (int tile = pair; tile < num_tiles && !failed; tile += num_pairs) {
             const PairTile t0 = pair_tile(tile, tiles_m, tiles_n, 2 * H_BM, H_BN, H_BAND);
             const int row0 = t0.m0 + static_cast<int>(rank) * H_BM + quarter * 32, row = row0 + lane;
             const int col0 = t0.n0 + half * 128, valid = h.cols - col0;
             uint32_t l[4][32];                               // fp32 bits
-            EntryWalk walk;                                  // its first entry is on its way while the products run
+            EntryWalk walk;                                  // its first entries are on their way while the products run
+            int col_ahead = 0;
+            float mass = 1.f;
             if (LISTS) {
                 walk.none();
-                if (row < h.N && valid > 0 && h.target[row] >= 0) walk.start(h.e, h.e.order[row], h.v0 + col0, 128);
+                if (ahead.token >= 0) {
+                    walk.begin(h.e, ahead.token, ahead.j, ahead.end, h.v0 + col0);
+                    if (STORES) mass = h.e.mass[ahead.token];
+                }
+                if (tile + num_pairs < num_tiles) {
+                    const PairTile t1 = pair_tile(tile + num_pairs, tiles_m, tiles_n, 2 * H_BM, H_BN, H_BAND);
+                    const int row1 = t1.m0 + static_cast<int>(rank) * H_BM + quarter * 32 + lane;
+                    col_ahead = t1.n0 + half * 128;
+                    ahead.find_token(h.e, h.target, row1, row1 < h.N && col_ahead < h.cols);
+                }
             }
             for (int k0 = 0; k0 < kblocks; k0 += kHeadSegment, ++seg) {
                 const uint32_t acc = seg & 1u, aph = (seg >> 1) & 1u;
@@ -207,14 +225,10 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(lead_tempty + 8 * acc);
             }
+            if (LISTS) ahead.find_entries(h.e, h.v0 + col_ahead);
             if (failed || valid <= 0) continue;
             const bool in = row < h.N;
-            if (LISTS && h.e.inverse_t != 1.f) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(__uint_as_float(l[c][i]) * h.e.inverse_t);
-            }
+            const float log2e = LISTS ? kHeadLog2e * h.e.inverse_t : kHeadLog2e;       // logits are divided by the temperature where they go into an exponent
             // Entries: this lane's 32 values through the warp's block of shared memory, a column of it that only this lane touches.
             float* turn = reinterpret_cast<float*>(smem_raw + (block - raw)) + lane;
             const int t = !LISTS && in ? h.target[row] - h.v0 - col0 : -1;                // in this warp's columns: 0 .. 127
@@ -237,7 +251,7 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                         if (__any_sync(0xffffffffu, walk.column < 32 * c + 32)) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i) turn[32 * i] = __uint_as_float(l[c][i]);
-                            for (; walk.column < 32 * c + 32; walk.next()) h.e.at[walk.list - h.e.entries + walk.j] = turn[32 * (walk.column - 32 * c)];
+                            for (; walk.column < 32 * c + 32; walk.next()) h.e.at[walk.list - h.e.entries + walk.j] = turn[32 * (walk.column - 32 * c)] * h.e.inverse_t;
                         }
                 }
                 const bool hit = !LISTS && t >= 0 && t < 128;
@@ -253,7 +267,7 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                 // 2^(l log2 e - c) with c = m log2 e as rounded, in one multiply-add each; what c lost is put right in the sum, or, where it is
                 // more than a first-order term can (m beyond 10^5), m is taken off first.
                 const float ref = m == -INFINITY ? 0.f : m;
-                float c2 = ref * kHeadLog2e, lost = fmaf(ref, kHeadLog2e, -c2);
+                float c2 = ref * log2e, lost = fmaf(ref, log2e, -c2);
                 if (__any_sync(0xffffffffu, fabsf(lost) > kHeadLost)) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
@@ -265,21 +279,21 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) s[i & 3] += head_exp2(fmaf(__uint_as_float(l[c][i]), kHeadLog2e, -c2));
+                    for (int i = 0; i < 32; ++i) s[i & 3] += head_exp2(fmaf(__uint_as_float(l[c][i]), log2e, -c2));
                 const float sum = ((s[0] + s[1]) + (s[2] + s[3])) * (1.f - lost * 0.69314718f);
-                if (in) h.running[static_cast<int64_t>((t0.n0 >> 7) + half) * h.N + row] = make_float2(m, sum);
+                if (in) h.running[static_cast<int64_t>((t0.n0 >> 7) + half) * h.N + row] = make_float2(LISTS ? m * h.e.inverse_t : m, sum);
             } else {
                 const bool is = in && h.target[row] >= 0;
                 const float g = is ? (LISTS ? h.scale[row] * h.e.inverse_t : h.scale[row]) : 0.f, lse = is ? h.lse[row] : 0.f;
-                float z = -lse * kHeadLog2e, lost = fmaf(-lse, kHeadLog2e, -z);                    // as for the statistics
+                float z = -lse * kHeadLog2e, lost = fmaf(-lse, kHeadLog2e, -z), scale = log2e;      // as for the statistics
                 if (__any_sync(0xffffffffu, fabsf(lost) > kHeadLost)) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(__uint_as_float(l[c][i]) - lse);
+                        for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint((LISTS ? __uint_as_float(l[c][i]) * h.e.inverse_t : __uint_as_float(l[c][i])) - lse);
                     z = lost = 0.f;
+                    scale = kHeadLog2e;
                 }
-                const float mass = LISTS ? (is ? h.e.mass[h.e.order[row]] : 0.f) : 1.f;
                 const float gp = (LISTS ? g * mass : g) * (1.f + lost * 0.69314718f);
                 if (LISTS && __any_sync(0xffffffffu, walk.column != kNoColumn)) {
                     if (lane == 0) bulk_wait_read();         // the last tile's outputs are out of the block
@@ -288,7 +302,7 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(head_exp2(fmaf(__uint_as_float(l[c][i]), kHeadLog2e, z)) * gp);
+                    for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(head_exp2(fmaf(__uint_as_float(l[c][i]), LISTS ? scale : kHeadLog2e, z)) * gp);
                     if (LISTS) {
                         if (__any_sync(0xffffffffu, walk.column < 32 * c + 32)) {
 #pragma unroll
