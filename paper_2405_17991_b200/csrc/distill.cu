@@ -20,7 +20,7 @@ struct ListsArgs {
     Entry* entries;
     unsigned short* starts;
     float* mass;
-    int N, V, pitch, size, shift;                          // size: K rounded up to a power of two, 2^shift
+    int N, V, pitch, size, shift;                          // size: K rounded up to a power of two, four at least, 2^shift
     float inverse_t;
 };
 
@@ -52,7 +52,8 @@ distill_lists_kernel(const ListsArgs a)
         for (int k = lane; k < a.size; k += 32) {
             const int64_t i = k < K ? a.t.index[n * a.t.ldi + k] : -1;
             const bool is = i >= 0 && i < a.V;
-            const float u = is ? teacher_logit(a.t, n * a.t.ldt + k) * a.inverse_t : -INFINITY;
+            const float t = k < K ? teacher_logit(a.t, n * a.t.ldt + k) : 0.f;              // does not wait for the column
+            const float u = is ? t * a.inverse_t : -INFINITY;
             bad |= i >= a.V;
             some |= is && u != -INFINITY;                  // a NaN is something
             m = fmaxf(m, u);
@@ -82,16 +83,20 @@ distill_lists_kernel(const ListsArgs a)
         Entry* out = a.entries + static_cast<int64_t>(n) * K;
         const unsigned place = (1u << a.shift) - 1u;
         if (FEW) {
-            for (int k = lane; k < a.size; k += 32) {
-                const KEY mine = key[k];
-                int rank = 0;
-#pragma unroll 8
-                for (int j = 0; j < a.size; ++j) rank += key[j] < mine;
-                if (mine != kLast) {
-                    sorted[rank] = mine;
-                    out[rank] = Entry{static_cast<int>(mine >> a.shift), p[k]};
-                }
+            const KEY mine[2] = {lane < a.size ? key[lane] : kLast, lane + 32 < a.size ? key[lane + 32] : kLast};
+            int rank[2] = {0, 0};
+#pragma unroll 4
+            for (int j = 0; j < a.size; j += 4) {
+                const uint4 x = *reinterpret_cast<const uint4*>(key + j);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) rank[i] += (x.x < mine[i]) + (x.y < mine[i]) + (x.z < mine[i]) + (x.w < mine[i]);
             }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (mine[i] != kLast) {
+                    sorted[rank[i]] = mine[i];
+                    out[rank[i]] = Entry{static_cast<int>(mine[i] >> a.shift), p[lane + 32 * i]};
+                }
         } else {
             for (int run = 2; run <= a.size; run *= 2)
                 for (int step = run / 2; step > 0; step /= 2) {
@@ -323,7 +328,8 @@ int launch_distill_lists(const HeadArgs& a, const HeadLayout& l)
     args.N = static_cast<int>(a.N);
     args.V = static_cast<int>(a.V);
     args.pitch = e.pitch;
-    args.size = 1;
+    args.size = 4;                                         // keys are compared four at a time
+    args.shift = 2;
     while (args.size < a.teacher->K) {
         args.size *= 2;
         ++args.shift;

@@ -46,6 +46,27 @@ constexpr size_t H_SMEM = 1024 + static_cast<size_t>(H_STAGES) * H_STAGE_BYTES +
 
 enum HeadRole { HEAD_STATS = 0, HEAD_GRADIENT = 1, DISTILL_STATS = 2, DISTILL_GRADIENT = 3 };
 
+// 32 values of a lane to and from 128 bytes of shared memory.
+__device__ __forceinline__ void put_values(uint32_t turn, uint32_t swap, const uint32_t (&l)[32])
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(turn + (16 * k ^ swap)), "r"(l[4 * k]), "r"(l[4 * k + 1]), "r"(l[4 * k + 2]), "r"(l[4 * k + 3]) : "memory");
+}
+__device__ __forceinline__ void get_values(uint32_t turn, uint32_t swap, uint32_t (&l)[32])
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(l[4 * k]), "=r"(l[4 * k + 1]), "=r"(l[4 * k + 2]), "=r"(l[4 * k + 3]) : "r"(turn + (16 * k ^ swap)) : "memory");
+}
+__device__ __forceinline__ float ld_shared(uint32_t at)
+{
+    float x;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
+    return x;
+}
+__device__ __forceinline__ void st_shared(uint32_t at, float x) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory"); }
+
 template <int ROLE>
 __global__ void __launch_bounds__(H_THREADS, 1)
 head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmG,
@@ -229,8 +250,9 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
             if (failed || valid <= 0) continue;
             const bool in = row < h.N;
             const float log2e = LISTS ? kHeadLog2e * h.e.inverse_t : kHeadLog2e;       // logits are divided by the temperature where they go into an exponent
-            // Entries: this lane's 32 values through the warp's block of shared memory, a column of it that only this lane touches.
-            float* turn = reinterpret_cast<float*>(smem_raw + (block - raw)) + lane;
+            // Entries: 32 of this lane's values through its 128 bytes of the warp's block of shared memory, 16 at a time in an order that keeps the lanes apart.
+            const uint32_t turn = block + lane * 128, swap = (lane & 7) << 4;
+            auto value = [&](int column) { return turn + ((static_cast<uint32_t>(column) << 2 & 0x70u) ^ swap) + (static_cast<uint32_t>(column) << 2 & 0xcu); };
             const int t = !LISTS && in ? h.target[row] - h.v0 - col0 : -1;                // in this warp's columns: 0 .. 127
             if (!STORES) {
                 if (valid < 128) {
@@ -249,9 +271,8 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
                         if (__any_sync(0xffffffffu, walk.column < 32 * c + 32)) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) turn[32 * i] = __uint_as_float(l[c][i]);
-                            for (; walk.column < 32 * c + 32; walk.next()) h.e.at[walk.list - h.e.entries + walk.j] = turn[32 * (walk.column - 32 * c)] * h.e.inverse_t;
+                            put_values(turn, swap, l[c]);
+                            for (; walk.column < 32 * c + 32; walk.next()) h.e.at[walk.list - h.e.entries + walk.j] = ld_shared(value(walk.column - 32 * c)) * h.e.inverse_t;
                         }
                 }
                 const bool hit = !LISTS && t >= 0 && t < 128;
@@ -305,11 +326,12 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                     for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(head_exp2(fmaf(__uint_as_float(l[c][i]), LISTS ? scale : kHeadLog2e, z)) * gp);
                     if (LISTS) {
                         if (__any_sync(0xffffffffu, walk.column < 32 * c + 32)) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) turn[32 * i] = __uint_as_float(l[c][i]);
-                            for (; walk.column < 32 * c + 32; walk.next()) turn[32 * (walk.column - 32 * c)] -= g * walk.p;
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint(turn[32 * i]);
+                            put_values(turn, swap, l[c]);
+                            for (; walk.column < 32 * c + 32; walk.next()) {
+                                const uint32_t at = value(walk.column - 32 * c);
+                                st_shared(at, ld_shared(at) - g * walk.p);
+                            }
+                            get_values(turn, swap, l[c]);
                         }
                     } else if (__any_sync(0xffffffffu, t >= 32 * c && t < 32 * c + 32)) {
 #pragma unroll
