@@ -205,12 +205,17 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
             uint32_t l[4][32];                               // fp32 bits
             EntryWalk walk;                                  // its first entries are on their way while the products run
             int col_ahead = 0;
-            float mass = 1.f;
+            const bool part = LISTS && ahead.token >= 0;     // whether this row has any
+            float g_row = 0.f, lse_row = 0.f, mass = 1.f;    // loaded before the products are waited for, with a list; without one behind them
             if (LISTS) {
                 walk.none();
-                if (ahead.token >= 0) {
+                if (part) {
                     walk.begin(h.e, ahead.token, ahead.j, ahead.end, h.v0 + col0);
-                    if (STORES) mass = h.e.mass[ahead.token];
+                    if (STORES) {
+                        g_row = h.scale[row];
+                        lse_row = h.lse[row];
+                        mass = h.e.mass[ahead.token];
+                    }
                 }
                 if (tile + num_pairs < num_tiles) {
                     const PairTile t1 = pair_tile(tile + num_pairs, tiles_m, tiles_n, 2 * H_BM, H_BN, H_BAND);
@@ -304,8 +309,8 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                 const float sum = ((s[0] + s[1]) + (s[2] + s[3])) * (1.f - lost * 0.69314718f);
                 if (in) h.running[static_cast<int64_t>((t0.n0 >> 7) + half) * h.N + row] = make_float2(LISTS ? m * h.e.inverse_t : m, sum);
             } else {
-                const bool is = in && h.target[row] >= 0;
-                const float g = is ? (LISTS ? h.scale[row] * h.e.inverse_t : h.scale[row]) : 0.f, lse = is ? h.lse[row] : 0.f;
+                const bool is = LISTS ? part : in && h.target[row] >= 0;
+                const float g = LISTS ? g_row * h.e.inverse_t : (is ? h.scale[row] : 0.f), lse = LISTS ? lse_row : (is ? h.lse[row] : 0.f);
                 float z = -lse * kHeadLog2e, lost = fmaf(-lse, kHeadLog2e, -z), scale = log2e;      // as for the statistics
                 if (__any_sync(0xffffffffu, fabsf(lost) > kHeadLost)) {
 #pragma unroll
