@@ -31,9 +31,9 @@ norm_grad_odd_kernel(const NormGradArgs a, int stages, int share)
     char* slots = ring + mine * stages * stage;
     const uint32_t slots_at = static_cast<uint32_t>(__cvta_generic_to_shared(slots));
     auto fetch = [&](int slot) {
-        dY.fetch(slots + slot * stage, D, t);
-        H.fetch(slots + slot * stage + share, D, t);
-        if (MORE) dH.fetch(slots + slot * stage + 2 * share, D, t);
+        dY.template fetch<N>(slots + slot * stage, D, t);
+        H.template fetch<N>(slots + slot * stage + share, D, t);
+        if (MORE) dH.template fetch<N>(slots + slot * stage + 2 * share, D, t);
     };
     for (int s = 0; s < stages - 1; ++s) {
         if (s < rows) fetch(s);

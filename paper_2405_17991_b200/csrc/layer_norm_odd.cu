@@ -30,8 +30,8 @@ norm_odd_kernel(const NormArgs a, int stages, int share)
     char* slots = ring + mine * stages * stage;
     const uint32_t slots_at = static_cast<uint32_t>(__cvta_generic_to_shared(slots));
     auto fetch = [&](int slot) {
-        X.fetch(slots + slot * stage, D, t);
-        if (RESIDUAL) R.fetch(slots + slot * stage + share, D, t);
+        X.template fetch<N>(slots + slot * stage, D, t);
+        if (RESIDUAL) R.template fetch<N>(slots + slot * stage + share, D, t);
     };
     for (int s = 0; s < stages - 1; ++s) {
         if (s < rows) fetch(s);

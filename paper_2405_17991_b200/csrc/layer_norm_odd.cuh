@@ -26,21 +26,22 @@ template <typename T, int P> struct OddRows {
     __device__ __forceinline__ OddRows(const void* p, int64_t ld, int64_t first)
         : base(static_cast<const char*>(p)), next(base + first * ld * static_cast<int64_t>(sizeof(T))), pitch(ld * static_cast<int64_t>(sizeof(T))),
           low(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(next) & 15)) {}
-    // To `slot`.  Bytes in front of the matrix are not touched (that word comes element by element), nor any behind the row; those in front of a row are its
-    // neighbour's, and nobody looks at them.
-    __device__ __forceinline__ void fetch(char* slot, int D, int t)
+    // To `slot`; N P columns at most.  Bytes in front of the matrix are not touched (a first word that has some comes element by element), nor any behind the row;
+    // those in front of a row are its neighbour's, and nobody looks at them.
+    template <int N> __device__ __forceinline__ void fetch(char* slot, int D, int t)
     {
-        const char* from = next - (reinterpret_cast<uintptr_t>(next) & 15);
-        const char* end = next + D * static_cast<int>(sizeof(T));
+        const int skip = static_cast<int>(reinterpret_cast<uintptr_t>(next) & 15), bytes = skip + D * static_cast<int>(sizeof(T));
+        const char* from = next - skip;
         const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(slot));
-        int at = 16 * t;
-        for (const char* p = from + at; p < end; p += 16 * P, at += 16 * P) {
-            if (p >= base) {
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + at), "l"(p), "r"(static_cast<int>(end - p < 16 ? end - p : 16)) : "memory");
-            } else {
-                for (const char* q = base; q < p + 16 && q < end; q += sizeof(T)) *reinterpret_cast<T*>(slot + at + (q - p)) = *reinterpret_cast<const T*>(q);
-            }
+        const bool whole = from >= base;                         // the same for all threads
+#pragma unroll
+        for (int k = 0; k < N * static_cast<int>(sizeof(T)) / 16 + 1; ++k) {
+            const int at = 16 * (t + k * P);
+            if (at < bytes && (whole || at > 0))
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + at), "l"(from + at), "r"(min(16, bytes - at)) : "memory");
         }
+        if (!whole && t == 0)
+            for (int at = skip; at < 16 && at < bytes; at += sizeof(T)) *reinterpret_cast<T*>(slot + at) = *reinterpret_cast<const T*>(from + at);
         next += pitch;
     }
     __device__ __forceinline__ void step() { low = (low + static_cast<uint32_t>(pitch)) & 15u; }
