@@ -177,6 +177,12 @@ def test_long_lists_and_small_vocabularies(vl, guard, N, D, V, K, dtype):
     run(vl, guard, batch(N, D, V, K, dtype, 17, 1.0, "none", True))
 
 
+def test_a_vocabulary_of_millions(vl, guard):
+    """Columns and places in a list of 1024 that do not fit 32 bits together, and, at 1000 entries fewer, do."""
+    for K in (1024, 24):
+        run(vl, guard, batch(3, 8, 4200001, K, torch.bfloat16, 41, 1.0, "none", False))
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("N", [3, 64, 100, 300])
 def test_where_entries_lie(vl, guard, N, dtype):
@@ -361,6 +367,21 @@ def test_gradients_against_differences(vl):
             slope = (grad.double() * d.double()).sum().item()
             moved = 8 * U * grad.double().abs().sum().item() / h
             assert abs((total(h) - total(-h)) / (2 * h) - slope) <= h * h * r ** 3 / 3 + err / h + moved
+
+
+def test_refused_on_the_card(vl):
+    p = batch(6, 64, 100, 5, torch.bfloat16, 3)
+    _, lse = forward(vl, p)
+    for q in ({"i": p["i"].int()}, {"i": p["i"][:5]}, {"t": p["t"][:, :4]}, {"i": p["i"].t().contiguous().t()}, {"W": p["W"].float()}, {"i": p["i"].cpu()},
+              {"lse": p["t"][:, 0].double()}, {"t": p["t"].half()}):
+        for call in (lambda: forward(vl, {**p, **q}), lambda: backward(vl, {**p, **q}, lse)):
+            with pytest.raises((ValueError, TypeError)):
+                call()
+    for q in ({"T": 0.0}, {"T": float("nan")}, {"i": p["i"][:1].expand(6, 5), "t": p["t"]}, {"i": torch.zeros((6, 1025), dtype=torch.int64, device=DEV), "t": torch.zeros((6, 1025), device=DEV)},
+              {"i": p["i"][:, :0], "t": p["t"][:, :0]}):
+        for call in (lambda: forward(vl, {**p, **q}), lambda: backward(vl, {**p, **q}, lse)):
+            with pytest.raises(vl.VeloraError):
+                call()
 
 
 def test_empty_batch(vl):

@@ -192,6 +192,23 @@ def test_without_weight_bias_or_some_gradients(vl, guard, N, D):
     assert vl.velora_layer_norm_backward(p["dY"], H, mean, rstd, need_dX=False, need_dweight=False, need_dbias=False) == (None, None, None)
 
 
+@pytest.mark.parametrize("p_dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N,D", [(9, 64), (30, 768), (20, 4096), (9, 5461), (5, 11008), (3, 16400)])
+def test_weights_and_their_gradients_anywhere(vl, guard, N, D, p_dtype):
+    """Vectors that start on any element."""
+    p = batch(N, D, torch.bfloat16, 8, p_dtype)
+    off = lambda x, k: torch.cat([torch.full((k,), float("nan"), device=DEV, dtype=x.dtype), x])[k:]  # noqa: E731
+    want = vl.velora_layer_norm(p["X"], p["w"], p["b"], residual=p["R"])
+    back = vl.velora_layer_norm_backward(p["dY"], *want[1:], p["w"], dH=p["dH"])
+    for k in (1, 3):
+        w, b = off(p["w"], k), off(p["b"], k + 1)
+        got = vl.velora_layer_norm(p["X"], w, b, residual=p["R"])
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+        dw, db = (off(torch.empty_like(w), j) for j in (k, k + 1))
+        got = vl.velora_layer_norm_backward(p["dY"], *got[1:], w, dH=p["dH"], dweight=dw, dbias=db)
+        assert all(torch.equal(x, y) for x, y in zip(got, back))
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("N,D", [(1, 96), (77, 513), (600, 2048), (4, 20000)])
 def test_gradients_are_added(vl, guard, N, D, dtype):
