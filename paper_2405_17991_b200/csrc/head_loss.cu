@@ -105,8 +105,8 @@ HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D, int64_t V,
         l.sum = take(n * static_cast<size_t>(l.ldx) * 4 * static_cast<size_t>(l.splits));
     } else {
         l.at_target = take(4 * n);
-        // fp32: one of a row; bf16: one of each 128 columns (of 256 rounded up), of a tile for few tokens.
-        const size_t parts = dtype != VELORA_BF16 ? 1 : static_cast<size_t>(N <= kHeadFew ? ceil_div64(V, kHeadFewHeight) : 2 * ceil_div64(V, 256));
+        // fp32: one of a row, with a teacher one of 256 columns at most; bf16: one of each 128 columns (of 256 rounded up), of a tile for few tokens.
+        const size_t parts = dtype != VELORA_BF16 ? static_cast<size_t>(K > 0 ? ceil_div64(V, kPieceStep) : 1) : static_cast<size_t>(N <= kHeadFew ? ceil_div64(V, kHeadFewHeight) : 2 * ceil_div64(V, 256));
         l.running = take(8 * n * parts);
     }
     l.rows = backward ? gradient_rows(dtype, N) : 1;
@@ -586,13 +586,14 @@ int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
                               reinterpret_cast<int*>(a.ws + l.order), h.target, h.at_target, loss, lse);
     }
     float* piece = reinterpret_cast<float*>(a.ws + l.piece);
+    int slices = 0;
     for (int64_t v0 = 0; v0 < a.V; v0 += l.piece_cols) {
         const int64_t cols = a.V - v0 < l.piece_cols ? a.V - v0 : l.piece_cols;
         const int64_t part_stride = a.N * l.piece_cols;
         const int parts = fp32_logits(a, l, W + static_cast<size_t>(v0) * ldw * 4, ldw, cols, &rc);
         if (rc != VELORA_OK) return rc;
         if (a.teacher) {
-            rc = launch_distill_stats(piece, l.piece_cols, parts, part_stride, head_tile(a, l, v0, cols), v0 == 0, a.stream);
+            rc = launch_distill_stats(piece, l.piece_cols, parts, part_stride, head_tile(a, l, v0, cols), &slices, a.stream);
             if (rc != VELORA_OK) return rc;
             continue;
         }
@@ -603,7 +604,7 @@ int launch_head_loss(const HeadArgs& a, float* loss, float* lse)
                             v0 + cols == a.V ? 1 : 0, loss, lse);
         if (rc != VELORA_OK) return rc;
     }
-    return a.teacher ? launch_distill_merge(head_tile(a, l, 0, a.V), 1, loss, lse, a.stream) : VELORA_OK;
+    return a.teacher ? launch_distill_merge(head_tile(a, l, 0, a.V), slices, loss, lse, a.stream) : VELORA_OK;
 }
 
 int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* dloss, void* dX, int64_t lddx,

@@ -204,7 +204,8 @@ size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V
 // Distillation's own kernels (distill.cu).
 Entries distill_entries(const HeadArgs& a, const HeadLayout& l);
 int launch_distill_lists(const HeadArgs& a, const HeadLayout& l);
-int launch_distill_stats(float* logits, int64_t ld, int parts, int64_t part_stride, const HeadTile& h, bool first, cudaStream_t stream);
+// fp32: parts of the rows' statistics to `running`, from row *part on, which moves behind them; never more than one for 256 columns.
+int launch_distill_stats(const float* logits, int64_t ld, int parts, int64_t part_stride, const HeadTile& h, int* part, cudaStream_t stream);
 int launch_distill_gradient(float* logits, int64_t ld, int parts, int64_t part_stride, const HeadTile& h, cudaStream_t stream);
 int launch_distill_merge(const HeadTile& h, int parts, float* loss, float* lse, cudaStream_t stream);
 int launch_head_loss(const HeadArgs& a, float* loss, float* lse);
