@@ -65,8 +65,11 @@ int fp32_parts(int64_t M, int64_t N, int64_t K)
 
 // Parts of the contraction that dX's products are cut into, where its tiles are few: waves of units on 74 pairs, each its k-blocks and about
 // 4 more for its sums' way.
-int gradient_splits(int dtype, int64_t N, int64_t D, int64_t V)
+bool few_f32(int dtype, int64_t N, int K) { return K > 0 && dtype == VELORA_F32 && N <= kDistillFew; }
+
+int gradient_splits(int dtype, int64_t N, int64_t D, int64_t V, int K)
 {
+    if (few_f32(dtype, N, K)) return distill_few_slices(D);
     if (dtype != VELORA_BF16) return fp32_parts(N, D, piece_width(N, D, V, room_wanted(dtype, N, V)));
     if (N <= kHeadFew) return gradient_rows(dtype, N);          // the rows' sums, one behind the other
     const int64_t tiles = ceil_div64(N, 256) * ceil_div64(D, 256), kblocks = ceil_div64(piece_width(N, D, V, room_wanted(dtype, N, V)), 64);
@@ -124,7 +127,7 @@ HeadLayout head_front(bool backward, int dtype, int64_t N, int64_t D, int64_t V,
     return l;
 }
 
-int logit_parts(int dtype, int64_t N, int64_t D, int64_t V) { return dtype == VELORA_BF16 ? 1 : fp32_parts(N, piece_width(N, D, V, room_wanted(dtype, N, V)), D); }
+int logit_parts(int dtype, int64_t N, int64_t D, int64_t V, int K) { return dtype == VELORA_BF16 || few_f32(dtype, N, K) ? 1 : fp32_parts(N, piece_width(N, D, V, room_wanted(dtype, N, V)), D); }
 
 // As many columns a piece as there is room for.
 int head_layout(HeadLayout* l, bool backward, const HeadArgs& a)
@@ -132,8 +135,8 @@ int head_layout(HeadLayout* l, bool backward, const HeadArgs& a)
     const bool pack_w = a.dtype == VELORA_BF16 && !tc_operand_ok(a.W, a.ldw);
     const int K = a.teacher ? a.teacher->K : 0;
     size_t column = piece_element(a.dtype, backward, a.N) * static_cast<size_t>(a.N);
-    *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, backward ? gradient_splits(a.dtype, a.N, a.D, a.V) : 1, K);
-    l->parts = logit_parts(a.dtype, a.N, a.D, a.V);
+    *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, backward ? gradient_splits(a.dtype, a.N, a.D, a.V, K) : 1, K);
+    l->parts = logit_parts(a.dtype, a.N, a.D, a.V, K);
     if (a.ws_bytes < l->piece + column * l->parts * kPieceStep) {             // less room than asked for: no partial sums
         *l = head_front(backward, a.dtype, a.N, a.D, a.V, pack_w, backward ? gradient_rows(a.dtype, a.N) : 1, K);
         l->parts = 1;
@@ -503,9 +506,9 @@ int product(int kind, const void* A, int a_dtype, int64_t lda, const void* B, in
 size_t head_loss_bytes(bool backward, int dtype, int64_t N, int64_t D, int64_t V, bool any_rows, int K)
 {
     if (N < 1) return kStatusBytes;
-    const size_t front = head_front(backward, dtype, N, D, V, any_rows && dtype == VELORA_BF16, backward ? gradient_splits(dtype, N, D, V) : 1, K).piece;
+    const size_t front = head_front(backward, dtype, N, D, V, any_rows && dtype == VELORA_BF16, backward ? gradient_splits(dtype, N, D, V, K) : 1, K).piece;
     if (dtype == VELORA_BF16 && !backward) return front;
-    return front + up256(piece_element(dtype, backward, N) * static_cast<size_t>(logit_parts(dtype, N, D, V)) * static_cast<size_t>(N) *
+    return front + up256(piece_element(dtype, backward, N) * static_cast<size_t>(logit_parts(dtype, N, D, V, K)) * static_cast<size_t>(N) *
                          static_cast<size_t>(room_wanted(dtype, N, V)));
 }
 
@@ -528,6 +531,10 @@ int fp32_logits(const HeadArgs& a, const HeadLayout& l, const char* w, int64_t l
 {
     const float* x = reinterpret_cast<const float*>(a.ws + l.x);
     float* c = reinterpret_cast<float*>(a.ws + l.piece);
+    if (a.teacher && few_f32(a.dtype, a.N, a.teacher->K)) {
+        *rc = launch_distill_few_logits(x, l.ldx, reinterpret_cast<const float*>(w), ldw, c, l.piece_cols, a.N, a.D, cols, a.stream);
+        return 1;
+    }
     const int parts = l.parts > 1 ? fp32_parts(a.N, cols, a.D) : 1;
     if (parts > 1 && parts <= l.parts) {
         *rc = launch_gemm_simt_parts(simt_parts(a.N, cols, a.D), x, l.ldx, 1, reinterpret_cast<const float*>(w), ldw, 1, c, l.piece_cols,
@@ -659,7 +666,11 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
                          GemmMore{l.rows > 1 ? nullptr : live, take_common ? common : nullptr, 1, 0, kBand}, a.stream);
             if (rc != VELORA_OK) return rc;
         }
-        if (dX && a.dtype != VELORA_BF16 && l.splits > 1) {
+        if (dX && a.teacher && few_f32(a.dtype, a.N, a.teacher->K)) {
+            rc = launch_distill_few_grad(reinterpret_cast<float*>(G), l.piece_cols, reinterpret_cast<const float*>(w), ldw, reinterpret_cast<float*>(a.ws + l.sum),
+                                         l.ldx, l.splits, v0 > 0 ? 1 : 0, a.N, a.D, cols, a.stream);
+            if (rc != VELORA_OK) return rc;
+        } else if (dX && a.dtype != VELORA_BF16 && l.splits > 1) {
             SimtParts shape = simt_parts(a.N, a.D, l.piece_cols);
             shape.parts = l.splits;
             rc = launch_gemm_simt_parts(shape, reinterpret_cast<float*>(G), l.piece_cols, 1, reinterpret_cast<const float*>(w), 1, ldw,
@@ -675,6 +686,8 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
     const float* sum = reinterpret_cast<float*>(a.ws + l.sum);
     const int d = static_cast<int>(a.D);
     const int* order = reinterpret_cast<const int*>(a.ws + l.order);
+    if (a.teacher && few_f32(a.dtype, a.N, a.teacher->K))            // no common factor has been taken out
+        return launch_distill_few_rows_back(sum, l.ldx, l.splits, a.N, a.D, live, order, static_cast<float*>(dX), lddx, a.stream);
     const bool vec = a.D % 8 == 0 && c_rows_vec(dX, lddx, dtype_size(a.dtype));
     const int64_t blocks = ceil_div64(a.N, kRowThreads / 32), steps = ceil_div64(a.D, vec ? 256 : 32), fill = 592 / blocks;
     const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(fill < 1 ? 1 : (fill < steps ? fill : steps)));

@@ -208,6 +208,15 @@ int launch_distill_lists(const HeadArgs& a, const HeadLayout& l);
 int launch_distill_stats(const float* logits, int64_t ld, int parts, int64_t part_stride, const HeadTile& h, int* part, cudaStream_t stream);
 int launch_distill_gradient(float* logits, int64_t ld, int parts, int64_t part_stride, const HeadTile& h, cudaStream_t stream);
 int launch_distill_merge(const HeadTile& h, int parts, float* loss, float* lse, cudaStream_t stream);
+// Its fp32 products for up to kDistillFew tokens (distill_few.cu): logits, and slices of dX's sums, N lds apart, that are added to what is there (`add`) or
+// written; then those to dX.
+constexpr int kDistillFew = 16;
+int distill_few_slices(int64_t D);
+int launch_distill_few_logits(const float* x, int64_t ldx, const float* W, int64_t ldw, float* C, int64_t ldc, int64_t N, int64_t D, int64_t V, cudaStream_t stream);
+int launch_distill_few_rows_back(const float* sum, int64_t lds, int slices, int64_t N, int64_t D, const int* live, const int* order, float* dX, int64_t lddx,
+                                 cudaStream_t stream);
+int launch_distill_few_grad(const float* G, int64_t ldg, const float* W, int64_t ldw, float* sum, int64_t lds, int slices, int add, int64_t N, int64_t D, int64_t V,
+                            cudaStream_t stream);
 int launch_head_loss(const HeadArgs& a, float* loss, float* lse);
 int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* dloss, void* dX, int64_t lddx,
                               void* dW, int dw_dtype, int64_t lddw, int beta);

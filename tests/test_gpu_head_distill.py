@@ -177,6 +177,27 @@ def test_long_lists_and_small_vocabularies(vl, guard, N, D, V, K, dtype):
     run(vl, guard, batch(N, D, V, K, dtype, 17, 1.0, "none", True))
 
 
+@pytest.mark.parametrize("N", [1, 4, 5, 15, 16, 17])
+@pytest.mark.parametrize("D,V", [(4, 3), (200, 1000), (203, 1001), (2052, 700), (4099, 130), (9000, 260)])
+def test_few_tokens_in_fp32(vl, guard, N, D, V):
+    """Up to 16 tokens have products of their own: tokens on both sides of their sizes, rows that shared memory holds and longer ones, of any width."""
+    run(vl, guard, batch(N, D, V, 3, torch.float32, N + D, 1.0, "some" if N > 4 else "none", True))
+    p = batch(N, D, V, 3, torch.float32, 5)
+    _, lse = forward(vl, p)
+    ref = Reference(p)
+    tiny = vl.velora_workspace_bytes(vl.OP_HEAD_DISTILL_BACKWARD | vl.OP_F32, N, D, 256, 3, False)         # fewer slices of dX's sums, and pieces of the vocabulary
+    tiny -= (vl.velora_workspace_bytes(vl.OP_HEAD_DISTILL_BACKWARD | vl.OP_F32, N, D, 256, 3, False) - 256) // 2 if V <= 256 else -2 * N * (V // 128 + 2) - 256
+    full = vl.velora_workspace_bytes(vl.OP_HEAD_DISTILL_BACKWARD | vl.OP_F32, N, D, V, 3, False)
+    for size in (tiny, full):
+        try:
+            dX, dW = backward(vl, p, lse, ws=guard.workspace(vl, size))
+        except vl.VeloraError:
+            assert size == tiny and V <= 256                  # half of it may be too little
+            continue
+        check(dX, ref.dX, ref.dX_bound, "dX")
+        check(dW, ref.dW, ref.dW_bound, "dW")
+
+
 def test_a_vocabulary_of_millions(vl, guard):
     """Columns and places in a list of 1024 that do not fit 32 bits together, and, at 1000 entries fewer, do."""
     for K in (1024, 24):
