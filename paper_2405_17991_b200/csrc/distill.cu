@@ -286,7 +286,10 @@ distill_merge_kernel(const HeadTile h, int parts, int rows, float* loss, float* 
         for (int p0 = static_cast<int>(threadIdx.x) / rows; p0 < parts; p0 += slices * 16) {
             float2 x[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = p0 + slices * i < parts ? p[static_cast<int64_t>(p0 + slices * i) * h.N] : make_float2(-INFINITY, 0.f);
+            for (int i = 0; i < 16; ++i) x[i] = p[static_cast<int64_t>(min(p0 + slices * i, parts - 1)) * h.N];          // no branch: all under way
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (p0 + slices * i >= parts) x[i] = make_float2(-INFINITY, 0.f);
             float m = ms.x;
 #pragma unroll
             for (int i = 0; i < 16; ++i) m = x[i].x > m ? x[i].x : (x[i].x == x[i].x ? m : x[i].x);      // a NaN stays one

@@ -126,23 +126,23 @@ norm_slices_kernel(const float* partials, int slices, int D, void* dw, void* db,
     pdl_trigger();
     void* out = blockIdx.y ? db : dw;
     if (!out) return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = (blockIdx.x * 32 + lane) * V;
-    const int64_t pitch = norm_pitch(D);                      // a multiple of eight
-    const float* p = partials + blockIdx.y * slices * pitch + d;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t pitch = norm_pitch(D), d = (static_cast<int64_t>(blockIdx.x) * 32 + lane) * V;          // the pitch is a multiple of eight
+    const float* p = partials + blockIdx.y * slices * pitch + (d < pitch ? d : 0);                       // columns behind the last: any, nobody has their sums
     float2 s = make_float2(0.f, 0.f);
     for (int first = warp; first < slices; first += WARPS * LOADS) {
         float2 x[LOADS];
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const bool is = d < D && first + WARPS * i < slices;
-            const float* q = p + (first + WARPS * i) * pitch;
-            if (V == 2) x[i] = is ? *reinterpret_cast<const float2*>(q) : make_float2(0.f, 0.f);
-            else x[i].x = is ? *q : 0.f;
+            const float* q = p + min(first + WARPS * i, slices - 1) * pitch;          // no branch: all under way
+            if (V == 2) x[i] = *reinterpret_cast<const float2*>(q);
+            else x[i].x = *q;
         }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            s.x += x[i].x;
-            if (V == 2) s.y += x[i].y;
+            const bool is = first + WARPS * i < slices;
+            s.x += is ? x[i].x : 0.f;
+            if (V == 2) s.y += is ? x[i].y : 0.f;
         }
     }
     if (V == 2) *reinterpret_cast<float2*>(&part[warp][2 * lane]) = s;
