@@ -9,7 +9,7 @@ namespace velora {
 namespace {
 
 // E columns' sums, at a 16-byte boundary.  WIDE: 16 bytes at a time, for which they have to lie in four neighbouring registers all along: right where there are
-// registers to spare (8192 x 4096 bf16: 39 us, two at a time 42), but 8192 x 11008, dX alone, takes 112 us instead of 94.
+// registers to spare (8192 x 4096 bf16: 39 us, two at a time 42), but 8192 x 11008, dX alone, takes 112 us instead of 92.
 template <int E, bool WIDE> __device__ __forceinline__ void store_sums(float* p, const F2 (&x)[E / 2])
 {
     if (WIDE) {

@@ -164,7 +164,7 @@ int launch_rows(const NormGradArgs& a, int sm_count, cudaStream_t stream)
     return launch_norm_slices(a, static_cast<int>(blocks), stream);
 }
 
-// 4096 x 5461 bf16 48 us (the same rows on 16-byte boundaries 36), 12608 x 769 26, 8192 x 10001 170.
+// 4096 x 5461 bf16 46 us (the same rows on 16-byte boundaries 37), 12608 x 769 25, 8192 x 10001 143.
 template <typename T, bool MORE>
 int launch_width(const NormGradArgs& a, int sm_count, cudaStream_t stream)
 {

