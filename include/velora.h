@@ -470,7 +470,7 @@ int velora_head_distill_backward(const void* X, int64_t ldx, const void* W, int6
  * dX is the gradient of X and of R.  (dX, dweight or dbias NULL: skipped.)  beta is 0 or 1.
  * `dtype` (bf16 or f32): X, R, H, Y, dY, dH, dX, [N, D] with pitches of their own; p_dtype: weight and bias, dw_dtype: dweight and dbias, [D], dense.
  * mean, rstd: fp32 [N], m and r for the backward pass (velora_layer_norm: NULL where there is none; H may be NULL, too).  eps >= 0, finite
- * (with eps == 0 a row of equal values is NaN).
+ * (eps == 0 leaves a row of equal values without a result).
  * Statistics, sums and products are fp32, every output is rounded once; the variance is taken about the mean; sums have a fixed order.  Squares of H - m
  * must stay in fp32's range; an infinity or a NaN makes its row NaN.
  * H or Y may lie where X or R does, dX where dY, dH or H does (the same address and pitch; nothing else may overlap).

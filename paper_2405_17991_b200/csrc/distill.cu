@@ -104,7 +104,7 @@ distill_lists_kernel(const ListsArgs a)
             const int64_t i = k < K ? a.t.index[n * a.t.ldi + k] : -1;
             const float x = k < K ? teacher_logit(a.t, n * a.t.ldt + k) : 0.f;              // does not wait for the column
             const bool is = i >= 0 && i < a.V;
-            const float u = is ? x * a.inverse_t : -INFINITY;
+            const float over_t = x * a.inverse_t, u = is ? (over_t == INFINITY ? __int_as_float(0x7fc00000) : over_t) : -INFINITY;     // also beside a given s
             if (i >= a.V) kind = 2.f;
             else if (is && u != -INFINITY) kind = fmaxf(kind, 1.f);
             m = fmaxf(m, u);

@@ -293,10 +293,11 @@ def test_an_entry_that_is_no_column(vl, dtype, N):
         assert vl.velora_workspace_status(ws) == 0
 
 
+@pytest.mark.parametrize("whole", [False, True])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("N", [10, 200])
-def test_non_finite_logits_stay_with_their_token(vl, dtype, N):
-    p = batch(N, 64, 500, 5, dtype, 40)
+def test_non_finite_logits_stay_with_their_token(vl, dtype, N, whole):
+    p = batch(N, 64, 500, 5, dtype, 40, whole=whole)
     p["i"][:, 0] = torch.arange(N, device=DEV)
     loss, lse = forward(vl, p)
     p["t"][3, 0], p["t"][6, 0] = float("nan"), float("inf")
