@@ -1,7 +1,8 @@
 // fp32 products of a head's distillation for up to 16 tokens, which tiles of more rows waste most of themselves on: both read W once and are bound by that.
 //   l[n, v] = sum_d X[n, d] W[v, d]      a warp takes four rows of W against all tokens, whose rows lie in shared memory; 64 sums a warp, halved from lane to lane
 //   dX[n, d] = sum_v G[n, v] W[v, d]     a thread takes four columns of a slice of W's rows; the slices' sums are added where rows go back to their tokens
-// 12 x 656 of 45362: 52 and 48 us, and 6 for the sums of the second (W alone 18; tiles of the CUDA-core product 109 and 208).
+// Calls for 4096 columns and a vocabulary of 32000 (W alone 80 us): forward 101 us for 1 token, 123 for 8, 225 for 16, dX 196, 251, 345 (both read W for the
+// logits).  4095 columns, 16 tokens: 255 and 443.  (Tiles of the CUDA-core product took 109 and 208 us for 12 x 656 of 45362, these two 48 and 43.)
 #include "head_loss.cuh"
 
 namespace velora {
@@ -9,7 +10,8 @@ namespace velora {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 32768;                              // floats of X in shared memory: columns of a chunk times tokens
+constexpr int kChunk = 26624;                              // floats of X in shared memory at most: columns of a chunk times tokens; two blocks fit an SM
+constexpr int kStep = 128;                                 // columns that a warp takes at a time
 constexpr int kColumnThreads = 128, kRows = 64;            // of dX: columns (or fours) of a block, rows of W whose gradients are in shared memory at a time
 
 template <int V> struct Wide;
@@ -20,7 +22,7 @@ template <> struct Wide<1> {
     static __device__ __forceinline__ float4 load(const float* p) { return make_float4(*p, 0.f, 0.f, 0.f); }
 };
 
-// VEC: four columns a lane, rows of W on 16-byte boundaries and D a multiple of four.
+// VEC 4: a lane takes four neighbouring columns (rows of W on 16-byte boundaries, D a multiple of four); 1: four that are 32 apart.
 template <int TOKENS, int VEC>
 __global__ void __launch_bounds__(kThreads, 2)
 few_logits_kernel(const float* x, int64_t ldx, const float* W, int64_t ldw, float* C, int64_t ldc, int N, int D, int V, int pitch)
@@ -31,14 +33,14 @@ few_logits_kernel(const float* x, int64_t ldx, const float* W, int64_t ldw, floa
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), warps = gridDim.x * (kThreads / 32);
     for (int d0 = 0; d0 < D; d0 += pitch) {
-        const int columns = min(pitch, D - d0), padded = (columns + 32 * VEC - 1) / (32 * VEC) * (32 * VEC);
+        const int columns = min(pitch, D - d0), padded = (columns + kStep - 1) / kStep * kStep;
         __syncthreads();                                   // the last chunk has been read
         for (int d = threadIdx.x; d < padded; d += kThreads) {
             float y[TOKENS];
 #pragma unroll
-            for (int n = 0; n < TOKENS; ++n) y[n] = n < N && d < columns ? x[n * ldx + d0 + d] : 0.f;
+            for (int n = 0; n < TOKENS; ++n) y[n] = x[min(n, N - 1) * ldx + d0 + min(d, columns - 1)];          // no branch: all under way
 #pragma unroll
-            for (int n = 0; n < TOKENS; ++n) rows[n * pitch + d] = y[n];
+            for (int n = 0; n < TOKENS; ++n) rows[n * pitch + d] = n < N && d < columns ? y[n] : 0.f;
         }
         __syncthreads();
         for (int v = 4 * warp; v < V; v += 4 * warps) {
@@ -48,19 +50,37 @@ few_logits_kernel(const float* x, int64_t ldx, const float* W, int64_t ldw, floa
             float s[kSums];
 #pragma unroll
             for (int i = 0; i < kSums; ++i) s[i] = 0.f;
-#pragma unroll 2
-            for (int d = VEC * lane; d < padded; d += 32 * VEC) {
-                float4 y[4];
+#pragma unroll (TOKENS == 16 ? 1 : 2)
+            for (int d = VEC * lane; d < padded; d += kStep) {          // 16 tokens leave no registers for a second step's loads (225 us -> 247)
+                float y[4][4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) y[r] = d < columns ? Wide<VEC>::load(w[r] + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int r = 0; r < 4; ++r) {              // columns that are not there: the last ones, no branch
+                    if (VEC == 4) {
+                        const float4 u = *reinterpret_cast<const float4*>(w[r] + min(d, columns - 4));
+                        y[r][0] = u.x; y[r][1] = u.y; y[r][2] = u.z; y[r][3] = u.w;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[r][e] = w[r][min(d + 32 * e, columns - 1)];
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[r][e] = d + (VEC == 4 ? e : 32 * e) < columns ? y[r][e] : 0.f;
 #pragma unroll
                 for (int n = 0; n < TOKENS; ++n) {
-                    const float4 z = Wide<VEC>::load(rows + n * pitch + d);
+                    float z[4];
+                    if (VEC == 4) {
+                        const float4 u = *reinterpret_cast<const float4*>(rows + n * pitch + d);
+                        z[0] = u.x; z[1] = u.y; z[2] = u.z; z[3] = u.w;
+                    } else {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        s[4 * n + r] = fmaf(y[r].x, z.x, s[4 * n + r]);
-                        if (VEC == 4) s[4 * n + r] = fmaf(y[r].w, z.w, fmaf(y[r].z, z.z, fmaf(y[r].y, z.y, s[4 * n + r])));
+                        for (int e = 0; e < 4; ++e) z[e] = rows[n * pitch + d + 32 * e];
                     }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[4 * n + r] = fmaf(y[r][e], z[e], s[4 * n + r]);
                 }
             }
             // Lanes halve the sums that they carry until each has kSums / 32, or one that several share.
@@ -177,8 +197,7 @@ int launch_logits(const float* x, int64_t ldx, const float* W, int64_t ldw, floa
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kChunk * 4) != cudaSuccess) return VELORA_ERR_CUDA;
         configured.set(dev);
     }
-    constexpr int kColumns = kChunk / TOKENS;              // a multiple of 32 VEC
-    const int64_t all = ceil_div64(D, 32 * VEC) * 32 * VEC, pitch = all < kColumns ? all : kColumns;
+    const int64_t steps = ceil_div64(D, kStep), chunks = ceil_div64(steps, kChunk / TOKENS / kStep), pitch = ceil_div64(steps, chunks) * kStep;
     const size_t smem = static_cast<size_t>(TOKENS) * static_cast<size_t>(pitch) * 4;
     const int64_t fit = static_cast<int64_t>(216 * 1024 / smem), blocks = ceil_div64(V, 4 * (kThreads / 32)), most = static_cast<int64_t>(sm_count) * (fit < 2 ? fit : 2);
     return launch_chained(kern, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), kThreads, smem, stream, x, ldx, W, ldw, C, ldc,
@@ -207,16 +226,24 @@ int launch_distill_few_logits(const float* x, int64_t ldx, const float* W, int64
     const int rc = device_info(&di);
     if (rc != VELORA_OK) return rc;
     if (four(W, ldw, D))
-        return N <= 4 ? launch_logits<4, 4>(x, ldx, W, ldw, C, ldc, N, D, V, di.sm_count, stream) : launch_logits<16, 4>(x, ldx, W, ldw, C, ldc, N, D, V, di.sm_count, stream);
-    return N <= 4 ? launch_logits<4, 1>(x, ldx, W, ldw, C, ldc, N, D, V, di.sm_count, stream) : launch_logits<16, 1>(x, ldx, W, ldw, C, ldc, N, D, V, di.sm_count, stream);
+        return N <= 4   ? launch_logits<4, 4>(x, ldx, W, ldw, C, ldc, N, D, V, di.sm_count, stream)
+               : N <= 8 ? launch_logits<8, 4>(x, ldx, W, ldw, C, ldc, N, D, V, di.sm_count, stream)
+                        : launch_logits<16, 4>(x, ldx, W, ldw, C, ldc, N, D, V, di.sm_count, stream);
+    return N <= 4   ? launch_logits<4, 1>(x, ldx, W, ldw, C, ldc, N, D, V, di.sm_count, stream)
+           : N <= 8 ? launch_logits<8, 1>(x, ldx, W, ldw, C, ldc, N, D, V, di.sm_count, stream)
+                    : launch_logits<16, 1>(x, ldx, W, ldw, C, ldc, N, D, V, di.sm_count, stream);
 }
 
 int launch_distill_few_grad(const float* G, int64_t ldg, const float* W, int64_t ldw, float* sum, int64_t lds, int slices, int add, int64_t N, int64_t D, int64_t V,
                             cudaStream_t stream)
 {
     if (four(W, ldw, D))
-        return N <= 4 ? launch_grad<4, 4>(G, ldg, W, ldw, sum, lds, slices, add, N, D, V, stream) : launch_grad<16, 4>(G, ldg, W, ldw, sum, lds, slices, add, N, D, V, stream);
-    return N <= 4 ? launch_grad<4, 1>(G, ldg, W, ldw, sum, lds, slices, add, N, D, V, stream) : launch_grad<16, 1>(G, ldg, W, ldw, sum, lds, slices, add, N, D, V, stream);
+        return N <= 4   ? launch_grad<4, 4>(G, ldg, W, ldw, sum, lds, slices, add, N, D, V, stream)
+               : N <= 8 ? launch_grad<8, 4>(G, ldg, W, ldw, sum, lds, slices, add, N, D, V, stream)
+                        : launch_grad<16, 4>(G, ldg, W, ldw, sum, lds, slices, add, N, D, V, stream);
+    return N <= 4   ? launch_grad<4, 1>(G, ldg, W, ldw, sum, lds, slices, add, N, D, V, stream)
+           : N <= 8 ? launch_grad<8, 1>(G, ldg, W, ldw, sum, lds, slices, add, N, D, V, stream)
+                    : launch_grad<16, 1>(G, ldg, W, ldw, sum, lds, slices, add, N, D, V, stream);
 }
 
 int launch_distill_few_rows_back(const float* sum, int64_t lds, int slices, int64_t N, int64_t D, const int* live, const int* order, float* dX, int64_t lddx,

@@ -153,7 +153,7 @@ struct EntryWalk {
         p = next_p;
         fetch(j + 1);
     }
-    // Entries j0 .. before j1 of a token's list, the first of which is not in front of column `from`.
+    // Entries j0 .. before j1 of a token's list, counted from column `from` on (negative: in front of it).
     __device__ __forceinline__ void begin(const Entries& e, int token, int j0, int j1, int from)
     {
         list = e.entries + static_cast<int64_t>(token) * e.K;
@@ -165,11 +165,16 @@ struct EntryWalk {
         p = next_p;
         fetch(j + 1);
     }
-    __device__ __forceinline__ void start(const Entries& e, int token, int from, int columns)
+    // The first of which, where there is one, has been loaded.
+    __device__ __forceinline__ void begin(const Entries& e, int token, int j0, int j1, int from, Entry head)
     {
-        const unsigned short* s = e.starts + static_cast<int64_t>(token) * e.pitch;
-        begin(e, token, s[from / kEntryColumns], s[(from + columns - 1) / kEntryColumns + 1], from);      // some of them may lie behind
-        while (column < 0) next();                  // of the same 128 columns, but in front
+        list = e.entries + static_cast<int64_t>(token) * e.K;
+        j = j0;
+        end = j1;
+        first = from;
+        column = j < end ? head.column - first : kNoColumn;
+        p = head.p;
+        fetch(j + 1);
     }
     __device__ __forceinline__ void none()
     {

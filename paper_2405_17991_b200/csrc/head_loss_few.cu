@@ -42,6 +42,57 @@ __device__ __forceinline__ bool epilogue_any(bool p)
     return any != 0;
 }
 
+// Of a lane's rows 32 c + lane: the tokens (negative: the row has no part in it), where their entries in a warp's columns are, the first of those, what a
+// gradient takes.
+template <int C> struct FewLists {
+    int token[C], j[C], end[C];
+    Entry head[C];
+    float scale[C], lse[C], mass[C];
+    template <bool GRADIENT> __device__ __forceinline__ void find(const HeadTile& h, int lane, int v0, int valid)
+    {
+        if (valid <= 0) {                                    // for the warp
+#pragma unroll
+            for (int c = 0; c < C; ++c) token[c] = -1;
+            return;
+        }
+        const int from = h.v0 + v0;
+        bool live[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {                        // rows that are not there: the last one, no branch
+            const int row = min(32 * c + lane, h.N - 1);
+            live[c] = h.target[row] >= 0;
+            token[c] = h.e.order[row];
+            if (GRADIENT) {
+                scale[c] = h.scale[row];
+                lse[c] = h.lse[row];
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            live[c] &= 32 * c + lane < h.N;
+            const unsigned short* s = h.e.starts + static_cast<int64_t>(token[c]) * h.e.pitch;
+            j[c] = s[from / kEntryColumns];                  // of a token without entries: anything
+            end[c] = s[(from + valid - 1) / kEntryColumns + 1];
+            if (GRADIENT) mass[c] = h.e.mass[token[c]];
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) head[c] = h.e.entries[static_cast<int64_t>(token[c]) * h.e.K + (live[c] ? min(j[c], h.e.K - 1) : 0)];
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (!live[c]) {
+                token[c] = -1;
+                scale[c] = lse[c] = mass[c] = 0.f;
+            }
+    }
+    __device__ __forceinline__ void walk(EntryWalk& w, const Entries& e, int c, int from) const
+    {
+        w.none();
+        if (token[c] < 0) return;
+        w.begin(e, token[c], j[c], end[c], from, head[c]);
+        while (w.column < 0) w.next();                       // of the same 128 columns, but in front
+    }
+};
+
 template <bool GRADIENT, bool LISTS, int NT>
 __global__ void __launch_bounds__(W_THREADS, 1)
 head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const HeadTile h, int height, __nv_bfloat16* G, int64_t ldg,
@@ -149,6 +200,9 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
         float* block = staging + quarter * (32 * W_PITCH);
         uint32_t seg = 0;
         for (int tile = blockIdx.x; tile < num_tiles && !failed; tile += gridDim.x) {
+            const int v0 = tile * height + quarter * 32, valid = min(min(32, height - quarter * 32), h.cols - v0);      // this warp's columns; may be none
+            FewLists<LISTS ? NT / 32 : 1> lists;             // looked up while the products run: four loads, each with the address of the next
+            if (LISTS) lists.template find<GRADIENT>(h, lane, v0, valid);
             uint32_t l[NT / 32][32];                         // fp32 bits
 #pragma unroll
             for (int c = 0; c < NT / 32; ++c)
@@ -171,7 +225,6 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
                 if (lane == 0) mbar_arrive(tempty + 8 * acc);
             }
             if (GRADIENT ? failed : (failed = epilogue_any(failed))) break;      // behind it nobody reads the last tile's parts any more
-            const int v0 = tile * height + quarter * 32, valid = min(min(32, height - quarter * 32), h.cols - v0);      // this warp's columns; may be none
 #pragma unroll
             for (int c = 0; c < NT / 32; ++c) {
                 const int row = 32 * c + lane;               // this lane's token behind the turn
@@ -180,13 +233,10 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
                 for (int i = 0; i < 32; ++i) block[i * W_PITCH + lane] = LISTS ? __uint_as_float(l[c][i]) * h.e.inverse_t : __uint_as_float(l[c][i]);
                 __syncwarp();
                 if (32 * c >= h.N) break;                    // for all epilogue warps
-                const int target = row < h.N ? h.target[row] : -1, t = target - h.v0 - v0;
+                const int target = !LISTS && row < h.N ? h.target[row] : -1, t = target - h.v0 - v0;
                 float* mine = block + lane * W_PITCH;
                 EntryWalk walk;
-                if (LISTS) {
-                    walk.none();
-                    if (target >= 0 && valid > 0) walk.start(h.e, h.e.order[row], h.v0 + v0, valid);
-                }
+                if (LISTS) lists.walk(walk, h.e, c, h.v0 + v0);
                 if (!GRADIENT) {
                     float m = -INFINITY, s = 0.f;
                     for (int i = 0; i < valid; ++i) m = fmaxf(m, mine[i]);
@@ -205,15 +255,15 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
                         h.at_target[row] = mine[t];
                     }
                 } else if (row < h.N && valid > 0) {
-                    const bool is = target >= 0;
-                    const float g = is ? (LISTS ? h.scale[row] * h.e.inverse_t : h.scale[row]) : 0.f, lse = is ? h.lse[row] : 0.f;
+                    const bool is = LISTS ? lists.token[LISTS ? c : 0] >= 0 : target >= 0;
+                    const float g = LISTS ? lists.scale[LISTS ? c : 0] * h.e.inverse_t : (is ? h.scale[row] : 0.f);
+                    const float lse = LISTS ? lists.lse[LISTS ? c : 0] : (is ? h.lse[row] : 0.f);
                     float off = 0.f, z = -lse * kHeadLog2e, lost = fmaf(-lse, kHeadLog2e, -z);
                     if (fabsf(lost) > kHeadLost) {
                         off = lse;
                         z = lost = 0.f;
                     }
-                    const float mass = LISTS ? (is ? h.e.mass[h.e.order[row]] : 0.f) : 1.f;
-                    const float gp = (LISTS ? g * mass : g) * (1.f + lost * 0.69314718f);
+                    const float gp = (LISTS ? g * lists.mass[LISTS ? c : 0] : g) * (1.f + lost * 0.69314718f);
                     if (LISTS) {                             // complete before they are rounded
                         for (int i = 0; i < valid; ++i) mine[i] = head_exp2(fmaf(mine[i] - off, kHeadLog2e, z)) * gp;
                         for (; walk.column < valid; walk.next()) mine[walk.column] -= g * walk.p;
