@@ -1,8 +1,10 @@
-// fp32 products of a head's distillation for up to 16 tokens, which tiles of more rows waste most of themselves on: both read W once and are bound by that.
+// fp32 products of a head's distillation for up to 16 tokens, which tiles of more rows waste most of themselves on: two read W once and are bound by that.
 //   l[n, v] = sum_d X[n, d] W[v, d]      a warp takes four rows of W against all tokens, whose rows lie in shared memory; 64 sums a warp, halved from lane to lane
+//   dW[v, d] = sum_n G[n, v] X[n, d]     bound by writing it, see there
 //   dX[n, d] = sum_v G[n, v] W[v, d]     a thread takes four columns of a slice of W's rows; the slices' sums are added where rows go back to their tokens
-// Calls for 4096 columns and a vocabulary of 32000 (W alone 80 us): forward 101 us for 1 token, 123 for 8, 225 for 16, dX 196, 251, 345 (both read W for the
-// logits).  4095 columns, 16 tokens: 255 and 443.  (Tiles of the CUDA-core product took 109 and 208 us for 12 x 656 of 45362, these two 48 and 43.)
+// Calls for 4096 columns and a vocabulary of 32000 (W alone 80 us): forward 101 us for 1 token, 123 for 8, 225 for 16, dX 196, 251, 345, dW 209, 225, 349 (all with
+// the logits).  4095 columns, 16 tokens: 255, 443, 367.  (Tiles of the CUDA-core product: 109 and 208 us for the first two of 12 x 656 of 45362, now 48 and
+// 43; dW calls of 1 x 4096 287, of 16 x 4095 506.)
 #include "head_loss.cuh"
 
 namespace velora {
@@ -158,6 +160,67 @@ few_input_grad_kernel(const float* G, int64_t ldg, const float* W, int64_t ldw, 
             for (int e = 0; e < VEC; ++e) out[n * lds + e] = add ? out[n * lds + e] + s[n][e] : s[n][e];
 }
 
+// A thread has four columns, VEC 4: neighbouring ones (rows of dW on 16-byte boundaries, D a multiple of four), 1: every 128th of the block's 512, and all
+// tokens' X there in registers; a block walks along a slice of dW's rows.
+template <int TOKENS, int VEC, typename T>
+__global__ void __launch_bounds__(kColumnThreads)
+few_weight_grad_kernel(const float* G, int64_t ldg, const float* x, int64_t ldx, T* dW, int64_t lddw, int beta, int N, int D, int V)
+{
+    constexpr int kApart = VEC == 4 ? 1 : kColumnThreads;
+    __shared__ __align__(16) float g[kRows][TOKENS];
+    pdl_wait();
+    pdl_trigger();
+    const int d = blockIdx.x * 4 * kColumnThreads + threadIdx.x * VEC, slice = blockIdx.y, slices = gridDim.y;
+    const int v0 = static_cast<int>(static_cast<int64_t>(V) * slice / slices), v1 = static_cast<int>(static_cast<int64_t>(V) * (slice + 1) / slices);
+    float y[TOKENS][4];
+#pragma unroll
+    for (int n = 0; n < TOKENS; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[n][e] = x[min(n, N - 1) * ldx + min(d + e * kApart, D - 1)];       // no branch: all under way; tokens that are not there have g = 0
+#pragma unroll
+    for (int n = 0; n < TOKENS; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[n][e] = n < N ? y[n][e] : 0.f;
+    for (int v = v0; v < v1; v += kRows) {
+        const int count = min(kRows, v1 - v);
+        __syncthreads();                                   // the last rows have been read
+        for (int i = threadIdx.x; i < kRows * TOKENS; i += kColumnThreads) {
+            const int n = i / kRows, r = i % kRows;
+            g[r][n] = n < N && r < count ? G[n * ldg + v + r] : 0.f;
+        }
+        __syncthreads();
+        if (d >= D) continue;
+        T* out = dW + static_cast<int64_t>(v) * lddw + d;
+#pragma unroll 2
+        for (int r = 0; r < count; ++r, out += lddw) {
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int n = 0; n < TOKENS; n += 4) {
+                const float4 z = *reinterpret_cast<const float4*>(&g[r][n]);
+                const float zs[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[e] = fmaf(zs[k], y[n + k][e], s[e]);
+            }
+            if (beta) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (VEC == 4 || d + e * kApart < D) s[e] += Elem<T>::load(out + e * kApart);
+            }
+            if (VEC == 4 && sizeof(T) == 4) {
+                *reinterpret_cast<float4*>(out) = make_float4(s[0], s[1], s[2], s[3]);
+            } else if (VEC == 4) {
+                *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (d + e * kApart < D) Elem<T>::store(out + e * kApart, s[e]);
+            }
+        }
+    }
+}
+
 // The slices' sums, in order, to where the rows' tokens are: a block takes 32 columns of a row, a warp every eighth slice, 16 of them under way at once.
 __global__ void __launch_bounds__(kThreads)
 few_rows_back_kernel(const float* sum, int64_t lds, int64_t slice_stride, int slices, int D, const int* live, const int* order, float* dX, int64_t lddx)
@@ -212,7 +275,38 @@ int launch_grad(const float* G, int64_t ldg, const float* W, int64_t ldw, float*
                           kColumnThreads, 0, stream, G, ldg, W, ldw, sum, lds, N * lds, add, static_cast<int>(N), static_cast<int>(D), static_cast<int>(V));
 }
 
+template <int TOKENS, int VEC, typename T>
+int launch_weight_grad(const float* G, int64_t ldg, const float* x, int64_t ldx, void* dW, int64_t lddw, int beta, int64_t N, int64_t D, int64_t V, int sm_count,
+                       cudaStream_t stream)
+{
+    const int64_t across = ceil_div64(D, 4 * kColumnThreads), most = ceil_div64(V, kRows), fill = ceil_div64(static_cast<int64_t>(sm_count) * 8, across);
+    return launch_chained(few_weight_grad_kernel<TOKENS, VEC, T>, dim3(static_cast<unsigned>(across), static_cast<unsigned>(fill < most ? fill : most)),
+                          kColumnThreads, 0, stream, G, ldg, x, ldx, static_cast<T*>(dW), lddw, beta, static_cast<int>(N), static_cast<int>(D), static_cast<int>(V));
+}
+template <int VEC, typename T>
+int launch_weight_grad(const float* G, int64_t ldg, const float* x, int64_t ldx, void* dW, int64_t lddw, int beta, int64_t N, int64_t D, int64_t V, int sm_count,
+                       cudaStream_t stream)
+{
+    return N <= 4   ? launch_weight_grad<4, VEC, T>(G, ldg, x, ldx, dW, lddw, beta, N, D, V, sm_count, stream)
+           : N <= 8 ? launch_weight_grad<8, VEC, T>(G, ldg, x, ldx, dW, lddw, beta, N, D, V, sm_count, stream)
+                    : launch_weight_grad<16, VEC, T>(G, ldg, x, ldx, dW, lddw, beta, N, D, V, sm_count, stream);
+}
+
 }  // namespace
+
+int launch_distill_few_weight_grad(const float* G, int64_t ldg, const float* x, int64_t ldx, void* dW, int dw_dtype, int64_t lddw, int beta, int64_t N, int64_t D,
+                                   int64_t V, cudaStream_t stream)
+{
+    DeviceInfo di;
+    const int rc = device_info(&di);
+    if (rc != VELORA_OK) return rc;
+    const bool vec = D % 4 == 0 && aligned16(dW) && lddw * static_cast<int64_t>(dtype_size(dw_dtype)) % 16 == 0;
+    if (dw_dtype == VELORA_BF16)
+        return vec ? launch_weight_grad<4, __nv_bfloat16>(G, ldg, x, ldx, dW, lddw, beta, N, D, V, di.sm_count, stream)
+                   : launch_weight_grad<1, __nv_bfloat16>(G, ldg, x, ldx, dW, lddw, beta, N, D, V, di.sm_count, stream);
+    return vec ? launch_weight_grad<4, float>(G, ldg, x, ldx, dW, lddw, beta, N, D, V, di.sm_count, stream)
+               : launch_weight_grad<1, float>(G, ldg, x, ldx, dW, lddw, beta, N, D, V, di.sm_count, stream);
+}
 
 int distill_few_slices(int64_t D)
 {

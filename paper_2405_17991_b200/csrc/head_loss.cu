@@ -662,8 +662,12 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
         if (rc != VELORA_OK) return rc;
         if (dW) {
             char* dw = static_cast<char*>(dW) + static_cast<size_t>(v0) * lddw * dtype_size(dw_dtype);
-            rc = product(GEMM_TN_MN_MN, G, a.dtype, l.piece_cols, a.ws + l.x, a.dtype, l.ldx, dw, dw_dtype, lddw, beta, cols, a.D, a.N * l.rows, status,
-                         GemmMore{l.rows > 1 ? nullptr : live, take_common ? common : nullptr, 1, 0, kBand}, a.stream);
+            if (a.teacher && few_f32(a.dtype, a.N, a.teacher->K))
+                rc = launch_distill_few_weight_grad(reinterpret_cast<float*>(G), l.piece_cols, reinterpret_cast<float*>(a.ws + l.x), l.ldx, dw, dw_dtype, lddw,
+                                                    beta, a.N, a.D, cols, a.stream);
+            else
+                rc = product(GEMM_TN_MN_MN, G, a.dtype, l.piece_cols, a.ws + l.x, a.dtype, l.ldx, dw, dw_dtype, lddw, beta, cols, a.D, a.N * l.rows, status,
+                             GemmMore{l.rows > 1 ? nullptr : live, take_common ? common : nullptr, 1, 0, kBand}, a.stream);
             if (rc != VELORA_OK) return rc;
         }
         if (dX && a.teacher && few_f32(a.dtype, a.N, a.teacher->K)) {

@@ -222,6 +222,9 @@ int launch_distill_few_rows_back(const float* sum, int64_t lds, int slices, int6
                                  cudaStream_t stream);
 int launch_distill_few_grad(const float* G, int64_t ldg, const float* W, int64_t ldw, float* sum, int64_t lds, int slices, int add, int64_t N, int64_t D, int64_t V,
                             cudaStream_t stream);
+// dW or, with beta, more of it, from the piece's gradients and the rows of X.
+int launch_distill_few_weight_grad(const float* G, int64_t ldg, const float* x, int64_t ldx, void* dW, int dw_dtype, int64_t lddw, int beta, int64_t N, int64_t D,
+                                   int64_t V, cudaStream_t stream);
 int launch_head_loss(const HeadArgs& a, float* loss, float* lse);
 int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* dloss, void* dX, int64_t lddx,
                               void* dW, int dw_dtype, int64_t lddw, int beta);

@@ -177,8 +177,8 @@ def test_long_lists_and_small_vocabularies(vl, guard, N, D, V, K, dtype):
     run(vl, guard, batch(N, D, V, K, dtype, 17, 1.0, "none", True))
 
 
-@pytest.mark.parametrize("N", [1, 4, 5, 15, 16, 17])
-@pytest.mark.parametrize("D,V", [(4, 3), (200, 1000), (203, 1001), (2052, 700), (4099, 130), (9000, 260)])
+@pytest.mark.parametrize("N", [1, 4, 5, 8, 9, 15, 16, 17])
+@pytest.mark.parametrize("D,V", [(4, 3), (200, 1000), (203, 1001), (1664, 515), (2052, 700), (4099, 130), (9000, 260)])
 def test_few_tokens_in_fp32(vl, guard, N, D, V):
     """Up to 16 tokens have products of their own: tokens on both sides of their sizes, rows that shared memory holds and longer ones, of any width."""
     run(vl, guard, batch(N, D, V, 3, torch.float32, N + D, 1.0, "some" if N > 4 else "none", True))
@@ -196,6 +196,27 @@ def test_few_tokens_in_fp32(vl, guard, N, D, V):
             continue
         check(dX, ref.dX, ref.dX_bound, "dX")
         check(dW, ref.dW, ref.dW_bound, "dW")
+
+
+@pytest.mark.parametrize("dw_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N", [1, 7, 16])
+@pytest.mark.parametrize("D,V,ld,offset", [(96, 300, 96, 0), (96, 300, 104, 8), (96, 300, 97, 0), (96, 300, 104, 3), (131, 4001, 131, 1), (513, 700, 516, 0), (1024, 9500, 1024, 0)])
+def test_weight_gradient_of_few_tokens_anywhere(vl, N, D, V, ld, offset, dw_dtype):
+    """dW in fp32 products' own kernel: rows on any boundary, added to or not, and nothing beside them touched."""
+    p = batch(N, D, V, 4, torch.float32, N + D, 1.5)
+    _, lse = forward(vl, p)
+    ref = Reference(p)
+    room = torch.randn(offset + V * ld + 64, device=DEV).to(dw_dtype)
+    before = room.clone()
+    for beta in (0, 1):
+        dW = room[offset:offset + V * ld].as_strided((V, D), (ld, 1))
+        old = dW.double() if beta else torch.zeros((V, D), dtype=torch.float64, device=DEV)
+        backward(vl, p, lse, dW=dW, beta=beta, need_dX=False)
+        # the sum's own bound, its rounding, and, with beta, one more of fp32
+        check(dW, ref.dW + old, ref.dW_bound + 2.0 ** -23 * old.abs(), "dW", half_step(dw_dtype))
+    inside = torch.zeros_like(room, dtype=torch.bool)
+    inside[offset:offset + V * ld].as_strided((V, D), (ld, 1)).fill_(True)
+    assert torch.equal(room[~inside], before[~inside])
 
 
 def test_a_vocabulary_of_millions(vl, guard):
