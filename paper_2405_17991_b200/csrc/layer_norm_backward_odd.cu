@@ -144,8 +144,8 @@ template <typename T, int N, int LEAST, bool MORE, int TEAM, int P, bool KEEP, i
 int launch_rows(const NormGradArgs& a, int sm_count, cudaStream_t stream)
 {
     static_assert(TEAM == 0 || P == 32 * TEAM, "a team's threads");
-    constexpr int kTeams = TEAM ? 8 / TEAM : 1, kBudget = 216 * 1024 / BLOCKS;
-    const int share = odd_share(a.D, a.dtype), row = share * (MORE ? 3 : 2) * kTeams, stages = kBudget / row < 4 ? kBudget / row : 4;
+    constexpr int kTeams = TEAM ? 8 / TEAM : 1, kRoom = 216 * 1024 / BLOCKS;
+    const int share = odd_share(a.D, a.dtype), row = share * (MORE ? 3 : 2) * kTeams, stages = kRoom / row < 4 ? kRoom / row : 4;
     if (a.D > N * P || a.D < LEAST * P) return VELORA_ERR_UNSUPPORTED;
     if (stages < 2) return launch_layer_norm_backward_any(a, sm_count, stream);
     static DeviceOnce configured;
@@ -153,7 +153,7 @@ int launch_rows(const NormGradArgs& a, int sm_count, cudaStream_t stream)
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return VELORA_ERR_CUDA;
     auto kern = norm_grad_odd_kernel<T, N, LEAST, MORE, TEAM, P, KEEP, BLOCKS>;
     if (!configured.get(dev)) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBudget) != cudaSuccess) return VELORA_ERR_CUDA;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRoom) != cudaSuccess) return VELORA_ERR_CUDA;
         configured.set(dev);
     }
     size_t smem = static_cast<size_t>(stages) * row;

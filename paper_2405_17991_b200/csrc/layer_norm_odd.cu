@@ -108,8 +108,8 @@ norm_odd_kernel(const NormArgs a, int stages, int share)
 template <typename T, int N, int LEAST, bool RESIDUAL, int TEAM, int P, int BLOCKS>
 int launch_rows(const NormArgs& a, int sm_count, cudaStream_t stream)
 {
-    constexpr int kTeams = TEAM ? 8 : 1, kBudget = 216 * 1024 / BLOCKS;
-    const int share = odd_share(a.D, a.dtype), row = share * (RESIDUAL ? 2 : 1) * kTeams, stages = kBudget / row < 4 ? kBudget / row : 4;
+    constexpr int kTeams = TEAM ? 8 : 1, kRoom = 216 * 1024 / BLOCKS;
+    const int share = odd_share(a.D, a.dtype), row = share * (RESIDUAL ? 2 : 1) * kTeams, stages = kRoom / row < 4 ? kRoom / row : 4;
     if (a.D > N * P || a.D < LEAST * P) return VELORA_ERR_UNSUPPORTED;
     if (stages < 2) return launch_layer_norm_any(a, sm_count, stream);
     static DeviceOnce configured;
@@ -117,7 +117,7 @@ int launch_rows(const NormArgs& a, int sm_count, cudaStream_t stream)
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return VELORA_ERR_CUDA;
     auto kern = norm_odd_kernel<T, N, LEAST, RESIDUAL, TEAM, P, BLOCKS>;
     if (!configured.get(dev)) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBudget) != cudaSuccess) return VELORA_ERR_CUDA;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRoom) != cudaSuccess) return VELORA_ERR_CUDA;
         configured.set(dev);
     }
     const int64_t blocks = ceil_div64(a.N, kTeams), most = static_cast<int64_t>(sm_count) * BLOCKS;
