@@ -96,7 +96,7 @@ def velora_layer_norm(X: torch.Tensor, weight: Optional[torch.Tensor] = None, bi
                       residual: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None, H: Optional[torch.Tensor] = None,
                       mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, stream=None):
     """Layer norm of the rows of H = X + residual (of X without one): (Y, H, mean, rstd), the last three for the backward pass.  H is X itself
-    where nothing is added."""
+    where nothing is added, and None where Y is written over it: then nothing is left for the backward pass."""
     if stream is not None and (Y is None or mean is None or rstd is None or (residual is not None and H is None)):
         return b._on(stream, velora_layer_norm, X, weight, bias, eps, residual, Y, H, mean, rstd)
     xp, ldx = b._mat(X, "X")
@@ -130,6 +130,8 @@ def velora_layer_norm(X: torch.Tensor, weight: Optional[torch.Tensor] = None, bi
     else:
         yp, ldy = _rows_like(Y, X, "Y")
         given.append(Y)
+        if residual is None and N and yp == xp:
+            H = None
     if mean is None:
         mean = torch.empty(N, dtype=torch.float32, device=X.device)
         mp = mean.data_ptr()
@@ -156,6 +158,8 @@ def velora_layer_norm_backward(dY: torch.Tensor, H: torch.Tensor, mean: torch.Te
     if stream is not None and ((need_dX and dX is None) or (need_dweight and dweight is None) or (need_dbias and dbias is None) or ws is None):
         return b._on(stream, velora_layer_norm_backward, dY, H, mean, rstd, weight, dH, dX, dweight, dbias, need_dX, need_dweight, need_dbias,
                      dw_dtype, beta, ws)
+    if H is None:
+        raise ValueError("H is None: velora_layer_norm wrote Y over it")
     hp, ldh = b._mat(H, "H")
     N, D = H.shape
     yp, lddy = _rows_like(dY, H, "dY")

@@ -1,0 +1,29 @@
+"""Layer norms whose outputs lie on their inputs, rows of one very large value, fp32 rows around the longest that a backward pass with dH holds: against the
+formula in 64 bits, with the bounds of test_gpu_layer_norm."""
+import pytest
+import torch
+
+from test_gpu_layer_norm import EPS, Backward, Forward, batch, check, guard, half_step, run, vl  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N,D", [(40, 768), (40, 1001), (3, 16400)])
+def test_a_norm_in_place_leaves_nothing_for_the_backward_pass(vl, N, D, dtype):  # noqa: F811
+    """Y on X, nothing added: H would be X, which holds Y by then."""
+    p = batch(N, D, dtype, 10)
+    Y, H, mean, rstd = vl.velora_layer_norm(p["X"], p["w"], p["b"])
+    assert H is p["X"]
+    want = vl.velora_layer_norm_backward(p["dY"], H, mean, rstd, p["w"])
+    for same in (lambda X: X, lambda X: X[:], lambda X: X.view(N, D)):
+        X = p["X"].clone()
+        at, gone, m, r = vl.velora_layer_norm(X, p["w"], p["b"], Y=same(X))
+        assert gone is None and torch.equal(at, Y) and torch.equal(m, mean) and torch.equal(r, rstd)
+        with pytest.raises(ValueError):
+            vl.velora_layer_norm_backward(p["dY"], gone, m, r, p["w"])
+    kept = p["X"].clone()                                     # what a caller does who wants both
+    X = p["X"].clone()
+    vl.velora_layer_norm(X, p["w"], p["b"], Y=X, mean=mean, rstd=rstd)
+    assert all(torch.equal(x, y) for x, y in zip(vl.velora_layer_norm_backward(p["dY"], kept, mean, rstd, p["w"]), want))
