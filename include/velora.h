@@ -473,8 +473,8 @@ int velora_head_distill_backward(const void* X, int64_t ldx, const void* W, int6
  * (eps == 0 leaves a row of equal values without a result).
  * Statistics, sums and products are fp32, every output is rounded once; the variance is taken about the mean; sums have a fixed order.  Squares of H - m
  * must stay in fp32's range; an infinity or a NaN makes its row NaN.
- * H or Y may lie where X or R does, dX where dY, dH or H does (the same address and pitch; nothing else may overlap).  The backward pass reads H: where
- * nothing is added and Y lies on X, only an H of its own leaves it something.
+ * H or Y may lie where X or R does, dX where dY, dH or H does (the same address and pitch; nothing else may overlap; H and Y at
+ * one address are refused).  The backward pass reads H: where nothing is added and Y lies on X, only an H of its own leaves it something.
  * ws of the backward pass: velora_workspace_bytes(VELORA_OP_LAYER_NORM_BACKWARD, N, D, 1, 1) bytes, for dweight and dbias (NULL without both).
  * N == 0: nothing is written, but dweight = beta * dweight, dbias = beta * dbias.
  */

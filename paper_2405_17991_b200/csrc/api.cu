@@ -832,6 +832,7 @@ int velora_layer_norm(const void* X, int64_t ldx, const void* R, int64_t ldr, co
     if ((rc = check_rows(X, ldx, dtype, D, false)) != VELORA_OK || (rc = check_rows(R, ldr, dtype, D, true)) != VELORA_OK ||
         (rc = check_rows(H, ldh, dtype, D, true)) != VELORA_OK || (rc = check_rows(Y, ldy, dtype, D, false)) != VELORA_OK) return rc;
     if ((mean && !elem_aligned(mean, VELORA_F32)) || (rstd && !elem_aligned(rstd, VELORA_F32))) return VELORA_ERR_ALIGNMENT;
+    if (H == Y) return VELORA_ERR_INVALID_ARG;               /* one would be lost */
     return launch_layer_norm(NormArgs{X, ldx, R, ldr, weight, bias, p_dtype, eps, H, ldh, Y, ldy, mean, rstd, dtype, N, static_cast<int>(D)},
                              static_cast<cudaStream_t>(stream));
 }

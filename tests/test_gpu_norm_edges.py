@@ -27,3 +27,13 @@ def test_a_norm_in_place_leaves_nothing_for_the_backward_pass(vl, N, D, dtype): 
     X = p["X"].clone()
     vl.velora_layer_norm(X, p["w"], p["b"], Y=X, mean=mean, rstd=rstd)
     assert all(torch.equal(x, y) for x, y in zip(vl.velora_layer_norm_backward(p["dY"], kept, mean, rstd, p["w"]), want))
+
+
+@pytest.mark.parametrize("N,D", [(4, 64), (4, 1001)])
+def test_one_address_for_h_and_y_is_refused(vl, N, D):  # noqa: F811
+    p = batch(N, D, torch.bfloat16, 1)
+    out = torch.full_like(p["X"], 3.0)
+    for Y, H in ((out, out), (p["X"], p["X"]), (p["R"], p["R"])):
+        with pytest.raises(vl.VeloraError):
+            vl.velora_layer_norm(p["X"], p["w"], p["b"], residual=p["R"], Y=Y, H=H)
+    assert bool((out == 3.0).all())

@@ -18,3 +18,11 @@ def test_a_norm_in_place_returns_no_rows_for_the_backward_pass(seen):  # noqa: F
     R = torch.ones_like(X)
     assert t.velora_layer_norm(X, w, residual=R, Y=X)[1] is not None
     assert t.velora_layer_norm(X, w, residual=R, Y=R, H=X)[1] is X
+
+
+def test_one_address_for_h_and_y_is_refused():
+    from paper_2405_17991_b200 import binding, build
+    from test_norm_distill_host import P, norm
+    build.build()
+    f = norm(binding)
+    assert f() == f(R=P(0)) == f(H=P(0x20000), Y=P(0x20000)) == binding.ERR_INVALID_ARG
