@@ -46,7 +46,8 @@ norm_grad_odd_kernel(const NormGradArgs a, int stages, int share)
     float m_next = rows > 0 ? mean_at[0] : 0.f, s_next = rows > 0 ? rstd_at[0] : 0.f;
     int slot = 0, turn = 0;
     for (int64_t row = 0; row < rows; ++row) {
-        const F2 minus_m = f2(-m_next), scale = f2(s_next);
+        const float m = m_next;
+        const F2 minus_m = f2(-m), scale = f2(s_next);
         if (row + 1 < rows) {
             m_next = mean_at[row + 1];
             s_next = rstd_at[row + 1];
@@ -63,12 +64,12 @@ norm_grad_odd_kernel(const NormGradArgs a, int stages, int share)
         dY.step();
         H.step();
         if (MORE) dH.step();
-        // Columns that are not there: dy and w are zeros.
+        // Columns that are not there: dy and w are zeros, and h is the mean, since m s may be beyond fp32 where every h - m is zero.
         F2 xhat[N / 2], c[N / 2], sums = f2(0.f), along = f2(0.f);
         {
             F2 dy[N / 2], h[N / 2];
             odd_load<T, P, N>(dy, dy_row, has);
-            odd_load<T, P, N>(h, h_row, has);
+            odd_load<T, P, N>(h, h_row, has, m);
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
                 xhat[i] = mul(add(h[i], minus_m), scale);
@@ -93,7 +94,7 @@ norm_grad_odd_kernel(const NormGradArgs a, int stages, int share)
         if (!KEEP) {
             F2 dy[N / 2], h[N / 2];
             odd_load<T, P, N>(dy, dy_row, has);
-            odd_load<T, P, N>(h, h_row, has);
+            odd_load<T, P, N>(h, h_row, has, m);
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
                 xhat[i] = mul(add(h[i], minus_m), scale);

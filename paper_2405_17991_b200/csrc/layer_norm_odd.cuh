@@ -73,13 +73,13 @@ __device__ __forceinline__ float load_shared(uint32_t at, float)
     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
     return x;
 }
-// Missing ones are zeros.
-template <typename T, int P, int N, int LEAST> __device__ __forceinline__ void odd_load(F2 (&x)[N / 2], uint32_t row, const OddColumns<LEAST>& c)
+// `none` stands for missing ones.
+template <typename T, int P, int N, int LEAST> __device__ __forceinline__ void odd_load(F2 (&x)[N / 2], uint32_t row, const OddColumns<LEAST>& c, float none = 0.f)
 {
     constexpr uint32_t kStep = P * sizeof(T);
 #pragma unroll
     for (int i = 0; i < N; i += 2) {
-        float lo = 0.f, hi = 0.f;
+        float lo = none, hi = none;
         if (c.has(i)) lo = load_shared(row + i * kStep, T());
         if (c.has(i + 1)) hi = load_shared(row + (i + 1) * kStep, T());
         x[i / 2] = f2(lo, hi);

@@ -37,3 +37,25 @@ def test_one_address_for_h_and_y_is_refused(vl, N, D):  # noqa: F811
         with pytest.raises(vl.VeloraError):
             vl.velora_layer_norm(p["X"], p["w"], p["b"], residual=p["R"], Y=Y, H=H)
     assert bool((out == 3.0).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D,power,eps", [(65, 120, EPS), (100, 120, EPS), (250, 120, EPS), (513, 110, 1e-12), (1001, 110, 1e-12), (2050, 110, 1e-12), (5461, 110, 1e-12), (9001, 110, 1e-12)])
+def test_rows_of_one_very_large_value(vl, D, power, eps, dtype):  # noqa: F811
+    """xhat is zero, although the mean times 1 / sqrt(eps) is beyond fp32: nothing of that may come in from columns that a thread does not have."""
+    g = torch.Generator(device=DEV).manual_seed(D)
+    X = torch.full((6, D), 2.0 ** power, device=DEV).to(dtype)
+    X[3:] *= -1
+    dY = torch.randn((6, D), generator=g, device=DEV).to(dtype)
+    dH = torch.randn((6, D), generator=g, device=DEV).to(dtype)
+    w, b = 1 + 0.3 * torch.randn(D, generator=g, device=DEV), torch.randn(D, generator=g, device=DEV)
+    Y, H, mean, rstd = vl.velora_layer_norm(X, w, b, eps)
+    assert torch.equal(mean, X[:, 0].float()) and bool((mean.abs().double() * rstd.double() > 3.5e38).all())
+    ref = Forward(X, None, w, b, eps)
+    check(Y, ref.Y, ref.Y_bound, "Y", half_step(dtype))
+    for more in (None, dH):
+        back = Backward(dY, X, mean, rstd, w, more)
+        dX, dw, db = vl.velora_layer_norm_backward(dY, H, mean, rstd, w, dH=more)
+        check(dX, back.dX, back.dX_bound, "dX", half_step(dtype))
+        check(dw, back.dw, back.dw_bound, "dweight")
+        check(db, back.db, back.db_bound, "dbias")
