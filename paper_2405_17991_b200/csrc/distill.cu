@@ -104,7 +104,7 @@ distill_lists_kernel(const ListsArgs a)
             const int64_t i = k < K ? a.t.index[n * a.t.ldi + k] : -1;
             const float x = k < K ? teacher_logit(a.t, n * a.t.ldt + k) : 0.f;              // does not wait for the column
             const bool is = i >= 0 && i < a.V;
-            const float over_t = x * a.inverse_t, u = is ? (over_t == INFINITY ? __int_as_float(0x7fc00000) : over_t) : -INFINITY;     // also beside a given s
+            const float u = is ? (x == INFINITY ? __int_as_float(0x7fc00000) : x) : -INFINITY;         // over T below: a finite one stays one until then
             if (i >= a.V) kind = 2.f;
             else if (is && u != -INFINITY) kind = fmaxf(kind, 1.f);
             m = fmaxf(m, u);
@@ -119,10 +119,10 @@ distill_lists_kernel(const ListsArgs a)
         float s = 0.f;
         if (a.t.lse) {
             m = a.t.lse[n];
-            for (int k = t; k < K; k += kTeam) s += p[k] = p[k] == -INFINITY ? 0.f : expf(p[k] - m);
+            for (int k = t; k < K; k += kTeam) s += p[k] = p[k] == -INFINITY ? 0.f : expf(p[k] * a.inverse_t - m);
         } else {
             m = row_all<WARPS>(m, part, most);
-            for (int k = t; k < K; k += kTeam) s += p[k] = expf(p[k] - m);
+            for (int k = t; k < K; k += kTeam) s += p[k] = expf((p[k] - m) * a.inverse_t);
             const float scale = 1.f / row_all<WARPS>(s, part, sum);
             s = 0.f;
             for (int k = t; k < K; k += kTeam) s += p[k] *= scale;
