@@ -254,7 +254,10 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
             if (LISTS) ahead.find_entries(h.e, h.v0 + col_ahead);
             if (failed || valid <= 0) continue;
             const bool in = row < h.N;
-            const float log2e = LISTS ? kHeadLog2e * h.e.inverse_t : kHeadLog2e;       // logits are divided by the temperature where they go into an exponent
+            // Logits are divided by the temperature where they go into an exponent.  What log2 e / T has lost by its rounding, and a maximum over T by its own, would
+            // move a row's logits against its lse; sums and gradients make up for both (one column, l / T up to 3000, T = 1.1: G off by 1.4 times what
+            // lse's rounding accounts for).
+            const float log2e = LISTS ? kHeadLog2e * h.e.inverse_t : kHeadLog2e;
             // Entries: 32 of this lane's values through its 128 bytes of the warp's block of shared memory, 16 at a time in an order that keeps the lanes apart.
             const uint32_t turn = block + lane * 128, swap = (lane & 7) << 4;
             auto value = [&](int column) { return turn + ((static_cast<uint32_t>(column) << 2 & 0x70u) ^ swap) + (static_cast<uint32_t>(column) << 2 & 0xcu); };
@@ -306,8 +309,10 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) s[i & 3] += head_exp2(fmaf(__uint_as_float(l[c][i]), log2e, -c2));
-                const float sum = ((s[0] + s[1]) + (s[2] + s[3])) * (1.f - lost * 0.69314718f);
-                if (in) h.running[static_cast<int64_t>((t0.n0 >> 7) + half) * h.N + row] = make_float2(LISTS ? m * h.e.inverse_t : m, sum);
+                float back = 1.f - lost * 0.69314718f;
+                if (LISTS) back += fmaf(ref, h.e.inverse_t, -__fmul_rn(ref, h.e.inverse_t));
+                const float sum = ((s[0] + s[1]) + (s[2] + s[3])) * back;
+                if (in) h.running[static_cast<int64_t>((t0.n0 >> 7) + half) * h.N + row] = make_float2(LISTS ? __fmul_rn(m, h.e.inverse_t) : m, sum);
             } else {
                 const bool is = LISTS ? part : in && h.target[row] >= 0;
                 const float g = LISTS ? g_row * h.e.inverse_t : (is ? h.scale[row] : 0.f), lse = LISTS ? lse_row : (is ? h.lse[row] : 0.f);
@@ -319,6 +324,8 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                         for (int i = 0; i < 32; ++i) l[c][i] = __float_as_uint((LISTS ? __uint_as_float(l[c][i]) * h.e.inverse_t : __uint_as_float(l[c][i])) - lse);
                     z = lost = 0.f;
                     scale = kHeadLog2e;
+                } else if (LISTS) {                          // at l / T = lse, where it counts
+                    lost = fmaf(-z, __fdividef(fmaf(kHeadLog2e, h.e.inverse_t, -log2e), log2e), lost);
                 }
                 const float gp = (LISTS ? g * mass : g) * (1.f + lost * 0.69314718f);
                 if (LISTS && __any_sync(0xffffffffu, walk.column != kNoColumn)) {

@@ -38,3 +38,56 @@ def test_logits_at_the_ends_of_their_type(vl, N, K, t_dtype, whole):  # noqa: F8
     dX, dW = backward(vl, p, lse)
     check(dX, ref.dX, ref.dX_bound, "dX", half_step(torch.bfloat16))
     check(dW, ref.dW, ref.dW_bound, "dW", half_step(torch.bfloat16))
+
+
+@pytest.mark.parametrize("T", [1.0, 1.1, 1.5, 2.5, 5.0, 0.7])
+@pytest.mark.parametrize("N", [10, 100, 300])
+def test_one_column_has_the_whole_share(vl, N, T):  # noqa: F811
+    """G = g / T (exp(l / T - lse) - 1) would be zero, and shows what the two passes' l / T and lse differ by.  That is lse's rounding to fp32, u |lse|, and
+    2^-20 for an exponential in each pass (2^-22) and the
+    roundings of products and sums near one behind them: a temperature is no source of its own."""
+    g = torch.Generator(device=DEV).manual_seed(N)
+    r = lambda *s: torch.randn(s, generator=g, device=DEV)  # noqa: E731
+    D = 64
+    p = {"X": (100 * r(N, D)).bfloat16(), "W": r(1, D).bfloat16(), "i": torch.zeros((N, 1), dtype=torch.int64, device=DEV), "t": r(N, 1), "lse": None,
+         "g": torch.ones(N, device=DEV), "T": T}
+    loss, lse = forward(vl, p)
+    dX, _ = backward(vl, p, lse, need_dW=False)
+    bound = (U * lse.double().abs() + 2.0 ** -20)[:, None] / T * p["W"].double().abs() * (1 + 2.0 ** -6)          # two roundings to bf16
+    worst = (dX.double().abs() / bound).max().item()
+    assert worst <= 1.0, worst
+
+
+@pytest.mark.parametrize("T", [1.1, 2.5])
+@pytest.mark.parametrize("N", [4, 100, 300])
+def test_a_student_that_agrees_at_another_temperature(vl, N, T):  # noqa: F811
+    D, V = 256, 600
+    p = batch(N, D, V, V, torch.bfloat16, 33, T)
+    l = p["X"].double() @ p["W"].double().t()
+    p["i"] = torch.stack([torch.randperm(V, device=DEV) for _ in range(N)])
+    p["t"] = l.gather(1, p["i"]).float()
+    ref = Reference(p)
+    loss, lse = forward(vl, p)
+    check(loss, ref.loss, ref.loss_bound, "loss")
+    dX, dW = backward(vl, p, lse)
+    check(dX, ref.dX, ref.dX_bound, "dX", half_step(torch.bfloat16))
+    check(dW, ref.dW, ref.dW_bound, "dW", half_step(torch.bfloat16))
+    q = torch.softmax(l / T, 1)
+    assert dX.double().norm() <= 2.0 ** -12 / T * ((q * p["g"].double()[:, None].abs()) @ p["W"].double().abs()).norm()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [1.5, 0.7])
+@pytest.mark.parametrize("N", [8, 100, 300])
+def test_gradients_of_sure_tokens_at_another_temperature(vl, N, T, dtype):  # noqa: F811
+    """Logits over T as in test_gpu_head_confident; its reference takes W / T for W."""
+    D, V = 2048, 2000
+    X, W, t, dloss = sure_batch(N, D, V, dtype, False, N + D)
+    X = (X.double() * T).to(dtype)
+    ref = SureReference(X, W.double() / T, t, dloss, N)
+    p = {"X": X, "W": W, "i": t[:, None].contiguous(), "t": torch.zeros((N, 1), device=DEV), "lse": None, "g": dloss, "T": T}
+    loss, lse = forward(vl, p)
+    dX, dW = backward(vl, p, lse)
+    check_rows(dX, ref.dX, ref.dX_bound, "dX")
+    hit = torch.unique(t)
+    check_rows(dW[hit], ref.dW[hit] / T, ref.dW_bound[hit] / T, "dW")
