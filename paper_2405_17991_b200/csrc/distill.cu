@@ -183,6 +183,9 @@ distill_lists_kernel(const ListsArgs a)
     }
 }
 
+// A logit over the temperature, rounded to the same number in both passes: contracted into the subtraction behind it, it would differ from what is in lse.
+__device__ __forceinline__ float over_t(float l, const Entries& e) { return __fmul_rn(l, e.inverse_t); }
+
 // fp32: a block takes a slice of a row's logits, 1024 columns, in registers: its maximum, its exponentials, the entries' logits.  (A block a row, three times
 // over it: 1 x 24008 88 us, 8904 x 501 46 us.)
 constexpr int kSliceColumns = 4 * kThreads;
@@ -203,7 +206,7 @@ distill_stats_kernel(const float* logits, int64_t ld, int parts, int64_t part_st
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int c = threadIdx.x + kThreads * i;
-        x[i] = c0 + c < h.cols ? (parts > 1 ? sum_of_parts(l + c, parts, part_stride) : l[c]) * h.e.inverse_t : -INFINITY;
+        x[i] = c0 + c < h.cols ? over_t(parts > 1 ? sum_of_parts(l + c, parts, part_stride) : l[c], h.e) : -INFINITY;
         value[c] = x[i];
         m = fmaxf(m, x[i]);
     }
@@ -246,7 +249,7 @@ distill_gradient_kernel(float* logits, int64_t ld, int parts, int64_t part_strid
             x[i] = is && c0 + lane + 32 * i < h.cols ? (parts > 1 ? sum_of_parts(at, parts, part_stride) : *at) : 0.f;
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = is ? q * expf(x[i] * h.e.inverse_t - z) : 0.f;
+        for (int i = 0; i < 4; ++i) x[i] = is ? q * expf(over_t(x[i], h.e) - z) : 0.f;
         if (is) {
             const int b = (h.v0 + c0) / kEntryColumns;
             for (int j = starts[b]; j < starts[b + 1]; ++j) {

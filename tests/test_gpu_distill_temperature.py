@@ -91,3 +91,17 @@ def test_gradients_of_sure_tokens_at_another_temperature(vl, N, T, dtype):  # no
     check_rows(dX, ref.dX, ref.dX_bound, "dX")
     hit = torch.unique(t)
     check_rows(dW[hit], ref.dW[hit] / T, ref.dW_bound[hit] / T, "dW")
+
+
+@pytest.mark.parametrize("T", [1.0, 1.1, 1.5, 2.5, 5.0, 0.7])
+@pytest.mark.parametrize("N", [10, 100, 300])
+def test_one_column_in_fp32(vl, N, T):  # noqa: F811
+    """A logit over T is rounded once, to the same number in both passes, and is lse here: exp(0) - 1 is zero."""
+    g = torch.Generator(device=DEV).manual_seed(N)
+    r = lambda *s: torch.randn(s, generator=g, device=DEV)  # noqa: E731
+    D = 64
+    p = {"X": 100 * r(N, D), "W": r(1, D), "i": torch.zeros((N, 1), dtype=torch.int64, device=DEV), "t": r(N, 1), "lse": None,
+         "g": torch.ones(N, device=DEV), "T": T}
+    loss, lse = forward(vl, p)
+    dX, _ = backward(vl, p, lse, need_dW=False)
+    assert not dX.any() and not loss.any()
