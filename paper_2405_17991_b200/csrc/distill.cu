@@ -238,7 +238,7 @@ distill_gradient_kernel(float* logits, int64_t ld, int parts, int64_t part_strid
     float* l = logits + row * ld;
     const bool is = h.target[row] >= 0;
     const int n = h.e.order[row];
-    const float g = h.scale[row] * h.e.inverse_t, z = h.lse[row], q = is ? g * h.e.mass[n] : 0.f;
+    const float g = h.scale[row], z = h.lse[row], q = is ? g * h.e.mass[n] : 0.f;
     const unsigned short* starts = h.e.starts + static_cast<int64_t>(n) * h.e.pitch;
     const Entry* entries = h.e.entries + static_cast<int64_t>(n) * h.e.K;
     for (int c0 = (static_cast<int>(blockIdx.y) * kWarps + warp) * kEntryColumns; c0 < h.cols; c0 += static_cast<int>(gridDim.y) * kWarps * kEntryColumns) {

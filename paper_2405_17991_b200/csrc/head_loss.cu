@@ -165,6 +165,7 @@ struct RowsArgs {
     const float* dloss;             // backward only
     const float* lse;
     int take_common;                // whether a factor is taken out of the dloss
+    float inverse_t;                // 1 / temperature (1 without a teacher): in `common`, or, where that is 1, in `scale_out`
     int N, V, D, rows_per_cta, copies;
     int* live;
     int* order;
@@ -218,12 +219,18 @@ head_rows_kernel(const RowsArgs a)
     __syncthreads();
     before = counts[0];
     total = counts[1];
-    // The common factor: none where it could not be divided by.
-    float common = __int_as_float(counts[2]);
-    if (!(common >= 1.17549435e-38f && common <= 3.4e38f)) common = 1.f;
+    // The common factor: none where it could not be divided by, or is out of range with the temperature's.
+    auto normal = [](float x) { return x >= 1.17549435e-38f && x <= 3.4e38f; };
+    float common = __int_as_float(counts[2]), rest = 1.f;
+    if (!normal(common)) common = 1.f;
+    float factor = common * a.inverse_t;
+    if (!a.take_common || !normal(factor)) {
+        common = factor = 1.f;
+        rest = a.inverse_t;
+    }
     if (blockIdx.x == 0 && blockIdx.y == 0 && t == 0) {
         *a.live = total;
-        if (a.scale_out) *a.common = common;
+        if (a.scale_out) *a.common = factor;
     }
     for (int b0 = r0; b0 < r1; b0 += kRowThreads) {
         const int n = b0 + t;
@@ -245,7 +252,7 @@ head_rows_kernel(const RowsArgs a)
                 a.order[to] = n;
                 a.target_out[to] = is ? static_cast<int>(v) : (v < 0 ? -1 : -2);
                 if (a.scale_out) {
-                    a.scale_out[to] = is ? a.dloss[n] / common : 0.f;
+                    a.scale_out[to] = is ? a.dloss[n] / common * rest : 0.f;
                     a.lse_out[to] = is ? a.lse[n] : 0.f;
                 }
                 if (v >= a.V && a.status) atomicCAS(a.status, 0, VELORA_ERR_INVALID_ARG);
@@ -300,6 +307,7 @@ int launch_rows(const HeadArgs& a, const HeadLayout& l, const float* lse, const 
         r.dloss = dloss;
         r.lse = lse;
         r.take_common = take_common ? 1 : 0;
+        r.inverse_t = a.teacher ? 1.f / a.teacher->temperature : 1.f;
         r.common = reinterpret_cast<float*>(a.ws + l.common);
         r.scale_out = reinterpret_cast<float*>(a.ws + l.scale);
         r.lse_out = reinterpret_cast<float*>(a.ws + l.lse);
@@ -627,7 +635,8 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
     if (rc != VELORA_OK) return rc;
     // In bf16 the logits' gradients are rounded once (more than 64 tokens), for the tensor cores: by half a step each.  A mean's 1 / count in
     // all of them would be the same rounding again and again, which does not average out (relative error of dX and dW up to 4e-3 by the
-    // count alone); so the largest dloss is taken out and multiplied back in fp32, wherever the product that writes dW takes a factor.
+    // count alone); so the largest dloss is taken out and multiplied back in fp32, wherever the product that writes dW takes a factor.  So is a
+    // temperature's 1 / T (512 x 256 of 4096, T = 1.5, one entry a token: fp32 dW off by 2.2e-3, now 2e-4).
     const bool take_common = a.dtype == VELORA_BF16 && (!dW || dw_dtype == VELORA_BF16 || c_rows_vec(dW, lddw, sizeof(float)));
     if (a.teacher) {
         rc = launch_distill_lists(a, l);

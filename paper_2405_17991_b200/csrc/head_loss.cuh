@@ -11,8 +11,8 @@ struct HeadLayout {
     size_t live;            // int32: how many rows have a target
     size_t order;           // int32[N]
     size_t target;          // int32[N]: column, -1 without one, -2 where it is no column
-    size_t common;          // fp32: the largest |dloss| of a row with a target, a factor taken out of all of them (backward)
-    size_t scale, lse;      // fp32[N]: what is left of the row's dloss, log sum exp (backward)
+    size_t common;          // fp32: the largest |dloss| of a row with a target, over the temperature, a factor taken out of all of them (backward)
+    size_t scale, lse;      // fp32[N]: what is left of the row's dloss over the temperature, log sum exp (backward)
     size_t at_target;       // fp32[N]: logit of the target (forward)
     size_t running;         // float2[N], or float2[parts of the vocabulary][N]: maximum, and the sum of exponentials relative to it (forward)
     size_t x;               // the rows of X, pitch ldx elements; zeros for rows without a target

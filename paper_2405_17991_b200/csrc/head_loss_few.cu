@@ -256,7 +256,7 @@ head_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
                     }
                 } else if (row < h.N && valid > 0) {
                     const bool is = LISTS ? lists.token[LISTS ? c : 0] >= 0 : target >= 0;
-                    const float g = LISTS ? lists.scale[LISTS ? c : 0] * h.e.inverse_t : (is ? h.scale[row] : 0.f);
+                    const float g = LISTS ? lists.scale[LISTS ? c : 0] : (is ? h.scale[row] : 0.f);
                     const float lse = LISTS ? lists.lse[LISTS ? c : 0] : (is ? h.lse[row] : 0.f);
                     float off = 0.f, z = -lse * kHeadLog2e, lost = fmaf(-lse, kHeadLog2e, -z);
                     if (fabsf(lost) > kHeadLost) {

@@ -315,7 +315,7 @@ head_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant_
                 if (in) h.running[static_cast<int64_t>((t0.n0 >> 7) + half) * h.N + row] = make_float2(LISTS ? __fmul_rn(m, h.e.inverse_t) : m, sum);
             } else {
                 const bool is = LISTS ? part : in && h.target[row] >= 0;
-                const float g = LISTS ? g_row * h.e.inverse_t : (is ? h.scale[row] : 0.f), lse = LISTS ? lse_row : (is ? h.lse[row] : 0.f);
+                const float g = LISTS ? g_row : (is ? h.scale[row] : 0.f), lse = LISTS ? lse_row : (is ? h.lse[row] : 0.f);
                 float z = -lse * kHeadLog2e, lost = fmaf(-lse, kHeadLog2e, -z), scale = log2e;      // as for the statistics
                 if (__any_sync(0xffffffffu, fabsf(lost) > kHeadLost)) {
 #pragma unroll

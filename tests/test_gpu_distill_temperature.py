@@ -105,3 +105,28 @@ def test_one_column_in_fp32(vl, N, T):  # noqa: F811
     loss, lse = forward(vl, p)
     dX, _ = backward(vl, p, lse, need_dW=False)
     assert not dX.any() and not loss.any()
+
+
+@pytest.mark.parametrize("dw_dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [1.5, 3.0, 6.0, 256 / 257])
+def test_a_temperature_is_not_rounded_into_every_gradient(vl, T, dw_dtype):  # noqa: F811
+    """bf16, more than 64 tokens, each with one entry that the student knows nothing of: G at the entries is -g / T (1 - q), q below 2^-10.  1 / T rounded to bf16 in
+    all of them would be off by up to 2^-8, always the same way; without that factor they are within q of -g, g equal for all.  The other
+    columns' q g round by 2^-8 of themselves, N / V of them to an entry, so that they are 2^-5 of dW in norm at the most.  Then the output's own rounding:
+    bf16's root mean square of 1.66e-3 and a tenth more."""
+    N, D, V = 512, 256, 4096
+    g = torch.Generator(device=DEV).manual_seed(7)
+    r = lambda *s: torch.randn(s, generator=g, device=DEV)  # noqa: E731
+    p = {"X": r(N, D).bfloat16(), "W": (0.002 * r(V, D)).bfloat16(), "i": torch.randint(V, (N, 1), generator=g, device=DEV), "t": r(N, 1), "lse": None,
+         "g": torch.full((N,), T * T / N, device=DEV), "T": T}
+    _, lse = forward(vl, p)
+    x, w = p["X"].double(), p["W"].double()
+    q = torch.softmax(x @ w.t() / T, 1)
+    assert q.max() < 2.0 ** -10
+    G = q.clone().scatter_add_(1, p["i"], torch.full((N, 1), -1.0, device=DEV, dtype=torch.float64)) * (T / N)
+    dX, dW = backward(vl, p, lse, dw_dtype=dw_dtype)
+    own = {torch.bfloat16: 1.83e-3, torch.float32: 0.0}
+    for got, ref, rounding in ((dX, G @ w, own[torch.bfloat16]), (dW, G.t() @ x, own[dw_dtype])):
+        bound = ((2.0 ** -10 + 2.0 ** -13) ** 2 + rounding ** 2) ** 0.5
+        error = ((got.double() - ref).norm() / ref.norm()).item()
+        assert error <= bound, error
