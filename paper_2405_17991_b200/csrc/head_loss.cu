@@ -636,7 +636,7 @@ int launch_head_loss_backward(const HeadArgs& a, const float* lse, const float* 
     // In bf16 the logits' gradients are rounded once (more than 64 tokens), for the tensor cores: by half a step each.  A mean's 1 / count in
     // all of them would be the same rounding again and again, which does not average out (relative error of dX and dW up to 4e-3 by the
     // count alone); so the largest dloss is taken out and multiplied back in fp32, wherever the product that writes dW takes a factor.  So is a
-    // temperature's 1 / T (512 x 256 of 4096, T = 1.5, one entry a token: fp32 dW off by 2.2e-3, now 2e-4).
+    // temperature's 1 / T (512 x 256 of 4096, T = 1.5, one entry a token: fp32 dW off by 2.2e-3, now 2.5e-4).
     const bool take_common = a.dtype == VELORA_BF16 && (!dW || dw_dtype == VELORA_BF16 || c_rows_vec(dW, lddw, sizeof(float)));
     if (a.teacher) {
         rc = launch_distill_lists(a, l);

@@ -147,8 +147,7 @@ int launch_rows(const NormGradArgs& a, int sm_count, cudaStream_t stream)
     static_assert(TEAM == 0 || P == 32 * TEAM, "a team's threads");
     constexpr int kTeams = TEAM ? 8 / TEAM : 1, kRoom = 216 * 1024 / BLOCKS;
     const int share = odd_share(a.D, a.dtype), row = share * (MORE ? 3 : 2) * kTeams, stages = kRoom / row < 4 ? kRoom / row : 4;
-    if (a.D > N * P || a.D < LEAST * P) return VELORA_ERR_UNSUPPORTED;
-    if (stages < 2) return launch_layer_norm_backward_any(a, sm_count, stream);
+    if (a.D > N * P || a.D < LEAST * P || stages < 2) return VELORA_ERR_UNSUPPORTED;
     static DeviceOnce configured;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return VELORA_ERR_CUDA;
@@ -165,6 +164,9 @@ int launch_rows(const NormGradArgs& a, int sm_count, cudaStream_t stream)
     return launch_norm_slices(a, static_cast<int>(blocks), stream);
 }
 
+// Longest rows of which two fit a block's 216 KB: with dH three operands of fp32, (ceil(4 D / 16) + 1) 16 bytes each.
+template <typename T, bool MORE> constexpr int kOddHeld = sizeof(T) == 4 && MORE ? 9212 : 12288;
+
 // 4096 x 5461 bf16 46 us (the same rows on 16-byte boundaries 37), 12608 x 769 25, 8192 x 10001 143.
 template <typename T, bool MORE>
 int launch_width(const NormGradArgs& a, int sm_count, cudaStream_t stream)
@@ -177,8 +179,9 @@ int launch_width(const NormGradArgs& a, int sm_count, cudaStream_t stream)
     if (a.D <= 4096) return launch_rows<T, 16, 10, MORE, 0, 256, true, 2>(a, sm_count, stream);
     if (a.D <= 5632) return launch_rows<T, 16, 11, MORE, 0, 352, true, 1>(a, sm_count, stream);
     if (a.D <= 8192) return launch_rows<T, 16, 11, MORE, 0, 512, true, 1>(a, sm_count, stream);
-    if (a.D <= 10240) return launch_rows<T, 20, 16, MORE, 0, 512, false, 1>(a, sm_count, stream);
-    if (a.D <= 12288) return launch_rows<T, 24, 20, MORE, 0, 512, false, 1>(a, sm_count, stream);
+    if (a.D <= 10240 && a.D <= kOddHeld<T, MORE>) return launch_rows<T, 20, 16, MORE, 0, 512, false, 1>(a, sm_count, stream);
+    if constexpr (kOddHeld<T, MORE> > 10240)
+        if (a.D <= 12288) return launch_rows<T, 24, 20, MORE, 0, 512, false, 1>(a, sm_count, stream);
     return launch_layer_norm_backward_any(a, sm_count, stream);
 }
 

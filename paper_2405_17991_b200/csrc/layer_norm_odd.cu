@@ -110,8 +110,7 @@ int launch_rows(const NormArgs& a, int sm_count, cudaStream_t stream)
 {
     constexpr int kTeams = TEAM ? 8 : 1, kRoom = 216 * 1024 / BLOCKS;
     const int share = odd_share(a.D, a.dtype), row = share * (RESIDUAL ? 2 : 1) * kTeams, stages = kRoom / row < 4 ? kRoom / row : 4;
-    if (a.D > N * P || a.D < LEAST * P) return VELORA_ERR_UNSUPPORTED;
-    if (stages < 2) return launch_layer_norm_any(a, sm_count, stream);
+    if (a.D > N * P || a.D < LEAST * P || stages < 2) return VELORA_ERR_UNSUPPORTED;
     static DeviceOnce configured;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return VELORA_ERR_CUDA;

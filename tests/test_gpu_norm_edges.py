@@ -59,3 +59,9 @@ def test_rows_of_one_very_large_value(vl, D, power, eps, dtype):  # noqa: F811
         check(dX, back.dX, back.dX_bound, "dX", half_step(dtype))
         check(dw, back.dw, back.dw_bound, "dweight")
         check(db, back.db, back.db_bound, "dbias")
+
+
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("D", [9209, 9211, 9213, 9217, 10239, 12285, 12287])
+def test_fp32_rows_around_the_longest_that_are_held(vl, guard, D, residual):  # noqa: F811
+    run(vl, guard, batch(300, D, torch.float32, D), residual, torch.float32, ld=D)
