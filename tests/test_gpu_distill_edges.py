@@ -130,3 +130,23 @@ def test_a_temperature_is_not_rounded_into_every_gradient(vl, T, dw_dtype):  # n
         bound = ((2.0 ** -10 + 2.0 ** -13) ** 2 + rounding ** 2) ** 0.5
         error = ((got.double() - ref).norm() / ref.norm()).item()
         assert error <= bound, error
+
+
+@pytest.mark.parametrize("N", [1, 5, 16])
+@pytest.mark.parametrize("D,V", [(200, 700), (203, 1000), (4099, 520)])
+def test_few_fp32_tokens_in_a_small_workspace(vl, guard, N, D, V):  # noqa: F811
+    """Room for one sum of dX instead of its slices, and for a piece of 256 columns: what every piece gives is added to that one."""
+    p = batch(N, D, V, 3, torch.float32, N + D, 1.5, "some" if N > 4 else "none", True)
+    ref = Reference(p)
+    _, lse = forward(vl, p)
+    up = lambda n: -(-n // 256) * 256  # noqa: E731
+    slices = min(256, 1184 // -(-D // 512))
+    one, pitch = N * (-(-D // 8) * 8), up(V)
+    front = vl.velora_workspace_bytes(vl.OP_HEAD_DISTILL_BACKWARD | vl.OP_F32, N, D, V, 3, False) - up(4 * N * pitch)
+    least = front - up(4 * one * slices) + up(4 * one)
+    for room in (256, 512):
+        dX, dW = backward(vl, p, lse, ws=guard.workspace(vl, least + 4 * N * room))
+        check(dX, ref.dX, ref.dX_bound, "dX")
+        check(dW, ref.dW, ref.dW_bound, "dW")
+    with pytest.raises(vl.VeloraError):
+        backward(vl, p, lse, ws=guard.workspace(vl, least + 4 * N * 256 - 1))
