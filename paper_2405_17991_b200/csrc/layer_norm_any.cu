@@ -1,5 +1,6 @@
 // Layer norm and its gradients (formulas: layer_norm.cu) of rows of any length, one element at a time, each row read several times (from L1 or L2 but for
-// the first): for rows that are too long to be held.  And the sum of the slices of dw and db, for these and the others.
+// the first): for rows that are too long to be held.  And the sum of the slices of dw and db, for these and the others.  8192 x 14336 bf16: 351 us forward, 458
+// backward (1.3 and 1.5 TB/s of x, y and dy, h, dx; 12288 columns, which are held: 71 and 113).
 #include "layer_norm.cuh"
 
 namespace velora {
